@@ -12,7 +12,12 @@
  *                           (Appendix A Eq. t_spa); _gqa_union: the same with
  *                           two query heads of a KV group per tile
  *   ei_dense_prefill_attn   dense (causal) GQA attention, the full-attention
- *                           baseline the paper compares against
+ *                           baseline the paper compares against;
+ *                           ei_packed_prefill_attn: several sequences of
+ *                           different lengths in one tensor
+ *   ei_cache_*              a paged 8-bit cache of keys and values: storing
+ *                           into it, attention of new tokens over it, copies
+ *                           of pages
  *
  * Conventions shared by every entry point
  *  - Tensors are contiguous, row-major, in device memory owned by the caller;
@@ -416,6 +421,134 @@ ei_status ei_rope_tables(int32_t seq_len, int32_t head_dim, float theta, float* 
  * else EI_ERR_UNSUPPORTED); out may be g or u.
  */
 ei_status ei_swiglu(const uint16_t* g, const uint16_t* u, int64_t n, uint16_t* out, void* stream);
+
+/*
+ * ei_packed_prefill_attn -- ei_dense_prefill_attn over sequences that lie one
+ * behind the other: sequence s is the rows cu_seqlens[s] .. cu_seqlens[s+1]-1
+ * of every head, and its queries attend to its own keys only (causal: j <= i).
+ *
+ *   q, k, v, o   bf16 [Hq][T][D], [Hkv][T][D]; dims.batch must be 1 (else
+ *                EI_ERR_SHAPE) and dims.seq_len is T
+ *   cu_seqlens   i32 [n_seqs + 1], ascending, on the device.  Values are
+ *                clamped to [0, T] and a sequence that does not end after it
+ *                starts is empty, so no list leads out of the tensors; rows
+ *                that two sequences share hold the result of either.
+ *
+ * Rows of o that belong to no sequence are left as they were.  A sequence's
+ * bits depend, by roundings, on T and n_seqs as the bits of
+ * ei_dense_prefill_attn do on its launch.
+ *
+ * Errors: as ei_dense_prefill_attn; EI_ERR_SHAPE also for n_seqs < 0.
+ */
+ei_status ei_packed_prefill_attn(const uint16_t* q, const uint16_t* k, const uint16_t* v,
+                                 ei_dims dims, const int32_t* cu_seqlens, int32_t n_seqs,
+                                 float softmax_scale, int32_t causal, uint16_t* o, void* stream);
+
+/*
+ * The cache.  A page holds page_len tokens of every KV head: codes
+ * [n_kv_heads][page_len][D], and for each KV head one fp32 scale; an element
+ * is code * scale.  K and V have pages and scales of their own, with the same
+ * page numbers.  A sequence's tokens p lie in row p % page_len of the page
+ * page_table[s][p / page_len].
+ *
+ * New tokens come packed: bf16 [heads][T][D] (T = n_tokens), sequence s being
+ * the rows cu_seqlens[s] .. cu_seqlens[s+1]-1 (clamped as in
+ * ei_packed_prefill_attn), or, with cu_seqlens NULL, T / n_seqs rows of each
+ * sequence (T must be a multiple, else EI_ERR_SHAPE).  lengths[s] is the number of
+ * tokens of sequence s in the cache, its new ones included: the last of them
+ * is at position lengths[s] - 1.
+ */
+typedef enum {
+  EI_CACHE_E4M3 = 0, /* 8-bit floating point, 4 exponent and 3 fraction bits */
+  EI_CACHE_INT8 = 1  /* integers -127 .. 127 */
+} ei_cache_format;
+
+/* page_len is 64 or 128 and head_dim 128 (else EI_ERR_UNSUPPORTED); format is
+ * an ei_cache_format, n_pages * n_kv_heads < 2^31 (else EI_ERR_SHAPE). */
+typedef struct {
+  int32_t n_pages, n_kv_heads, page_len, head_dim, format;
+} ei_cache_shape;
+
+/* k, v: codes [n_pages][n_kv_heads][page_len][head_dim], 16-byte aligned;
+ * k_scale, v_scale: fp32 [n_pages][n_kv_heads]. */
+typedef struct {
+  void *k, *v;
+  float *k_scale, *v_scale;
+} ei_cache_pages;
+
+/*
+ * ei_cache_store -- writes new keys and values to their places.
+ *
+ *   k, v         bf16 [n_kv_heads][T][D]
+ *   page_table   i32 [n_seqs][max_pages]
+ *
+ * For each page touched, KV head, and each of K and V: the scale is the least
+ * power of two (2^-126 at least) with which the largest new element lies
+ * within +-448 (e4m3) or +-127 (int8).  Where the page holds earlier tokens of the sequence (its first
+ * new row is not row 0), the scale is at least the one it has, and if it
+ * grows, the earlier rows are rounded again to it.  Codes are x / scale rounded
+ * to nearest even.  Being powers of two, the scales cost e4m3 no precision and
+ * keep the sum of an int8 code's roundings below one step.  A new element that
+ * is not finite makes the scale of its page and head NaN (the codes of the new
+ * rows 0), until a store to its row 0 begins the page anew.  Rows of the page
+ * behind the new ones are left as they were.
+ *
+ * Tokens at negative positions, past max_pages pages or on a page outside
+ * [0, n_pages) are not stored.  No two sequences of a call may store to the
+ * same page.
+ *
+ * Errors: EI_ERR_NULL, EI_ERR_SHAPE, EI_ERR_UNSUPPORTED, EI_ERR_LAUNCH.
+ */
+ei_status ei_cache_store(const uint16_t* k, const uint16_t* v, int32_t n_tokens,
+                         const int32_t* cu_seqlens, int32_t n_seqs, const int32_t* lengths,
+                         const int32_t* page_table, int32_t max_pages, ei_cache_shape shape,
+                         ei_cache_pages pages, void* stream);
+
+/* Workspace bytes ei_cache_attn needs (0: none, or invalid sizes); `packed`
+ * says whether cu_seqlens is given.  The workspace is scratch of one call: a
+ * later call on the same stream may use it again, calls that may run at the
+ * same time need one each. */
+size_t ei_cache_attn_workspace_bytes(int32_t n_q_heads, int32_t n_tokens, int32_t packed,
+                                     int32_t n_seqs, int32_t max_pages, ei_cache_shape shape);
+
+/*
+ * ei_cache_attn -- attention of the sequences' newest tokens over the cache
+ * (which holds them already): with n_s rows in sequence s, its i-th query is
+ * at position lengths[s] - n_s + i and attends to the keys up to its own;
+ * grouped heads as everywhere.  fp32 accumulation and online softmax, bf16
+ * output; the probabilities times V's scale are rounded to bf16 for the matrix
+ * cores, as in the prefill attention.
+ *
+ *   q, o        bf16 [n_q_heads][T][D]
+ *   workspace   ei_cache_attn_workspace_bytes(), 16-byte aligned
+ *
+ * Keys past max_pages pages or on pages outside [0, n_pages) are not attended
+ * to; a query with no key (a negative position, length 0) gets a zero row.
+ * Rows of o that belong to no sequence are left as they were.  Rows of a page
+ * behind the sequence's end are not read for their values.  Meant for few new
+ * tokens a sequence: every 16 rows (tokens times query heads of a group) read
+ * the sequence's keys once.
+ *
+ * Errors: EI_ERR_NULL, EI_ERR_SHAPE (also a softmax_scale that is not finite
+ * and positive), EI_ERR_UNSUPPORTED, EI_ERR_WORKSPACE, EI_ERR_LAUNCH.
+ */
+ei_status ei_cache_attn(const uint16_t* q, int32_t n_q_heads, int32_t n_tokens,
+                        const int32_t* cu_seqlens, int32_t n_seqs, const int32_t* lengths,
+                        const int32_t* page_table, int32_t max_pages, ei_cache_shape shape,
+                        ei_cache_pages pages, float softmax_scale, uint16_t* o, void* workspace,
+                        size_t workspace_bytes, void* stream);
+
+/*
+ * ei_cache_copy -- page dst[i] = page src[i] (codes and scales of K and V) in
+ * each of n_layers caches of the same shape that lie one behind the other
+ * (pages.k is [n_layers][n_pages][...], the scales alike).  i32 lists of n on
+ * the device; a pair with a page outside [0, n_pages) is skipped.  The pages of
+ * dst must differ from each other and from those of src.
+ *
+ * Errors: EI_ERR_NULL, EI_ERR_SHAPE, EI_ERR_UNSUPPORTED, EI_ERR_LAUNCH.
+ */
+ei_status ei_cache_copy(ei_cache_shape shape, int32_t n_layers, ei_cache_pages pages,
+                        const int32_t* src, const int32_t* dst, int32_t n, void* stream);
 
 #ifdef __cplusplus
 }

@@ -14,6 +14,7 @@ import functools
 import math
 import operator
 import os
+from typing import NamedTuple
 
 import torch
 
@@ -39,6 +40,17 @@ class BudgetParams(ctypes.Structure):
     _fields_ = [("entropy_threshold", ctypes.c_float), ("alpha", ctypes.c_double),
                 ("delta_t", ctypes.c_double), ("base_budget_tokens", ctypes.c_int32),
                 ("max_budget_mult", ctypes.c_int32)]
+
+
+class CacheShape(ctypes.Structure):
+    _fields_ = [("n_pages", ctypes.c_int32), ("n_kv_heads", ctypes.c_int32),
+                ("page_len", ctypes.c_int32), ("head_dim", ctypes.c_int32),
+                ("format", ctypes.c_int32)]
+
+
+class CachePointers(ctypes.Structure):   # ei_cache_pages
+    _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p),
+                ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
 
 
 class EIError(RuntimeError):
@@ -116,6 +128,21 @@ def lib() -> ctypes.CDLL:
         L.ei_rope_tables.argtypes = [ctypes.c_int32, ctypes.c_int32, ctypes.c_float, _VP, _VP, _VP]
         L.ei_swiglu.restype = ctypes.c_int
         L.ei_swiglu.argtypes = [_VP, _VP, ctypes.c_int64, _VP, _VP]
+        L.ei_packed_prefill_attn.restype = ctypes.c_int
+        L.ei_packed_prefill_attn.argtypes = [_VP, _VP, _VP, Dims, _VP, ctypes.c_int32,
+                                             ctypes.c_float, ctypes.c_int32, _VP, _VP]
+        L.ei_cache_store.restype = ctypes.c_int
+        L.ei_cache_store.argtypes = [_VP, _VP, ctypes.c_int32, _VP, ctypes.c_int32, _VP, _VP,
+                                     ctypes.c_int32, CacheShape, CachePointers, _VP]
+        L.ei_cache_attn_workspace_bytes.restype = ctypes.c_size_t
+        L.ei_cache_attn_workspace_bytes.argtypes = [ctypes.c_int32] * 5 + [CacheShape]
+        L.ei_cache_attn.restype = ctypes.c_int
+        L.ei_cache_attn.argtypes = [_VP, ctypes.c_int32, ctypes.c_int32, _VP, ctypes.c_int32, _VP,
+                                    _VP, ctypes.c_int32, CacheShape, CachePointers,
+                                    ctypes.c_float, _VP, _VP, ctypes.c_size_t, _VP]
+        L.ei_cache_copy.restype = ctypes.c_int
+        L.ei_cache_copy.argtypes = [CacheShape, ctypes.c_int32, CachePointers, _VP, _VP,
+                                    ctypes.c_int32, _VP]
         _LIB = L
     return _LIB
 
@@ -537,3 +564,178 @@ def swiglu(g, u, out=None):
         st = lib().ei_swiglu(_ptr(g), _ptr(u), g.numel(), _ptr(out), _stream(g))
     _check("ei_swiglu", st)
     return out
+
+
+# --------------------------------------------------------------------------
+# Packed sequences and the paged 8-bit cache
+# --------------------------------------------------------------------------
+
+def _req_packed(t, name: str, tokens: int | None = None) -> None:
+    """bf16 [1, heads, tokens, D]."""
+    _req(t, name, torch.bfloat16, 4)
+    if t.shape[0] != 1 or (tokens is not None and t.shape[2] != tokens):
+        raise ValueError(f"{name} {tuple(t.shape)} is not [1, heads, "
+                         f"{'tokens' if tokens is None else tokens}, head_dim]")
+
+
+def packed_prefill_attn(q, k, v, cu_seqlens, softmax_scale: float | None = None,
+                        causal: bool = True, out=None):
+    """ei_packed_prefill_attn: dense attention within each of the sequences
+    that lie one behind the other in q [1, Hq, T, D], k and v [1, Hkv, T, D];
+    sequence s is the rows cu_seqlens[s] .. cu_seqlens[s + 1] - 1 (int32, on the
+    device).  Rows of ``out`` outside every sequence are left as they were."""
+    for t, n in ((q, "q"), (k, "k"), (v, "v")):
+        _req_packed(t, n)
+    _req(cu_seqlens, "cu_seqlens", torch.int32, 1)
+    check_qkv_shapes(q.shape, k.shape, v.shape)
+    if cu_seqlens.numel() < 1:
+        raise ValueError("cu_seqlens holds one offset more than there are sequences")
+    if out is None:
+        out = torch.empty_like(q)
+    _req(out, "out", torch.bfloat16, 4)
+    if out.shape != q.shape:
+        raise ValueError(f"out {tuple(out.shape)} does not match q {tuple(q.shape)}")
+    sc = 1.0 / math.sqrt(q.shape[3]) if softmax_scale is None else float(softmax_scale)
+    _same_device(q, k, v, cu_seqlens, out)
+    with _on(q):
+        st = lib().ei_packed_prefill_attn(_ptr(q), _ptr(k), _ptr(v), dims_of(q, k),
+                                          _ptr(cu_seqlens), cu_seqlens.numel() - 1, sc,
+                                          1 if causal else 0, _ptr(out), _stream(q))
+    _check("ei_packed_prefill_attn", st)
+    return out
+
+
+class CachePages(NamedTuple):
+    """The pages of a cache (ei_cache_pages): codes k and v [n_pages, Hkv,
+    page_len, D] in float8_e4m3fn or int8, scales k_scale and v_scale
+    [n_pages, Hkv] in fp32; an element is code * scale.  A leading dimension
+    holds the caches of several layers (``layer`` picks one)."""
+    k: torch.Tensor
+    v: torch.Tensor
+    k_scale: torch.Tensor
+    v_scale: torch.Tensor
+
+    def layer(self, i: int) -> "CachePages":
+        return CachePages(self.k[i], self.v[i], self.k_scale[i], self.v_scale[i])
+
+
+CACHE_FORMATS = {torch.float8_e4m3fn: 0, torch.int8: 1}   # ei_cache_format
+
+
+def new_cache_pages(n_pages: int, n_kv_heads: int, page_len: int, head_dim: int = 128,
+                    dtype=torch.float8_e4m3fn, device="cuda", n_layers: int | None = None):
+    """Empty pages, of one layer or of n_layers."""
+    if dtype not in CACHE_FORMATS:
+        raise TypeError(f"cache pages are float8_e4m3fn or int8, not {dtype}")
+    lead = () if n_layers is None else (n_layers,)
+    codes = [torch.zeros((*lead, n_pages, n_kv_heads, page_len, head_dim), dtype=torch.uint8,
+                         device=device).view(dtype) for _ in range(2)]
+    return CachePages(*codes, *(torch.zeros((*lead, n_pages, n_kv_heads), dtype=torch.float32,
+                                            device=device) for _ in range(2)))
+
+
+def _cache_args(pages, layers: bool = False):
+    """(CacheShape, CachePointers) of checked pages; with ``layers`` the number
+    of layers comes first."""
+    k, v, ks, vs = pages
+    nd = k.dim() if layers and k.dim() == 5 else 4
+    fmt = CACHE_FORMATS.get(k.dtype)
+    if fmt is None:
+        raise TypeError(f"cache pages are float8_e4m3fn or int8, not {k.dtype}")
+    _req(k, "pages.k", k.dtype, nd)
+    _req(v, "pages.v", k.dtype, nd)
+    _req(ks, "pages.k_scale", torch.float32, nd - 2)
+    _req(vs, "pages.v_scale", torch.float32, nd - 2)
+    if v.shape != k.shape or ks.shape != k.shape[:-2] or vs.shape != ks.shape:
+        raise ValueError(f"pages: v {tuple(v.shape)}, k_scale {tuple(ks.shape)} or v_scale "
+                         f"{tuple(vs.shape)} do not match k {tuple(k.shape)}")
+    _same_device(k, v, ks, vs)
+    shape = CacheShape(*k.shape[nd - 4:], fmt)
+    ptrs = CachePointers(_ptr(k), _ptr(v), _ptr(ks), _ptr(vs))
+    return (k.shape[0] if nd == 5 else 1, shape, ptrs) if layers else (shape, ptrs)
+
+
+def _sequences(tokens: int, page_table, lengths, cu_seqlens) -> int:
+    """The number of sequences, after checks of what describes them."""
+    _req(page_table, "page_table", torch.int32, 2)
+    _req(lengths, "lengths", torch.int32, 1)
+    S = lengths.shape[0]
+    if page_table.shape[0] != S:
+        raise ValueError(f"page_table has {page_table.shape[0]} rows for {S} lengths")
+    if cu_seqlens is not None:
+        _req(cu_seqlens, "cu_seqlens", torch.int32, 1)
+        if cu_seqlens.shape[0] != S + 1:
+            raise ValueError(f"cu_seqlens has {cu_seqlens.shape[0]} offsets for {S} sequences")
+    elif tokens % S if S else tokens:
+        raise ValueError(f"{tokens} tokens do not divide among {S} sequences: pass cu_seqlens")
+    return S
+
+
+def cache_store(k, v, pages: CachePages, page_table, lengths, cu_seqlens=None) -> None:
+    """ei_cache_store: the new tokens k and v [1, Hkv, T, D] into the pages of
+    their sequences (page_table int32 [S, max_pages]).  lengths int32 [S] counts
+    each sequence's tokens with the new ones; cu_seqlens int32 [S + 1] says
+    which rows are whose (None: T / S rows each)."""
+    _req_packed(k, "k")
+    _req_packed(v, "v")
+    if v.shape != k.shape:
+        raise ValueError(f"v {tuple(v.shape)} does not match k {tuple(k.shape)}")
+    shape, ptrs = _cache_args(pages)
+    T = k.shape[2]
+    if k.shape[1] != shape.n_kv_heads or k.shape[3] != shape.head_dim:
+        raise ValueError(f"k {tuple(k.shape)} does not match the pages {tuple(pages.k.shape)}")
+    S = _sequences(T, page_table, lengths, cu_seqlens)
+    _same_device(k, v, pages.k, page_table, lengths, cu_seqlens)
+    with _on(k):
+        st = lib().ei_cache_store(_ptr(k), _ptr(v), T, _ptr(cu_seqlens), S, _ptr(lengths),
+                                  _ptr(page_table), page_table.shape[1], shape, ptrs, _stream(k))
+    _check("ei_cache_store", st)
+
+
+def cache_attn(q, pages: CachePages, page_table, lengths, cu_seqlens=None,
+               softmax_scale: float | None = None, out=None, workspace=None):
+    """ei_cache_attn: attention of each sequence's newest tokens q [1, Hq, T, D]
+    over the cache, which holds them already; page_table, lengths and
+    cu_seqlens as cache_store.  Returns bf16 [1, Hq, T, D].  ``workspace``
+    (optional, uint8) is scratch of this call alone."""
+    _req_packed(q, "q")
+    shape, ptrs = _cache_args(pages)
+    _, Hq, T, D = q.shape
+    if D != shape.head_dim or Hq % shape.n_kv_heads:
+        raise ValueError(f"q {tuple(q.shape)} does not match the pages {tuple(pages.k.shape)}")
+    S = _sequences(T, page_table, lengths, cu_seqlens)
+    if out is None:
+        out = torch.empty_like(q)
+    _req(out, "out", torch.bfloat16, 4)
+    if out.shape != q.shape:
+        raise ValueError(f"out {tuple(out.shape)} does not match q {tuple(q.shape)}")
+    _same_device(q, pages.k, page_table, lengths, out, cu_seqlens)
+    cols = page_table.shape[1]
+    if workspace is None:
+        need = lib().ei_cache_attn_workspace_bytes(Hq, T, cu_seqlens is not None, S, cols, shape)
+        workspace = torch.empty((need,), dtype=torch.uint8, device=q.device) if need else None
+    else:
+        _same_device(q, workspace)
+    nb = 0 if workspace is None else workspace.numel() * workspace.element_size()
+    sc = 1.0 / math.sqrt(D) if softmax_scale is None else float(softmax_scale)
+    with _on(q):
+        st = lib().ei_cache_attn(_ptr(q), Hq, T, _ptr(cu_seqlens), S, _ptr(lengths),
+                                 _ptr(page_table), cols, shape, ptrs, sc, _ptr(out),
+                                 _ptr(workspace), nb, _stream(q))
+    _check("ei_cache_attn", st)
+    return out
+
+
+def cache_copy(pages: CachePages, src, dst) -> None:
+    """ei_cache_copy: page dst[i] = page src[i] (int32 lists on the device) in
+    every layer of the pages.  dst must hold each page once and none of src."""
+    layers, shape, ptrs = _cache_args(pages, layers=True)
+    _req(src, "src", torch.int32, 1)
+    _req(dst, "dst", torch.int32, 1)
+    if src.shape != dst.shape:
+        raise ValueError(f"{src.numel()} source pages for {dst.numel()} destinations")
+    _same_device(pages.k, src, dst)
+    with _on(src):
+        st = lib().ei_cache_copy(shape, layers, ptrs, _ptr(src), _ptr(dst), src.numel(),
+                                 _stream(src))
+    _check("ei_cache_copy", st)

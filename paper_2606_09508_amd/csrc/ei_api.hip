@@ -340,4 +340,22 @@ ei_status ei_dense_prefill_attn(const uint16_t* q, const uint16_t* k, const uint
                                        nullptr, o, nullptr, false, (hipStream_t)stream));
 }
 
+ei_status ei_packed_prefill_attn(const uint16_t* q, const uint16_t* k, const uint16_t* v,
+                                 ei_dims dims, const int32_t* cu_seqlens, int32_t n_seqs,
+                                 float softmax_scale, int32_t causal, uint16_t* o, void* stream) {
+  ei_status st = check_dims(dims);
+  if (st != EI_OK) return st;
+  if (dims.batch > 1 || n_seqs < 0 || !scale_ok(softmax_scale)) return EI_ERR_SHAPE;
+  // a workgroup for each head and 128 rows, and one more for each sequence
+  if (((int64_t)dims.seq_len / 128 + n_seqs) > INT_MAX / dims.n_q_heads) return EI_ERR_SHAPE;
+  if (dims.batch == 0 || dims.seq_len == 0 || n_seqs == 0) return EI_OK;
+  if (!q || !k || !v || !cu_seqlens || !o) return EI_ERR_NULL;
+  if (!aligned16({q, k, v, o}) || !aligned4({cu_seqlens})) return EI_ERR_UNSUPPORTED;
+  const ei::AttnShape as{1, dims.n_q_heads, dims.n_kv_heads, dims.seq_len, 128, 64, 0, 0, 0,
+                         softmax_scale};
+  return from_hip(ei::launch_attention_packed(q, k, v, as,
+                                              causal ? ei::kDenseCausal : ei::kDenseFull,
+                                              cu_seqlens, n_seqs, o, (hipStream_t)stream));
+}
+
 }  // extern "C"

@@ -1067,6 +1067,112 @@ hipError_t launch_union_t(const uint16_t* q, const uint16_t* k, const uint16_t* 
   return hipGetLastError();
 }
 
+
+// ---------------------------------------------------------------------------
+// Packed sequences.  Sequence s is the rows cu[s] .. cu[s + 1] - 1 of every
+// head, so a tile of it is a dense tile of a tensor of cu[s + 1] - cu[s] rows
+// that starts cu[s] rows further on: attn_kernel's steps on shifted pointers.
+// The host does not know the lengths.  Sequence s owns the slots cu[s] / 128 + s
+// up to the next one's first, one for each of its tiles and at most one more.
+struct PackedTile {
+  int first, N, tile;   // the sequence's first row and rows, and its tile (or -1)
+};
+__device__ __forceinline__ int packed_row(const int32_t* __restrict__ cu, int s, int T) {
+  return min(max(cu[s], 0), T);
+}
+__device__ __forceinline__ PackedTile packed_tile(const int32_t* __restrict__ cu, int S, int T,
+                                                  int slot) {
+  int lo = 0, hi = S - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) / 2;
+    if (packed_row(cu, mid, T) / kTileQ + mid <= slot) lo = mid; else hi = mid - 1;
+  }
+  const int a = packed_row(cu, lo, T), e = packed_row(cu, lo + 1, T);
+  const int n = max(e - a, 0), i = slot - (a / kTileQ + lo);
+  const int tiles = (n + kTileQ - 1) / kTileQ;
+  return {a, n, tiles - 1 - i};   // heavier tiles first
+}
+
+template <int MODE>
+__global__ __launch_bounds__(kThreads, 2) void attn_packed_kernel(
+    const uint16_t* __restrict__ q, const uint16_t* __restrict__ k,
+    const uint16_t* __restrict__ v, uint16_t* __restrict__ o, int Hq, int Hkv, int T,
+    const int32_t* __restrict__ cu, int S, int slots, float sc_log2) {
+  __shared__ __attribute__((aligned(1024))) unsigned char stage0[kStageBytes];
+  __shared__ __attribute__((aligned(1024))) unsigned char stage1[kStageBytes];
+  const unsigned G = (unsigned)(Hq / Hkv);
+  const unsigned per_xcd = gridDim.x / kXcds;
+  unsigned t = (blockIdx.x % kXcds) * per_xcd + blockIdx.x / kXcds;
+  if (t >= (unsigned)Hq * (unsigned)slots) return;
+  const int hh = (int)(t % G);
+  t /= G;
+  const PackedTile pt = packed_tile(cu, S, T, (int)(t % (unsigned)slots));
+  const int g = (int)(t / (unsigned)slots);
+  if (pt.tile < 0) return;
+  const int N = pt.N, h = g * (int)G + hh;
+
+  const int tid = threadIdx.x;
+  const int wave = tid >> 6, lane = tid & 63;
+  const int jq = lane & 31, hf = lane >> 5;
+  const int q0 = pt.tile * kTileQ;
+  const int q_last = min(q0 + kTileQ - 1, N - 1);
+  const int qw0 = q0 + wave * 32;          // first query row of this wave
+  const int qrow = qw0 + jq;               // this lane's query row
+  const uint16_t* kh = k + ((size_t)g * T + pt.first) * kHeadDim;
+  const uint16_t* vh = v + ((size_t)g * T + pt.first) * kHeadDim;
+  const size_t row_base = (size_t)h * T + pt.first + qrow;
+
+  bf16x8 qf[8];
+#pragma unroll
+  for (int s = 0; s < 8; ++s)
+    qf[s] = as_bf16x8(qrow < N ? *(const uint4*)(q + row_base * kHeadDim + 8 * hf + 16 * s)
+                               : make_uint4(0, 0, 0, 0));
+  const int n_steps = MODE == kDenseCausal ? q_last / kSub + 1 : (N + kSub - 1) / kSub;
+
+  uint32_t koff[4], voff;
+  stage_offsets<4>(wave, lane, koff, voff);
+  f32x16 oacc[4];
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) oacc[d][r] = 0.0f;
+  float m_i = -INFINITY, l_i = 0.0f;
+
+  // the two-stage ring of attn_kernel
+  auto step = [&](const int i, unsigned char* st) {
+    if (i + 1 < n_steps) EI_WAIT_VMCNT(8); else EI_WAIT_VMCNT(0);
+    __syncthreads();
+    const int k0 = i * kSub;
+    if ((MODE == kDenseFull || k0 <= qw0 + 31) && qw0 < N)
+      compute_step<MODE>(st, k0, qw0, qrow, N, jq, hf, lane, qf, sc_log2, oacc, m_i, l_i);
+    if (i + 2 < n_steps) {
+      __syncthreads();   // every wave is done reading this stage
+      issue_stage<4>(st, kh, vh, (i + 2) * kSub, N, wave, lane, koff, voff);
+    }
+  };
+  EI_WAIT_VMCNT(0);
+  issue_stage<4>(stage0, kh, vh, 0, N, wave, lane, koff, voff);
+  if (n_steps > 1) issue_stage<4>(stage1, kh, vh, kSub, N, wave, lane, koff, voff);
+  for (int i = 0; i < n_steps; i += 2) {
+    step(i, stage0);
+    if (i + 1 < n_steps) step(i + 1, stage1);
+  }
+  if (qrow < N) store_rows(o, row_base, hf, oacc, l_i);
+}
+
+template <int MODE>
+hipError_t launch_packed_t(const uint16_t* q, const uint16_t* k, const uint16_t* v,
+                           const AttnShape& s, const int32_t* cu, int n_seqs, uint16_t* o,
+                           hipStream_t stream) {
+  const int slots = s.N / kTileQ + n_seqs;
+  const int64_t grid = ((int64_t)s.Hq * slots + kXcds - 1) / kXcds * kXcds;
+  if (!launch_fits(grid, kThreads)) return hipErrorInvalidConfiguration;
+  const float sc_log2 = (float)((double)s.softmax_scale * 1.4426950408889634);
+  hipLaunchKernelGGL((attn_packed_kernel<MODE>), dim3((unsigned)grid), dim3(kThreads), 0, stream,
+                     q, k, v, o, s.Hq, s.Hkv, s.N, cu, n_seqs, slots, sc_log2);
+  return hipGetLastError();
+}
+
 }  // namespace
 
 bool attention_union_supported(const AttnShape& s) {
@@ -1099,6 +1205,14 @@ hipError_t launch_attention(const uint16_t* q, const uint16_t* k, const uint16_t
     default:
       return launch_t<kDenseFull, 1>(q, k, v, s, nullptr, nullptr, o, nullptr, false, stream);
   }
+}
+
+hipError_t launch_attention_packed(const uint16_t* q, const uint16_t* k, const uint16_t* v,
+                                   const AttnShape& s, AttnMode mode, const int32_t* cu_seqlens,
+                                   int n_seqs, uint16_t* o, hipStream_t stream) {
+  return mode == kDenseCausal
+             ? launch_packed_t<kDenseCausal>(q, k, v, s, cu_seqlens, n_seqs, o, stream)
+             : launch_packed_t<kDenseFull>(q, k, v, s, cu_seqlens, n_seqs, o, stream);
 }
 
 }  // namespace ei

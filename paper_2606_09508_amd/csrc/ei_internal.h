@@ -185,4 +185,10 @@ hipError_t launch_attention(const uint16_t* q, const uint16_t* k, const uint16_t
                             const int32_t* block_cnt, uint16_t* o, void* sched_ws,
                             bool sched_zeroed, hipStream_t stream);
 
+// Dense attention over the n_seqs sequences that cu_seqlens (on the device)
+// marks off in the s.N rows of a batch of one.
+hipError_t launch_attention_packed(const uint16_t* q, const uint16_t* k, const uint16_t* v,
+                                   const AttnShape& s, AttnMode mode, const int32_t* cu_seqlens,
+                                   int n_seqs, uint16_t* o, hipStream_t stream);
+
 }  // namespace ei

@@ -24,6 +24,22 @@ typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 
+// Loads and stores of data that a launch touches once.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ uint4 load_once4(const void* p) {
+  return __builtin_bit_cast(uint4, __builtin_nontemporal_load((const u32x4*)p));
+}
+__device__ __forceinline__ uint2 load_once2(const void* p) {
+  return __builtin_bit_cast(uint2, __builtin_nontemporal_load((const u32x2*)p));
+}
+__device__ __forceinline__ void store_once4(void* p, uint4 w) {
+  __builtin_nontemporal_store(__builtin_bit_cast(u32x4, w), (u32x4*)p);
+}
+__device__ __forceinline__ void store_once2(void* p, uint2 w) {
+  __builtin_nontemporal_store(__builtin_bit_cast(u32x2, w), (u32x2*)p);
+}
+
 __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
   const f32x2 x = {lo, hi};
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
@@ -252,135 +268,191 @@ __device__ __forceinline__ bf16x8 widen8(uint32_t x, uint32_t y) {
 struct Part {          // of a row: sums against the maximum m (base 2)
   float m, l;
 };
+// An item (16 RT rows of a sequence and KV head) whose keys several waves
+// share, left for combine_kernel by the one with its first key.  Its parts in
+// the order of the keys: at first_slot and at 2 (worker + 1) ..: n_waves of
+// them (waves of the first workgroup); n_groups at 2 kWaves group ..
+// (workgroups after it); the rest at 2 last .. (waves of the last one).
+// parts = 0: none.
+struct SplitItem {
+  int s, kvh, row0, parts, first_slot, n_waves, group, n_groups, last, pad[3];
+};
 
-template <int FMT, int P>
-__global__ __launch_bounds__(kThreads) void attend_kernel(
-    const uint16_t* __restrict__ q, Tokens tk, const int32_t* __restrict__ lengths, Pages pg,
-    int Hq, int per_seq, int n_split, float sc_log2, uint16_t* __restrict__ o,
-    Part* __restrict__ part_ml, float* __restrict__ part_o, int64_t unit0) {
-  __shared__ float sm[kWaves][kRows], sl[kWaves][kRows];
-  __shared__ __attribute__((aligned(16))) float so[kWaves][kRows * kHeadDim];
-  const int G = Hq / pg.Hkv;
-  const int64_t unit = unit0 + blockIdx.x;
-  const int split = (int)(unit % n_split);
-  const int64_t item = unit / n_split;
-  const int kvh = (int)(item % pg.Hkv);
-  int s, tile, first, n;
-  find_slot(tk, (int)(item / pg.Hkv), per_seq, G, kRows, 1, s, tile);
-  seq_rows(tk, s, first, n);
-  const int row0 = tile * kRows;
-  if (row0 >= n * G) return;
-  const int lane = threadIdx.x % kWave, wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+struct AttendArgs {
+  const uint16_t* q;
+  uint16_t* o;
+  Tokens tk;
+  const int32_t* lengths;
+  Pages pg;
+  int Hq;
+  float sc_log2;
+  Part* part_ml;
+  float* part_o;
+  SplitItem* split;
+};
+
+// What a wave has of its 16 RT rows: lane l holds row j = l % 16 of each tile,
+// the dims 8 (4g + r) + i of oacc[.][i][r], and its own keys' part of l.
+template <int RT>
+struct WaveSums {
+  float m[RT], l[RT];
+  f32x4 o[RT][8];
+};
+
+// The rows row0 .. row0 + 16 RT - 1 of sequence s (n tokens from packed row
+// `first` on, seq_len of them in the cache) over every `stride`-th step of 32
+// keys from the w-th on, of the keys key0 .. key1 - 1.
+template <int FMT, int P, int RT>
+__device__ __forceinline__ void attend_steps(const AttendArgs& a, int s, int kvh, int row0,
+                                             int first, int n, int seq_len, int key0, int key1,
+                                             int w, int stride, WaveSums<RT>& ws) {
+  const int G = a.Hq / a.pg.Hkv, rows = n * G;
+  const int lane = threadIdx.x % kWave;
   const int j = lane & 15, g = lane >> 4;
-  const int len = (int)min((int64_t)max(lengths[s], 0), (int64_t)pg.max_pages * P);
 
-  // this lane's row: token and head; its last visible key
-  const int row = row0 + j;
-  const bool real = row < n * G;
-  const int t = min(row, n * G - 1) / G, head = kvh * G + min(row, n * G - 1) % G;
-  const int pos = lengths[s] - n + t;   // (rows past the last one repeat it)
-  const int64_t qrow = (int64_t)head * tk.T + first + t;
-  // the tile's keys: those its last row sees
-  const int last = lengths[s] - n + min(row0 + kRows - 1, n * G - 1) / G;
-  const int keys = max(min(last + 1, len), 0);
-  const int steps = (keys + kKeys - 1) / kKeys;
-  const int per = (steps + n_split - 1) / n_split;
-  const int step0 = split * per, step1 = min(step0 + per, steps);
-
-  bf16x8 qf[4];
+  bf16x8 qf[RT][4];
+  int pos[RT];   // this lane's rows: the last key each sees (rows past the last repeat it)
 #pragma unroll
-  for (int a = 0; a < 4; ++a)   // dims 64 (a / 2) + 16 g + 8 (a % 2) ..
-    qf[a] = __builtin_bit_cast(
-        bf16x8, *(const uint4*)(q + qrow * kHeadDim + 64 * (a >> 1) + 16 * g + 8 * (a & 1)));
-
-  f32x4 oacc[8];
+  for (int rt = 0; rt < RT; ++rt) {
+    const int row = min(row0 + kRows * rt + j, rows - 1);
+    pos[rt] = seq_len - n + row / G;
+    const uint16_t* qp =
+        a.q + ((int64_t)(kvh * G + row % G) * a.tk.T + first + row / G) * kHeadDim + 16 * g;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) oacc[i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  float m_i = -INFINITY, l_i = 0.0f;
+    for (int c = 0; c < 4; ++c)   // dims 64 (c / 2) + 16 g + 8 (c % 2) ..
+      qf[rt][c] = __builtin_bit_cast(bf16x8, *(const uint4*)(qp + 64 * (c >> 1) + 8 * (c & 1)));
+  }
+  const int pos_min = seq_len - n + row0 / G;
 
-  for (int st = step0 + wave; st < step1; st += kWaves) {
-    const int k0 = st * kKeys;
-    const int page = page_at(pg, s, k0 / P);
-    if (page < 0) continue;
-    const int64_t hp = (int64_t)page * pg.Hkv + kvh;
-    const uint8_t* kp = pg.k + (hp * P + k0 % P) * kHeadDim;
-    const uint8_t* vp = pg.v + (hp * P + k0 % P) * kHeadDim;
-    uint4 kw[2][2];
-    uint2 vw[2][4];
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    ws.m[rt] = -INFINITY;
+    ws.l[rt] = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) ws.o[rt][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+
+  const uint32_t koff = (uint32_t)(j * kHeadDim + 16 * g), voff = (uint32_t)(4 * g * kHeadDim + 8 * j);
+  // A step's operands.  The next step's are asked for as soon as this one's have
+  // been read out of their registers, so K is on its way during the softmax and
+  // the second product, V during the next step's first.  (Deeper pipelines, of
+  // up to four steps a wave, were slower wherever all CUs work: 8 sequences of
+  // up to 128k tokens 251 us, with a second step in flight 256, with two 259.)
+  uint4 kw[2][2];
+  uint2 vw[2][4];
+  // The loads go through buffer descriptors of the step's rows, of no length
+  // where there is no step to load for (such a load fetches nothing): loads
+  // behind a branch the compiler would wait for at once.
+  constexpr int kOnce = 2;   // nontemporal
+  auto rows_of = [&](uint8_t* base, int page, int k0, bool real) {
+    const int64_t at = real ? (((int64_t)page * a.pg.Hkv + kvh) * P + k0 % P) * kHeadDim : 0;
+    return __builtin_amdgcn_make_buffer_rsrc(base + at, 0, real ? kKeys * kHeadDim : 0, 0x00027000);
+  };
+  auto load_k = [&](int page, int k0, bool real) {
+    const auto rsrc = rows_of(a.pg.k, page, k0, real);
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
-      for (int a = 0; a < 2; ++a)
-        kw[u][a] = *(const uint4*)(kp + (16 * u + j) * kHeadDim + 64 * a + 16 * g);
+      for (int c = 0; c < 2; ++c)
+        kw[u][c] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(
+            rsrc, (int)koff + 16 * u * kHeadDim + 64 * c, 0, kOnce));
+  };
+  auto load_v = [&](int page, int k0, bool real) {
+    const auto rsrc = rows_of(a.pg.v, page, k0, real);
 #pragma unroll
     for (int u = 0; u < 2; ++u)
 #pragma unroll
       for (int r = 0; r < 4; ++r)
-        vw[u][r] = *(const uint2*)(vp + (16 * u + 4 * g + r) * kHeadDim + 8 * j);
-    const float kf = pg.ks[hp] * sc_log2, vf = pg.vs[hp];
-    f32x4 sacc[2];
+        vw[u][r] = __builtin_bit_cast(uint2, __builtin_amdgcn_raw_buffer_load_b64(
+            rsrc, (int)voff + (16 * u + r) * kHeadDim, 0, kOnce));
+  };
+
+  // `k_read` and `v_read` run once K and V have been read out.
+  auto compute = [&](int k0, float kf, float vf, auto k_read, auto v_read) {
+    f32x4 sacc[RT][2];
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
-      sacc[u] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
-      for (int a = 0; a < 2; ++a) {
-        sacc[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8<FMT>(kw[u][a].x, kw[u][a].y),
-                                                          qf[2 * a], sacc[u], 0, 0, 0);
-        sacc[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8<FMT>(kw[u][a].z, kw[u][a].w),
-                                                          qf[2 * a + 1], sacc[u], 0, 0, 0);
+      for (int rt = 0; rt < RT; ++rt) sacc[rt][u] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+      for (int c = 0; c < 2; ++c) {
+        const bf16x8 k_lo = widen8<FMT>(kw[u][c].x, kw[u][c].y);
+        const bf16x8 k_hi = widen8<FMT>(kw[u][c].z, kw[u][c].w);
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+          sacc[rt][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k_lo, qf[rt][2 * c], sacc[rt][u], 0, 0, 0);
+          sacc[rt][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k_hi, qf[rt][2 * c + 1], sacc[rt][u], 0, 0, 0);
+        }
       }
     }
-    float x[8];
-    bool seen[8];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const int key = k0 + 16 * (e >> 2) + 4 * g + (e & 3);
-      seen[e] = key <= pos && key < len;
-      x[e] = seen[e] ? sacc[e >> 2][e & 3] * kf : -INFINITY;
-    }
-    // rows behind the sequence's end hold anything, NaN codes included
-    if (k0 + kKeys > len) {
+    k_read();
+    // steps that reach past a row's last key (the others see every key); the
+    // asm statements keep the compiler from doing their work in every step
+    const bool edge = k0 + kKeys - 1 > pos_min || k0 + kKeys > key1;
+    if (k0 + kKeys > key1) {
+      int left = key1 - k0 - 4 * g;
+      asm volatile("" : "+v"(left));
+      // rows behind the sequence's end hold anything, NaN codes included
 #pragma unroll
       for (int e = 0; e < 8; ++e)
-        if (k0 + 16 * (e >> 2) + 4 * g + (e & 3) >= len) vw[e >> 2][e & 3] = make_uint2(0u, 0u);
+        if (16 * (e >> 2) + (e & 3) >= left) vw[e >> 2][e & 3] = make_uint2(0u, 0u);
     }
-    float p[8], lsum;
-    auto probs = [&](float mneg) {
-      lsum = 0.0f;
+    // the probabilities times V's scale as the sum of two bf16 numbers: one
+    // alone would double the variance that the output's rounding has, and the
+    // matrix cores have the time
+    bf16x8 p_hi[RT], p_lo[RT];
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        p[e] = __builtin_amdgcn_exp2f(x[e] + mneg);
-        lsum += p[e];
+    for (int rt = 0; rt < RT; ++rt) {
+      const int lim = min(pos[rt], key1 - 1) - k0 - 4 * g;
+      auto place = [](int e) { return 16 * (e >> 2) + (e & 3); };
+      auto hide = [&](float (&x)[8]) {
+        int most = lim;
+        asm volatile("" : "+v"(most));
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = place(e) <= most ? x[e] : 0.0f;
+      };
+      auto score = [&](int e) { return sacc[rt][e >> 2][e & 3]; };
+      float p[8], lsum;
+      auto probs = [&](float mneg) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(fmaf(score(e), kf, mneg));
+        if (edge) hide(p);
+        lsum = ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+      };
+      bool kept = false;
+      if (__builtin_amdgcn_ballot_w64(ws.m[rt] == -INFINITY) == 0) {
+        probs(-ws.m[rt]);
+        kept = __builtin_amdgcn_ballot_w64(!(lsum <= kFastLimit)) == 0;
       }
-    };
-    bool kept = false;
-    if (__builtin_amdgcn_ballot_w64(m_i == -INFINITY) == 0) {
-      probs(-m_i);
-      kept = __builtin_amdgcn_ballot_w64(!(lsum <= kFastLimit)) == 0;
-    }
-    if (!kept) {
-      float mx = x[0];
+      if (!kept) {
+        float mx = -INFINITY;
 #pragma unroll
-      for (int e = 1; e < 8; ++e) mx = fmaxf(mx, x[e]);
-      mx = fmaxf(mx, __shfl_xor(mx, 16));
-      mx = fmaxf(mx, __shfl_xor(mx, 32));
-      if (__builtin_amdgcn_ballot_w64(mx > m_i + kRescaleThreshold) != 0) {
-        const float m_new = fmaxf(m_i, mx);
-        const float alpha = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(m_i - m_new);
-        l_i *= alpha;
+        for (int e = 0; e < 8; ++e) mx = fmaxf(mx, place(e) <= lim ? score(e) * kf : -INFINITY);
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        if (__builtin_amdgcn_ballot_w64(mx > ws.m[rt] + kRescaleThreshold) != 0) {
+          const float m_new = fmaxf(ws.m[rt], mx);
+          const float alpha = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(ws.m[rt] - m_new);
+          ws.l[rt] *= alpha;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) oacc[i] *= alpha;
-        m_i = m_new;
+          for (int i = 0; i < 8; ++i) ws.o[rt][i] *= alpha;
+          ws.m[rt] = m_new;
+        }
+        probs(ws.m[rt] == -INFINITY ? 0.0f : -ws.m[rt]);
       }
-      probs(m_i == -INFINITY ? 0.0f : -m_i);
-    }
-    l_i += lsum;
-    uint32_t pw[4];
+      ws.l[rt] += lsum;
 #pragma unroll
-    for (int e = 0; e < 4; ++e)
-      pw[e] = pack_bf16x2(seen[2 * e] ? p[2 * e] * vf : 0.0f,
-                          seen[2 * e + 1] ? p[2 * e + 1] * vf : 0.0f);
-    const bf16x8 pf = __builtin_bit_cast(bf16x8, make_uint4(pw[0], pw[1], pw[2], pw[3]));
+      for (int e = 0; e < 8; ++e) p[e] *= vf;
+      if (edge) hide(p);   // (a masked probability is 0, but V's scale may be NaN)
+      uint32_t hi[4], lo[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        hi[e] = pack_bf16x2(p[2 * e], p[2 * e + 1]);
+        lo[e] = pack_bf16x2(p[2 * e] - bf16_lo(hi[e]), p[2 * e + 1] - bf16_hi(hi[e]));
+      }
+      p_hi[rt] = __builtin_bit_cast(bf16x8, make_uint4(hi[0], hi[1], hi[2], hi[3]));
+      p_lo[rt] = __builtin_bit_cast(bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3]));
+    }
     // byte i of keys (0, 1), (2, 3) of each half, next to each other
 #pragma unroll
     for (int half = 0; half < 2; ++half) {     // dims 8j + 4 half ..
@@ -389,100 +461,464 @@ __global__ __launch_bounds__(kThreads) void attend_kernel(
       for (int u = 0; u < 2; ++u)
 #pragma unroll
         for (int c = 0; c < 2; ++c) {
-          const uint32_t a = half ? vw[u][2 * c].y : vw[u][2 * c].x;
-          const uint32_t b = half ? vw[u][2 * c + 1].y : vw[u][2 * c + 1].x;
-          pr[u][c][0] = __builtin_amdgcn_perm(b, a, 0x05010400u);
-          pr[u][c][1] = __builtin_amdgcn_perm(b, a, 0x07030602u);
+          const uint32_t x = half ? vw[u][2 * c].y : vw[u][2 * c].x;
+          const uint32_t y = half ? vw[u][2 * c + 1].y : vw[u][2 * c + 1].x;
+          pr[u][c][0] = __builtin_amdgcn_perm(y, x, 0x05010400u);
+          pr[u][c][1] = __builtin_amdgcn_perm(y, x, 0x07030602u);
         }
 #pragma unroll
-      for (int w = 0; w < 2; ++w) {
+      for (int i2 = 0; i2 < 2; ++i2) {
         const bf16x8 v0 = __builtin_bit_cast(
-            bf16x8, make_uint4(widen2<FMT, false>(pr[0][0][w]), widen2<FMT, false>(pr[0][1][w]),
-                               widen2<FMT, false>(pr[1][0][w]), widen2<FMT, false>(pr[1][1][w])));
+            bf16x8, make_uint4(widen2<FMT, false>(pr[0][0][i2]), widen2<FMT, false>(pr[0][1][i2]),
+                               widen2<FMT, false>(pr[1][0][i2]), widen2<FMT, false>(pr[1][1][i2])));
         const bf16x8 v1 = __builtin_bit_cast(
-            bf16x8, make_uint4(widen2<FMT, true>(pr[0][0][w]), widen2<FMT, true>(pr[0][1][w]),
-                               widen2<FMT, true>(pr[1][0][w]), widen2<FMT, true>(pr[1][1][w])));
-        oacc[4 * half + 2 * w] =
-            __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, pf, oacc[4 * half + 2 * w], 0, 0, 0);
-        oacc[4 * half + 2 * w + 1] =
-            __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, pf, oacc[4 * half + 2 * w + 1], 0, 0, 0);
+            bf16x8, make_uint4(widen2<FMT, true>(pr[0][0][i2]), widen2<FMT, true>(pr[0][1][i2]),
+                               widen2<FMT, true>(pr[1][0][i2]), widen2<FMT, true>(pr[1][1][i2])));
+        const int i = 4 * half + 2 * i2;
+#pragma unroll
+        for (int rt = 0; rt < RT; ++rt) {
+          ws.o[rt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, p_hi[rt], ws.o[rt][i], 0, 0, 0);
+          ws.o[rt][i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, p_hi[rt], ws.o[rt][i + 1], 0, 0, 0);
+          ws.o[rt][i] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v0, p_lo[rt], ws.o[rt][i], 0, 0, 0);
+          ws.o[rt][i + 1] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v1, p_lo[rt], ws.o[rt][i + 1], 0, 0, 0);
+        }
+      }
+    }
+    v_read();
+  };
+
+  // The wave's steps, 64 at a time: lane i looks up the page and the scales of
+  // the i-th.
+  const int steps = (key1 - key0 + kKeys - 1) / kKeys;
+  const int mine = (steps - w + stride - 1) / stride;
+  for (int base = 0; base < mine; base += kWave) {
+    auto key_of = [&](int i) { return key0 + kKeys * (w + stride * (base + i)); };
+    const int page_l = base + lane < mine ? page_at(a.pg, s, key_of(lane) / P) : -1;
+    float kf_l = 0.0f, vf_l = 0.0f;
+    if (page_l >= 0) {
+      const int64_t hp = (int64_t)page_l * a.pg.Hkv + kvh;
+      kf_l = a.pg.ks[hp] * a.sc_log2;
+      vf_l = a.pg.vs[hp];
+    }
+    const int cnt = min(mine - base, kWave);
+    auto lane_i = [&](int x, int i) { return __builtin_amdgcn_readlane(x, i & (kWave - 1)); };
+    auto lane_f = [&](float x, int i) {
+      return __builtin_bit_cast(float, lane_i(__builtin_bit_cast(int, x), i));
+    };
+    auto real = [&](int i) { return i < cnt && lane_i(page_l, i) >= 0; };
+    load_k(lane_i(page_l, 0), key_of(0), real(0));
+    load_v(lane_i(page_l, 0), key_of(0), real(0));
+    for (int i = 0; i < cnt; ++i)
+      // (keys on no page: zeros at places that no row sees)
+      compute(real(i) ? key_of(i) : INT_MAX - 2 * kKeys, lane_f(kf_l, i), lane_f(vf_l, i),
+              [&]() { load_k(lane_i(page_l, i + 1), key_of(i + 1), real(i + 1)); },
+              [&]() { load_v(lane_i(page_l, i + 1), key_of(i + 1), real(i + 1)); });
+  }
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    ws.l[rt] += __shfl_xor(ws.l[rt], 16);
+    ws.l[rt] += __shfl_xor(ws.l[rt], 32);
+  }
+}
+
+// 8 dims of an output row.
+__device__ __forceinline__ void store_dims(const AttendArgs& a, int kvh, int row, int first, int d,
+                                           const float (&x)[8], float l) {
+  const int G = a.Hq / a.pg.Hkv;
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  *(uint4*)(a.o + ((int64_t)(kvh * G + row % G) * a.tk.T + first + row / G) * kHeadDim + d) =
+      make_uint4(pack_bf16x2(x[0] * inv, x[1] * inv), pack_bf16x2(x[2] * inv, x[3] * inv),
+                 pack_bf16x2(x[4] * inv, x[5] * inv), pack_bf16x2(x[6] * inv, x[7] * inv));
+}
+
+// Keys of sequence s that the table has room for.
+template <int P>
+__device__ __forceinline__ int keys_of(const AttendArgs& a, int s) {
+  return (int)min((int64_t)max(a.lengths[s], 0), (int64_t)a.pg.max_pages * P);
+}
+
+// The sums of a workgroup's waves over different keys of the same rows, joined
+// in LDS; `out` gets row (in the item), dims d .. d + 7 of it, m, l and the sums.
+template <int WAVES>
+struct MergeSmem {
+  static constexpr int kPitch = kHeadDim + 4;   // (a row's start moves on by 4 banks)
+  float m[WAVES][kRows], l[WAVES][kRows];
+  __attribute__((aligned(16))) float o[WAVES][kRows * kPitch];
+};
+template <int RT, int WAVES, class Out>
+__device__ __forceinline__ void merge_waves(MergeSmem<WAVES>& sm, const WaveSums<RT>& ws, int rows,
+                                            Out out) {
+  constexpr int kPitch = MergeSmem<WAVES>::kPitch;
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave, j = lane & 15, g = lane >> 4;
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt) {
+    if (rt > 0) __syncthreads();   // (the rows before have been read)
+    if (g == 0) {
+      sm.m[wave][j] = ws.m[rt];
+      sm.l[wave][j] = ws.l[rt];
+    }
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      float* at = &sm.o[wave][j * kPitch + 8 * (4 * g + r)];
+      *(float4*)at = make_float4(ws.o[rt][0][r], ws.o[rt][1][r], ws.o[rt][2][r], ws.o[rt][3][r]);
+      *(float4*)(at + 4) = make_float4(ws.o[rt][4][r], ws.o[rt][5][r], ws.o[rt][6][r], ws.o[rt][7][r]);
+    }
+    __syncthreads();
+    const int mr = threadIdx.x >> 4, md = (threadIdx.x & 15) * 8;   // row, dims
+    if (mr < kRows && kRows * rt + mr < rows) {
+      float m = sm.m[0][mr];
+#pragma unroll
+      for (int w = 1; w < WAVES; ++w) m = fmaxf(m, sm.m[w][mr]);
+      float l = 0.0f, acc[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
+#pragma unroll
+      for (int w = 0; w < WAVES; ++w) {
+        const float f = sm.m[w][mr] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(sm.m[w][mr] - m);
+        l += f * sm.l[w][mr];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) acc[e] += f * sm.o[w][mr * kPitch + md + e];
+      }
+      out(kRows * rt + mr, md, m, l, acc);
+    }
+  }
+}
+
+// 8 dims of a part's row.
+template <int RT>
+__device__ __forceinline__ void store_part(const AttendArgs& a, int slot, int row, int d, float m,
+                                           float l, const float (&x)[8]) {
+  const int64_t pr = (int64_t)slot * (kRows * RT) + row;
+  if (d == 0) a.part_ml[pr] = Part{m, l};
+  float* at = a.part_o + pr * kHeadDim + d;
+  *(float4*)at = make_float4(x[0], x[1], x[2], x[3]);
+  *(float4*)(at + 4) = make_float4(x[4], x[5], x[6], x[7]);
+}
+
+constexpr int attend_occupancy(int rt) { return rt == 1 ? 3 : 2; }   // waves a SIMD holds
+
+// Short tables: a workgroup per item, its waves merged through LDS.
+template <int FMT, int P, int RT, int WAVES>
+__global__ __launch_bounds__(WAVES* kWave, attend_occupancy(RT)) void attend_kernel(AttendArgs a, int per_seq,
+                                                                int64_t item0) {
+  __shared__ MergeSmem<WAVES> sm;
+  const int64_t item = item0 + blockIdx.x;
+  const int G = a.Hq / a.pg.Hkv, kvh = (int)(item % a.pg.Hkv);
+  int s, tile, first, n;
+  find_slot(a.tk, (int)(item / a.pg.Hkv), per_seq, G, kRows * RT, 1, s, tile);
+  seq_rows(a.tk, s, first, n);
+  const int row0 = tile * kRows * RT, rows = n * G;
+  if (row0 >= rows) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  WaveSums<RT> ws;
+  attend_steps<FMT, P, RT>(a, s, kvh, row0, first, n, a.lengths[s], 0, keys_of<P>(a, s), wave, WAVES,
+                           ws);
+  merge_waves<RT>(sm, ws, rows - row0, [&](int r, int d, float, float l, const float (&x)[8]) {
+    store_dims(a, kvh, row0 + r, first, d, x, l);
+  });
+}
+
+// Long tables, whose sequences may be of any lengths: the device decides.
+//
+// By item, a workgroup each, where the longest item is no longer than what a
+// CU takes of all of them: a CU takes a step in about 0.24 us alone, the chip
+// together one in 1.34 ns, and sharing costs about 5 us more.
+//
+// Otherwise the items' steps are dealt out evenly over kShareGroups x kWaves
+// waves.  With the items one behind the other (by sequence, KV head and row
+// tile), each kItemCost steps longer than it is (what a wave waits for before an
+// item's first step), every wave takes an equal run of them: a last part of an
+// item, whole items, a first part of one.  Whole items are written out, parts
+// left for combine_kernel: nothing in here waits for another wave, except where
+// the runs of a workgroup's waves lie in one item: they then share the item's
+// steps and leave one part.
+//
+// Each wave adds the sequences up for itself.  Two waves a SIMD are what HBM
+// needs; with three the oldest goes first and the youngest ends a third later (8
+// sequences of up to 128k tokens 248 -> 293 us).
+constexpr int kCus = 256;
+constexpr int kShareGroups = 2 * kCus;
+constexpr int kItemCost = 8;
+constexpr int kShareLeast = 4;   // steps and costs a wave takes at least
+constexpr int kItemSteps = 180;  // steps of the chip in a step of one CU alone
+constexpr int kItemExtra = 3700; // steps of the chip in 5 us
+
+// A value that all lanes share, in scalar registers.
+__device__ __forceinline__ int64_t uniform(int64_t x) {
+  const uint32_t lo = __builtin_amdgcn_readfirstlane((uint32_t)x);
+  const uint32_t hi = __builtin_amdgcn_readfirstlane((uint32_t)((uint64_t)x >> 32));
+  return (int64_t)((uint64_t)hi << 32 | lo);
+}
+
+template <int FMT, int P, int RT>
+__global__ __launch_bounds__(kThreads, attend_occupancy(RT)) void attend_share_kernel(AttendArgs a,
+                                                                                 int groups) {
+  __shared__ MergeSmem<kWaves> sm;
+  const int G = a.Hq / a.pg.Hkv, lane = threadIdx.x % kWave;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int group = (int)blockIdx.x, worker = group * kWaves + wave;
+  const int workers = groups * kWaves;   // of a shared launch
+  auto items_of = [&](int s, int& steps, int& tiles) -> int {
+    int first, n;
+    seq_rows(a.tk, s, first, n);
+    steps = (keys_of<P>(a, s) + kKeys - 1) / kKeys;
+    tiles = (n * G + kRows * RT - 1) / (kRows * RT);
+    return tiles * a.pg.Hkv;
+  };
+  int steps = 0, tiles = 0;
+  // the first 64 sequences stay in registers
+  const int my_items = lane < a.tk.S ? items_of(lane, steps, tiles) : 0, my_steps = steps;
+  int longest = my_items > 0 ? steps : 0;
+  int64_t items = my_items, all_steps = (int64_t)steps * my_items;
+  for (int s = kWave + lane; s < a.tk.S; s += kWave) {
+    const int it = items_of(s, steps, tiles);
+    items += it;
+    all_steps += (int64_t)steps * it;
+    longest = max(longest, it > 0 ? steps : 0);
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    items += __shfl_xor(items, o);
+    all_steps += __shfl_xor(all_steps, o);
+    longest = max(longest, __shfl_xor(longest, o));
+  }
+  items = uniform(items);
+  all_steps = uniform(all_steps);
+  longest = __builtin_amdgcn_readfirstlane(longest);
+  if (lane == 0 && worker < workers) a.split[worker].parts = 0;
+  const bool by_item = (int64_t)longest * kItemSteps <= all_steps + kItemExtra;
+  // (by item: an item is one unit)
+  const int item_cost = by_item ? 1 : kItemCost, step_cost = by_item ? 0 : 1;
+  const int64_t total = by_item ? items : all_steps + items * kItemCost;
+  auto cost_of = [&](int s) -> int64_t {
+    const int it = items_of(s, steps, tiles);
+    return (int64_t)(steps * step_cost + item_cost) * it;
+  };
+  // the sequence that unit u < total lies in, and the unit it starts at
+  int s;
+  int64_t start;
+  auto find = [&](int64_t u) {
+    int64_t before = 0;
+    for (s = 0; s < a.tk.S; s += kWave) {
+      const int64_t cost = s == 0 ? (int64_t)(my_steps * step_cost + item_cost) * my_items
+                                  : s + lane < a.tk.S ? cost_of(s + lane) : 0;
+      int64_t incl = cost;
+#pragma unroll
+      for (int o = 1; o < kWave; o <<= 1) {
+        const int64_t up = __shfl_up(incl, o);
+        if (lane >= o) incl += up;
+      }
+      const uint64_t past = __builtin_amdgcn_ballot_w64(before + incl > u);
+      if (past != 0) {
+        const int at = (int)__builtin_ctzll(past);
+        start = uniform(__shfl(before + incl - cost, at));
+        s = __builtin_amdgcn_readfirstlane(s + at);
+        return;
+      }
+      before += uniform(__shfl(incl, kWave - 1));
+    }
+  };
+  const int64_t even = (total + workers - 1) / workers;
+  const int64_t per = even < kShareLeast ? kShareLeast : even;
+  const int64_t g0 = by_item ? group : group * kWaves * per;
+  const int64_t g1 = by_item ? total : min(g0 + kWaves * per, total);
+  if (g0 >= g1) return;
+  // The units u .. end - 1 of the item that unit u lies in (after cost_of(s)).
+  struct Run {
+    int item, st0, st1;     // of the sequence; its steps
+    int64_t base, next;     // the item's first unit, the one behind it
+    bool none, full;
+  };
+  auto run_at = [&](int64_t u, int64_t end) -> Run {
+    const int whole = steps * step_cost + item_cost;
+    const int off = (int)(u - start), at = off % whole;
+    const int to = (int)min((int64_t)whole, at + (end - u));
+    Run r;
+    r.item = off / whole;
+    r.st0 = by_item ? 0 : max(at - kItemCost, 0);
+    r.st1 = by_item ? steps : max(to - kItemCost, 0);
+    r.base = u - at;
+    r.next = r.base + whole;
+    // without steps it is none (an item without keys counts with its last unit)
+    r.none = steps == 0 ? to < whole : r.st0 == r.st1;
+    r.full = r.st0 == 0 && r.st1 == steps;
+    return r;
+  };
+  // Leaves the list of an item's parts, the first of which is at `slot`, left
+  // by wave w0 or, with `joint`, by this workgroup's waves together.
+  auto leave_item = [&](const Run& r, int kvh, int row0, int slot, int w0, bool joint) {
+    const int last = (int)((r.next - 1) / per), last_group = last / kWaves;
+    int64_t last_end = (last_group + 1) * kWaves * per;
+    if (last_end > total) last_end = total;
+    SplitItem it{};
+    it.s = s;
+    it.kvh = kvh;
+    it.row0 = row0;
+    it.first_slot = slot;
+    it.group = group + 1;
+    it.n_waves = joint ? 1 : min((group + 1) * kWaves - 1, last) - w0 + 1;
+    it.last = last_group * kWaves;
+    int n_last = 0;
+    if (last_group > group) {
+      const bool joint_last = last_end <= r.next;
+      it.n_groups = last_group - group - 1 + (joint_last ? 1 : 0);
+      n_last = joint_last ? 0 : last - it.last + 1;
+    }
+    it.parts = it.n_waves + it.n_groups + n_last;
+    a.split[w0] = it;
+  };
+
+  find(g0);
+  if (s >= a.tk.S) return;
+  cost_of(s);
+  // whether the workgroup's waves go together: over items, or over the one that
+  // all their runs lie in
+  const bool joint = by_item || g1 <= run_at(g0, g1).next;
+  const int64_t u0 = joint ? g0 : worker * per, u1 = joint ? g1 : min(u0 + per, total);
+  if (u0 >= u1) return;
+  if (!joint && wave > 0) find(u0);
+  for (int64_t u = u0; u < u1 && s < a.tk.S;) {
+    const int64_t cost = cost_of(s);
+    if (u >= start + cost) {   // (also past sequences without new tokens: they cost nothing)
+      start += cost;
+      ++s;
+      continue;
+    }
+    const Run r = run_at(u, u1);
+    const int first_worker = joint ? group * kWaves : worker;
+    const int slot = 2 * first_worker + (u == u0 ? 0 : 1);
+    u = by_item ? u + gridDim.x : r.next;
+    if (r.none) continue;
+    int first, n;
+    seq_rows(a.tk, s, first, n);
+    const int kvh = r.item / tiles, row0 = r.item % tiles * kRows * RT;
+    if (!r.full && r.st0 == 0 && lane == 0 && (!joint || wave == 0))
+      leave_item(r, kvh, row0, slot, first_worker, joint);
+    WaveSums<RT> ws;
+    attend_steps<FMT, P, RT>(a, s, kvh, row0, first, n, a.lengths[s], r.st0 * kKeys,
+                             min(r.st1 * kKeys, keys_of<P>(a, s)), joint ? wave : 0,
+                             joint ? kWaves : 1, ws);
+    auto store = [&](int row, int d, float m, float l, const float (&x)[8]) {
+      if (r.full) store_dims(a, kvh, row0 + row, first, d, x, l);
+      else store_part<RT>(a, slot, row, d, m, l, x);
+    };
+    if (joint) {
+      __syncthreads();   // (the rows before have been read)
+      merge_waves<RT>(sm, ws, n * G - row0, store);
+    } else {
+      const int j = lane & 15, g = lane >> 4;
+#pragma unroll
+      for (int rt = 0; rt < RT; ++rt) {
+        const int row = kRows * rt + j;
+        if (row0 + row >= n * G) continue;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          float x[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) x[i] = ws.o[rt][i][q];
+          store(row, 8 * (4 * g + q), ws.m[rt], ws.l[rt], x);
+        }
       }
     }
   }
-
-  // merge the waves
-  l_i += __shfl_xor(l_i, 16);
-  l_i += __shfl_xor(l_i, 32);
-  if (g == 0) {
-    sm[wave][j] = m_i;
-    sl[wave][j] = l_i;
-  }
-#pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    float* at = &so[wave][j * kHeadDim + 8 * (4 * g + r)];
-    *(float4*)at = make_float4(oacc[0][r], oacc[1][r], oacc[2][r], oacc[3][r]);
-    *(float4*)(at + 4) = make_float4(oacc[4][r], oacc[5][r], oacc[6][r], oacc[7][r]);
-  }
-  __syncthreads();
-  const int mr = threadIdx.x >> 4, md = (threadIdx.x & 15) * 8;   // row, dims
-  float m = sm[0][mr];
-#pragma unroll
-  for (int w = 1; w < kWaves; ++w) m = fmaxf(m, sm[w][mr]);
-  float l = 0.0f, acc[8];
-#pragma unroll
-  for (int e = 0; e < 8; ++e) acc[e] = 0.0f;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    const float f = sm[w][mr] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(sm[w][mr] - m);
-    l += f * sl[w][mr];
-#pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e] += f * so[w][mr * kHeadDim + md + e];
-  }
-  if (row0 + mr >= n * G) return;
-  if (n_split > 1) {
-    const int64_t pr = unit * kRows + mr;
-    if (md == 0) part_ml[pr] = Part{m, l};
-#pragma unroll
-    for (int e = 0; e < 8; e += 4)
-      *(float4*)(part_o + pr * kHeadDim + md + e) =
-          make_float4(acc[e], acc[e + 1], acc[e + 2], acc[e + 3]);
-    return;
-  }
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  const int mt = (row0 + mr) / G, mh = kvh * G + (row0 + mr) % G;
-  *(uint4*)(o + ((int64_t)mh * tk.T + first + mt) * kHeadDim + md) =
-      make_uint4(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv),
-                 pack_bf16x2(acc[4] * inv, acc[5] * inv), pack_bf16x2(acc[6] * inv, acc[7] * inv));
 }
 
-// The parts of each row joined, in order.
-__global__ __launch_bounds__(kThreads) void combine_kernel(
-    Tokens tk, int Hq, int Hkv, int per_seq, int n_split, const Part* __restrict__ part_ml,
-    const float* __restrict__ part_o, uint16_t* __restrict__ o, int64_t item0) {
-  const int G = Hq / Hkv;
-  const int64_t item = item0 + blockIdx.x;
-  const int kvh = (int)(item % Hkv);
-  int s, tile, first, n;
-  find_slot(tk, (int)(item / Hkv), per_seq, G, kRows, 1, s, tile);
-  seq_rows(tk, s, first, n);
-  const int mr = threadIdx.x >> 4, md = (threadIdx.x & 15) * 8;
-  const int row = tile * kRows + mr;
-  if (row >= n * G) return;
-  float m = -INFINITY;
-  for (int w = 0; w < n_split; ++w) m = fmaxf(m, part_ml[(item * n_split + w) * kRows + mr].m);
-  float l = 0.0f, acc[8] = {};
-  for (int w = 0; w < n_split; ++w) {
-    const int64_t pr = (item * n_split + w) * kRows + mr;
-    const Part ml = part_ml[pr];
-    const float f = ml.m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml.m - m);
-    l += f * ml.l;
+// The parts of a shared item joined, in the order of their keys.  A workgroup
+// looks after 8 rows of the items that kWaves workers left, at once: a group of
+// 32 lanes adds up a row's 128 dims over every stripes-th part, then the stripes
+// are added up in order.
+constexpr int kCombineThreads = 1024;
+constexpr int kCombineRows = 8;
+constexpr int kCombineAhead = 8;   // parts in flight per group
+__global__ __launch_bounds__(kCombineThreads) void combine_kernel(AttendArgs a, int tile_rows) {
+  constexpr int kGroups = kCombineThreads / 32;
+  __shared__ float sm_m[kGroups], sm_l[kGroups];
+  __shared__ __attribute__((aligned(16))) float sm_o[kGroups][kHeadDim];
+  const int G = a.Hq / a.pg.Hkv;
+  const int grp = threadIdx.x / 32, d = (threadIdx.x % 32) * 4;
+  // one item: all groups take it; several: a share of the groups each
+  int parts[kWaves], items = 0, only = 0;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) acc[e] += f * part_o[pr * kHeadDim + md + e];
+  for (int w = 0; w < kWaves; ++w) {
+    parts[w] = a.split[(int)blockIdx.x * kWaves + w].parts;
+    if (parts[w] > 0) {
+      ++items;
+      only = w;
+    }
+  }
+  if (items == 0) return;
+  const int mine = items == 1 ? kGroups : kGroups / kWaves;
+  const int w = items == 1 ? only : grp / mine;
+  const int worker = (int)blockIdx.x * kWaves + w;
+  SplitItem it{};
+  int first = 0, n = 0;
+  if (a.split[worker].parts > 0) {   // (else nothing else of it is set)
+    it = a.split[worker];
+    seq_rows(a.tk, it.s, first, n);
+  }
+  const int r0 = (int)blockIdx.y * kCombineRows;
+  const int rows = min(min(n * G - it.row0, tile_rows) - r0, kCombineRows);
+  auto slot_row = [&](int p, int r) -> int64_t {
+    int slot = it.first_slot;
+    if (p >= it.n_waves + it.n_groups) slot = 2 * (it.last + p - it.n_waves - it.n_groups);
+    else if (p >= it.n_waves) slot = 2 * kWaves * (it.group + p - it.n_waves);
+    else if (p > 0) slot = 2 * (worker + p);
+    return (int64_t)slot * tile_rows + r0 + r;
+  };
+  // rows by the power of two above them, the rest of the groups in stripes
+  int lanes_r = 1;
+  while (lanes_r < rows) lanes_r *= 2;   // (at most 8)
+  const int stripes = mine / lanes_r, at = grp % mine, stripe = at / lanes_r, r = at % lanes_r;
+  float m = -INFINITY, l = 0.0f;
+  float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  if (r < rows)
+    for (int p0 = stripe; p0 < it.parts; p0 += stripes * kCombineAhead) {
+      Part ml[kCombineAhead];
+      float4 x[kCombineAhead];
+#pragma unroll
+      for (int k = 0; k < kCombineAhead; ++k) {
+        const int64_t pr = slot_row(min(p0 + k * stripes, it.parts - 1), r);
+        ml[k] = a.part_ml[pr];
+        x[k] = *(const float4*)(a.part_o + pr * kHeadDim + d);
+      }
+#pragma unroll
+      for (int k = 0; k < kCombineAhead; ++k) {
+        if (p0 + k * stripes >= it.parts) break;
+        const float mn = fmaxf(m, ml[k].m);
+        const float f = m == mn ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
+        const float h = ml[k].m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml[k].m - mn);
+        l = l * f + ml[k].l * h;
+        acc.x = acc.x * f + x[k].x * h;
+        acc.y = acc.y * f + x[k].y * h;
+        acc.z = acc.z * f + x[k].z * h;
+        acc.w = acc.w * f + x[k].w * h;
+        m = mn;
+      }
+    }
+  if (d == 0) {
+    sm_m[grp] = m;
+    sm_l[grp] = l;
+  }
+  *(float4*)&sm_o[grp][d] = acc;
+  __syncthreads();
+  if (stripe != 0 || r >= rows) return;
+  for (int k = 1; k < stripes; ++k) m = fmaxf(m, sm_m[grp + k * lanes_r]);
+  l = 0.0f;
+  acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  for (int k = 0; k < stripes; ++k) {
+    const int from = grp + k * lanes_r;
+    const float h = sm_m[from] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(sm_m[from] - m);
+    const float4 x = *(const float4*)&sm_o[from][d];
+    l += sm_l[from] * h;
+    acc.x += x.x * h;
+    acc.y += x.y * h;
+    acc.z += x.z * h;
+    acc.w += x.w * h;
   }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  *(uint4*)(o + ((int64_t)(kvh * G + row % G) * tk.T + first + row / G) * kHeadDim + md) =
-      make_uint4(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv),
-                 pack_bf16x2(acc[4] * inv, acc[5] * inv), pack_bf16x2(acc[6] * inv, acc[7] * inv));
+  const int row = it.row0 + r0 + r;
+  *(uint2*)(a.o + ((int64_t)(it.kvh * G + row % G) * a.tk.T + first + row / G) * kHeadDim + d) =
+      make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
 }
 
 // ----------------------------------------------------------------------------
@@ -558,34 +994,73 @@ Pages pages_of(const ei_cache_shape& c, const ei_cache_pages& p, const int32_t* 
                c.n_pages, cols,          c.n_kv_heads, c.page_len};
 }
 
+constexpr int kShortKeys = 2048;   // a table of no more keys: one workgroup per item
+constexpr int kShortWaves = 4;
+constexpr int kItemGroups = 16384;
+
 struct AttendPlan {
-  int per_seq, n_split;
+  int rt, per_seq, item_rows;   // item_rows: of an item, at most
+  int groups;                   // workgroups of the shared launch, 0: one per item
   int64_t items;
-  size_t ml_bytes, bytes;
+  size_t ml_bytes, split_bytes, bytes;
+  bool fits;
 };
-// n_split: enough workgroups for the chip, at least 256 keys each.
 AttendPlan attend_plan(int Hq, int n_tokens, bool ragged, int n_seqs, int max_pages,
                        const ei_cache_shape& c) {
   const int64_t G = Hq / c.n_kv_heads;
   AttendPlan p{};
-  int64_t slots;
+  // rows of a tile: 16, or 32 where a sequence has more than 16 (on average)
+  p.rt = (int64_t)n_tokens * G > (int64_t)kRows * n_seqs ? 2 : 1;
+  const int tile = p.item_rows = kRows * p.rt;
+  int64_t slots, tiles;   // row tiles of all sequences, of one
   if (ragged) {
-    slots = (int64_t)n_tokens * G / kRows + n_seqs;
+    slots = (int64_t)n_tokens * G / tile + n_seqs;
+    tiles = (int64_t)n_tokens * G / tile + 1;
   } else {
-    p.per_seq = (int)((n_tokens / n_seqs * G + kRows - 1) / kRows);
-    slots = (int64_t)n_seqs * p.per_seq;
+    tiles = (n_tokens / n_seqs * G + tile - 1) / tile;
+    p.per_seq = (int)tiles;
+    if (n_tokens / n_seqs * G < tile) p.item_rows = (int)(n_tokens / n_seqs * G);
+    slots = n_seqs * tiles;
   }
   p.items = slots * c.n_kv_heads;
-  const int64_t most = ((int64_t)max_pages * c.page_len + 255) / 256;
-  int64_t sp = p.items > 0 ? (1024 + p.items - 1) / p.items : 1;
-  if (sp > most) sp = most;
-  p.n_split = (int)(sp < 1 ? 1 : sp);
-  if (p.n_split > 1) {
-    const size_t rows = (size_t)p.items * p.n_split * kRows;
+  const int64_t keys = (int64_t)max_pages * c.page_len;
+  const int64_t cost = keys / kKeys + kItemCost;   // of an item, at most
+  p.fits = p.items <= INT_MAX && cost <= INT_MAX / (tiles * c.n_kv_heads);
+  if (keys > kShortKeys && p.fits) {
+    const int64_t waves = (p.items * cost + kShareLeast - 1) / kShareLeast;
+    const int64_t most = (waves + kWaves - 1) / kWaves;
+    p.groups = (int)(most < kShareGroups ? most : kShareGroups);
+    const size_t workers = (size_t)p.groups * kWaves, rows = workers * 2 * tile;
+    p.split_bytes = (workers * sizeof(SplitItem) + 255) / 256 * 256;
     p.ml_bytes = (rows * sizeof(Part) + 255) / 256 * 256;
-    p.bytes = p.ml_bytes + rows * kHeadDim * sizeof(float);
+    p.bytes = p.split_bytes + p.ml_bytes + rows * kHeadDim * sizeof(float);
   }
   return p;
+}
+
+template <int FMT, int P, int RT>
+void launch_attend_t(const AttendPlan& pl, const AttendArgs& a, hipStream_t stream) {
+  if (pl.groups) {
+    // (by item: a workgroup for each, up to some number)
+    const int64_t by_item = pl.items < kItemGroups ? pl.items : kItemGroups;
+    hipLaunchKernelGGL((attend_share_kernel<FMT, P, RT>),
+                       dim3((unsigned)(pl.groups > by_item ? pl.groups : by_item)), dim3(kThreads),
+                       0, stream, a, pl.groups);
+    const unsigned row_blocks = (unsigned)((pl.item_rows + kCombineRows - 1) / kCombineRows);
+    hipLaunchKernelGGL(combine_kernel, dim3((unsigned)pl.groups, row_blocks), dim3(kCombineThreads),
+                       0, stream, a, kRows * RT);
+    return;
+  }
+  constexpr int64_t kMost = (1ll << 31) / (kShortWaves * kWave);
+  for (int64_t i = 0; i < pl.items; i += kMost)
+    hipLaunchKernelGGL((attend_kernel<FMT, P, RT, kShortWaves>),
+                       dim3((unsigned)(pl.items - i < kMost ? pl.items - i : kMost)),
+                       dim3(kShortWaves * kWave), 0, stream, a, pl.per_seq, i);
+}
+template <int FMT, int P>
+void launch_attend(const AttendPlan& pl, const AttendArgs& a, hipStream_t stream) {
+  if (pl.rt == 1) launch_attend_t<FMT, P, 1>(pl, a, stream);
+  else launch_attend_t<FMT, P, 2>(pl, a, stream);
 }
 
 }  // namespace
@@ -636,6 +1111,8 @@ size_t ei_cache_attn_workspace_bytes(int32_t n_q_heads, int32_t n_tokens, int32_
   if (ei::check_shape(shape) != EI_OK || n_q_heads <= 0 || n_q_heads % shape.n_kv_heads ||
       n_tokens <= 0 || n_seqs <= 0 || max_pages <= 0 || (!packed && n_tokens % n_seqs))
     return 0;
+  if ((int64_t)n_tokens * n_q_heads > INT_MAX || (int64_t)max_pages * shape.page_len > INT_MAX)
+    return 0;
   return ei::attend_plan(n_q_heads, n_tokens, packed != 0, n_seqs, max_pages, shape).bytes;
 }
 
@@ -655,7 +1132,7 @@ ei_status ei_cache_attn(const uint16_t* q, int32_t n_q_heads, int32_t n_tokens,
   if (n_tokens == 0 || n_seqs == 0) return EI_OK;
   const ei::AttendPlan pl = ei::attend_plan(n_q_heads, n_tokens, cu_seqlens != nullptr, n_seqs,
                                             max_pages, shape);
-  if (pl.items > INT_MAX) return EI_ERR_SHAPE;
+  if (!pl.fits) return EI_ERR_SHAPE;
   if (!q || !o || !lengths || !page_table) return EI_ERR_NULL;
   if ((st = ei::check_pages(pages)) != EI_OK) return st;
   if (!ei::aligned(q, 16) || !ei::aligned(o, 16) || !ei::aligned(lengths, 4) ||
@@ -665,28 +1142,19 @@ ei_status ei_cache_attn(const uint16_t* q, int32_t n_q_heads, int32_t n_tokens,
   if (!ei::aligned(workspace, 16)) return EI_ERR_UNSUPPORTED;
   const ei::Tokens tk{cu_seqlens, n_tokens, n_seqs, n_tokens / n_seqs};
   const ei::Pages pg = ei::pages_of(shape, pages, page_table, max_pages);
-  const float sc_log2 = (float)((double)softmax_scale * 1.4426950408889634);
-  ei::Part* ml = (ei::Part*)workspace;
-  float* po = (float*)((char*)workspace + pl.ml_bytes);
-  const int64_t units = pl.items * pl.n_split;
+  char* ws = (char*)workspace;
+  const ei::AttendArgs a{q, o, tk, lengths, pg, n_q_heads,
+                         (float)((double)softmax_scale * 1.4426950408889634),
+                         (ei::Part*)(ws + pl.split_bytes),
+                         (float*)(ws + pl.split_bytes + pl.ml_bytes), (ei::SplitItem*)ws};
   hipStream_t s0 = (hipStream_t)stream;
-  for (int64_t u = 0; u < units; u += ei::kMaxGrid) {
-    const dim3 grid(ei::launch_grid(units - u)), block(ei::kThreads);
-#define EI_ATTEND(F, PL)                                                                       \
-  hipLaunchKernelGGL((ei::attend_kernel<F, PL>), grid, block, 0, s0, q, tk, lengths, pg,       \
-                     n_q_heads, pl.per_seq, pl.n_split, sc_log2, o, ml, po, u)
-    if (shape.format == EI_CACHE_E4M3) {
-      if (shape.page_len == 64) EI_ATTEND(EI_CACHE_E4M3, 64); else EI_ATTEND(EI_CACHE_E4M3, 128);
-    } else {
-      if (shape.page_len == 64) EI_ATTEND(EI_CACHE_INT8, 64); else EI_ATTEND(EI_CACHE_INT8, 128);
-    }
-#undef EI_ATTEND
+  if (shape.format == EI_CACHE_E4M3) {
+    if (shape.page_len == 64) ei::launch_attend<EI_CACHE_E4M3, 64>(pl, a, s0);
+    else ei::launch_attend<EI_CACHE_E4M3, 128>(pl, a, s0);
+  } else {
+    if (shape.page_len == 64) ei::launch_attend<EI_CACHE_INT8, 64>(pl, a, s0);
+    else ei::launch_attend<EI_CACHE_INT8, 128>(pl, a, s0);
   }
-  if (pl.n_split > 1)
-    for (int64_t u = 0; u < pl.items; u += ei::kMaxGrid)
-      hipLaunchKernelGGL(ei::combine_kernel, dim3(ei::launch_grid(pl.items - u)),
-                         dim3(ei::kThreads), 0, s0, tk, n_q_heads, shape.n_kv_heads, pl.per_seq,
-                         pl.n_split, ml, po, o, u);
   return ei::from_hip(hipGetLastError());
 }
 

@@ -308,12 +308,28 @@ def test_attn_wide_table():
 
 
 @pytest.mark.parametrize("dtype", [E4M3, INT8])
+@pytest.mark.parametrize("hq,hkv", [(4, 1), (16, 2), (24, 1)])
+@pytest.mark.parametrize("held,new", [
+    ([30] * 5, [1, 0, 3, 0, 2]),                       # items alike: a workgroup each
+    ([0, 0, 1500, 0, 3], [1, 0, 2, 5, 0]),             # one far longer than the others
+    ([7, 2500, 64, 0, 0, 900], [0, 1, 9, 0, 0, 1]),
+    ([5] * 70 + [1100], [i % 2 for i in range(70)] + [3]),
+    ([2000] + [1] * 130, [1] + [0] * 129 + [4]),       # the last of many without tokens
+])
+def test_attn_wide_table_of_ragged_sequences(held, new, hq, hkv, dtype):
+    """The launches that find their share of the work on the device."""
+    run_attn(held, new, hq, hkv, 64, dtype, spare=40)
+
+
+@pytest.mark.parametrize("dtype", [E4M3, INT8])
 def test_attn_rows_without_keys(dtype):
     """Length zero, and queries before the first position."""
     def edit(pages, table, lengths):
         lengths[0], lengths[1] = 0, 2      # 1 and 5 queries
         lengths[2] = -4
+    wide = run_attn([3, 10, 8], [1, 5, 2], 4, 2, 64, dtype, edit=edit, spare=100)
     got = run_attn([3, 10, 8], [1, 5, 2], 4, 2, 64, dtype, edit=edit)
+    assert bool((wide[0, :, [0, 1, 2, 3, 6, 7]] == 0).all())
     assert bool((got[0, :, [0, 1, 2, 3, 6, 7]] == 0).all())
     assert bool((got[0, :, 4:6] != 0).any())
 

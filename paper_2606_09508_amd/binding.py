@@ -570,12 +570,31 @@ def swiglu(g, u, out=None):
 # Packed sequences and the paged 8-bit cache
 # --------------------------------------------------------------------------
 
-def _req_packed(t, name: str, tokens: int | None = None) -> None:
-    """bf16 [1, heads, tokens, D]."""
-    _req(t, name, torch.bfloat16, 4)
-    if t.shape[0] != 1 or (tokens is not None and t.shape[2] != tokens):
-        raise ValueError(f"{name} {tuple(t.shape)} is not [1, heads, "
-                         f"{'tokens' if tokens is None else tokens}, head_dim]")
+# (A decoding step makes one store and one attention per layer, of a few us on
+# the GPU each: as above, the good case is one test per tensor.)
+def _good(t, dtype, ndim: int, dev: int) -> bool:
+    return isinstance(t, torch.Tensor) and t.dtype is dtype and t.dim() == ndim \
+        and t.get_device() == dev and t.is_contiguous()
+
+
+def _device_of(t) -> int:
+    """The GPU that t is on, -1 where it is on none (or no tensor)."""
+    return t.get_device() if isinstance(t, torch.Tensor) and t.is_cuda else -1
+
+
+def _req_packed(t, name: str, dev: int) -> None:
+    """bf16 [1, heads, tokens, D] on GPU dev."""
+    if dev < 0 or not _good(t, torch.bfloat16, 4, dev):
+        _req(t, name, torch.bfloat16, 4)
+        raise ValueError(f"tensors on different devices: {name} on {t.device}")
+    if t.shape[0] != 1:
+        raise ValueError(f"{name} {tuple(t.shape)} is not [1, heads, tokens, head_dim]")
+
+
+def _req_i32(t, name: str, ndim: int, dev: int) -> None:
+    if not _good(t, torch.int32, ndim, dev):
+        _req(t, name, torch.int32, ndim)
+        raise ValueError(f"tensors on different devices: {name} on {t.device}")
 
 
 def packed_prefill_attn(q, k, v, cu_seqlens, softmax_scale: float | None = None,
@@ -584,19 +603,22 @@ def packed_prefill_attn(q, k, v, cu_seqlens, softmax_scale: float | None = None,
     that lie one behind the other in q [1, Hq, T, D], k and v [1, Hkv, T, D];
     sequence s is the rows cu_seqlens[s] .. cu_seqlens[s + 1] - 1 (int32, on the
     device).  Rows of ``out`` outside every sequence are left as they were."""
-    for t, n in ((q, "q"), (k, "k"), (v, "v")):
-        _req_packed(t, n)
-    _req(cu_seqlens, "cu_seqlens", torch.int32, 1)
-    check_qkv_shapes(q.shape, k.shape, v.shape)
+    dev = _device_of(q)
+    _req_packed(q, "q", dev)
+    _req_packed(k, "k", dev)
+    _req_packed(v, "v", dev)
+    _req_i32(cu_seqlens, "cu_seqlens", 1, dev)
+    shape = q.shape
+    check_qkv_shapes(shape, k.shape, v.shape)
     if cu_seqlens.numel() < 1:
         raise ValueError("cu_seqlens holds one offset more than there are sequences")
     if out is None:
         out = torch.empty_like(q)
-    _req(out, "out", torch.bfloat16, 4)
-    if out.shape != q.shape:
-        raise ValueError(f"out {tuple(out.shape)} does not match q {tuple(q.shape)}")
-    sc = 1.0 / math.sqrt(q.shape[3]) if softmax_scale is None else float(softmax_scale)
-    _same_device(q, k, v, cu_seqlens, out)
+    else:
+        _req_packed(out, "out", dev)
+        if out.shape != shape:
+            raise ValueError(f"out {tuple(out.shape)} does not match q {tuple(shape)}")
+    sc = 1.0 / math.sqrt(shape[3]) if softmax_scale is None else float(softmax_scale)
     with _on(q):
         st = lib().ei_packed_prefill_attn(_ptr(q), _ptr(k), _ptr(v), dims_of(q, k),
                                           _ptr(cu_seqlens), cu_seqlens.numel() - 1, sc,
@@ -634,36 +656,47 @@ def new_cache_pages(n_pages: int, n_kv_heads: int, page_len: int, head_dim: int 
                                             device=device) for _ in range(2)))
 
 
-def _cache_args(pages, layers: bool = False):
-    """(CacheShape, CachePointers) of checked pages; with ``layers`` the number
-    of layers comes first."""
+@functools.lru_cache(maxsize=256)   # a pure function of five plain integers
+def _cache_shape(n_pages: int, hkv: int, page_len: int, head_dim: int, fmt: int) -> CacheShape:
+    return CacheShape(n_pages, hkv, page_len, head_dim, fmt)
+
+
+def _cache_args(pages, dev: int, layers: bool = False):
+    """(CacheShape, CachePointers) of pages on GPU dev, checked; with ``layers``
+    there may be a leading dimension, whose size then comes first."""
     k, v, ks, vs = pages
-    nd = k.dim() if layers and k.dim() == 5 else 4
-    fmt = CACHE_FORMATS.get(k.dtype)
-    if fmt is None:
-        raise TypeError(f"cache pages are float8_e4m3fn or int8, not {k.dtype}")
-    _req(k, "pages.k", k.dtype, nd)
-    _req(v, "pages.v", k.dtype, nd)
-    _req(ks, "pages.k_scale", torch.float32, nd - 2)
-    _req(vs, "pages.v_scale", torch.float32, nd - 2)
-    if v.shape != k.shape or ks.shape != k.shape[:-2] or vs.shape != ks.shape:
-        raise ValueError(f"pages: v {tuple(v.shape)}, k_scale {tuple(ks.shape)} or v_scale "
-                         f"{tuple(vs.shape)} do not match k {tuple(k.shape)}")
-    _same_device(k, v, ks, vs)
-    shape = CacheShape(*k.shape[nd - 4:], fmt)
-    ptrs = CachePointers(_ptr(k), _ptr(v), _ptr(ks), _ptr(vs))
-    return (k.shape[0] if nd == 5 else 1, shape, ptrs) if layers else (shape, ptrs)
+    dtype = k.dtype if isinstance(k, torch.Tensor) else None
+    fmt = CACHE_FORMATS.get(dtype)
+    nd = 5 if layers and fmt is not None and k.dim() == 5 else 4
+    if dev < 0 or fmt is None or not (_good(k, dtype, nd, dev) and _good(v, dtype, nd, dev)
+                                      and _good(ks, torch.float32, nd - 2, dev)
+                                      and _good(vs, torch.float32, nd - 2, dev)):
+        if fmt is None:
+            raise TypeError(f"cache pages are float8_e4m3fn or int8, not {dtype or type(k)}")
+        for t, n, dt, d in ((k, "k", dtype, nd), (v, "v", dtype, nd),
+                            (ks, "k_scale", torch.float32, nd - 2),
+                            (vs, "v_scale", torch.float32, nd - 2)):
+            _req(t, "pages." + n, dt, d)
+        raise ValueError(f"tensors on different devices: pages on {k.device}, {v.device}, "
+                         f"{ks.device}, {vs.device}")
+    shape, lead = k.shape, ks.shape
+    if v.shape != shape or lead != shape[:-2] or vs.shape != lead:
+        raise ValueError(f"pages: v {tuple(v.shape)}, k_scale {tuple(lead)} or v_scale "
+                         f"{tuple(vs.shape)} do not match k {tuple(shape)}")
+    cs = _cache_shape(*shape[nd - 4:], fmt)
+    ptrs = CachePointers(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr())
+    return (shape[0] if nd == 5 else 1, cs, ptrs) if layers else (cs, ptrs)
 
 
-def _sequences(tokens: int, page_table, lengths, cu_seqlens) -> int:
+def _sequences(tokens: int, page_table, lengths, cu_seqlens, dev: int) -> int:
     """The number of sequences, after checks of what describes them."""
-    _req(page_table, "page_table", torch.int32, 2)
-    _req(lengths, "lengths", torch.int32, 1)
+    _req_i32(page_table, "page_table", 2, dev)
+    _req_i32(lengths, "lengths", 1, dev)
     S = lengths.shape[0]
     if page_table.shape[0] != S:
         raise ValueError(f"page_table has {page_table.shape[0]} rows for {S} lengths")
     if cu_seqlens is not None:
-        _req(cu_seqlens, "cu_seqlens", torch.int32, 1)
+        _req_i32(cu_seqlens, "cu_seqlens", 1, dev)
         if cu_seqlens.shape[0] != S + 1:
             raise ValueError(f"cu_seqlens has {cu_seqlens.shape[0]} offsets for {S} sequences")
     elif tokens % S if S else tokens:
@@ -676,19 +709,20 @@ def cache_store(k, v, pages: CachePages, page_table, lengths, cu_seqlens=None) -
     their sequences (page_table int32 [S, max_pages]).  lengths int32 [S] counts
     each sequence's tokens with the new ones; cu_seqlens int32 [S + 1] says
     which rows are whose (None: T / S rows each)."""
-    _req_packed(k, "k")
-    _req_packed(v, "v")
-    if v.shape != k.shape:
-        raise ValueError(f"v {tuple(v.shape)} does not match k {tuple(k.shape)}")
-    shape, ptrs = _cache_args(pages)
-    T = k.shape[2]
-    if k.shape[1] != shape.n_kv_heads or k.shape[3] != shape.head_dim:
-        raise ValueError(f"k {tuple(k.shape)} does not match the pages {tuple(pages.k.shape)}")
-    S = _sequences(T, page_table, lengths, cu_seqlens)
-    _same_device(k, v, pages.k, page_table, lengths, cu_seqlens)
+    dev = _device_of(k)
+    _req_packed(k, "k", dev)
+    _req_packed(v, "v", dev)
+    shape = k.shape
+    if v.shape != shape:
+        raise ValueError(f"v {tuple(v.shape)} does not match k {tuple(shape)}")
+    cs, ptrs = _cache_args(pages, dev)
+    _, hkv, T, D = shape
+    if hkv != cs.n_kv_heads or D != cs.head_dim:
+        raise ValueError(f"k {tuple(shape)} does not match the pages {tuple(pages.k.shape)}")
+    S = _sequences(T, page_table, lengths, cu_seqlens, dev)
     with _on(k):
         st = lib().ei_cache_store(_ptr(k), _ptr(v), T, _ptr(cu_seqlens), S, _ptr(lengths),
-                                  _ptr(page_table), page_table.shape[1], shape, ptrs, _stream(k))
+                                  _ptr(page_table), page_table.shape[1], cs, ptrs, _stream(k))
     _check("ei_cache_store", st)
 
 
@@ -697,45 +731,58 @@ def cache_attn(q, pages: CachePages, page_table, lengths, cu_seqlens=None,
     """ei_cache_attn: attention of each sequence's newest tokens q [1, Hq, T, D]
     over the cache, which holds them already; page_table, lengths and
     cu_seqlens as cache_store.  Returns bf16 [1, Hq, T, D].  ``workspace``
-    (optional, uint8) is scratch of this call alone."""
-    _req_packed(q, "q")
-    shape, ptrs = _cache_args(pages)
-    _, Hq, T, D = q.shape
-    if D != shape.head_dim or Hq % shape.n_kv_heads:
-        raise ValueError(f"q {tuple(q.shape)} does not match the pages {tuple(pages.k.shape)}")
-    S = _sequences(T, page_table, lengths, cu_seqlens)
+    (optional, uint8, of cache_attn_workspace_bytes) is scratch of this call."""
+    dev = _device_of(q)
+    _req_packed(q, "q", dev)
+    cs, ptrs = _cache_args(pages, dev)
+    _, Hq, T, D = shape = q.shape
+    if D != cs.head_dim or Hq % cs.n_kv_heads:
+        raise ValueError(f"q {tuple(shape)} does not match the pages {tuple(pages.k.shape)}")
+    S = _sequences(T, page_table, lengths, cu_seqlens, dev)
     if out is None:
         out = torch.empty_like(q)
-    _req(out, "out", torch.bfloat16, 4)
-    if out.shape != q.shape:
-        raise ValueError(f"out {tuple(out.shape)} does not match q {tuple(q.shape)}")
-    _same_device(q, pages.k, page_table, lengths, out, cu_seqlens)
+    else:
+        _req_packed(out, "out", dev)
+        if out.shape != shape:
+            raise ValueError(f"out {tuple(out.shape)} does not match q {tuple(shape)}")
     cols = page_table.shape[1]
+    L = lib()
     if workspace is None:
-        need = lib().ei_cache_attn_workspace_bytes(Hq, T, cu_seqlens is not None, S, cols, shape)
-        workspace = torch.empty((need,), dtype=torch.uint8, device=q.device) if need else None
+        nb = L.ei_cache_attn_workspace_bytes(Hq, T, cu_seqlens is not None, S, cols, cs)
+        if nb:
+            workspace = torch.empty((nb,), dtype=torch.uint8, device=q.device)
     else:
         _same_device(q, workspace)
-    nb = 0 if workspace is None else workspace.numel() * workspace.element_size()
+        if not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous")
+        nb = workspace.numel() * workspace.element_size()
     sc = 1.0 / math.sqrt(D) if softmax_scale is None else float(softmax_scale)
     with _on(q):
-        st = lib().ei_cache_attn(_ptr(q), Hq, T, _ptr(cu_seqlens), S, _ptr(lengths),
-                                 _ptr(page_table), cols, shape, ptrs, sc, _ptr(out),
-                                 _ptr(workspace), nb, _stream(q))
+        st = L.ei_cache_attn(_ptr(q), Hq, T, _ptr(cu_seqlens), S, _ptr(lengths),
+                             _ptr(page_table), cols, cs, ptrs, sc, _ptr(out), _ptr(workspace), nb,
+                             _stream(q))
     _check("ei_cache_attn", st)
     return out
+
+
+def cache_attn_workspace_bytes(n_q_heads: int, n_tokens: int, packed: bool, n_seqs: int,
+                               max_pages: int, pages: CachePages) -> int:
+    """Bytes of the workspace that cache_attn takes for such a call (``packed``:
+    with cu_seqlens)."""
+    shape = _cache_shape(*pages.k.shape[-4:], CACHE_FORMATS[pages.k.dtype])
+    return int(lib().ei_cache_attn_workspace_bytes(n_q_heads, n_tokens, packed, n_seqs, max_pages,
+                                                   shape))
 
 
 def cache_copy(pages: CachePages, src, dst) -> None:
     """ei_cache_copy: page dst[i] = page src[i] (int32 lists on the device) in
     every layer of the pages.  dst must hold each page once and none of src."""
-    layers, shape, ptrs = _cache_args(pages, layers=True)
-    _req(src, "src", torch.int32, 1)
-    _req(dst, "dst", torch.int32, 1)
+    dev = _device_of(pages[0])
+    layers, cs, ptrs = _cache_args(pages, dev, layers=True)
+    _req_i32(src, "src", 1, dev)
+    _req_i32(dst, "dst", 1, dev)
     if src.shape != dst.shape:
         raise ValueError(f"{src.numel()} source pages for {dst.numel()} destinations")
-    _same_device(pages.k, src, dst)
     with _on(src):
-        st = lib().ei_cache_copy(shape, layers, ptrs, _ptr(src), _ptr(dst), src.numel(),
-                                 _stream(src))
+        st = lib().ei_cache_copy(cs, layers, ptrs, _ptr(src), _ptr(dst), src.numel(), _stream(src))
     _check("ei_cache_copy", st)

@@ -26,18 +26,11 @@ typedef float f32x2 __attribute__((ext_vector_type(2)));
 
 // Loads and stores of data that a launch touches once.
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint4 load_once4(const void* p) {
   return __builtin_bit_cast(uint4, __builtin_nontemporal_load((const u32x4*)p));
 }
-__device__ __forceinline__ uint2 load_once2(const void* p) {
-  return __builtin_bit_cast(uint2, __builtin_nontemporal_load((const u32x2*)p));
-}
 __device__ __forceinline__ void store_once4(void* p, uint4 w) {
   __builtin_nontemporal_store(__builtin_bit_cast(u32x4, w), (u32x4*)p);
-}
-__device__ __forceinline__ void store_once2(void* p, uint2 w) {
-  __builtin_nontemporal_store(__builtin_bit_cast(u32x2, w), (u32x2*)p);
 }
 
 __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
@@ -100,12 +93,12 @@ __device__ __forceinline__ int page_at(const Pages& pg, int s, int c) {
 }
 
 // ----------------------------------------------------------------------------
-// Store.  One workgroup takes one page of one KV head and one of K and V: the
-// largest magnitude of the new rows (as integers: bf16 magnitudes are ordered
-// like their bits), the scale, the codes; each element is read once and kept
-// in registers in between.  Where the page held rows of the sequence already
-// and the scale grows, those are rounded again: by powers of two, so an e4m3
-// code changes only where it leaves the normal range, and int8 errors of all
+// Store.  One workgroup takes a page of one KV head, K and V: the largest
+// magnitude of the new rows (as integers: bf16 magnitudes are ordered like
+// their bits), the scale, the codes; each element is read once and kept in
+// registers in between.  Where the page held rows of the sequence already and
+// the scale grows, those are rounded again: by powers of two, so an e4m3 code
+// changes only where it leaves the normal range, and int8 errors of all
 // roundings together stay below one step (1/2 + 1/4 + ...).
 // ----------------------------------------------------------------------------
 template <int FMT>
@@ -145,19 +138,18 @@ __device__ __forceinline__ void decode4(uint32_t w, float (&f)[4]) {
   }
 }
 
-// P / 16 chunks of 8 elements per thread.
+// P / 16 chunks of 8 elements of K and of V per thread.
 template <int FMT, int P>
 __global__ __launch_bounds__(kThreads) void store_kernel(const uint16_t* __restrict__ k,
                                                          const uint16_t* __restrict__ v, Tokens tk,
                                                          const int32_t* __restrict__ lengths,
                                                          Pages pg, int per_seq, int64_t unit0) {
   constexpr int CH = P * kHeadDim / 8 / kThreads;
-  __shared__ uint32_t part[kWaves];
+  __shared__ uint32_t part[2][kWaves];
   const int64_t unit = unit0 + blockIdx.x;
-  const int side = (int)(unit & 1);
-  const int h = (int)((unit >> 1) % pg.Hkv);
+  const int h = (int)(unit % pg.Hkv);
   int s, i, first, n;
-  find_slot(tk, (int)((unit >> 1) / pg.Hkv), per_seq, 1, P, 2, s, i);
+  find_slot(tk, (int)(unit / pg.Hkv), per_seq, 1, P, 2, s, i);
   seq_rows(tk, s, first, n);
   const int64_t begin = (int64_t)lengths[s] - n;      // position of the first new token
   const int64_t from = begin > 0 ? begin : 0;         // (tokens before position 0 are dropped)
@@ -169,56 +161,66 @@ __global__ __launch_bounds__(kThreads) void store_kernel(const uint16_t* __restr
   const int page = page_at(pg, s, (int)c);
   if (page < 0) return;
   const int64_t hp = (int64_t)page * pg.Hkv + h;
-  float* sp = (side ? pg.vs : pg.ks) + hp;
-  uint8_t* dst = (side ? pg.v : pg.k) + hp * P * kHeadDim;
-  const uint16_t* src = (side ? v : k) +
-                        ((int64_t)h * tk.T + first + (c * P - begin)) * kHeadDim;   // row 0
-  const float s_old = r0 > 0 ? *sp : 0.0f;
-  uint4 w[CH];
-  uint32_t top = 0;
+  const int64_t src = ((int64_t)h * tk.T + first + (c * P - begin)) * kHeadDim;   // row 0
+  float* const scales[2] = {pg.ks + hp, pg.vs + hp};
+  const float s_old[2] = {r0 > 0 ? *scales[0] : 0.0f, r0 > 0 ? *scales[1] : 0.0f};
+  uint4 w[2][CH];
 #pragma unroll
-  for (int j = 0; j < CH; ++j) {
-    const int ch = threadIdx.x + j * kThreads, r = ch >> 4;
-    if (r >= r0 && r < r1) {
-      w[j] = *(const uint4*)(src + (int64_t)ch * 8);
-      const uint32_t ww[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
+  for (int side = 0; side < 2; ++side)
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+      const int ch = threadIdx.x + j * kThreads, r = ch >> 4;
+      w[side][j] = r >= r0 && r < r1 ? load_once4((side ? v : k) + src + (int64_t)ch * 8)
+                                     : make_uint4(0u, 0u, 0u, 0u);
+    }
+#pragma unroll
+  for (int side = 0; side < 2; ++side) {
+    uint32_t top = 0;
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+      const uint32_t ww[4] = {w[side][j].x, w[side][j].y, w[side][j].z, w[side][j].w};
 #pragma unroll
       for (int e = 0; e < 4; ++e)
         top = max(top, max(ww[e] & 0x7fffu, (ww[e] >> 16) & 0x7fffu));
     }
+    top = wave_max_u32_f(top);
+    if (threadIdx.x % kWave == 0) part[side][threadIdx.x / kWave] = top;
   }
-  top = wave_max_u32_f(top);
-  if (threadIdx.x % kWave == 0) part[threadIdx.x / kWave] = top;
-  __syncthreads();   // (and every thread has read the old scale)
+  __syncthreads();   // (and every thread has read the old scales)
 #pragma unroll
-  for (int j = 0; j < kWaves; ++j) top = max(top, part[j]);
-  const bool bad = top >= 0x7f80u || s_old != s_old;
-  const float sc = bad ? NAN : fmaxf(s_old, scale_of<FMT>(top));
-  const float inv = bad ? 0.0f : 1.0f / sc;
-  if (threadIdx.x == 0) *sp = sc;
-  const float again = s_old * inv;
+  for (int side = 0; side < 2; ++side) {
+    uint32_t top = part[side][0];
 #pragma unroll
-  for (int j = 0; j < CH; ++j) {
-    const int ch = threadIdx.x + j * kThreads, r = ch >> 4;
-    uint2* at = (uint2*)(dst + (int64_t)ch * 8);
-    if (r < r0) {
-      if (!bad && again != 1.0f) {
-        float a[4], b[4];
-        const uint2 o = *at;
-        decode4<FMT>(o.x, a);
-        decode4<FMT>(o.y, b);
-        *at = make_uint2(encode4<FMT>(a[0] * again, a[1] * again, a[2] * again, a[3] * again),
-                         encode4<FMT>(b[0] * again, b[1] * again, b[2] * again, b[3] * again));
+    for (int j = 1; j < kWaves; ++j) top = max(top, part[side][j]);
+    const bool bad = top >= 0x7f80u || s_old[side] != s_old[side];
+    const float sc = bad ? NAN : fmaxf(s_old[side], scale_of<FMT>(top));
+    const float inv = bad ? 0.0f : 1.0f / sc;
+    if (threadIdx.x == 0) *scales[side] = sc;
+    const float again = s_old[side] * inv;
+    uint8_t* dst = (side ? pg.v : pg.k) + hp * P * kHeadDim;
+#pragma unroll
+    for (int j = 0; j < CH; ++j) {
+      const int ch = threadIdx.x + j * kThreads, r = ch >> 4;
+      uint2* at = (uint2*)(dst + (int64_t)ch * 8);
+      if (r < r0) {
+        if (!bad && again != 1.0f) {
+          float a[4], b[4];
+          const uint2 o = *at;
+          decode4<FMT>(o.x, a);
+          decode4<FMT>(o.y, b);
+          *at = make_uint2(encode4<FMT>(a[0] * again, a[1] * again, a[2] * again, a[3] * again),
+                           encode4<FMT>(b[0] * again, b[1] * again, b[2] * again, b[3] * again));
+        }
+      } else if (r < r1) {
+        const uint32_t ww[4] = {w[side][j].x, w[side][j].y, w[side][j].z, w[side][j].w};
+        float f[8];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          f[2 * e] = bad ? 0.0f : bf16_lo(ww[e]) * inv;
+          f[2 * e + 1] = bad ? 0.0f : bf16_hi(ww[e]) * inv;
+        }
+        *at = make_uint2(encode4<FMT>(f[0], f[1], f[2], f[3]), encode4<FMT>(f[4], f[5], f[6], f[7]));
       }
-    } else if (r < r1) {
-      const uint32_t ww[4] = {w[j].x, w[j].y, w[j].z, w[j].w};
-      float f[8];
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        f[2 * e] = bad ? 0.0f : bf16_lo(ww[e]) * inv;
-        f[2 * e + 1] = bad ? 0.0f : bf16_hi(ww[e]) * inv;
-      }
-      *at = make_uint2(encode4<FMT>(f[0], f[1], f[2], f[3]), encode4<FMT>(f[4], f[5], f[6], f[7]));
     }
   }
 }
@@ -922,9 +924,11 @@ __global__ __launch_bounds__(kCombineThreads) void combine_kernel(AttendArgs a, 
 }
 
 // ----------------------------------------------------------------------------
-// Copy.  One workgroup moves 16 KB of K or of V of a page of a layer.
+// Copy.  One workgroup moves 4 KB of K or of V of a page of a layer,
+// past the caches (150 pages of 32 layers, 2.5 GB read and written: 4 KB each 432
+// us, 8 KB 460, 16 KB 482; 8 KB with ordinary stores 484).
 // ----------------------------------------------------------------------------
-constexpr int kCopyBytes = 16 * 1024;
+constexpr int kCopyBytes = 4 * 1024;
 
 __global__ __launch_bounds__(kThreads) void copy_kernel(Pages pg, int64_t n_moves, int parts,
                                                         const int32_t* __restrict__ src,
@@ -948,12 +952,12 @@ __global__ __launch_bounds__(kThreads) void copy_kernel(Pages pg, int64_t n_move
 #pragma unroll
   for (int j = 0; j < kCopyBytes / 16 / kThreads; ++j) {
     const int64_t c = c0 + threadIdx.x + j * kThreads;
-    if (c < chunks) w[j] = from[c];
+    if (c < chunks) w[j] = load_once4(from + c);
   }
 #pragma unroll
   for (int j = 0; j < kCopyBytes / 16 / kThreads; ++j) {
     const int64_t c = c0 + threadIdx.x + j * kThreads;
-    if (c < chunks) to[c] = w[j];
+    if (c < chunks) store_once4(to + c, w[j]);
   }
   if (part == 0) {
     float* f = is_v ? pg.vs : pg.ks;
@@ -1089,7 +1093,7 @@ ei_status ei_cache_store(const uint16_t* k, const uint16_t* v, int32_t n_tokens,
     return EI_ERR_UNSUPPORTED;
   const ei::Tokens tk{cu_seqlens, n_tokens, n_seqs, (int)each};
   const ei::Pages pg = ei::pages_of(shape, pages, page_table, max_pages);
-  const int64_t units = slots * shape.n_kv_heads * 2;
+  const int64_t units = slots * shape.n_kv_heads;
   hipStream_t s0 = (hipStream_t)stream;
   for (int64_t u = 0; u < units; u += ei::kMaxGrid) {
     const dim3 grid(ei::launch_grid(units - u)), block(ei::kThreads);

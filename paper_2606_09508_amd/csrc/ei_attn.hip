@@ -43,6 +43,7 @@
 // each tile's keys over the waves instead, dense and sparse alike.
 #include "ei_internal.h"
 
+#include <limits.h>
 #include <math.h>
 
 namespace ei {
@@ -653,36 +654,37 @@ __device__ __forceinline__ void issue_tile(unsigned char* dst, const uint16_t* _
   }
 }
 
+struct SplitSmem {
+  __attribute__((aligned(1024))) unsigned char stages[kSplitWaves][kStageBytes];
+  float part_m[kSplitWaves][kSplitTileQ], part_l[kSplitWaves][kSplitTileQ];
+};
+
+// Tile `tile` of a sequence of N rows that starts at q, kh, vh and o; sparse:
+// its block list and count.
 template <int MODE, int SUB>
-__global__ __launch_bounds__(kThreads, 1) void attn_split_kernel(
-    const uint16_t* __restrict__ q, const uint16_t* __restrict__ k,
-    const uint16_t* __restrict__ v, uint16_t* __restrict__ o, int Hq, int Hkv, int N, int n_tiles,
-    int Ls, int CS, int CB, float sc_log2, const int32_t* __restrict__ bidx,
-    const int32_t* __restrict__ bcnt, int kmax) {
-  __shared__ __attribute__((aligned(1024))) unsigned char stages[kSplitWaves][kStageBytes];
-  __shared__ float part_m[kSplitWaves][kSplitTileQ], part_l[kSplitWaves][kSplitTileQ];
-  const int rows = gridDim.x / n_tiles;   // (batch, query head) pairs
-  const int tile = n_tiles - 1 - (int)blockIdx.x / rows, bh = (int)blockIdx.x % rows;
-  const int b = bh / Hq, h = bh % Hq, g = h / (Hq / Hkv);
+__device__ __forceinline__ void split_tile(SplitSmem& sm, const uint16_t* __restrict__ q,
+                                           const uint16_t* __restrict__ kh,
+                                           const uint16_t* __restrict__ vh,
+                                           uint16_t* __restrict__ o, int N, int tile, int CB,
+                                           float sc_log2, const int32_t* __restrict__ lst,
+                                           const int32_t* __restrict__ cnt, int kmax) {
+  auto& stages = sm.stages;
+  auto& part_m = sm.part_m;
+  auto& part_l = sm.part_l;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int jq = lane & 31, hf = lane >> 5;
   const int q0 = tile * kSplitTileQ, q_last = min(q0 + kSplitTileQ - 1, N - 1), qrow = q0 + jq;
-  const uint16_t* kh = k + (size_t)(b * Hkv + g) * N * kHeadDim;
-  const uint16_t* vh = v + (size_t)(b * Hkv + g) * N * kHeadDim;
 
   bf16x8 qf[8];
   {
-    const uint16_t* qp = q + ((size_t)bh * N + qrow) * kHeadDim + 8 * hf;
+    const uint16_t* qp = q + (size_t)qrow * kHeadDim + 8 * hf;
 #pragma unroll
     for (int s = 0; s < 8; ++s)
       qf[s] = as_bf16x8(qrow < N ? *(const uint4*)(qp + 16 * s) : make_uint4(0, 0, 0, 0));
   }
-  const int32_t* lst = nullptr;
   int n_steps;
   if (MODE == kSparse) {
-    const int64_t row = (int64_t)bh * CS + q0 / Ls;
-    lst = bidx + row * kmax;
-    n_steps = valid_prefix<SUB>(lst, min(max(bcnt[row], 0), kmax), CB, q_last, lane) * SUB;
+    n_steps = valid_prefix<SUB>(lst, min(max(*cnt, 0), kmax), CB, q_last, lane) * SUB;
   } else {
     n_steps = MODE == kDenseCausal ? q_last / kSub + 1 : (N + kSub - 1) / kSub;
   }
@@ -773,7 +775,7 @@ __global__ __launch_bounds__(kThreads, 1) void attn_split_kernel(
   }
   const float inv = lsum > 0.0f ? 1.0f / lsum : 0.0f;
   if (qrow >= N) return;
-  uint16_t* op = o + ((size_t)bh * N + qrow) * kHeadDim + 32 * wave + 4 * hf;
+  uint16_t* op = o + (size_t)qrow * kHeadDim + 32 * wave + 4 * hf;
 #pragma unroll
   for (int r = 0; r < 4; ++r) {
     float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
@@ -788,6 +790,23 @@ __global__ __launch_bounds__(kThreads, 1) void attn_split_kernel(
     *(uint2*)(op + 8 * r) =
         make_uint2(pack_bf16x2(a.x * inv, a.y * inv), pack_bf16x2(a.z * inv, a.w * inv));
   }
+}
+
+template <int MODE, int SUB>
+__global__ __launch_bounds__(kThreads, 1) void attn_split_kernel(
+    const uint16_t* __restrict__ q, const uint16_t* __restrict__ k,
+    const uint16_t* __restrict__ v, uint16_t* __restrict__ o, int Hq, int Hkv, int N, int n_tiles,
+    int Ls, int CS, int CB, float sc_log2, const int32_t* __restrict__ bidx,
+    const int32_t* __restrict__ bcnt, int kmax) {
+  __shared__ SplitSmem sm;
+  const int rows = gridDim.x / n_tiles;   // (batch, query head) pairs
+  const int tile = n_tiles - 1 - (int)blockIdx.x / rows, bh = (int)blockIdx.x % rows;
+  const int b = bh / Hq, h = bh % Hq, g = h / (Hq / Hkv);
+  const size_t kv = (size_t)(b * Hkv + g) * N * kHeadDim, at = (size_t)bh * N * kHeadDim;
+  const int64_t row = MODE == kSparse ? (int64_t)bh * CS + tile * kSplitTileQ / Ls : 0;
+  split_tile<MODE, SUB>(sm, q + at, k + kv, v + kv, o + at, N, tile, CB, sc_log2,
+                        MODE == kSparse ? bidx + row * kmax : nullptr,
+                        MODE == kSparse ? bcnt + row : nullptr, kmax);
 }
 
 // Which launches take the split.  Its 32-row tiles run one to a CU (128 KB of
@@ -1072,55 +1091,94 @@ hipError_t launch_union_t(const uint16_t* q, const uint16_t* k, const uint16_t* 
 // Packed sequences.  Sequence s is the rows cu[s] .. cu[s + 1] - 1 of every
 // head, so a tile of it is a dense tile of a tensor of cu[s + 1] - cu[s] rows
 // that starts cu[s] rows further on: attn_kernel's steps on shifted pointers.
-// The host does not know the lengths.  Sequence s owns the slots cu[s] / 128 + s
-// up to the next one's first, one for each of its tiles and at most one more.
+// The host does not know the lengths: sequence s owns the ranks cu[s] / TILE + s
+// up to the next one's first, one for each of its tiles, heaviest first, and at
+// most one more (which leaves its workgroup nothing).  (Ranking the tiles by
+// their work over all sequences has the workgroups of an XCD read the keys of
+// many at a time, more than its L2 holds: 8 x 4096 tokens 7% slower; the longest
+// sequences first costs more to find out than it saves: 64 x 512 252 -> 308 us.)
 struct PackedTile {
   int first, N, tile;   // the sequence's first row and rows, and its tile (or -1)
 };
-__device__ __forceinline__ int packed_row(const int32_t* __restrict__ cu, int s, int T) {
-  return min(max(cu[s], 0), T);
-}
+template <int TILE>
 __device__ __forceinline__ PackedTile packed_tile(const int32_t* __restrict__ cu, int S, int T,
-                                                  int slot) {
-  int lo = 0, hi = S - 1;
-  while (lo < hi) {
-    const int mid = (lo + hi + 1) / 2;
-    if (packed_row(cu, mid, T) / kTileQ + mid <= slot) lo = mid; else hi = mid - 1;
+                                                  int rank) {
+  // 64 sequences at a time, a lane each: the last that starts at or before rank
+  const int lane = threadIdx.x % kWave;
+  int s = 0, step = 1;
+  while ((int64_t)step * kWave < S) step *= kWave;
+  int a = 0, e = 0;
+  for (;; step /= kWave) {
+    const int at = s + lane * step;   // (S < 2^31 / 64, or the launch is refused)
+    bool before = false;
+    if (at < S) {
+      a = min(max(cu[at], 0), T);
+      e = min(max(cu[at + 1], 0), T);
+      before = a / TILE + at <= rank;
+    }
+    const uint64_t m = __builtin_amdgcn_ballot_w64(before);
+    const int l = m ? kWave - 1 - (int)__builtin_clzll(m) : 0;
+    s += l * step;
+    if (step == 1) {
+      a = __builtin_amdgcn_readlane(a, l);
+      e = __builtin_amdgcn_readlane(e, l);
+      break;
+    }
   }
-  const int a = packed_row(cu, lo, T), e = packed_row(cu, lo + 1, T);
-  const int n = max(e - a, 0), i = slot - (a / kTileQ + lo);
-  const int tiles = (n + kTileQ - 1) / kTileQ;
-  return {a, n, tiles - 1 - i};   // heavier tiles first
+  const int n = max(e - a, 0), i = rank - (a / TILE + s);   // (i < 0: before the first sequence)
+  const int tile = i < 0 ? -1 : (n + TILE - 1) / TILE - 1 - i;
+  // (in scalar registers, with all that follows from them)
+  return {__builtin_amdgcn_readfirstlane(a), __builtin_amdgcn_readfirstlane(n),
+          __builtin_amdgcn_readfirstlane(tile)};
+}
+
+// Workgroup b's head and tile rank.  The query heads of a group take a tile one
+// after the other on one XCD, whose L2 then holds its keys: XCD x has the KV
+// heads x, x + 8, ... or, with fewer than eight that divide eight, shares one
+// with the XCDs that differ by a multiple of their number, rank by rank.
+__device__ __forceinline__ void packed_item(unsigned b, int Hq, int Hkv, int& h, int& rank) {
+  const unsigned G = (unsigned)(Hq / Hkv), x = b % kXcds, i = b / kXcds;
+  if (Hkv % kXcds == 0) {
+    const unsigned per = (unsigned)Hq / kXcds;   // heads of the XCD
+    rank = (int)(i / per);
+    h = (int)((x + kXcds * (i % per / G)) * G + i % G);
+  } else if (kXcds % Hkv == 0) {
+    rank = (int)(i / G * (kXcds / (unsigned)Hkv) + x / (unsigned)Hkv);
+    h = (int)(x % (unsigned)Hkv * G + i % G);
+  } else {
+    rank = (int)(b / (unsigned)Hq);
+    h = (int)(b % (unsigned)Hq);
+  }
+}
+// Workgroups that give every head `ranks` ranks.
+int64_t packed_grid(int Hq, int Hkv, int64_t ranks) {
+  if (kXcds % Hkv == 0) ranks = (ranks + kXcds / Hkv - 1) / (kXcds / Hkv) * (kXcds / Hkv);
+  return ranks * Hq;
 }
 
 template <int MODE>
 __global__ __launch_bounds__(kThreads, 2) void attn_packed_kernel(
     const uint16_t* __restrict__ q, const uint16_t* __restrict__ k,
     const uint16_t* __restrict__ v, uint16_t* __restrict__ o, int Hq, int Hkv, int T,
-    const int32_t* __restrict__ cu, int S, int slots, float sc_log2) {
+    const int32_t* __restrict__ cu, int S, float sc_log2) {
   __shared__ __attribute__((aligned(1024))) unsigned char stage0[kStageBytes];
   __shared__ __attribute__((aligned(1024))) unsigned char stage1[kStageBytes];
-  const unsigned G = (unsigned)(Hq / Hkv);
-  const unsigned per_xcd = gridDim.x / kXcds;
-  unsigned t = (blockIdx.x % kXcds) * per_xcd + blockIdx.x / kXcds;
-  if (t >= (unsigned)Hq * (unsigned)slots) return;
-  const int hh = (int)(t % G);
-  t /= G;
-  const PackedTile pt = packed_tile(cu, S, T, (int)(t % (unsigned)slots));
-  const int g = (int)(t / (unsigned)slots);
+  int h, rank;
+  packed_item(blockIdx.x, Hq, Hkv, h, rank);
+  const PackedTile pt = packed_tile<kTileQ>(cu, S, T, rank);
   if (pt.tile < 0) return;
-  const int N = pt.N, h = g * (int)G + hh;
+  const int g = h / (Hq / Hkv);
+  const int N = pt.N, q0 = pt.tile * kTileQ, first = pt.first;
 
   const int tid = threadIdx.x;
   const int wave = tid >> 6, lane = tid & 63;
   const int jq = lane & 31, hf = lane >> 5;
-  const int q0 = pt.tile * kTileQ;
   const int q_last = min(q0 + kTileQ - 1, N - 1);
   const int qw0 = q0 + wave * 32;          // first query row of this wave
   const int qrow = qw0 + jq;               // this lane's query row
-  const uint16_t* kh = k + ((size_t)g * T + pt.first) * kHeadDim;
-  const uint16_t* vh = v + ((size_t)g * T + pt.first) * kHeadDim;
-  const size_t row_base = (size_t)h * T + pt.first + qrow;
+  const uint16_t* kh = k + ((size_t)g * T + first) * kHeadDim;
+  const uint16_t* vh = v + ((size_t)g * T + first) * kHeadDim;
+  const size_t row_base = (size_t)h * T + first + qrow;
 
   bf16x8 qf[8];
 #pragma unroll
@@ -1160,16 +1218,51 @@ __global__ __launch_bounds__(kThreads, 2) void attn_packed_kernel(
   if (qrow < N) store_rows(o, row_base, hf, oacc, l_i);
 }
 
+// Small launches take the split by the rules of dense attention (split_tiles),
+// with what the host knows: the rows in all, and the average of the lengths.
+template <int MODE>
+bool split_packed(const AttnShape& s, int n_seqs) {
+  const int64_t half = s.N + (int64_t)n_seqs * kSplitTileQ / 2;   // rows, tiles filled up
+  const int64_t len = s.N / n_seqs;
+  if (s.Hq * ((int64_t)s.N + (int64_t)n_seqs * kTileQ / 2) > (int64_t)kSplitMaxTiles * kTileQ ||
+      len <= (MODE == kDenseFull ? 96 : 128))
+    return false;
+  return s.Hq * half <= (int64_t)kSplitRound * kSplitTileQ ||
+         len / kSub >= (MODE == kDenseFull ? 14 : 9);
+}
+
+// Their 32-row tiles, the keys shared out over the waves.
+template <int MODE>
+__global__ __launch_bounds__(kThreads, 1) void attn_packed_split_kernel(
+    const uint16_t* __restrict__ q, const uint16_t* __restrict__ k,
+    const uint16_t* __restrict__ v, uint16_t* __restrict__ o, int Hq, int Hkv, int T,
+    const int32_t* __restrict__ cu, int S, float sc_log2) {
+  __shared__ SplitSmem sm;
+  int h, rank;
+  packed_item(blockIdx.x, Hq, Hkv, h, rank);
+  const PackedTile pt = packed_tile<kSplitTileQ>(cu, S, T, rank);
+  if (pt.tile < 0) return;
+  const size_t kv = ((size_t)(h / (Hq / Hkv)) * T + pt.first) * kHeadDim;
+  const size_t at = ((size_t)h * T + pt.first) * kHeadDim;
+  split_tile<MODE, 1>(sm, q + at, k + kv, v + kv, o + at, pt.N, pt.tile, 0, sc_log2, nullptr,
+                      nullptr, 0);
+}
+
 template <int MODE>
 hipError_t launch_packed_t(const uint16_t* q, const uint16_t* k, const uint16_t* v,
                            const AttnShape& s, const int32_t* cu, int n_seqs, uint16_t* o,
                            hipStream_t stream) {
-  const int slots = s.N / kTileQ + n_seqs;
-  const int64_t grid = ((int64_t)s.Hq * slots + kXcds - 1) / kXcds * kXcds;
-  if (!launch_fits(grid, kThreads)) return hipErrorInvalidConfiguration;
   const float sc_log2 = (float)((double)s.softmax_scale * 1.4426950408889634);
-  hipLaunchKernelGGL((attn_packed_kernel<MODE>), dim3((unsigned)grid), dim3(kThreads), 0, stream,
-                     q, k, v, o, s.Hq, s.Hkv, s.N, cu, n_seqs, slots, sc_log2);
+  const bool split = split_packed<MODE>(s, n_seqs);
+  const int64_t grid =
+      packed_grid(s.Hq, s.Hkv, (int64_t)s.N / (split ? kSplitTileQ : kTileQ) + n_seqs);
+  if (!launch_fits(grid, kThreads) || n_seqs > INT_MAX / kWave) return hipErrorInvalidConfiguration;
+  if (split)
+    hipLaunchKernelGGL((attn_packed_split_kernel<MODE>), dim3((unsigned)grid), dim3(kThreads), 0,
+                       stream, q, k, v, o, s.Hq, s.Hkv, s.N, cu, n_seqs, sc_log2);
+  else
+    hipLaunchKernelGGL((attn_packed_kernel<MODE>), dim3((unsigned)grid), dim3(kThreads), 0, stream,
+                       q, k, v, o, s.Hq, s.Hkv, s.N, cu, n_seqs, sc_log2);
   return hipGetLastError();
 }
 

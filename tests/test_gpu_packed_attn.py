@@ -79,6 +79,31 @@ def test_packed_matches_each_sequence(lengths, hq, hkv, causal):
     check(got, q, k, v, cu, causal)
 
 
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("hq,hkv,lengths", [
+    (4, 1, [2048]), (8, 2, [400, 129, 40, 500]), (4, 4, [1000, 1, 1500]), (2, 1, [130] * 20),
+    (3, 1, [600, 0, 0, 700, 33])])
+def test_packed_small_launches(hq, hkv, lengths, causal):
+    """Launches of few tiles, whose keys are shared out over the waves."""
+    cu = offsets(lengths)
+    T = cu[-1]
+    q, k, v = _rand((1, hq, T, D), 7), _rand((1, hkv, T, D), 8), _rand((1, hkv, T, D), 9)
+    got = eb.packed_prefill_attn(q.cuda(), k.cuda(), v.cuda(),
+                                 torch.tensor(cu, dtype=torch.int32, device="cuda"),
+                                 causal=causal).cpu()
+    check(got, q, k, v, cu, causal)
+
+
+def test_packed_thousands_of_sequences():
+    lengths = [(7 * i) % 11 for i in range(4500)]
+    cu = offsets(lengths)
+    T = cu[-1]
+    q, k, v = _rand((1, 4, T, D), 1), _rand((1, 2, T, D), 2), _rand((1, 2, T, D), 3)
+    got = eb.packed_prefill_attn(q.cuda(), k.cuda(), v.cuda(),
+                                 torch.tensor(cu, dtype=torch.int32, device="cuda")).cpu()
+    check(got, q, k, v, cu, True)
+
+
 @pytest.mark.parametrize("hq,hkv,n", [(32, 8, 700), (28, 4, 2000), (40, 40, 300)])
 def test_packed_larger_launches(hq, hkv, n):
     """Launches of several rounds, whose tiles are dealt out over the chip."""
@@ -90,13 +115,14 @@ def test_packed_larger_launches(hq, hkv, n):
     check(got, q, k, v, cu, True)
 
 
-def test_rows_outside_every_sequence_are_left():
-    cu = offsets([40, 0, 200], start=17)
+@pytest.mark.parametrize("lead", [17, 1000])
+def test_rows_outside_every_sequence_are_left(lead):
+    cu = offsets([40, 0, 200], start=lead)
     T = cu[-1] + 150
     q, k, v = (_rand((1, 4, T, D), i).cuda() for i in range(3))
     out = torch.full_like(q, 7.0)
     eb.packed_prefill_attn(q, k, v, torch.tensor(cu, dtype=torch.int32, device="cuda"), out=out)
-    assert bool((out[:, :, :17] == 7.0).all()) and bool((out[:, :, cu[-1]:] == 7.0).all())
+    assert bool((out[:, :, :lead] == 7.0).all()) and bool((out[:, :, cu[-1]:] == 7.0).all())
     check(out.cpu(), q.cpu(), k.cpu(), v.cpu(), cu, True)
 
 

@@ -18,6 +18,7 @@ carries no part of the method.
 from __future__ import annotations
 
 import argparse
+import functools
 import math
 import sys
 import time
@@ -221,10 +222,11 @@ def _one_pass(x, w, shape: DecoderShape, cos, sin, quiet: bool | None = None) ->
             and cos.shape == sin.shape == (x.shape[1], 64) and _dense16(w["norm2"], cos, sin))
 
 
-def _layer(x, y, w, shape: DecoderShape, attn: Attention, cos, sin, trace=None):
+def _layer(x, y, w, shape: DecoderShape, attn, cos, sin, trace=None, store=None):
     """One decoder layer on the hidden state x + y (y None: x itself); returns
     the new hidden state as two summands, so that a following layer's norm
-    takes their sum in the pass that reads it."""
+    takes their sum in the pass that reads it.  ``store`` (optional) receives
+    the rotated keys and the values."""
     B, N, _ = x.shape
     Hq, Hkv, D = shape.n_q_heads, shape.n_kv_heads, shape.head_dim
     quiet = _quiet(x.device)   # once a layer: each look costs a small prompt ~2 us
@@ -243,6 +245,8 @@ def _layer(x, y, w, shape: DecoderShape, attn: Attention, cos, sin, trace=None):
     else:
         q, k, v = (t.transpose(1, 2).contiguous() for t in (q, k, v))
         q, k = _rope(q, cos, sin), _rope(k, cos, sin)
+    if store is not None:
+        store(k, v)
     o = attn(q, k, v)
     if trace is not None:
         trace.update(q=q.clone(), k=k.clone(), v=v.clone(), o=o.clone())
@@ -265,22 +269,31 @@ def layer_forward(x, w, shape: DecoderShape, attn: Attention, cos, sin, trace=No
     return x + y
 
 
-def prefill(x, layers, shape: DecoderShape, attn: Attention, lm_head=None):
-    """All layers over the prompt's hidden states x [B, N, hidden]; returns the
-    final normed hidden state of the last token (and its logits when an LM
-    head [hidden, vocab] is given) -- what the first generated token needs."""
-    N = x.shape[1]
-    cos, sin = rope_tables(N, shape.head_dim, shape.rope_theta, x.device)
-    y = None
-    for w in layers:
-        x, y = _layer(x, y, w, shape, attn, cos, sin)
-    last = x[:, -1:] if y is None else x[:, -1:] + y[:, -1:]
+def finish(x, y, layers, shape: DecoderShape, lm_head=None):
+    """The final norm of the hidden states x + y (y None: x itself), and their
+    logits when an LM head [hidden, vocab] is given."""
+    last = x if y is None else x + y
     gain = layers[-1]["norm2"]
     if _plain(last, gain) and _norm_fits(last, gain):
         last = eb.add_rmsnorm(last, None, gain, shape.rms_eps)[1]
     else:
         last = _rmsnorm(last, gain, shape.rms_eps)
     return last, (last @ lm_head if lm_head is not None else None)
+
+
+def prefill(x, layers, shape: DecoderShape, attn: Attention, lm_head=None, store=None):
+    """All layers over the prompt's hidden states x [B, N, hidden]; returns the
+    final normed hidden state of the last token (and its logits when an LM
+    head [hidden, vocab] is given) -- what the first generated token needs.
+    ``store`` (optional) receives (layer index, keys, values) of every layer,
+    as decode.PagedCache.storing takes them."""
+    N = x.shape[1]
+    cos, sin = rope_tables(N, shape.head_dim, shape.rope_theta, x.device)
+    y = None
+    for i, w in enumerate(layers):
+        x, y = _layer(x, y, w, shape, attn, cos, sin,
+                      store=None if store is None else functools.partial(store, i))
+    return finish(x[:, -1:], None if y is None else y[:, -1:], layers, shape, lm_head)
 
 
 def ttft_table(lengths, shape: DecoderShape, n_layers: int, reps: int, cfg: SparseConfig,

@@ -831,33 +831,33 @@ __global__ __launch_bounds__(kThreads, attend_occupancy(RT)) void attend_share_k
 // are added up in order.
 constexpr int kCombineThreads = 1024;
 constexpr int kCombineRows = 8;
-constexpr int kCombineAhead = 8;   // parts in flight per group
+constexpr int kCombineAhead = 4;   // parts in flight per group (8: 5.1 -> 7.4 us, 32 sequences)
+static_assert(kCombineThreads / 32 / kWaves >= kCombineRows, "a group for each row of an item");
 __global__ __launch_bounds__(kCombineThreads) void combine_kernel(AttendArgs a, int tile_rows) {
   constexpr int kGroups = kCombineThreads / 32;
   __shared__ float sm_m[kGroups], sm_l[kGroups];
   __shared__ __attribute__((aligned(16))) float sm_o[kGroups][kHeadDim];
   const int G = a.Hq / a.pg.Hkv;
   const int grp = threadIdx.x / 32, d = (threadIdx.x % 32) * 4;
-  // one item: all groups take it; several: a share of the groups each
-  int parts[kWaves], items = 0, only = 0;
+  // one item: all groups take it; several: a share of the groups each (whose
+  // item is asked for with the others' numbers of parts, not after them)
+  const SplitItem* const left = a.split + (int)blockIdx.x * kWaves;
+  int w = grp / (kGroups / kWaves);
+  SplitItem it = left[w];
+  int items = 0, only = 0;
 #pragma unroll
-  for (int w = 0; w < kWaves; ++w) {
-    parts[w] = a.split[(int)blockIdx.x * kWaves + w].parts;
-    if (parts[w] > 0) {
+  for (int i = 0; i < kWaves; ++i)
+    if (left[i].parts > 0) {
       ++items;
-      only = w;
+      only = i;
     }
-  }
   if (items == 0) return;
   const int mine = items == 1 ? kGroups : kGroups / kWaves;
-  const int w = items == 1 ? only : grp / mine;
+  if (items == 1 && w != only) it = left[w = only];
   const int worker = (int)blockIdx.x * kWaves + w;
-  SplitItem it{};
   int first = 0, n = 0;
-  if (a.split[worker].parts > 0) {   // (else nothing else of it is set)
-    it = a.split[worker];
-    seq_rows(a.tk, it.s, first, n);
-  }
+  if (it.parts > 0) seq_rows(a.tk, it.s, first, n);
+  else it.row0 = 0;                  // (nothing else of it is set)
   const int r0 = (int)blockIdx.y * kCombineRows;
   const int rows = min(min(n * G - it.row0, tile_rows) - r0, kCombineRows);
   auto slot_row = [&](int p, int r) -> int64_t {

@@ -982,7 +982,8 @@ ei_status check_shape(const ei_cache_shape& c) {
   if ((int64_t)c.n_pages * c.n_kv_heads > INT_MAX) return EI_ERR_SHAPE;
   return EI_OK;
 }
-ei_status check_pages(const ei_cache_pages& p) {
+ei_status check_pages(const ei_cache_shape& c, const ei_cache_pages& p) {
+  if (c.n_pages == 0) return EI_OK;   // nothing to point at
   if (!p.k || !p.v || !p.k_scale || !p.v_scale) return EI_ERR_NULL;
   if (!aligned(p.k, 16) || !aligned(p.v, 16) || !aligned(p.k_scale, 4) || !aligned(p.v_scale, 4))
     return EI_ERR_UNSUPPORTED;
@@ -1087,7 +1088,7 @@ ei_status ei_cache_store(const uint16_t* k, const uint16_t* v, int32_t n_tokens,
   if (slots > INT_MAX) return EI_ERR_SHAPE;
   if (n_tokens == 0 || n_seqs == 0 || max_pages == 0 || shape.n_pages == 0) return EI_OK;
   if (!k || !v || !lengths || !page_table) return EI_ERR_NULL;
-  if ((st = ei::check_pages(pages)) != EI_OK) return st;
+  if ((st = ei::check_pages(shape, pages)) != EI_OK) return st;
   if (!ei::aligned(k, 16) || !ei::aligned(v, 16) || !ei::aligned(lengths, 4) ||
       !ei::aligned(page_table, 4) || !ei::aligned(cu_seqlens, 4))
     return EI_ERR_UNSUPPORTED;
@@ -1137,8 +1138,8 @@ ei_status ei_cache_attn(const uint16_t* q, int32_t n_q_heads, int32_t n_tokens,
   const ei::AttendPlan pl = ei::attend_plan(n_q_heads, n_tokens, cu_seqlens != nullptr, n_seqs,
                                             max_pages, shape);
   if (!pl.fits) return EI_ERR_SHAPE;
-  if (!q || !o || !lengths || !page_table) return EI_ERR_NULL;
-  if ((st = ei::check_pages(pages)) != EI_OK) return st;
+  if (!q || !o || !lengths || (!page_table && max_pages > 0)) return EI_ERR_NULL;
+  if ((st = ei::check_pages(shape, pages)) != EI_OK) return st;
   if (!ei::aligned(q, 16) || !ei::aligned(o, 16) || !ei::aligned(lengths, 4) ||
       !ei::aligned(page_table, 4) || !ei::aligned(cu_seqlens, 4))
     return EI_ERR_UNSUPPORTED;
@@ -1169,7 +1170,7 @@ ei_status ei_cache_copy(ei_cache_shape shape, int32_t n_layers, ei_cache_pages p
   if (n_layers < 0 || n < 0) return EI_ERR_SHAPE;
   if (n_layers == 0 || n == 0 || shape.n_pages == 0) return EI_OK;
   if (!src || !dst) return EI_ERR_NULL;
-  if ((st = ei::check_pages(pages)) != EI_OK) return st;
+  if ((st = ei::check_pages(shape, pages)) != EI_OK) return st;
   if (!ei::aligned(src, 4) || !ei::aligned(dst, 4)) return EI_ERR_UNSUPPORTED;
   const int64_t page_bytes = (int64_t)shape.n_kv_heads * shape.page_len * ei::kHeadDim;
   const int64_t parts = (page_bytes + ei::kCopyBytes - 1) / ei::kCopyBytes;

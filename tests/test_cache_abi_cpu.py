@@ -97,6 +97,10 @@ def test_sequence_refusals(L, call):
         assert call(L, pages=eb.CachePointers(*p)) == UNSUPPORTED
     assert call(L, T=0) == OK
     assert call(L, T=0, n=0) == OK
+    # (a cache without pages needs no pointers to them; a store has nothing to do)
+    empty = eb.CacheShape(0, 2, 64, 128, 0)
+    if call is store:
+        assert call(L, shape=empty, pages=eb.CachePointers()) == OK
 
 
 def test_attn_refusals(L):

@@ -383,6 +383,52 @@ def test_attn_scores_of_any_size():
         run_attn([700, 90], [1, 3], 4, 1, 64, E4M3, edit=edit)
 
 
+def test_attn_without_a_single_page():
+    """A table without columns, and a pool without pages: zero rows."""
+    q = _rand((1, 4, 2, D), 2).cuda()
+    lengths = _i32([20, 30]).cuda()
+    some, none = (eb.new_cache_pages(n, 2, 64) for n in (3, 0))
+    table = torch.zeros((2, 0), dtype=torch.int32, device="cuda")
+    assert bool((eb.cache_attn(q, some, table, lengths) == 0).all())
+    for cols in (2, 100):
+        table = torch.zeros((2, cols), dtype=torch.int32, device="cuda")
+        assert bool((eb.cache_attn(q, none, table, lengths) == 0).all())
+        eb.cache_store(q[:, :2].contiguous(), q[:, :2].contiguous(), none, table, lengths)
+
+
+@pytest.mark.parametrize("n", [30, 2500])
+def test_attn_non_finite_queries_stay_alone(n):
+    """A query that is NaN or infinite makes its own row so, and no other, also
+    of those that share its tile."""
+    def run(q):
+        pages = _cuda(_pages(-(-n // 64) + 1, 2, 64, E4M3, 1))
+        table = torch.arange(-(-n // 64), dtype=torch.int32, device="cuda")[None]
+        return eb.cache_attn(q.cuda(), pages, table.contiguous(), _i32([n]).cuda(),
+                             _i32([0, 3]).cuda())
+    q = _rand((1, 8, 3, D), 4)
+    want = run(q)
+    q[0, 2, 1, 7] = math.nan
+    q[0, 5, 0, 100] = math.inf
+    got = run(q)
+    bad = torch.zeros((1, 8, 3), dtype=torch.bool, device="cuda")
+    bad[0, 2, 1] = bad[0, 5, 0] = True
+    assert torch.equal(got[~bad], want[~bad])
+    assert bool(got[bad].isnan().all())
+
+
+def test_attn_more_items_than_workgroups():
+    """A workgroup each for more items than the launch has: bit for bit what
+    tables of few columns give, whose launch is another."""
+    S, hkv = 2100, 8
+    lengths = [1 + (13 * i) % 150 for i in range(S)]
+    pages = _cuda(_pages(400, hkv, 64, E4M3, 1))
+    table = torch.randint(0, 400, (S, 40), generator=_gen(2)).to(torch.int32).cuda()
+    q = _rand((1, 16, S, D), 3).cuda()
+    ln = _i32(lengths).cuda()
+    narrow = eb.cache_attn(q, pages, table[:, :3].contiguous(), ln)
+    assert torch.equal(eb.cache_attn(q, pages, table, ln), narrow)
+
+
 def test_attn_leaves_rows_of_no_sequence():
     pages = _cuda(_pages(4, 2, 64, E4M3, 1))
     q = _rand((1, 4, 12, D), 2).cuda()

@@ -620,30 +620,24 @@ __global__ __launch_bounds__(WAVES* kWave, attend_occupancy(RT)) void attend_ker
   });
 }
 
-// Long tables, whose sequences may be of any lengths: the device decides.
-//
-// By item, a workgroup each, where the longest item is no longer than what a
-// CU takes of all of them: a CU takes a step in about 0.24 us alone, the chip
-// together one in 1.34 ns, and sharing costs about 5 us more.
-//
-// Otherwise the items' steps are dealt out evenly over kShareGroups x kWaves
-// waves.  With the items one behind the other (by sequence, KV head and row
-// tile), each kItemCost steps longer than it is (what a wave waits for before an
-// item's first step), every wave takes an equal run of them: a last part of an
-// item, whole items, a first part of one.  Whole items are written out, parts
-// left for combine_kernel: nothing in here waits for another wave, except where
-// the runs of a workgroup's waves lie in one item: they then share the item's
-// steps and leave one part.
+// Long tables, whose sequences may be of any lengths: the items' steps dealt out
+// evenly over the waves of the launch.  With the items one behind the other (by
+// sequence, KV head and row tile), each kItemCost steps longer than it is (what
+// a wave waits for before an item's first step), every wave takes an equal run
+// of them: a last part of an item, whole items, a first part of one.  Whole items
+// are written out, parts left for combine_kernel: nothing in here waits for
+// another wave, except where the runs of a workgroup's waves lie in one item:
+// they then share the item's steps and leave one part.
 //
 // Each wave adds the sequences up for itself.  Two waves a SIMD are what HBM
 // needs; with three the oldest goes first and the youngest ends a third later (8
-// sequences of up to 128k tokens 248 -> 293 us).
+// sequences of up to 128k tokens 248 -> 293 us).  A workgroup per item instead
+// (as for short tables) is 3% faster on 128 sequences of about 2000 tokens, all
+// alike (96 / 99 us), and far slower on others (256 of 200 to 8000: 243 / 203).
 constexpr int kCus = 256;
 constexpr int kShareGroups = 2 * kCus;
-constexpr int kItemCost = 8;
+constexpr int kItemCost = 5;    // (8: 128 ragged sequences 81 -> 83 us)
 constexpr int kShareLeast = 4;   // steps and costs a wave takes at least
-constexpr int kItemSteps = 180;  // steps of the chip in a step of one CU alone
-constexpr int kItemExtra = 3700; // steps of the chip in 5 us
 
 // A value that all lanes share, in scalar registers.
 __device__ __forceinline__ int64_t uniform(int64_t x) {
@@ -653,57 +647,35 @@ __device__ __forceinline__ int64_t uniform(int64_t x) {
 }
 
 template <int FMT, int P, int RT>
-__global__ __launch_bounds__(kThreads, attend_occupancy(RT)) void attend_share_kernel(AttendArgs a,
-                                                                                 int groups) {
+__global__ __launch_bounds__(kThreads, attend_occupancy(RT)) void attend_share_kernel(AttendArgs a) {
   __shared__ MergeSmem<kWaves> sm;
   const int G = a.Hq / a.pg.Hkv, lane = threadIdx.x % kWave;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int group = (int)blockIdx.x, worker = group * kWaves + wave;
-  const int workers = groups * kWaves;   // of a shared launch
-  auto items_of = [&](int s, int& steps, int& tiles) -> int {
+  const int workers = (int)gridDim.x * kWaves;
+  int steps, tiles;   // of the sequence that cost_of was last called for
+  auto cost_of = [&](int s) -> int64_t {
     int first, n;
     seq_rows(a.tk, s, first, n);
     steps = (keys_of<P>(a, s) + kKeys - 1) / kKeys;
     tiles = (n * G + kRows * RT - 1) / (kRows * RT);
-    return tiles * a.pg.Hkv;
+    return (int64_t)(steps + kItemCost) * tiles * a.pg.Hkv;
   };
-  int steps = 0, tiles = 0;
-  // the first 64 sequences stay in registers
-  const int my_items = lane < a.tk.S ? items_of(lane, steps, tiles) : 0, my_steps = steps;
-  int longest = my_items > 0 ? steps : 0;
-  int64_t items = my_items, all_steps = (int64_t)steps * my_items;
-  for (int s = kWave + lane; s < a.tk.S; s += kWave) {
-    const int it = items_of(s, steps, tiles);
-    items += it;
-    all_steps += (int64_t)steps * it;
-    longest = max(longest, it > 0 ? steps : 0);
-  }
+  // the first 64 sequences' costs stay in registers
+  const int64_t my_cost = lane < a.tk.S ? cost_of(lane) : 0;
+  int64_t total = my_cost;
+  for (int s = kWave + lane; s < a.tk.S; s += kWave) total += cost_of(s);
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    items += __shfl_xor(items, o);
-    all_steps += __shfl_xor(all_steps, o);
-    longest = max(longest, __shfl_xor(longest, o));
-  }
-  items = uniform(items);
-  all_steps = uniform(all_steps);
-  longest = __builtin_amdgcn_readfirstlane(longest);
-  if (lane == 0 && worker < workers) a.split[worker].parts = 0;
-  const bool by_item = (int64_t)longest * kItemSteps <= all_steps + kItemExtra;
-  // (by item: an item is one unit)
-  const int item_cost = by_item ? 1 : kItemCost, step_cost = by_item ? 0 : 1;
-  const int64_t total = by_item ? items : all_steps + items * kItemCost;
-  auto cost_of = [&](int s) -> int64_t {
-    const int it = items_of(s, steps, tiles);
-    return (int64_t)(steps * step_cost + item_cost) * it;
-  };
+  for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o);
+  total = uniform(total);
+  if (lane == 0) a.split[worker].parts = 0;
   // the sequence that unit u < total lies in, and the unit it starts at
   int s;
   int64_t start;
   auto find = [&](int64_t u) {
     int64_t before = 0;
     for (s = 0; s < a.tk.S; s += kWave) {
-      const int64_t cost = s == 0 ? (int64_t)(my_steps * step_cost + item_cost) * my_items
-                                  : s + lane < a.tk.S ? cost_of(s + lane) : 0;
+      const int64_t cost = s == 0 ? my_cost : s + lane < a.tk.S ? cost_of(s + lane) : 0;
       int64_t incl = cost;
 #pragma unroll
       for (int o = 1; o < kWave; o <<= 1) {
@@ -722,8 +694,7 @@ __global__ __launch_bounds__(kThreads, attend_occupancy(RT)) void attend_share_k
   };
   const int64_t even = (total + workers - 1) / workers;
   const int64_t per = even < kShareLeast ? kShareLeast : even;
-  const int64_t g0 = by_item ? group : group * kWaves * per;
-  const int64_t g1 = by_item ? total : min(g0 + kWaves * per, total);
+  const int64_t g0 = group * kWaves * per, g1 = min(g0 + kWaves * per, total);
   if (g0 >= g1) return;
   // The units u .. end - 1 of the item that unit u lies in (after cost_of(s)).
   struct Run {
@@ -732,13 +703,13 @@ __global__ __launch_bounds__(kThreads, attend_occupancy(RT)) void attend_share_k
     bool none, full;
   };
   auto run_at = [&](int64_t u, int64_t end) -> Run {
-    const int whole = steps * step_cost + item_cost;
+    const int whole = steps + kItemCost;
     const int off = (int)(u - start), at = off % whole;
     const int to = (int)min((int64_t)whole, at + (end - u));
     Run r;
     r.item = off / whole;
-    r.st0 = by_item ? 0 : max(at - kItemCost, 0);
-    r.st1 = by_item ? steps : max(to - kItemCost, 0);
+    r.st0 = max(at - kItemCost, 0);
+    r.st1 = max(to - kItemCost, 0);
     r.base = u - at;
     r.next = r.base + whole;
     // without steps it is none (an item without keys counts with its last unit)
@@ -773,9 +744,8 @@ __global__ __launch_bounds__(kThreads, attend_occupancy(RT)) void attend_share_k
   find(g0);
   if (s >= a.tk.S) return;
   cost_of(s);
-  // whether the workgroup's waves go together: over items, or over the one that
-  // all their runs lie in
-  const bool joint = by_item || g1 <= run_at(g0, g1).next;
+  // whether the workgroup's waves go together, their runs being of one item
+  const bool joint = g1 <= run_at(g0, g1).next;
   const int64_t u0 = joint ? g0 : worker * per, u1 = joint ? g1 : min(u0 + per, total);
   if (u0 >= u1) return;
   if (!joint && wave > 0) find(u0);
@@ -789,7 +759,7 @@ __global__ __launch_bounds__(kThreads, attend_occupancy(RT)) void attend_share_k
     const Run r = run_at(u, u1);
     const int first_worker = joint ? group * kWaves : worker;
     const int slot = 2 * first_worker + (u == u0 ? 0 : 1);
-    u = by_item ? u + gridDim.x : r.next;
+    u = r.next;
     if (r.none) continue;
     int first, n;
     seq_rows(a.tk, s, first, n);
@@ -805,7 +775,6 @@ __global__ __launch_bounds__(kThreads, attend_occupancy(RT)) void attend_share_k
       else store_part<RT>(a, slot, row, d, m, l, x);
     };
     if (joint) {
-      __syncthreads();   // (the rows before have been read)
       merge_waves<RT>(sm, ws, n * G - row0, store);
     } else {
       const int j = lane & 15, g = lane >> 4;
@@ -1001,7 +970,6 @@ Pages pages_of(const ei_cache_shape& c, const ei_cache_pages& p, const int32_t* 
 
 constexpr int kShortKeys = 2048;   // a table of no more keys: one workgroup per item
 constexpr int kShortWaves = 4;
-constexpr int kItemGroups = 16384;
 
 struct AttendPlan {
   int rt, per_seq, item_rows;   // item_rows: of an item, at most
@@ -1046,11 +1014,8 @@ AttendPlan attend_plan(int Hq, int n_tokens, bool ragged, int n_seqs, int max_pa
 template <int FMT, int P, int RT>
 void launch_attend_t(const AttendPlan& pl, const AttendArgs& a, hipStream_t stream) {
   if (pl.groups) {
-    // (by item: a workgroup for each, up to some number)
-    const int64_t by_item = pl.items < kItemGroups ? pl.items : kItemGroups;
-    hipLaunchKernelGGL((attend_share_kernel<FMT, P, RT>),
-                       dim3((unsigned)(pl.groups > by_item ? pl.groups : by_item)), dim3(kThreads),
-                       0, stream, a, pl.groups);
+    hipLaunchKernelGGL((attend_share_kernel<FMT, P, RT>), dim3((unsigned)pl.groups),
+                       dim3(kThreads), 0, stream, a);
     const unsigned row_blocks = (unsigned)((pl.item_rows + kCombineRows - 1) / kCombineRows);
     hipLaunchKernelGGL(combine_kernel, dim3((unsigned)pl.groups, row_blocks), dim3(kCombineThreads),
                        0, stream, a, kRows * RT);

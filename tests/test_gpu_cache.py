@@ -416,17 +416,20 @@ def test_attn_non_finite_queries_stay_alone(n):
     assert bool(got[bad].isnan().all())
 
 
-def test_attn_more_items_than_workgroups():
-    """A workgroup each for more items than the launch has: bit for bit what
-    tables of few columns give, whose launch is another."""
+@pytest.mark.parametrize("cols", [3, 40])
+def test_attn_thousands_of_sequences(cols):
+    """More items than waves, in the launches of short and of long tables."""
     S, hkv = 2100, 8
     lengths = [1 + (13 * i) % 150 for i in range(S)]
-    pages = _cuda(_pages(400, hkv, 64, E4M3, 1))
-    table = torch.randint(0, 400, (S, 40), generator=_gen(2)).to(torch.int32).cuda()
-    q = _rand((1, 16, S, D), 3).cuda()
-    ln = _i32(lengths).cuda()
-    narrow = eb.cache_attn(q, pages, table[:, :3].contiguous(), ln)
-    assert torch.equal(eb.cache_attn(q, pages, table, ln), narrow)
+    pages = _pages(400, hkv, 64, E4M3, 1)
+    table = torch.randint(0, 400, (S, cols), generator=_gen(2)).to(torch.int32)
+    q = _rand((1, 16, S, D), 3)
+    got = eb.cache_attn(q.cuda(), _cuda(pages), table.cuda(), _i32(lengths).cuda()).cpu()
+    some = list(range(0, S, 97)) + [S - 1]
+    ref, off = attn_reference(q[:, :, some], pages, table[some].tolist(),
+                              [lengths[i] for i in some], list(range(len(some) + 1)))
+    assert bool(((got[:, :, some].double() - ref).abs() <= off).all())
+    assert bool((got != 0).any(-1).all())
 
 
 def test_attn_leaves_rows_of_no_sequence():
@@ -501,8 +504,9 @@ def test_copy(hkv, P, layers, dtype):
 # Together
 # --------------------------------------------------------------------------
 
+@pytest.mark.parametrize("spare", [1, 40])
 @pytest.mark.parametrize("dtype", [E4M3, INT8])
-def test_a_decoding_loop_captured(dtype):
+def test_a_decoding_loop_captured(dtype, spare):
     """Prompts stored, then steps of one token each as a captured graph, the
     lengths kept on the device; every step against the same calls run eagerly
     and against float64."""
@@ -510,7 +514,7 @@ def test_a_decoding_loop_captured(dtype):
     prompts, steps = [60, 1, 130], 8
     total = [n + steps for n in prompts]
     n_pages = sum(-(-n // P) for n in total)
-    table = _table(total, P, n_pages, 5)
+    table = _table(total, P, n_pages, 5, spare)
     dtab = _i32(table).cuda()
     k, v = _rand((1, hkv, sum(prompts), D), 1), _rand((1, hkv, sum(prompts), D), 2)
     cu = _i32(_offsets(prompts)).cuda()

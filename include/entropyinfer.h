@@ -464,7 +464,9 @@ typedef enum {
 } ei_cache_format;
 
 /* page_len is 64 or 128 and head_dim 128 (else EI_ERR_UNSUPPORTED); format is
- * an ei_cache_format, n_pages * n_kv_heads < 2^31 (else EI_ERR_SHAPE). */
+ * an ei_cache_format, n_pages * n_kv_heads < 2^31 (else EI_ERR_SHAPE).  A cache
+ * of no pages is valid (and its pointers may be NULL): nothing is stored in it
+ * and nothing attended to. */
 typedef struct {
   int32_t n_pages, n_kv_heads, page_len, head_dim, format;
 } ei_cache_shape;
@@ -516,8 +518,8 @@ size_t ei_cache_attn_workspace_bytes(int32_t n_q_heads, int32_t n_tokens, int32_
  * (which holds them already): with n_s rows in sequence s, its i-th query is
  * at position lengths[s] - n_s + i and attends to the keys up to its own;
  * grouped heads as everywhere.  fp32 accumulation and online softmax, bf16
- * output; the probabilities times V's scale are rounded to bf16 for the matrix
- * cores, as in the prefill attention.
+ * output; the probabilities times V's scale enter the second product with 16
+ * significant bits (as the sum of two bf16 numbers).
  *
  *   q, o        bf16 [n_q_heads][T][D]
  *   workspace   ei_cache_attn_workspace_bytes(), 16-byte aligned
@@ -525,12 +527,20 @@ size_t ei_cache_attn_workspace_bytes(int32_t n_q_heads, int32_t n_tokens, int32_
  * Keys past max_pages pages or on pages outside [0, n_pages) are not attended
  * to; a query with no key (a negative position, length 0) gets a zero row.
  * Rows of o that belong to no sequence are left as they were.  Rows of a page
- * behind the sequence's end are not read for their values.  Meant for few new
- * tokens a sequence: every 16 rows (tokens times query heads of a group) read
- * the sequence's keys once.
+ * behind the sequence's end may hold anything.  Meant for few new tokens a
+ * sequence: every 16 or 32 rows (tokens times query heads of a group) read the
+ * sequence's keys once.
+ *
+ * Scheduling: where a table has room for at most 2048 tokens, a workgroup per
+ * sequence, KV head and row tile.  Otherwise the keys of all sequences are dealt
+ * out evenly over the chip by what `lengths` holds at the time, and their parts
+ * are joined by a second kernel; the bits of a sequence's output then depend,
+ * by roundings, on the lengths of the others.
  *
  * Errors: EI_ERR_NULL, EI_ERR_SHAPE (also a softmax_scale that is not finite
- * and positive), EI_ERR_UNSUPPORTED, EI_ERR_WORKSPACE, EI_ERR_LAUNCH.
+ * and positive, n_tokens * n_q_heads or max_pages * page_len of 2^31 or more,
+ * and launches of 2^31 steps of 32 keys for a sequence), EI_ERR_UNSUPPORTED,
+ * EI_ERR_WORKSPACE, EI_ERR_LAUNCH.
  */
 ei_status ei_cache_attn(const uint16_t* q, int32_t n_q_heads, int32_t n_tokens,
                         const int32_t* cu_seqlens, int32_t n_seqs, const int32_t* lengths,

@@ -75,7 +75,8 @@ __device__ __forceinline__ void seq_rows(const Tokens& t, int s, int& first, int
 __device__ __forceinline__ int64_t slot_of(const Tokens& t, int s, int num, int den, int add) {
   return (int64_t)min(max(t.cu[s], 0), t.T) * num / den + (int64_t)add * s;
 }
-// The sequence that owns `slot`, and the slot's number in it.
+// The sequence that owns `slot`, and the slot's number in it (below zero for the
+// slots of the rows before the first sequence, which are nobody's).
 __device__ __forceinline__ void find_slot(const Tokens& t, int slot, int per_seq, int num, int den,
                                           int add, int& s, int& i) {
   if (!t.cu) {
@@ -170,7 +171,7 @@ __global__ __launch_bounds__(kThreads) void store_kernel(const uint16_t* __restr
   const int r0 = i == 0 ? (int)(from % P) : 0;        // the page's new rows: r0 .. r1 - 1
   const int64_t left = begin + n - c * P;
   const int r1 = (int)(left < P ? left : P);
-  if (n == 0 || left <= r0 || c >= pg.max_pages) return;
+  if (i < 0 || n == 0 || left <= r0 || c >= pg.max_pages) return;
   const int page = page_at(pg, s, (int)c);
   if (page < 0) return;
   const int64_t hp = (int64_t)page * pg.Hkv + h;
@@ -623,7 +624,7 @@ __global__ __launch_bounds__(WAVES* kWave, attend_occupancy(RT)) void attend_ker
   find_slot(a.tk, (int)(item / a.pg.Hkv), per_seq, G, kRows * RT, 1, s, tile);
   seq_rows(a.tk, s, first, n);
   const int row0 = tile * kRows * RT, rows = n * G;
-  if (row0 >= rows) return;
+  if (tile < 0 || row0 >= rows) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   WaveSums<RT> ws;
   attend_steps<FMT, P, RT>(a, s, kvh, row0, first, n, a.lengths[s], 0, keys_of<P>(a, s), wave, WAVES,

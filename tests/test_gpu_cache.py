@@ -201,6 +201,23 @@ def test_store_to_places_that_are_none():
     same_pages(dev, pages)
 
 
+@pytest.mark.parametrize("lead", [1, 70, 1000])
+def test_store_behind_rows_of_no_sequence(lead):
+    """The offsets begin at `lead`: the rows before are nobody's, also where the
+    first sequence begins pages into its table."""
+    hkv, P = 2, 64
+    pages = _pages(40, hkv, P, E4M3, 3)
+    lengths, new = [1200, 30, 129], [10, 30, 129]
+    table = _table(lengths, P, 40)
+    cu = [lead + c for c in _offsets(new)]
+    k, v = _rand((1, hkv, cu[-1] + 5, D), 4), _rand((1, hkv, cu[-1] + 5, D), 5)
+    dev = _cuda(pages)
+    eb.cache_store(k.cuda(), v.cuda(), dev, _i32(table).cuda(), _i32(lengths).cuda(),
+                   _i32(cu).cuda())
+    store_reference(pages, k, v, table, lengths, cu)
+    same_pages(dev, pages)
+
+
 def test_token_by_token_is_close_to_all_at_once():
     """Every roundings' sum stays below one step of the final scale: exact for
     e4m3 values of the normal range, under a step for int8."""
@@ -440,6 +457,23 @@ def test_attn_leaves_rows_of_no_sequence():
                   _i32([2, 3, 5]).cuda(), out=out)
     assert bool((out[:, :, :2] == 3.0).all()) and bool((out[:, :, 5:] == 3.0).all())
     assert bool((out[:, :, 2:5] != 3.0).any(-1).all())
+
+
+@pytest.mark.parametrize("lead", [1, 70, 1000])
+@pytest.mark.parametrize("spare", [1, 60])
+def test_attn_behind_rows_of_no_sequence(lead, spare):
+    lengths, new = [400, 30, 129], [10, 1, 3]
+    table = _table(lengths, 64, 12, spare=spare)
+    pages, cu = _pages(12, 2, 64, E4M3, 1), [lead + c for c in _offsets(new)]
+    q = _rand((1, 8, cu[-1] + 5, D), 2)
+    out = torch.full_like(q, 3.0).cuda()
+    eb.cache_attn(q.cuda(), _cuda(pages), _i32(table).cuda(), _i32(lengths).cuda(),
+                  _i32(cu).cuda(), out=out)
+    got = out.cpu()
+    assert bool((got[:, :, :lead] == 3.0).all()) and bool((got[:, :, cu[-1]:] == 3.0).all())
+    ref, off = attn_reference(q, pages, table, lengths, cu)
+    err = (got.double() - ref).abs()[:, :, lead:cu[-1]]
+    assert bool((err <= off[:, :, lead:cu[-1]]).all())
 
 
 def test_attn_is_the_same_every_time():

@@ -327,18 +327,19 @@ __device__ __forceinline__ void attend_steps(const AttendArgs& a, int s, int kvh
   const int j = lane & 15, g = lane >> 4;
 
   bf16x8 qf[RT][4];
-  int pos[RT];   // this lane's rows: the last key each sees (rows past the last repeat it)
+  // this lane's rows: the last key each sees, -1 for none (rows past the last repeat it)
+  int pos[RT];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
     const int row = min(row0 + kRows * rt + j, rows - 1);
-    pos[rt] = seq_len - n + row / G;
+    pos[rt] = max(max(seq_len, 0) - n + row / G, -1);
     const uint16_t* qp =
         a.q + ((int64_t)(kvh * G + row % G) * a.tk.T + first + row / G) * kHeadDim + 16 * g;
 #pragma unroll
     for (int c = 0; c < 4; ++c)   // dims 64 (c / 2) + 16 g + 8 (c % 2) ..
       qf[rt][c] = __builtin_bit_cast(bf16x8, *(const uint4*)(qp + 64 * (c >> 1) + 8 * (c & 1)));
   }
-  const int pos_min = seq_len - n + row0 / G;
+  const int pos_min = max(seq_len, 0) - n + row0 / G;
 
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {

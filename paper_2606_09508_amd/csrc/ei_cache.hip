@@ -810,101 +810,115 @@ __global__ __launch_bounds__(kThreads, attend_occupancy(RT)) void attend_share_k
 }
 
 // The parts of a shared item joined, in the order of their keys.  A workgroup
-// looks after 8 rows of the items that kWaves workers left, at once: a group of
-// 32 lanes adds up a row's 128 dims over every stripes-th part, then the stripes
-// are added up in order.
+// looks after 8 rows of the items that `per` workers left, up to four items at
+// once: a group of 32 lanes adds up a row's 128 dims over every stripes-th part,
+// then the stripes are added up in order.
 constexpr int kCombineThreads = 1024;
 constexpr int kCombineRows = 8;
+constexpr int kCombineItems = 4;
+// Workers a workgroup looks after, at most.  A workgroup that finds no item costs
+// its dispatch (16 waves), one that finds several shares its groups among them:
+// so as many as hold one item on average, kWaves at least (always kWaves /
+// by this rule: 48 items of 32 rows 9.6 / 5.0 us, 128 of them 12.5 / 8.0, 64 of 4
+// rows 5.3 / 4.7, 256 of them 5.3 / 5.7).
+constexpr int kCombineWorkers = 32;
+static_assert(kCombineWorkers <= kWave, "a lane reads what each of them left");
 constexpr int kCombineAhead = 4;   // parts in flight per group (8: 5.1 -> 7.4 us, 32 sequences)
-static_assert(kCombineThreads / 32 / kWaves >= kCombineRows, "a group for each row of an item");
-__global__ __launch_bounds__(kCombineThreads) void combine_kernel(AttendArgs a, int tile_rows) {
-  constexpr int kGroups = kCombineThreads / 32;
+static_assert(kCombineThreads / 32 / kCombineItems >= kCombineRows, "a group for each row of an item");
+__global__ __launch_bounds__(kCombineThreads) void combine_kernel(AttendArgs a, int tile_rows,
+                                                                  int workers, int per) {
+  constexpr int kGroupBits = 5, kGroups = 1 << kGroupBits;
+  static_assert(kGroups == kCombineThreads / 32, "groups of 32 lanes");
   __shared__ float sm_m[kGroups], sm_l[kGroups];
   __shared__ __attribute__((aligned(16))) float sm_o[kGroups][kHeadDim];
-  const int G = a.Hq / a.pg.Hkv;
+  const int G = a.Hq / a.pg.Hkv, lane = threadIdx.x % kWave;
   const int grp = threadIdx.x / 32, d = (threadIdx.x % 32) * 4;
-  // one item: all groups take it; several: a share of the groups each (whose
-  // item is asked for with the others' numbers of parts, not after them)
-  const SplitItem* const left = a.split + (int)blockIdx.x * kWaves;
-  int w = grp / (kGroups / kWaves);
-  SplitItem it = left[w];
-  int items = 0, only = 0;
-#pragma unroll
-  for (int i = 0; i < kWaves; ++i)
-    if (left[i].parts > 0) {
-      ++items;
-      only = i;
-    }
+  const int worker0 = (int)blockIdx.x * per;
+  SplitItem left{};   // of worker worker0 + lane
+  if (lane < per && worker0 + lane < workers) left = a.split[worker0 + lane];
+  uint64_t todo = __builtin_amdgcn_ballot_w64(left.parts > 0);
+  const int items = __builtin_popcountll(todo);
   if (items == 0) return;
-  const int mine = items == 1 ? kGroups : kGroups / kWaves;
-  if (items == 1 && w != only) it = left[w = only];
-  const int worker = (int)blockIdx.x * kWaves + w;
-  int first = 0, n = 0;
-  if (it.parts > 0) seq_rows(a.tk, it.s, first, n);
-  else it.row0 = 0;                  // (nothing else of it is set)
-  const int r0 = (int)blockIdx.y * kCombineRows;
-  const int rows = min(min(n * G - it.row0, tile_rows) - r0, kCombineRows);
-  auto slot_row = [&](int p, int r) -> int64_t {
-    int slot = it.first_slot;
-    if (p >= it.n_waves + it.n_groups) slot = 2 * (it.last + p - it.n_waves - it.n_groups);
-    else if (p >= it.n_waves) slot = 2 * kWaves * (it.group + p - it.n_waves);
-    else if (p > 0) slot = 2 * (worker + p);
-    return (int64_t)slot * tile_rows + r0 + r;
-  };
-  // rows by the power of two above them, the rest of the groups in stripes
-  int lanes_r = 1;
-  while (lanes_r < rows) lanes_r *= 2;   // (at most 8)
-  const int stripes = mine / lanes_r, at = grp % mine, stripe = at / lanes_r, r = at % lanes_r;
-  float m = -INFINITY, l = 0.0f;
-  float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  if (r < rows)
-    for (int p0 = stripe; p0 < it.parts; p0 += stripes * kCombineAhead) {
-      Part ml[kCombineAhead];
-      float4 x[kCombineAhead];
-#pragma unroll
-      for (int k = 0; k < kCombineAhead; ++k) {
-        const int64_t pr = slot_row(min(p0 + k * stripes, it.parts - 1), r);
-        ml[k] = a.part_ml[pr];
-        x[k] = *(const float4*)(a.part_o + pr * kHeadDim + d);
-      }
-#pragma unroll
-      for (int k = 0; k < kCombineAhead; ++k) {
-        if (p0 + k * stripes >= it.parts) break;
-        const float mn = fmaxf(m, ml[k].m);
-        const float f = m == mn ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
-        const float h = ml[k].m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml[k].m - mn);
-        l = l * f + ml[k].l * h;
-        acc.x = acc.x * f + x[k].x * h;
-        acc.y = acc.y * f + x[k].y * h;
-        acc.z = acc.z * f + x[k].z * h;
-        acc.w = acc.w * f + x[k].w * h;
-        m = mn;
-      }
+  // items at once: 1, 2 or 4, each with an equal share of the groups
+  const int many = items < 3 ? items - 1 : 2, mine = kGroups >> many;
+  const int ahead = __builtin_amdgcn_readfirstlane(grp >> (kGroupBits - many));
+  const int at = grp & (mine - 1), r0 = (int)blockIdx.y * kCombineRows;
+  for (int p = 0; p < items; p += 1 << many) {
+    uint64_t mask = todo;
+    for (int i = 0; i < 1 << many; ++i) {
+      if (i < ahead) mask &= mask - 1;
+      todo &= todo - 1;
     }
-  if (d == 0) {
-    sm_m[grp] = m;
-    sm_l[grp] = l;
+    const int w = mask ? (int)__builtin_ctzll(mask) : 0;
+    auto of = [&](int x) { return __builtin_amdgcn_readlane(x, w); };
+    const int parts = mask ? of(left.parts) : 0, s = of(left.s), kvh = of(left.kvh);
+    const int row0 = of(left.row0), first_slot = of(left.first_slot), n_waves = of(left.n_waves);
+    const int group = of(left.group), n_groups = of(left.n_groups), last = of(left.last);
+    int first = 0, n = 0;
+    if (parts > 0) seq_rows(a.tk, s, first, n);   // (else nothing of it is set)
+    const int rows = parts > 0 ? min(min(n * G - row0, tile_rows) - r0, kCombineRows) : 0;
+    auto slot_row = [&](int p, int r) -> int64_t {
+      int slot = first_slot;
+      if (p >= n_waves + n_groups) slot = 2 * (last + p - n_waves - n_groups);
+      else if (p >= n_waves) slot = 2 * kWaves * (group + p - n_waves);
+      else if (p > 0) slot = 2 * (worker0 + w + p);
+      return (int64_t)slot * tile_rows + r0 + r;
+    };
+    // rows by the power of two above them, the rest of the groups in stripes
+    const int bits = rows > 4 ? 3 : rows > 2 ? 2 : rows > 1 ? 1 : 0, lanes_r = 1 << bits;
+    const int stripes = mine >> bits, stripe = at >> bits, r = at & (lanes_r - 1);
+    float m = -INFINITY, l = 0.0f;
+    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (r < rows)
+      for (int p0 = stripe; p0 < parts; p0 += stripes * kCombineAhead) {
+        Part ml[kCombineAhead];
+        float4 x[kCombineAhead];
+#pragma unroll
+        for (int k = 0; k < kCombineAhead; ++k) {
+          const int64_t pr = slot_row(min(p0 + k * stripes, parts - 1), r);
+          ml[k] = a.part_ml[pr];
+          x[k] = *(const float4*)(a.part_o + pr * kHeadDim + d);
+        }
+#pragma unroll
+        for (int k = 0; k < kCombineAhead; ++k) {
+          if (p0 + k * stripes >= parts) break;
+          const float mn = fmaxf(m, ml[k].m);
+          const float f = m == mn ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
+          const float h = ml[k].m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml[k].m - mn);
+          l = l * f + ml[k].l * h;
+          acc.x = acc.x * f + x[k].x * h;
+          acc.y = acc.y * f + x[k].y * h;
+          acc.z = acc.z * f + x[k].z * h;
+          acc.w = acc.w * f + x[k].w * h;
+          m = mn;
+        }
+      }
+    if (p > 0) __syncthreads();   // (the sums before have been read)
+    if (d == 0) {
+      sm_m[grp] = m;
+      sm_l[grp] = l;
+    }
+    *(float4*)&sm_o[grp][d] = acc;
+    __syncthreads();
+    if (stripe != 0 || r >= rows) continue;
+    for (int k = 1; k < stripes; ++k) m = fmaxf(m, sm_m[grp + k * lanes_r]);
+    l = 0.0f;
+    acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int k = 0; k < stripes; ++k) {
+      const int from = grp + k * lanes_r;
+      const float h = sm_m[from] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(sm_m[from] - m);
+      const float4 x = *(const float4*)&sm_o[from][d];
+      l += sm_l[from] * h;
+      acc.x += x.x * h;
+      acc.y += x.y * h;
+      acc.z += x.z * h;
+      acc.w += x.w * h;
+    }
+    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+    const int row = row0 + r0 + r;
+    *(uint2*)(a.o + ((int64_t)(kvh * G + row % G) * a.tk.T + first + row / G) * kHeadDim + d) =
+        make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
   }
-  *(float4*)&sm_o[grp][d] = acc;
-  __syncthreads();
-  if (stripe != 0 || r >= rows) return;
-  for (int k = 1; k < stripes; ++k) m = fmaxf(m, sm_m[grp + k * lanes_r]);
-  l = 0.0f;
-  acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  for (int k = 0; k < stripes; ++k) {
-    const int from = grp + k * lanes_r;
-    const float h = sm_m[from] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(sm_m[from] - m);
-    const float4 x = *(const float4*)&sm_o[from][d];
-    l += sm_l[from] * h;
-    acc.x += x.x * h;
-    acc.y += x.y * h;
-    acc.z += x.z * h;
-    acc.w += x.w * h;
-  }
-  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  const int row = it.row0 + r0 + r;
-  *(uint2*)(a.o + ((int64_t)(it.kvh * G + row % G) * a.tk.T + first + row / G) * kHeadDim + d) =
-      make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
 }
 
 // ----------------------------------------------------------------------------
@@ -1032,8 +1046,11 @@ void launch_attend_t(const AttendPlan& pl, const AttendArgs& a, hipStream_t stre
     hipLaunchKernelGGL((attend_share_kernel<FMT, P, RT>), dim3((unsigned)pl.groups),
                        dim3(kThreads), 0, stream, a);
     const unsigned row_blocks = (unsigned)((pl.item_rows + kCombineRows - 1) / kCombineRows);
-    hipLaunchKernelGGL(combine_kernel, dim3((unsigned)pl.groups, row_blocks), dim3(kCombineThreads),
-                       0, stream, a, kRows * RT);
+    const int workers = pl.groups * kWaves;
+    int per = kWaves;
+    while (per < kCombineWorkers && pl.items * (2 * per) <= workers) per *= 2;
+    hipLaunchKernelGGL(combine_kernel, dim3((unsigned)((workers + per - 1) / per), row_blocks),
+                       dim3(kCombineThreads), 0, stream, a, kRows * RT, workers, per);
     return;
   }
   constexpr int64_t kMost = (1ll << 31) / (kShortWaves * kWave);

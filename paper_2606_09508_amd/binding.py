@@ -571,12 +571,8 @@ def swiglu(g, u, out=None):
 # --------------------------------------------------------------------------
 
 # (A decoding step makes one store and one attention per layer, of a few us on
-# the GPU each: as above, the good case is one test per tensor.)
-def _good(t, dtype, ndim: int, dev: int) -> bool:
-    return isinstance(t, torch.Tensor) and t.dtype is dtype and t.dim() == ndim \
-        and t.get_device() == dev and t.is_contiguous()
-
-
+# the GPU each: as above, the good case is one test per tensor, written out where
+# a function's call would cost as much as the test.)
 def _device_of(t) -> int:
     """The GPU that t is on, -1 where it is on none (or no tensor)."""
     return t.get_device() if isinstance(t, torch.Tensor) and t.is_cuda else -1
@@ -584,15 +580,17 @@ def _device_of(t) -> int:
 
 def _req_packed(t, name: str, dev: int) -> None:
     """bf16 [1, heads, tokens, D] on GPU dev."""
-    if dev < 0 or not _good(t, torch.bfloat16, 4, dev):
+    if dev < 0 or not (isinstance(t, torch.Tensor) and t.dtype is torch.bfloat16 and t.dim() == 4
+                       and t.get_device() == dev and t.is_contiguous()):
         _req(t, name, torch.bfloat16, 4)
         raise ValueError(f"tensors on different devices: {name} on {t.device}")
-    if t.shape[0] != 1:
+    if t.size(0) != 1:
         raise ValueError(f"{name} {tuple(t.shape)} is not [1, heads, tokens, head_dim]")
 
 
 def _req_i32(t, name: str, ndim: int, dev: int) -> None:
-    if not _good(t, torch.int32, ndim, dev):
+    if not (isinstance(t, torch.Tensor) and t.dtype is torch.int32 and t.dim() == ndim
+            and t.get_device() == dev and t.is_contiguous()):
         _req(t, name, torch.int32, ndim)
         raise ValueError(f"tensors on different devices: {name} on {t.device}")
 
@@ -661,29 +659,42 @@ def _cache_shape(n_pages: int, hkv: int, page_len: int, head_dim: int, fmt: int)
     return CacheShape(n_pages, hkv, page_len, head_dim, fmt)
 
 
+def _req_pages(pages, layers: bool) -> None:
+    """The error of pages that _cache_args does not take."""
+    k = pages[0]
+    dtype = k.dtype if isinstance(k, torch.Tensor) else None
+    if dtype not in CACHE_FORMATS:
+        raise TypeError(f"cache pages are float8_e4m3fn or int8, not {dtype or type(k)}")
+    nd = 5 if layers and k.dim() == 5 else 4
+    for t, name in zip(pages, CachePages._fields):
+        scale = name.endswith("scale")
+        _req(t, "pages." + name, torch.float32 if scale else dtype, nd - 2 if scale else nd)
+    raise ValueError("tensors on different devices: pages on "
+                     + ", ".join(str(t.device) for t in pages))
+
+
 def _cache_args(pages, dev: int, layers: bool = False):
     """(CacheShape, CachePointers) of pages on GPU dev, checked; with ``layers``
     there may be a leading dimension, whose size then comes first."""
     k, v, ks, vs = pages
-    dtype = k.dtype if isinstance(k, torch.Tensor) else None
-    fmt = CACHE_FORMATS.get(dtype)
-    nd = 5 if layers and fmt is not None and k.dim() == 5 else 4
-    if dev < 0 or fmt is None or not (_good(k, dtype, nd, dev) and _good(v, dtype, nd, dev)
-                                      and _good(ks, torch.float32, nd - 2, dev)
-                                      and _good(vs, torch.float32, nd - 2, dev)):
-        if fmt is None:
-            raise TypeError(f"cache pages are float8_e4m3fn or int8, not {dtype or type(k)}")
-        for t, n, dt, d in ((k, "k", dtype, nd), (v, "v", dtype, nd),
-                            (ks, "k_scale", torch.float32, nd - 2),
-                            (vs, "v_scale", torch.float32, nd - 2)):
-            _req(t, "pages." + n, dt, d)
-        raise ValueError(f"tensors on different devices: pages on {k.device}, {v.device}, "
-                         f"{ks.device}, {vs.device}")
+    T, f32 = torch.Tensor, torch.float32
+    fmt = CACHE_FORMATS.get(k.dtype) if isinstance(k, T) else None
+    if fmt is None or not (
+            isinstance(v, T) and isinstance(ks, T) and isinstance(vs, T) and dev >= 0
+            and k.get_device() == dev and v.get_device() == dev
+            and ks.get_device() == dev and vs.get_device() == dev
+            and v.dtype is k.dtype and ks.dtype is f32 and vs.dtype is f32
+            and k.is_contiguous() and v.is_contiguous()
+            and ks.is_contiguous() and vs.is_contiguous()):
+        _req_pages(pages, layers)
     shape, lead = k.shape, ks.shape
+    nd = len(shape)
+    if nd != 4 and not (layers and nd == 5):
+        _req_pages(pages, layers)
     if v.shape != shape or lead != shape[:-2] or vs.shape != lead:
         raise ValueError(f"pages: v {tuple(v.shape)}, k_scale {tuple(lead)} or v_scale "
                          f"{tuple(vs.shape)} do not match k {tuple(shape)}")
-    cs = _cache_shape(*shape[nd - 4:], fmt)
+    cs = _cache_shape(*shape[-4:], fmt)
     ptrs = CachePointers(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr())
     return (shape[0] if nd == 5 else 1, cs, ptrs) if layers else (cs, ptrs)
 
@@ -699,7 +710,7 @@ def _sequences(tokens: int, page_table, lengths, cu_seqlens, dev: int) -> int:
         _req_i32(cu_seqlens, "cu_seqlens", 1, dev)
         if cu_seqlens.shape[0] != S + 1:
             raise ValueError(f"cu_seqlens has {cu_seqlens.shape[0]} offsets for {S} sequences")
-    elif tokens % S if S else tokens:
+    elif tokens and (not S or tokens % S):
         raise ValueError(f"{tokens} tokens do not divide among {S} sequences: pass cu_seqlens")
     return S
 

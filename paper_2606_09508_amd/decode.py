@@ -142,7 +142,9 @@ class PagedCache:
         self._copy(src, dst)
 
     def truncate(self, seq: int, length: int) -> None:
-        """Drops a sequence's tokens from `length` on."""
+        """Drops a sequence's tokens from `length` on.  The scales of the page it
+        then ends in stay what the dropped tokens made them (NaN, and with it the
+        page's other tokens, where those were not finite)."""
         old = self.length(seq)
         if not 0 <= length <= old:
             raise ValueError(f"cannot cut {old} tokens to {length}")

@@ -338,6 +338,35 @@ def test_attn_wide_table_of_ragged_sequences(held, new, hq, hkv, dtype):
     run_attn(held, new, hq, hkv, 64, dtype, spare=40)
 
 
+def test_calls_of_no_tokens_and_of_no_sequences():
+    pages, no = _cuda(_pages(4, 2, 64, E4M3, 1)), torch.empty((1, 2, 0, D), dtype=torch.bfloat16)
+    before = [t.clone() for t in pages]
+    for rows in (0, 3):
+        table, lengths = torch.zeros((rows, 40), dtype=torch.int32), _i32([64] * rows)
+        for cu in (None, torch.zeros(rows + 1, dtype=torch.int32).cuda()):
+            eb.cache_store(no.cuda(), no.cuda(), pages, table.cuda(), lengths.cuda(), cu)
+            got = eb.cache_attn(no.cuda(), pages, table.cuda(), lengths.cuda(), cu)
+            assert got.shape == no.shape
+        q = torch.ones((1, 2, rows, D), dtype=torch.bfloat16).cuda()
+        assert eb.cache_attn(q[:, :, :0].contiguous(), pages, table[:, :0].contiguous().cuda(),
+                             lengths.cuda()).numel() == 0
+    none = torch.empty(0, dtype=torch.int32).cuda()
+    eb.cache_copy(pages, none, none)
+    assert all(torch.equal(_bytes(a), _bytes(b)) for a, b in zip(pages, before))
+
+
+@pytest.mark.parametrize("spare", [1, 100])
+def test_attn_far_before_the_first_position(spare):
+    """More new tokens than the sequence holds, on pages and on none: the rows
+    before position 0 see nothing."""
+    def edit(pages, table, lengths):
+        lengths[0], table[1][0] = 70, -1
+        lengths[1] = 3
+    got = run_attn([0, 0, 5], [400, 300, 2], 4, 2, 64, E4M3, edit=edit, spare=spare)
+    assert bool((got[0, :, :330] == 0).all()) and bool((got[0, :, 400:700] == 0).all())
+    assert bool((got[0, :, 330:400] != 0).any(-1).all())
+
+
 @pytest.mark.parametrize("dtype", [E4M3, INT8])
 def test_attn_rows_without_keys(dtype):
     """Length zero, and queries before the first position."""

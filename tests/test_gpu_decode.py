@@ -163,6 +163,21 @@ def test_cut_back_and_go_on():
     assert _rel(got, want) <= 1e-2
 
 
+def test_steps_that_leave_sequences_out():
+    """Counts of zero, and a step of no token at all."""
+    layers, head, cache, dec, g = _setup()
+    s, t = cache.add(), cache.add()
+    dec.prompts(_hidden(g, 100), [64, 36], [s, t])
+    x = _hidden(g, 3)
+    got, _ = dec.step(x, [s, t], [0, 3])
+    assert (cache.length(s), cache.length(t)) == (64, 39)
+    want, _ = _reference_step(dec, x, [s, t], [0, 3])
+    assert _rel(got, want) <= 1e-2
+    last, logits = dec.step(x[:, :0], [s, t], [0, 0])
+    assert last.shape == (0, SHAPE.hidden) and logits.shape == (0, SHAPE.vocab)
+    assert (cache.length(s), cache.length(t)) == (64, 39)
+
+
 def test_refusals():
     layers, head, cache, dec, g = _setup(n_pages=4)
     s = cache.add()

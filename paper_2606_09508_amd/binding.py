@@ -572,7 +572,11 @@ def swiglu(g, u, out=None):
 
 # (A decoding step makes one store and one attention per layer, of a few us on
 # the GPU each: as above, the good case is one test per tensor, written out where
-# a function's call would cost as much as the test.)
+# a function's call would cost as much as the test; where the tensors' device is
+# not the current one, a function calls itself with it made current.)
+_current_device, _raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+
+
 def _device_of(t) -> int:
     """The GPU that t is on, -1 where it is on none (or no tensor)."""
     return t.get_device() if isinstance(t, torch.Tensor) and t.is_cuda else -1
@@ -616,12 +620,17 @@ def packed_prefill_attn(q, k, v, cu_seqlens, softmax_scale: float | None = None,
         _req_packed(out, "out", dev)
         if out.shape != shape:
             raise ValueError(f"out {tuple(out.shape)} does not match q {tuple(shape)}")
-    sc = 1.0 / math.sqrt(shape[3]) if softmax_scale is None else float(softmax_scale)
-    with _on(q):
-        st = lib().ei_packed_prefill_attn(_ptr(q), _ptr(k), _ptr(v), dims_of(q, k),
-                                          _ptr(cu_seqlens), cu_seqlens.numel() - 1, sc,
-                                          1 if causal else 0, _ptr(out), _stream(q))
-    _check("ei_packed_prefill_attn", st)
+    if dev != _current_device():
+        with torch.cuda.device(dev):
+            return packed_prefill_attn(q, k, v, cu_seqlens, softmax_scale, causal, out)
+    _, Hq, T, D = shape
+    sc = 1.0 / math.sqrt(D) if softmax_scale is None else float(softmax_scale)
+    st = lib().ei_packed_prefill_attn(q.data_ptr(), k.data_ptr(), v.data_ptr(),
+                                      Dims(1, Hq, k.size(1), T, D), cu_seqlens.data_ptr(),
+                                      cu_seqlens.size(0) - 1, sc, 1 if causal else 0,
+                                      out.data_ptr(), _raw_stream(dev))
+    if st:
+        _check("ei_packed_prefill_attn", st)
     return out
 
 
@@ -674,8 +683,9 @@ def _req_pages(pages, layers: bool) -> None:
 
 
 def _cache_args(pages, dev: int, layers: bool = False):
-    """(CacheShape, CachePointers) of pages on GPU dev, checked; with ``layers``
-    there may be a leading dimension, whose size then comes first."""
+    """(KV heads, head_dim, CacheShape, CachePointers) of pages on GPU dev,
+    checked; with ``layers`` (layers, CacheShape, CachePointers), and there may be
+    a leading dimension."""
     k, v, ks, vs = pages
     T, f32 = torch.Tensor, torch.float32
     fmt = CACHE_FORMATS.get(k.dtype) if isinstance(k, T) else None
@@ -694,25 +704,27 @@ def _cache_args(pages, dev: int, layers: bool = False):
     if v.shape != shape or lead != shape[:-2] or vs.shape != lead:
         raise ValueError(f"pages: v {tuple(v.shape)}, k_scale {tuple(lead)} or v_scale "
                          f"{tuple(vs.shape)} do not match k {tuple(shape)}")
-    cs = _cache_shape(*shape[-4:], fmt)
+    n_pages, hkv, page_len, D = shape[-4:] if nd == 5 else shape
+    cs = _cache_shape(n_pages, hkv, page_len, D, fmt)
     ptrs = CachePointers(k.data_ptr(), v.data_ptr(), ks.data_ptr(), vs.data_ptr())
-    return (shape[0] if nd == 5 else 1, cs, ptrs) if layers else (cs, ptrs)
+    return (shape[0] if nd == 5 else 1, cs, ptrs) if layers else (hkv, D, cs, ptrs)
 
 
-def _sequences(tokens: int, page_table, lengths, cu_seqlens, dev: int) -> int:
-    """The number of sequences, after checks of what describes them."""
+def _sequences(tokens: int, page_table, lengths, cu_seqlens, dev: int):
+    """The number of sequences and of the table's columns, after checks of what
+    describes them."""
     _req_i32(page_table, "page_table", 2, dev)
     _req_i32(lengths, "lengths", 1, dev)
-    S = lengths.shape[0]
-    if page_table.shape[0] != S:
-        raise ValueError(f"page_table has {page_table.shape[0]} rows for {S} lengths")
+    S, cols = page_table.shape
+    if lengths.size(0) != S:
+        raise ValueError(f"page_table has {S} rows for {lengths.size(0)} lengths")
     if cu_seqlens is not None:
         _req_i32(cu_seqlens, "cu_seqlens", 1, dev)
-        if cu_seqlens.shape[0] != S + 1:
-            raise ValueError(f"cu_seqlens has {cu_seqlens.shape[0]} offsets for {S} sequences")
+        if cu_seqlens.size(0) != S + 1:
+            raise ValueError(f"cu_seqlens has {cu_seqlens.size(0)} offsets for {S} sequences")
     elif tokens and (not S or tokens % S):
         raise ValueError(f"{tokens} tokens do not divide among {S} sequences: pass cu_seqlens")
-    return S
+    return S, cols
 
 
 def cache_store(k, v, pages: CachePages, page_table, lengths, cu_seqlens=None) -> None:
@@ -726,15 +738,19 @@ def cache_store(k, v, pages: CachePages, page_table, lengths, cu_seqlens=None) -
     shape = k.shape
     if v.shape != shape:
         raise ValueError(f"v {tuple(v.shape)} does not match k {tuple(shape)}")
-    cs, ptrs = _cache_args(pages, dev)
-    _, hkv, T, D = shape
-    if hkv != cs.n_kv_heads or D != cs.head_dim:
+    hkv, head_dim, cs, ptrs = _cache_args(pages, dev)
+    _, heads, T, D = shape
+    if heads != hkv or D != head_dim:
         raise ValueError(f"k {tuple(shape)} does not match the pages {tuple(pages.k.shape)}")
-    S = _sequences(T, page_table, lengths, cu_seqlens, dev)
-    with _on(k):
-        st = lib().ei_cache_store(_ptr(k), _ptr(v), T, _ptr(cu_seqlens), S, _ptr(lengths),
-                                  _ptr(page_table), page_table.shape[1], cs, ptrs, _stream(k))
-    _check("ei_cache_store", st)
+    S, cols = _sequences(T, page_table, lengths, cu_seqlens, dev)
+    if dev != _current_device():
+        with torch.cuda.device(dev):
+            return cache_store(k, v, pages, page_table, lengths, cu_seqlens)
+    st = lib().ei_cache_store(k.data_ptr(), v.data_ptr(), T, _ptr(cu_seqlens), S,
+                              lengths.data_ptr(), page_table.data_ptr(), cols, cs, ptrs,
+                              _raw_stream(dev))
+    if st:
+        _check("ei_cache_store", st)
 
 
 def cache_attn(q, pages: CachePages, page_table, lengths, cu_seqlens=None,
@@ -745,18 +761,21 @@ def cache_attn(q, pages: CachePages, page_table, lengths, cu_seqlens=None,
     (optional, uint8, of cache_attn_workspace_bytes) is scratch of this call."""
     dev = _device_of(q)
     _req_packed(q, "q", dev)
-    cs, ptrs = _cache_args(pages, dev)
+    hkv, head_dim, cs, ptrs = _cache_args(pages, dev)
     _, Hq, T, D = shape = q.shape
-    if D != cs.head_dim or Hq % cs.n_kv_heads:
+    if D != head_dim or not hkv or Hq % hkv:
         raise ValueError(f"q {tuple(shape)} does not match the pages {tuple(pages.k.shape)}")
-    S = _sequences(T, page_table, lengths, cu_seqlens, dev)
-    if out is None:
-        out = torch.empty_like(q)
-    else:
+    S, cols = _sequences(T, page_table, lengths, cu_seqlens, dev)
+    if out is not None:
         _req_packed(out, "out", dev)
         if out.shape != shape:
             raise ValueError(f"out {tuple(out.shape)} does not match q {tuple(shape)}")
-    cols = page_table.shape[1]
+    if dev != _current_device():
+        with torch.cuda.device(dev):
+            return cache_attn(q, pages, page_table, lengths, cu_seqlens, softmax_scale, out,
+                              workspace)
+    if out is None:
+        out = torch.empty_like(q)
     L = lib()
     if workspace is None:
         nb = L.ei_cache_attn_workspace_bytes(Hq, T, cu_seqlens is not None, S, cols, cs)
@@ -768,11 +787,11 @@ def cache_attn(q, pages: CachePages, page_table, lengths, cu_seqlens=None,
             raise ValueError("workspace must be contiguous")
         nb = workspace.numel() * workspace.element_size()
     sc = 1.0 / math.sqrt(D) if softmax_scale is None else float(softmax_scale)
-    with _on(q):
-        st = L.ei_cache_attn(_ptr(q), Hq, T, _ptr(cu_seqlens), S, _ptr(lengths),
-                             _ptr(page_table), cols, cs, ptrs, sc, _ptr(out), _ptr(workspace), nb,
-                             _stream(q))
-    _check("ei_cache_attn", st)
+    st = L.ei_cache_attn(q.data_ptr(), Hq, T, _ptr(cu_seqlens), S, lengths.data_ptr(),
+                         page_table.data_ptr(), cols, cs, ptrs, sc, out.data_ptr(),
+                         _ptr(workspace), nb, _raw_stream(dev))
+    if st:
+        _check("ei_cache_attn", st)
     return out
 
 
@@ -794,6 +813,10 @@ def cache_copy(pages: CachePages, src, dst) -> None:
     _req_i32(dst, "dst", 1, dev)
     if src.shape != dst.shape:
         raise ValueError(f"{src.numel()} source pages for {dst.numel()} destinations")
-    with _on(src):
-        st = lib().ei_cache_copy(cs, layers, ptrs, _ptr(src), _ptr(dst), src.numel(), _stream(src))
-    _check("ei_cache_copy", st)
+    if dev != _current_device():
+        with torch.cuda.device(dev):
+            return cache_copy(pages, src, dst)
+    st = lib().ei_cache_copy(cs, layers, ptrs, src.data_ptr(), dst.data_ptr(), src.size(0),
+                             _raw_stream(dev))
+    if st:
+        _check("ei_cache_copy", st)

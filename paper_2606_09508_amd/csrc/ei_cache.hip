@@ -636,10 +636,10 @@ __global__ __launch_bounds__(WAVES* kWave, attend_occupancy(RT)) void attend_ker
 }
 
 // Long tables, whose sequences may be of any lengths: the items' steps dealt out
-// evenly over the waves of the launch.  With the items one behind the other (by
+// over the waves of the launch.  With the items one behind the other (by
 // sequence, KV head and row tile), each kItemCost steps longer than it is (what
-// a wave waits for before an item's first step), every wave takes an equal run
-// of them: a last part of an item, whole items, a first part of one.  Whole items
+// a wave waits for before an item's first step), every wave takes a run of
+// them, all equally long (but see kElderShare): a last part of an item, whole items, a first part of one.  Whole items
 // are written out, parts left for combine_kernel: nothing in here waits for
 // another wave, except where the runs of a workgroup's waves lie in one item:
 // they then share the item's steps and leave one part.
@@ -653,6 +653,15 @@ constexpr int kCus = 256;
 constexpr int kShareGroups = 2 * kCus;
 constexpr int kItemCost = 5;    // (8: 128 ragged sequences 81 -> 83 us)
 constexpr int kShareLeast = 4;   // steps and costs a wave takes at least
+// The first workgroup of a CU gets its loads before the second one's: with equal
+// runs its waves end first (8 sequences of up to 128k tokens after 213 us, the
+// second's after 246 to 254; 6 of 13000, 32 rows each: 29, 37 to 43), and what is
+// left does not fill HBM.  Wave priorities change nothing.  So where every CU has
+// two, the first half of the workgroups takes runs longer than the average by
+// 1 / kElderShare (attention alone, without / 8 / 6 / 4: the 6 sequences in int8
+// 46.5 / 42.4 / 42.6 / 41.5 us, 200 of 1000 to 4000 tokens 152 / 149 / 148 / 151, 256
+// of 200 to 8000 193 / 188 / 188 / 192, 32 of 131 to 7974 50 / 49.5 / 49.5 / 49).
+constexpr int kElderShare = 6;
 
 // A value that all lanes share, in scalar registers.
 __device__ __forceinline__ int64_t uniform(int64_t x) {
@@ -707,9 +716,20 @@ __global__ __launch_bounds__(kThreads, attend_occupancy(RT)) void attend_share_k
       before += uniform(__shfl(incl, kWave - 1));
     }
   };
+  // worker w's run: bound(w) .. bound(w + 1) - 1 (less what lies past the total)
   const int64_t even = (total + workers - 1) / workers;
-  const int64_t per = even < kShareLeast ? kShareLeast : even;
-  const int64_t g0 = group * kWaves * per, g1 = min(g0 + kWaves * per, total);
+  const int elders = workers == kShareGroups * kWaves && even > kShareLeast ? workers / 2 : 0;
+  const int64_t elder = even + even / kElderShare;
+  const int64_t per = elders ? (total - elders * elder + elders - 1) / elders
+                             : even < kShareLeast ? kShareLeast : even;
+  auto bound = [&](int w) -> int64_t {
+    return min(w, elders) * elder + max(w - elders, 0) * per;
+  };
+  auto owner = [&](int64_t u) -> int {
+    const int64_t rest = u - elders * elder;
+    return rest < 0 ? (int)(u / elder) : elders + (int)(rest / per);
+  };
+  const int64_t g0 = bound(group * kWaves), g1 = min(bound((group + 1) * kWaves), total);
   if (g0 >= g1) return;
   // The units u .. end - 1 of the item that unit u lies in (after cost_of(s)).
   struct Run {
@@ -735,9 +755,8 @@ __global__ __launch_bounds__(kThreads, attend_occupancy(RT)) void attend_share_k
   // Leaves the list of an item's parts, the first of which is at `slot`, left
   // by wave w0 or, with `joint`, by this workgroup's waves together.
   auto leave_item = [&](const Run& r, int kvh, int row0, int slot, int w0, bool joint) {
-    const int last = (int)((r.next - 1) / per), last_group = last / kWaves;
-    int64_t last_end = (last_group + 1) * kWaves * per;
-    if (last_end > total) last_end = total;
+    const int last = owner(r.next - 1), last_group = last / kWaves;
+    const int64_t last_end = min(bound((last_group + 1) * kWaves), total);
     SplitItem it{};
     it.s = s;
     it.kvh = kvh;
@@ -761,7 +780,7 @@ __global__ __launch_bounds__(kThreads, attend_occupancy(RT)) void attend_share_k
   cost_of(s);
   // whether the workgroup's waves go together, their runs being of one item
   const bool joint = g1 <= run_at(g0, g1).next;
-  const int64_t u0 = joint ? g0 : worker * per, u1 = joint ? g1 : min(u0 + per, total);
+  const int64_t u0 = joint ? g0 : bound(worker), u1 = joint ? g1 : min(bound(worker + 1), total);
   if (u0 >= u1) return;
   if (!joint && wave > 0) find(u0);
   for (int64_t u = u0; u < u1 && s < a.tk.S;) {

@@ -639,10 +639,11 @@ __global__ __launch_bounds__(WAVES* kWave, attend_occupancy(RT)) void attend_ker
 // over the waves of the launch.  With the items one behind the other (by
 // sequence, KV head and row tile), each kItemCost steps longer than it is (what
 // a wave waits for before an item's first step), every wave takes a run of
-// them, all equally long (but see kElderShare): a last part of an item, whole items, a first part of one.  Whole items
-// are written out, parts left for combine_kernel: nothing in here waits for
-// another wave, except where the runs of a workgroup's waves lie in one item:
-// they then share the item's steps and leave one part.
+// them, all equally long (but see kElderShare): a last part of an item, whole
+// items, a first part of one.  Whole items are written out, parts left for
+// combine_kernel: nothing in here waits for another wave, except where the runs
+// of a workgroup's waves lie in one item: they then share the item's steps and
+// leave one part.
 //
 // Each wave adds the sequences up for itself.  Two waves a SIMD are what HBM
 // needs; with three the oldest goes first and the youngest ends a third later (8
@@ -677,21 +678,44 @@ __global__ __launch_bounds__(kThreads, attend_occupancy(RT)) void attend_share_k
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int group = (int)blockIdx.x, worker = group * kWaves + wave;
   const int workers = (int)gridDim.x * kWaves;
-  int steps, tiles;   // of the sequence that cost_of was last called for
+  int steps = 0, tiles = 0;   // of the sequence that cost_of or look was last called for
+  auto cost = [&]() { return (int64_t)(steps + kItemCost) * tiles * a.pg.Hkv; };
   auto cost_of = [&](int s) -> int64_t {
     int first, n;
     seq_rows(a.tk, s, first, n);
     steps = (keys_of<P>(a, s) + kKeys - 1) / kKeys;
     tiles = (n * G + kRows * RT - 1) / (kRows * RT);
-    return (int64_t)(steps + kItemCost) * tiles * a.pg.Hkv;
+    return cost();
   };
-  // the first 64 sequences' costs stay in registers
-  const int64_t my_cost = lane < a.tk.S ? cost_of(lane) : 0;
-  int64_t total = my_cost;
-  for (int s = kWave + lane; s < a.tk.S; s += kWave) total += cost_of(s);
+  // of 64 sequences: the costs up to each lane's
+  auto up_to = [&](int64_t x) -> int64_t {
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) total += __shfl_xor(total, o);
-  total = uniform(total);
+    for (int o = 1; o < kWave; o <<= 1) {
+      const int64_t up = __shfl_up(x, o);
+      if (lane >= o) x += up;
+    }
+    return x;
+  };
+  // the first 64 sequences stay in registers
+  const int64_t my_cost = lane < a.tk.S ? cost_of(lane) : 0;
+  const int my_steps = steps, my_tiles = tiles;
+  const int64_t my_end = up_to(my_cost);
+  int64_t total = uniform(__shfl(my_end, kWave - 1));
+  if (a.tk.S > kWave) {
+    int64_t rest = 0;
+    for (int s = kWave + lane; s < a.tk.S; s += kWave) rest += cost_of(s);
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) rest += __shfl_xor(rest, o);
+    total += uniform(rest);
+  }
+  auto look = [&](int s) {   // (s the same in all lanes)
+    if (s < kWave) {
+      steps = __builtin_amdgcn_readlane(my_steps, s);
+      tiles = __builtin_amdgcn_readlane(my_tiles, s);
+    } else {
+      cost_of(s);
+    }
+  };
   if (lane == 0) a.split[worker].parts = 0;
   // the sequence that unit u < total lies in, and the unit it starts at
   int s;
@@ -699,17 +723,12 @@ __global__ __launch_bounds__(kThreads, attend_occupancy(RT)) void attend_share_k
   auto find = [&](int64_t u) {
     int64_t before = 0;
     for (s = 0; s < a.tk.S; s += kWave) {
-      const int64_t cost = s == 0 ? my_cost : s + lane < a.tk.S ? cost_of(s + lane) : 0;
-      int64_t incl = cost;
-#pragma unroll
-      for (int o = 1; o < kWave; o <<= 1) {
-        const int64_t up = __shfl_up(incl, o);
-        if (lane >= o) incl += up;
-      }
+      const int64_t own = s == 0 ? my_cost : s + lane < a.tk.S ? cost_of(s + lane) : 0;
+      const int64_t incl = s == 0 ? my_end : up_to(own);
       const uint64_t past = __builtin_amdgcn_ballot_w64(before + incl > u);
       if (past != 0) {
         const int at = (int)__builtin_ctzll(past);
-        start = uniform(__shfl(before + incl - cost, at));
+        start = uniform(__shfl(before + incl - own, at));
         s = __builtin_amdgcn_readfirstlane(s + at);
         return;
       }
@@ -731,7 +750,7 @@ __global__ __launch_bounds__(kThreads, attend_occupancy(RT)) void attend_share_k
   };
   const int64_t g0 = bound(group * kWaves), g1 = min(bound((group + 1) * kWaves), total);
   if (g0 >= g1) return;
-  // The units u .. end - 1 of the item that unit u lies in (after cost_of(s)).
+  // The units u .. end - 1 of the item that unit u lies in (after look(s)).
   struct Run {
     int item, st0, st1;     // of the sequence; its steps
     int64_t base, next;     // the item's first unit, the one behind it
@@ -777,17 +796,20 @@ __global__ __launch_bounds__(kThreads, attend_occupancy(RT)) void attend_share_k
 
   find(g0);
   if (s >= a.tk.S) return;
-  cost_of(s);
+  look(s);
   // whether the workgroup's waves go together, their runs being of one item
   const bool joint = g1 <= run_at(g0, g1).next;
   const int64_t u0 = joint ? g0 : bound(worker), u1 = joint ? g1 : min(bound(worker + 1), total);
   if (u0 >= u1) return;
-  if (!joint && wave > 0) find(u0);
+  if (!joint && wave > 0) {
+    find(u0);
+    if (s >= a.tk.S) return;
+    look(s);
+  }
   for (int64_t u = u0; u < u1 && s < a.tk.S;) {
-    const int64_t cost = cost_of(s);
-    if (u >= start + cost) {   // (also past sequences without new tokens: they cost nothing)
-      start += cost;
-      ++s;
+    if (u >= start + cost()) {   // (also past sequences without new tokens: they cost nothing)
+      start += cost();
+      if (++s < a.tk.S) cost_of(s);
       continue;
     }
     const Run r = run_at(u, u1);

@@ -46,6 +46,14 @@ __device__ __forceinline__ void store_once4(void* p, uint4 w) {
   __builtin_nontemporal_store(__builtin_bit_cast(u32x4, w), (u32x4*)p);
 }
 
+// Entry i of a list that the kernel only reads: where the lanes share i, through
+// the scalar cache.  (Vector loads return in order, behind the keys that all waves
+// of the CU have asked for.)
+template <class T>
+__device__ __forceinline__ T entry(const T* list, int64_t i) {
+  return ((const __attribute__((address_space(4))) T*)list)[i];
+}
+
 __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
   const f32x2 x = {lo, hi};
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
@@ -65,15 +73,15 @@ __device__ __forceinline__ void seq_rows(const Tokens& t, int s, int& first, int
     count = t.each;
     return;
   }
-  first = min(max(t.cu[s], 0), t.T);
-  count = max(min(max(t.cu[s + 1], 0), t.T) - first, 0);
+  first = min(max(entry(t.cu, s), 0), t.T);
+  count = max(min(max(entry(t.cu, s + 1), 0), t.T) - first, 0);
 }
 
 // Work items of sequences whose lengths only the device knows.  With `cu`,
 // sequence s owns the slots floor(cu[s] * num / den) + add * s up to the next
 // one's first, which is floor(n_s * num / den) + add of them or one more.
 __device__ __forceinline__ int64_t slot_of(const Tokens& t, int s, int num, int den, int add) {
-  return (int64_t)min(max(t.cu[s], 0), t.T) * num / den + (int64_t)add * s;
+  return (int64_t)min(max(entry(t.cu, s), 0), t.T) * num / den + (int64_t)add * s;
 }
 // The sequence that owns `slot`, and the slot's number in it (below zero for the
 // slots of the rows before the first sequence, which are nobody's).
@@ -102,7 +110,7 @@ struct Pages {
 // The page of table column c of sequence s, -1 where it is none.
 __device__ __forceinline__ int page_at(const Pages& pg, int s, int c) {
   if (c < 0 || c >= pg.max_pages) return -1;
-  const int p = pg.table[(int64_t)s * pg.max_pages + c];
+  const int p = entry(pg.table, (int64_t)s * pg.max_pages + c);
   return (unsigned)p < (unsigned)pg.n_pages ? p : -1;
 }
 
@@ -165,7 +173,7 @@ __global__ __launch_bounds__(kThreads) void store_kernel(const uint16_t* __restr
   int s, i, first, n;
   find_slot(tk, (int)(unit / pg.Hkv), per_seq, 1, P, 2, s, i);
   seq_rows(tk, s, first, n);
-  const int64_t begin = (int64_t)lengths[s] - n;      // position of the first new token
+  const int64_t begin = (int64_t)entry(lengths, s) - n;      // position of the first new token
   const int64_t from = begin > 0 ? begin : 0;         // (tokens before position 0 are dropped)
   const int64_t c = from / P + i;
   const int r0 = i == 0 ? (int)(from % P) : 0;        // the page's new rows: r0 .. r1 - 1
@@ -504,32 +512,39 @@ __device__ __forceinline__ void attend_steps(const AttendArgs& a, int s, int kvh
     v_read();
   };
 
-  // The wave's steps, 64 at a time: lane i looks up the page and the scales of
-  // the i-th.
+  // The wave's steps.  Pages are looked up two steps ahead, scales one.
   const int steps = (key1 - key0 + kKeys - 1) / kKeys;
   const int mine = (steps - w + stride - 1) / stride;
-  for (int base = 0; base < mine; base += kWave) {
-    auto key_of = [&](int i) { return key0 + kKeys * (w + stride * (base + i)); };
-    const int page_l = base + lane < mine ? page_at(a.pg, s, key_of(lane) / P) : -1;
-    float kf_l = 0.0f, vf_l = 0.0f;
-    if (page_l >= 0) {
-      const int64_t hp = (int64_t)page_l * a.pg.Hkv + kvh;
-      kf_l = a.pg.ks[hp] * a.sc_log2;
-      vf_l = a.pg.vs[hp];
-    }
-    const int cnt = min(mine - base, kWave);
-    auto lane_i = [&](int x, int i) { return __builtin_amdgcn_readlane(x, i & (kWave - 1)); };
-    auto lane_f = [&](float x, int i) {
-      return __builtin_bit_cast(float, lane_i(__builtin_bit_cast(int, x), i));
-    };
-    auto real = [&](int i) { return i < cnt && lane_i(page_l, i) >= 0; };
-    load_k(lane_i(page_l, 0), key_of(0), real(0));
-    load_v(lane_i(page_l, 0), key_of(0), real(0));
-    for (int i = 0; i < cnt; ++i)
+  if (mine > 0) {
+    auto key_of = [&](int i) { return key0 + kKeys * (w + stride * min(i, mine - 1)); };
+    // (the table has room for the keys: a step's column is one of it)
+    const int64_t row = (int64_t)s * a.pg.max_pages;
+    auto number_of = [&](int i) { return entry(a.pg.table, row + key_of(i) / P); };
+    auto page_of = [&](int number) { return (unsigned)number < (unsigned)a.pg.n_pages ? number : -1; };
+    // (where there is no page any scale will do, but a cache of none has no scales)
+    const float* const some = (const float*)a.lengths;
+    const float* const k_scales = a.pg.n_pages ? a.pg.ks : some;
+    const float* const v_scales = a.pg.n_pages ? a.pg.vs : some;
+    auto scale_at = [&](int page) { return page < 0 ? 0 : (int64_t)page * a.pg.Hkv + kvh; };
+    int page = page_of(number_of(0)), number = number_of(1);
+    float kf = entry(k_scales, scale_at(page)), vf = entry(v_scales, scale_at(page));
+    load_k(page, key_of(0), page >= 0);
+    load_v(page, key_of(0), page >= 0);
+    for (int i = 0; i < mine; ++i) {
+      // (scalar loads are waited for all together: here, for those of the step before)
+      asm volatile("" : "+s"(number), "+s"(kf), "+s"(vf));
+      const int next = page_of(number);
+      number = number_of(i + 2);
+      const float kf_next = entry(k_scales, scale_at(next)), vf_next = entry(v_scales, scale_at(next));
+      const bool real = i + 1 < mine && next >= 0;
       // (keys on no page: zeros at places that no row sees)
-      compute(real(i) ? key_of(i) : INT_MAX - 2 * kKeys, lane_f(kf_l, i), lane_f(vf_l, i),
-              [&]() { load_k(lane_i(page_l, i + 1), key_of(i + 1), real(i + 1)); },
-              [&]() { load_v(lane_i(page_l, i + 1), key_of(i + 1), real(i + 1)); });
+      compute(page >= 0 ? key_of(i) : INT_MAX - 2 * kKeys, page >= 0 ? kf * a.sc_log2 : 0.0f,
+              page >= 0 ? vf : 0.0f, [&]() { load_k(next, key_of(i + 1), real); },
+              [&]() { load_v(next, key_of(i + 1), real); });
+      page = next;
+      kf = kf_next;
+      vf = vf_next;
+    }
   }
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
@@ -551,7 +566,7 @@ __device__ __forceinline__ void store_dims(const AttendArgs& a, int kvh, int row
 // Keys of sequence s that the table has room for.
 template <int P>
 __device__ __forceinline__ int keys_of(const AttendArgs& a, int s) {
-  return (int)min((int64_t)max(a.lengths[s], 0), (int64_t)a.pg.max_pages * P);
+  return (int)min((int64_t)max(entry(a.lengths, s), 0), (int64_t)a.pg.max_pages * P);
 }
 
 // The sums of a workgroup's waves over different keys of the same rows, joined
@@ -628,8 +643,8 @@ __global__ __launch_bounds__(WAVES* kWave, attend_occupancy(RT)) void attend_ker
   if (tile < 0 || row0 >= rows) return;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   WaveSums<RT> ws;
-  attend_steps<FMT, P, RT>(a, s, kvh, row0, first, n, a.lengths[s], 0, keys_of<P>(a, s), wave, WAVES,
-                           ws);
+  attend_steps<FMT, P, RT>(a, s, kvh, row0, first, n, entry(a.lengths, s), 0, keys_of<P>(a, s), wave,
+                           WAVES, ws);
   merge_waves<RT>(sm, ws, rows - row0, [&](int r, int d, float, float l, const float (&x)[8]) {
     store_dims(a, kvh, row0 + r, first, d, x, l);
   });
@@ -823,7 +838,7 @@ __global__ __launch_bounds__(kThreads, attend_occupancy(RT)) void attend_share_k
     if (!r.full && r.st0 == 0 && lane == 0 && (!joint || wave == 0))
       leave_item(r, kvh, row0, slot, first_worker, joint);
     WaveSums<RT> ws;
-    attend_steps<FMT, P, RT>(a, s, kvh, row0, first, n, a.lengths[s], r.st0 * kKeys,
+    attend_steps<FMT, P, RT>(a, s, kvh, row0, first, n, entry(a.lengths, s), r.st0 * kKeys,
                              min(r.st1 * kKeys, keys_of<P>(a, s)), joint ? wave : 0,
                              joint ? kWaves : 1, ws);
     auto store = [&](int row, int d, float m, float l, const float (&x)[8]) {

@@ -13,13 +13,14 @@
 // All are bound by HBM once the calls are large (a copy of 1 GiB runs at 5.14
 // TB/s, nontemporal reads of 2 GB at 7.1, ordinary ones at 6.2), by their chain
 // of dependent loads when they are small:
-//   store, 32768 tokens of 8 heads:            41 us, 4.9 TB/s (one token of each
-//                                              of 64 sequences: 4.7 us)
+//   store, 32768 tokens of 8 heads:            40 us, 5.1 TB/s (one token of each
+//                                              of 64 sequences: 4.6 us)
 //   attention, 32 heads over 8 KV heads,
-//     8 sequences of up to 131072 tokens:      255 + 5 us, 6.3 TB/s
-//     32 sequences of 131 to 7974 tokens:      51 + 5 us, 5.2 TB/s
+//     8 sequences of up to 131072 tokens:      245 + 5 us, 6.6 TB/s
+//     32 sequences of 131 to 7974 tokens:      48 + 6 us, 5.5 TB/s
 //     1 sequence of 1000 tokens, 4 heads:      9 us
-//   copy, 150 pages of 128 tokens, 32 layers:  430 us, 5.8 TB/s
+//   64 heads, 6 of about 13000, 4 new, int8:   39 + 5 us, 4.0 TB/s
+//   copy, 150 pages of 128 tokens, 32 layers:  411 us, 6.1 TB/s
 #include "../../include/entropyinfer.h"
 #include "ei_internal.h"
 
@@ -667,7 +668,7 @@ __global__ __launch_bounds__(WAVES* kWave, attend_occupancy(RT)) void attend_ker
 // alike (96 / 99 us), and far slower on others (256 of 200 to 8000: 243 / 203).
 constexpr int kCus = 256;
 constexpr int kShareGroups = 2 * kCus;
-constexpr int kItemCost = 5;    // (8: 128 ragged sequences 81 -> 83 us)
+constexpr int kItemCost = 5;    // (7: 128 ragged sequences 78.5 -> 79.5 us, 64 of them the same)
 constexpr int kShareLeast = 4;   // steps and costs a wave takes at least
 // The first workgroup of a CU gets its loads before the second one's: with equal
 // runs its waves end first (8 sequences of up to 128k tokens after 213 us, the

@@ -505,6 +505,50 @@ def test_attn_behind_rows_of_no_sequence(lead, spare):
     assert bool((err <= off[:, :, lead:cu[-1]]).all())
 
 
+@pytest.mark.parametrize("cu", [[0, 500, 10, 600], [600, 300, 200, 0], [-5, 100, 9000, 350],
+                                [700, 800, 900, 1000]])
+@pytest.mark.parametrize("spare", [1, 60])
+def test_offsets_that_are_no_ascending_list(cu, spare):
+    """Nothing outside the tensors and the sequences' own pages is touched."""
+    T, lengths = 600, [650, 610, 30]
+    table = _table(lengths, 64, 24, spare=spare)
+    mine = sorted(p for row in table for p in row if p >= 0)
+    pages, q = _cuda(_pages(24, 2, 64, E4M3, 1)), _rand((1, 8, T, D), 2).cuda()
+    before = [t.clone() for t in pages]
+    room = torch.full((3 * q.numel(),), 3.0, dtype=torch.bfloat16, device="cuda")
+    out = room[q.numel():2 * q.numel()].view(q.shape)
+    args = _i32(table).cuda(), _i32(lengths).cuda(), _i32(cu).cuda()
+    eb.cache_attn(q, pages, *args, out=out)
+    assert bool((room[:q.numel()] == 3.0).all()) and bool((room[2 * q.numel():] == 3.0).all())
+    kv = q[:, :2].contiguous()
+    eb.cache_store(kv, kv, pages, *args)
+    others = [p for p in range(24) if p not in mine]
+    assert all(torch.equal(_bytes(a)[others], _bytes(b)[others]) for a, b in zip(pages, before))
+
+
+def test_on_a_device_that_is_not_the_current_one(monkeypatch):
+    """Each entry point calls itself with its tensors' device made current."""
+    pages, table, lengths = _cuda(_pages(8, 2, 64, E4M3, 1)), _i32([[0, 1], [2, 3]]).cuda(), \
+        _i32([70, 128]).cuda()
+    q, kv, cu = _rand((1, 4, 2, D), 2).cuda(), _rand((1, 2, 2, D), 3).cuda(), _i32([0, 1, 2]).cuda()
+    one = _i32([4]).cuda()
+
+    def run():
+        eb.cache_store(kv, kv, pages, table, lengths)
+        eb.cache_copy(pages, one - 4, one)
+        return (eb.cache_attn(q, pages, table, lengths, cu),
+                eb.packed_prefill_attn(q, kv, kv, cu), *(t.clone() for t in pages))
+    want, asked = run(), []
+
+    def elsewhere_first():
+        asked.append(len(asked) % 2)
+        return 1 - asked[-1]       # device 1, then (inside) device 0
+    monkeypatch.setattr(eb, "_current_device", elsewhere_first)
+    got = run()
+    assert len(asked) == 8
+    assert all(torch.equal(_bytes(a), _bytes(b)) for a, b in zip(got, want))
+
+
 def test_attn_is_the_same_every_time():
     pages = _cuda(_pages(200, 8, 64, E4M3, 1))
     table = torch.randperm(200, generator=_gen(1)).to(torch.int32).view(2, 100).cuda()

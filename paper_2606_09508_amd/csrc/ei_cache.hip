@@ -671,13 +671,14 @@ constexpr int kShareGroups = 2 * kCus;
 constexpr int kItemCost = 5;    // (7: 128 ragged sequences 78.5 -> 79.5 us, 64 of them the same)
 constexpr int kShareLeast = 4;   // steps and costs a wave takes at least
 // The first workgroup of a CU gets its loads before the second one's: with equal
-// runs its waves end first (8 sequences of up to 128k tokens after 213 us, the
-// second's after 246 to 254; 6 of 13000, 32 rows each: 29, 37 to 43), and what is
-// left does not fill HBM.  Wave priorities change nothing.  So where every CU has
-// two, the first half of the workgroups takes runs longer than the average by
-// 1 / kElderShare (attention alone, without / 8 / 6 / 4: the 6 sequences in int8
-// 46.5 / 42.4 / 42.6 / 41.5 us, 200 of 1000 to 4000 tokens 152 / 149 / 148 / 151, 256
-// of 200 to 8000 193 / 188 / 188 / 192, 32 of 131 to 7974 50 / 49.5 / 49.5 / 49).
+// runs its waves end first, and what is left does not fill HBM.  Wave priorities
+// change nothing.  So where every CU has two, the first half of the workgroups
+// takes runs longer than the average by 1 / kElderShare (attention alone, equal /
+// longer runs: 6 sequences of 13000, 32 rows each, int8 40.7 / 38.9 us, e4m3 40.0 /
+// 38.7; 40 of 300 to 6000 18.1 / 17.5; 8 of up to 128k 245.4 / 244.2; 256 of 200 to
+// 8000 188.7 / 187.6; by 1/8 or 1/5 within 1% of that), unless equal runs are whole
+// items (as many sequences of one length as make it so: 256 of 4096 and 8 KV heads
+// 322 / 341).
 constexpr int kElderShare = 6;
 
 // A value that all lanes share, in scalar registers.
@@ -753,7 +754,10 @@ __global__ __launch_bounds__(kThreads, attend_occupancy(RT)) void attend_share_k
   };
   // worker w's run: bound(w) .. bound(w + 1) - 1 (less what lies past the total)
   const int64_t even = (total + workers - 1) / workers;
-  const int elders = workers == kShareGroups * kWaves && even > kShareLeast ? workers / 2 : 0;
+  const int whole0 = __builtin_amdgcn_readlane(my_steps, 0) + kItemCost;
+  const bool whole_items = total == even * workers && even % whole0 == 0;
+  const int elders = workers == kShareGroups * kWaves && even > kShareLeast && !whole_items
+                         ? workers / 2 : 0;
   const int64_t elder = even + even / kElderShare;
   const int64_t per = elders ? (total - elders * elder + elders - 1) / elders
                              : even < kShareLeast ? kShareLeast : even;

@@ -81,8 +81,9 @@ __device__ __forceinline__ void seq_rows(const Tokens& t, int s, int& first, int
 // Work items of sequences whose lengths only the device knows.  With `cu`,
 // sequence s owns the slots floor(cu[s] * num / den) + add * s up to the next
 // one's first, which is floor(n_s * num / den) + add of them or one more.
-__device__ __forceinline__ int64_t slot_of(const Tokens& t, int s, int num, int den, int add) {
-  return (int64_t)min(max(entry(t.cu, s), 0), t.T) * num / den + (int64_t)add * s;
+// (T * num and the slots of all sequences are below 2^31, or the call is refused.)
+__device__ __forceinline__ int slot_of(const Tokens& t, int s, int num, int den, int add) {
+  return (int)((unsigned)(min(max(entry(t.cu, s), 0), t.T) * num) / (unsigned)den) + add * s;
 }
 // The sequence that owns `slot`, and the slot's number in it (below zero for the
 // slots of the rows before the first sequence, which are nobody's).
@@ -99,7 +100,7 @@ __device__ __forceinline__ void find_slot(const Tokens& t, int slot, int per_seq
     if (slot_of(t, mid, num, den, add) <= slot) lo = mid; else hi = mid - 1;
   }
   s = lo;
-  i = (int)(slot - slot_of(t, lo, num, den, add));
+  i = slot - slot_of(t, lo, num, den, add);
 }
 
 struct Pages {

@@ -1059,8 +1059,12 @@ Pages pages_of(const ei_cache_shape& c, const ei_cache_pages& p, const int32_t* 
                c.n_pages, cols,          c.n_kv_heads, c.page_len};
 }
 
-constexpr int kShortKeys = 2048;   // a table of no more keys: one workgroup per item
-constexpr int kShortWaves = 4;
+// A table of no more keys: one workgroup per item.  (It reads about 50 KB per us,
+// whatever its waves; dealt out, with the second kernel: 1 sequence of 1500 tokens
+// 13.7 / 10 + 4 us, 32 of 1900 21.8 / 26 + 5, 100 of up to 1900 49.5 / 41 + 5; tables
+// of 3900 here / dealt out: 1 28 / 10 + 4, 32 41 / 45 + 5, 100 of up to 3900 96 / 72 + 6.)
+constexpr int kShortKeys = 2048;
+constexpr int kShortWaves = 4;     // (8 / 16: 1 of 1000 9.2 -> 9.2 / 10.8 us, 200 51 -> 59 / 72)
 
 struct AttendPlan {
   int rt, per_seq, item_rows;   // item_rows: of an item, at most

@@ -656,7 +656,7 @@ __global__ __launch_bounds__(WAVES* kWave, attend_occupancy(RT)) void attend_ker
 // over the waves of the launch.  With the items one behind the other (by
 // sequence, KV head and row tile), each kItemCost steps longer than it is (what
 // a wave waits for before an item's first step), every wave takes a run of
-// them, all equally long (but see kElderShare): a last part of an item, whole
+// them, all equally long (but see elder_share): a last part of an item, whole
 // items, a first part of one.  Whole items are written out, parts left for
 // combine_kernel: nothing in here waits for another wave, except where the runs
 // of a workgroup's waves lie in one item: they then share the item's steps and
@@ -674,13 +674,14 @@ constexpr int kShareLeast = 4;   // steps and costs a wave takes at least
 // The first workgroup of a CU gets its loads before the second one's: with equal
 // runs its waves end first, and what is left does not fill HBM.  Wave priorities
 // change nothing.  So where every CU has two, the first half of the workgroups
-// takes runs longer than the average by 1 / kElderShare (attention alone, equal /
-// longer runs: 6 sequences of 13000, 32 rows each, int8 40.7 / 38.9 us, e4m3 40.0 /
-// 38.7; 40 of 300 to 6000 18.1 / 17.5; 8 of up to 128k 245.4 / 244.2; 256 of 200 to
-// 8000 188.7 / 187.6; by 1/8 or 1/5 within 1% of that), unless equal runs are whole
-// items (as many sequences of one length as make it so: 256 of 4096 and 8 KV heads
-// 322 / 341).
-constexpr int kElderShare = 6;
+// takes runs longer than the average by a sixth, with 32 rows, whose arithmetic
+// goes to the first one's waves too, by a third (attention alone, equal / sixth /
+// third: 6 sequences of 13000, 32 rows, int8 40.7 / 38.9 / 36.6 us, e4m3 40.0 / 38.4 /
+// 36.4, 16 of 500 to 8000 33.6 / 32.9 / 30.9; 16 rows, equal / sixth: 40 of 300 to
+// 6000 18.1 / 17.5; 8 of up to 128k 245.4 / 244.2; 256 of 200 to 8000 188.7 / 187.6; an
+// eighth or a fifth within 1% of that), unless equal runs are whole items (as many
+// sequences of one length as make it so: 256 of 4096 and 8 KV heads 322 / 341).
+constexpr int elder_share(int rt) { return rt == 1 ? 6 : 3; }
 
 // A value that all lanes share, in scalar registers.
 __device__ __forceinline__ int64_t uniform(int64_t x) {
@@ -759,7 +760,7 @@ __global__ __launch_bounds__(kThreads, attend_occupancy(RT)) void attend_share_k
   const bool whole_items = total == even * workers && even % whole0 == 0;
   const int elders = workers == kShareGroups * kWaves && even > kShareLeast && !whole_items
                          ? workers / 2 : 0;
-  const int64_t elder = even + even / kElderShare;
+  const int64_t elder = even + even / elder_share(RT);
   const int64_t per = elders ? (total - elders * elder + elders - 1) / elders
                              : even < kShareLeast ? kShareLeast : even;
   auto bound = [&](int w) -> int64_t {

@@ -19,7 +19,7 @@
 //     8 sequences of up to 131072 tokens:      245 + 5 us, 6.6 TB/s
 //     32 sequences of 131 to 7974 tokens:      48 + 6 us, 5.5 TB/s
 //     1 sequence of 1000 tokens, 4 heads:      9 us
-//   64 heads, 6 of about 13000, 4 new, int8:   39 + 5 us, 4.0 TB/s
+//   64 heads, 6 of about 13000, 4 new, int8:   37 + 5 us, 4.2 TB/s
 //   copy, 150 pages of 128 tokens, 32 layers:  411 us, 6.1 TB/s
 #include "../../include/entropyinfer.h"
 #include "ei_internal.h"

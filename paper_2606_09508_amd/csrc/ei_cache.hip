@@ -874,9 +874,10 @@ __global__ __launch_bounds__(kThreads, attend_occupancy(RT)) void attend_share_k
 
 // The parts of a shared item joined, in the order of their keys.  A workgroup
 // looks after 8 rows of the items that `per` workers left, up to four items at
-// once: a group of 32 lanes adds up a row's 128 dims over every stripes-th part,
+// once: a group of 16 lanes adds up a row's 128 dims over every stripes-th part,
 // then the stripes are added up in order.
-constexpr int kCombineThreads = 1024;
+constexpr int kCombineThreads = 512;
+constexpr int kCombineLanes = 16;
 constexpr int kCombineRows = 8;
 constexpr int kCombineItems = 4;
 // Workers a workgroup looks after, at most.  A workgroup that finds no item costs
@@ -887,15 +888,17 @@ constexpr int kCombineItems = 4;
 constexpr int kCombineWorkers = 32;
 static_assert(kCombineWorkers <= kWave, "a lane reads what each of them left");
 constexpr int kCombineAhead = 4;   // parts in flight per group (8: 5.1 -> 7.4 us, 32 sequences)
-static_assert(kCombineThreads / 32 / kCombineItems >= kCombineRows, "a group for each row of an item");
+static_assert(kCombineThreads / kCombineLanes / kCombineItems >= kCombineRows,
+              "a group for each row of an item");
 __global__ __launch_bounds__(kCombineThreads) void combine_kernel(AttendArgs a, int tile_rows,
                                                                   int workers, int per) {
   constexpr int kGroupBits = 5, kGroups = 1 << kGroupBits;
-  static_assert(kGroups == kCombineThreads / 32, "groups of 32 lanes");
+  static_assert(kGroups == kCombineThreads / kCombineLanes, "groups of 16 lanes");
+  constexpr int kHalves = kHeadDim / (4 * kCombineLanes);   // four dims of each a lane
   __shared__ float sm_m[kGroups], sm_l[kGroups];
   __shared__ __attribute__((aligned(16))) float sm_o[kGroups][kHeadDim];
   const int G = a.Hq / a.pg.Hkv, lane = threadIdx.x % kWave;
-  const int grp = threadIdx.x / 32, d = (threadIdx.x % 32) * 4;
+  const int grp = threadIdx.x / kCombineLanes, d = (threadIdx.x % kCombineLanes) * 4;
   const int worker0 = (int)blockIdx.x * per;
   SplitItem left{};   // of worker worker0 + lane
   if (lane < per && worker0 + lane < workers) left = a.split[worker0 + lane];
@@ -931,28 +934,38 @@ __global__ __launch_bounds__(kCombineThreads) void combine_kernel(AttendArgs a, 
     const int bits = rows > 4 ? 3 : rows > 2 ? 2 : rows > 1 ? 1 : 0, lanes_r = 1 << bits;
     const int stripes = mine >> bits, stripe = at >> bits, r = at & (lanes_r - 1);
     float m = -INFINITY, l = 0.0f;
-    float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    float4 acc[kHalves];
+#pragma unroll
+    for (int h = 0; h < kHalves; ++h) acc[h] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    auto add = [&](float4 (&sum)[kHalves], float f, const float4 (&x)[kHalves], float g) {
+#pragma unroll
+      for (int h = 0; h < kHalves; ++h) {
+        sum[h].x = sum[h].x * f + x[h].x * g;
+        sum[h].y = sum[h].y * f + x[h].y * g;
+        sum[h].z = sum[h].z * f + x[h].z * g;
+        sum[h].w = sum[h].w * f + x[h].w * g;
+      }
+    };
     if (r < rows)
       for (int p0 = stripe; p0 < parts; p0 += stripes * kCombineAhead) {
         Part ml[kCombineAhead];
-        float4 x[kCombineAhead];
+        float4 x[kCombineAhead][kHalves];
 #pragma unroll
         for (int k = 0; k < kCombineAhead; ++k) {
           const int64_t pr = slot_row(min(p0 + k * stripes, parts - 1), r);
           ml[k] = a.part_ml[pr];
-          x[k] = *(const float4*)(a.part_o + pr * kHeadDim + d);
+#pragma unroll
+          for (int h = 0; h < kHalves; ++h)
+            x[k][h] = *(const float4*)(a.part_o + pr * kHeadDim + 4 * kCombineLanes * h + d);
         }
 #pragma unroll
         for (int k = 0; k < kCombineAhead; ++k) {
           if (p0 + k * stripes >= parts) break;
           const float mn = fmaxf(m, ml[k].m);
           const float f = m == mn ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
-          const float h = ml[k].m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml[k].m - mn);
-          l = l * f + ml[k].l * h;
-          acc.x = acc.x * f + x[k].x * h;
-          acc.y = acc.y * f + x[k].y * h;
-          acc.z = acc.z * f + x[k].z * h;
-          acc.w = acc.w * f + x[k].w * h;
+          const float g = ml[k].m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml[k].m - mn);
+          l = l * f + ml[k].l * g;
+          add(acc, f, x[k], g);
           m = mn;
         }
       }
@@ -961,26 +974,31 @@ __global__ __launch_bounds__(kCombineThreads) void combine_kernel(AttendArgs a, 
       sm_m[grp] = m;
       sm_l[grp] = l;
     }
-    *(float4*)&sm_o[grp][d] = acc;
+#pragma unroll
+    for (int h = 0; h < kHalves; ++h) *(float4*)&sm_o[grp][4 * kCombineLanes * h + d] = acc[h];
     __syncthreads();
     if (stripe != 0 || r >= rows) continue;
     for (int k = 1; k < stripes; ++k) m = fmaxf(m, sm_m[grp + k * lanes_r]);
     l = 0.0f;
-    acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+    for (int h = 0; h < kHalves; ++h) acc[h] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
     for (int k = 0; k < stripes; ++k) {
       const int from = grp + k * lanes_r;
-      const float h = sm_m[from] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(sm_m[from] - m);
-      const float4 x = *(const float4*)&sm_o[from][d];
-      l += sm_l[from] * h;
-      acc.x += x.x * h;
-      acc.y += x.y * h;
-      acc.z += x.z * h;
-      acc.w += x.w * h;
+      const float g = sm_m[from] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(sm_m[from] - m);
+      float4 x[kHalves];
+#pragma unroll
+      for (int h = 0; h < kHalves; ++h) x[h] = *(const float4*)&sm_o[from][4 * kCombineLanes * h + d];
+      l += sm_l[from] * g;
+      add(acc, 1.0f, x, g);
     }
     const float inv = l == 0.0f ? 0.0f : 1.0f / l;
     const int row = row0 + r0 + r;
-    *(uint2*)(a.o + ((int64_t)(kvh * G + row % G) * a.tk.T + first + row / G) * kHeadDim + d) =
-        make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
+    uint16_t* at_row = a.o + ((int64_t)(kvh * G + row % G) * a.tk.T + first + row / G) * kHeadDim + d;
+#pragma unroll
+    for (int h = 0; h < kHalves; ++h)
+      *(uint2*)(at_row + 4 * kCombineLanes * h) =
+          make_uint2(pack_bf16x2(acc[h].x * inv, acc[h].y * inv),
+                     pack_bf16x2(acc[h].z * inv, acc[h].w * inv));
   }
 }
 

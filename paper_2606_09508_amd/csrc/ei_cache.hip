@@ -17,7 +17,7 @@
 //                                              of 64 sequences: 4.6 us)
 //   attention, 32 heads over 8 KV heads,
 //     8 sequences of up to 131072 tokens:      245 + 5 us, 6.6 TB/s
-//     32 sequences of 131 to 7974 tokens:      48 + 6 us, 5.5 TB/s
+//     32 sequences of 131 to 7974 tokens:      47 + 5 us, 5.6 TB/s
 //     1 sequence of 1000 tokens, 4 heads:      9 us
 //   64 heads, 6 of about 13000, 4 new, int8:   37 + 5 us, 4.2 TB/s
 //   copy, 150 pages of 128 tokens, 32 layers:  411 us, 6.1 TB/s
@@ -881,13 +881,14 @@ constexpr int kCombineLanes = 16;
 constexpr int kCombineRows = 8;
 constexpr int kCombineItems = 4;
 // Workers a workgroup looks after, at most.  A workgroup that finds no item costs
-// its dispatch (16 waves), one that finds several shares its groups among them:
-// so as many as hold one item on average, kWaves at least (always kWaves /
-// by this rule: 48 items of 32 rows 9.6 / 5.0 us, 128 of them 12.5 / 8.0, 64 of 4
-// rows 5.3 / 4.7, 256 of them 5.3 / 5.7).
+// its dispatch (8 waves), one that finds several shares its groups among them: so
+// kWaves, and twice as many while four in five then find one (4 / 8 / 16 / 32
+// workers, us: 48 items of 32 rows 7.1 / 7.4 / 6.1 / 5.4, 128 of them 7.2 / 6.8 / 7.6,
+// 256 items of 4 rows 4.7 / 5.4).
 constexpr int kCombineWorkers = 32;
 static_assert(kCombineWorkers <= kWave, "a lane reads what each of them left");
-constexpr int kCombineAhead = 4;   // parts in flight per group (8: 5.1 -> 7.4 us, 32 sequences)
+constexpr int kCombineAhead = 4;   // parts in flight per group (2 / 4 / 8: 40 sequences 6.1 / 5.1 us,
+                                   // 64 4.7 / 4.7 / 5.5)
 static_assert(kCombineThreads / kCombineLanes / kCombineItems >= kCombineRows,
               "a group for each row of an item");
 __global__ __launch_bounds__(kCombineThreads) void combine_kernel(AttendArgs a, int tile_rows,
@@ -1133,7 +1134,7 @@ void launch_attend_t(const AttendPlan& pl, const AttendArgs& a, hipStream_t stre
     const unsigned row_blocks = (unsigned)((pl.item_rows + kCombineRows - 1) / kCombineRows);
     const int workers = pl.groups * kWaves;
     int per = kWaves;
-    while (per < kCombineWorkers && pl.items * (2 * per) <= workers) per *= 2;
+    while (per < kCombineWorkers && pl.items * (5 * per) <= 2 * workers) per *= 2;
     hipLaunchKernelGGL(combine_kernel, dim3((unsigned)((workers + per - 1) / per), row_blocks),
                        dim3(kCombineThreads), 0, stream, a, kRows * RT, workers, per);
     return;

@@ -663,8 +663,8 @@ __global__ __launch_bounds__(WAVES* kWave, attend_occupancy(RT)) void attend_ker
 // leave one part.
 //
 // Each wave adds the sequences up for itself.  Two waves a SIMD are what HBM
-// needs; with three the oldest goes first and the youngest ends a third later (8
-// sequences of up to 128k tokens 248 -> 293 us).  A workgroup per item instead
+// needs (with three, equal runs: 8 sequences of up to 128k tokens 245.6 -> 248.6 us,
+// 200 of 1000 to 4000 150 -> 156).  A workgroup per item instead
 // (as for short tables) is 3% faster on 128 sequences of about 2000 tokens, all
 // alike (96 / 99 us), and far slower on others (256 of 200 to 8000: 243 / 203).
 constexpr int kCus = 256;

@@ -592,6 +592,22 @@ def _req_packed(t, name: str, dev: int) -> None:
         raise ValueError(f"{name} {tuple(t.shape)} is not [1, heads, tokens, head_dim]")
 
 
+def _tokens(k, v):
+    """(device, shape) of new keys and values, which both must share."""
+    T, bf16 = torch.Tensor, torch.bfloat16
+    dev = _device_of(k)
+    if not (dev >= 0 and isinstance(v, T) and k.dtype is bf16 and v.dtype is bf16
+            and v.get_device() == dev and k.is_contiguous() and v.is_contiguous()):
+        _req_packed(k, "k", dev)
+        _req_packed(v, "v", dev)
+    shape = k.shape
+    if len(shape) != 4 or shape[0] != 1:
+        _req_packed(k, "k", dev)
+    if v.shape != shape:
+        raise ValueError(f"v {tuple(v.shape)} does not match k {tuple(shape)}")
+    return dev, shape
+
+
 def _req_i32(t, name: str, ndim: int, dev: int) -> None:
     if not (isinstance(t, torch.Tensor) and t.dtype is torch.int32 and t.dim() == ndim
             and t.get_device() == dev and t.is_contiguous()):
@@ -713,8 +729,13 @@ def _cache_args(pages, dev: int, layers: bool = False):
 def _sequences(tokens: int, page_table, lengths, cu_seqlens, dev: int):
     """The number of sequences and of the table's columns, after checks of what
     describes them."""
-    _req_i32(page_table, "page_table", 2, dev)
-    _req_i32(lengths, "lengths", 1, dev)
+    T, i32 = torch.Tensor, torch.int32
+    if not (isinstance(page_table, T) and isinstance(lengths, T) and page_table.dtype is i32
+            and lengths.dtype is i32 and page_table.get_device() == dev
+            and lengths.get_device() == dev and page_table.dim() == 2 and lengths.dim() == 1
+            and page_table.is_contiguous() and lengths.is_contiguous()):
+        _req_i32(page_table, "page_table", 2, dev)
+        _req_i32(lengths, "lengths", 1, dev)
     S, cols = page_table.shape
     if lengths.size(0) != S:
         raise ValueError(f"page_table has {S} rows for {lengths.size(0)} lengths")
@@ -732,12 +753,7 @@ def cache_store(k, v, pages: CachePages, page_table, lengths, cu_seqlens=None) -
     their sequences (page_table int32 [S, max_pages]).  lengths int32 [S] counts
     each sequence's tokens with the new ones; cu_seqlens int32 [S + 1] says
     which rows are whose (None: T / S rows each)."""
-    dev = _device_of(k)
-    _req_packed(k, "k", dev)
-    _req_packed(v, "v", dev)
-    shape = k.shape
-    if v.shape != shape:
-        raise ValueError(f"v {tuple(v.shape)} does not match k {tuple(shape)}")
+    dev, shape = _tokens(k, v)
     hkv, head_dim, cs, ptrs = _cache_args(pages, dev)
     _, heads, T, D = shape
     if heads != hkv or D != head_dim:

@@ -593,7 +593,7 @@ def _req_packed(t, name: str, dev: int) -> None:
 
 
 def _tokens(k, v):
-    """(device, shape) of new keys and values, which both must share."""
+    """(device, shape) of packed keys and values, which both must share."""
     T, bf16 = torch.Tensor, torch.bfloat16
     dev = _device_of(k)
     if not (dev >= 0 and isinstance(v, T) and k.dtype is bf16 and v.dtype is bf16
@@ -621,14 +621,15 @@ def packed_prefill_attn(q, k, v, cu_seqlens, softmax_scale: float | None = None,
     that lie one behind the other in q [1, Hq, T, D], k and v [1, Hkv, T, D];
     sequence s is the rows cu_seqlens[s] .. cu_seqlens[s + 1] - 1 (int32, on the
     device).  Rows of ``out`` outside every sequence are left as they were."""
-    dev = _device_of(q)
+    dev, kv_shape = _tokens(k, v)
     _req_packed(q, "q", dev)
-    _req_packed(k, "k", dev)
-    _req_packed(v, "v", dev)
     _req_i32(cu_seqlens, "cu_seqlens", 1, dev)
     shape = q.shape
-    check_qkv_shapes(shape, k.shape, v.shape)
-    if cu_seqlens.numel() < 1:
+    _, Hq, T, D = shape
+    _, Hkv, kv_T, kv_D = kv_shape
+    if kv_T != T or kv_D != D or not Hkv or Hq % Hkv:
+        check_qkv_shapes(shape, kv_shape)
+    if cu_seqlens.size(0) < 1:
         raise ValueError("cu_seqlens holds one offset more than there are sequences")
     if out is None:
         out = torch.empty_like(q)
@@ -639,10 +640,9 @@ def packed_prefill_attn(q, k, v, cu_seqlens, softmax_scale: float | None = None,
     if dev != _current_device():
         with torch.cuda.device(dev):
             return packed_prefill_attn(q, k, v, cu_seqlens, softmax_scale, causal, out)
-    _, Hq, T, D = shape
     sc = 1.0 / math.sqrt(D) if softmax_scale is None else float(softmax_scale)
     st = lib().ei_packed_prefill_attn(q.data_ptr(), k.data_ptr(), v.data_ptr(),
-                                      Dims(1, Hq, k.size(1), T, D), cu_seqlens.data_ptr(),
+                                      Dims(1, Hq, Hkv, T, D), cu_seqlens.data_ptr(),
                                       cu_seqlens.size(0) - 1, sc, 1 if causal else 0,
                                       out.data_ptr(), _raw_stream(dev))
     if st:

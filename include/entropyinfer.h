@@ -318,6 +318,8 @@ ei_status ei_sparse_prefill_attn_gqa_union(const uint16_t* q, const uint16_t* k,
  * ei_dense_prefill_attn -- dense GQA attention (Section 2's A_h V), causal
  * (keys j <= i) when `causal` is non-zero, else over all N keys; same tile
  * code and numerics as ei_sparse_prefill_attn.
+ * A value that is infinite or NaN makes NaN of the queries before it, too, that
+ * share its 64 keys (ei_packed_prefill_attn's do not).
  *
  * Errors: EI_ERR_NULL, EI_ERR_SHAPE (also a softmax_scale that is not finite
  * and positive), EI_ERR_UNSUPPORTED, EI_ERR_LAUNCH.
@@ -434,7 +436,10 @@ ei_status ei_swiglu(const uint16_t* g, const uint16_t* u, int64_t n, uint16_t* o
  *                starts is empty, so no list leads out of the tensors; rows
  *                that two sequences share hold the result of either.
  *
- * Rows of o that belong to no sequence are left as they were.  A sequence's
+ * Rows of o that belong to no sequence are left as they were.  Keys and values
+ * that a query does not attend to reach no element of its row, whatever they
+ * hold; an infinite or NaN value makes the elements that do attend to it so.  (A
+ * tile of rows whose result holds an infinity or NaN is computed twice.)  A sequence's
  * bits depend, by roundings, on T and n_seqs as the bits of
  * ei_dense_prefill_attn do on its launch.
  *

@@ -46,6 +46,7 @@
 
 #include <limits.h>
 #include <math.h>
+#include <type_traits>
 
 namespace ei {
 namespace {
@@ -306,19 +307,86 @@ __device__ __forceinline__ int valid_prefix(const int32_t* lst, int c, int CB, i
   return min(nv, c);
 }
 
+// A value that a query does not see has a probability of 0, but 0 times an
+// infinite or NaN value is NaN.  Only the step of a wave's tile that has masked
+// places holds such values; they can be left out of its product
+// (add_finite_values) and added behind the loop to the queries that see them
+// (add_odd_values).
+// Two bf16 numbers added to `odd`, which becomes NaN where one is infinite or NaN.
+__device__ __forceinline__ float odd_or(uint32_t w, float odd) {
+  const bf16x2 zero = {(__bf16)0.0f, (__bf16)0.0f};
+  return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(bf16x2, w), zero, odd, false);
+}
+
+// Whether a value of a step is infinite or NaN.
+__device__ __forceinline__ bool odd_values(const unsigned char* st, int lane) {
+  float odd = 0.0f;
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      const uint4 w = __builtin_bit_cast(uint4, read_vt(st, d, s, lane));
+      odd = odd_or(w.w, odd_or(w.z, odd_or(w.y, odd_or(w.x, odd))));
+    }
+  return __builtin_amdgcn_ballot_w64(odd != odd) != 0;
+}
+// O^T += V^T P^T of such a step without them.
+__device__ __forceinline__ void add_finite_values(const unsigned char* st, int lane,
+                                                  const uint4* pw, f32x16* oacc) {
+  auto finite = [](uint32_t w) {   // (an exponent of ones carries into bit 15 or 31)
+    return w & ~(((((w & 0x7f807f80u) + 0x00800080u) & 0x80008000u) >> 15) * 0xffffu);
+  };
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      asm volatile("" : "+v"(lane)::"memory");   // (nothing of it kept across the loop)
+      const uint4 w = __builtin_bit_cast(uint4, read_vt(st, d, s, lane));
+      oacc[d] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+          as_bf16x8(make_uint4(finite(w.x), finite(w.y), finite(w.z), finite(w.w))),
+          as_bf16x8(pw[s]), oacc[d], 0, 0, 0);
+    }
+}
+// What add_finite_values left out, to the queries that see it.  The step is the one
+// that holds the wave's rows qw0 .. qw0 + 31, or the sequence's last.
+template <int MODE>
+__device__ __forceinline__ void add_odd_values(const uint16_t* __restrict__ vh, int qw0, int qrow,
+                                               int N, int hf, f32x16* oacc) {
+  const int k0 = (MODE == kDenseFull ? N - 1 : qw0) / kSub * kSub;
+  for (int key = k0; key < min(k0 + kSub, N); ++key) {
+    const uint16_t* row = vh + (size_t)key * kHeadDim + 4 * hf;
+    const bool sees = MODE == kDenseFull || key <= qrow;
+#pragma unroll
+    for (int d = 0; d < 4; ++d)
+#pragma unroll
+      for (int gq = 0; gq < 4; ++gq) {
+        const uint2 w = *(const uint2*)(row + 32 * d + 8 * gq);
+        const float x[4] = {bf16_lo(w.x), bf16_hi(w.x), bf16_lo(w.y), bf16_hi(w.y)};
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          oacc[d][4 * gq + e] += sees && !(fabsf(x[e]) < INFINITY) ? x[e] : 0.0f;
+      }
+  }
+}
+
 // One 64-key sub-block (staged at st, first key k0) for the wave's 32 query
 // rows: S^T = K Q^T, the causal / length mask, the online softmax with lazy
 // rescaling, and O^T += V^T P^T.
 // `scored` runs once the K operands have been read.  With LATE_V the V tile is
 // read after the softmax only, behind `v_ready`.
+// With GUARD, values that a query does not see stay out of its sums whatever they
+// are (odd_values): where a step with masked places has infinite or NaN values,
+// it adds the finite ones and sets `odd`.
 struct Nothing {
   __device__ __forceinline__ void operator()() const {}
 };
-template <int MODE, bool LATE_V = false, class Scored = Nothing, class VReady = Nothing>
+template <int MODE, bool LATE_V = false, bool GUARD = false, class Scored = Nothing,
+          class VReady = Nothing>
 __device__ __forceinline__ void compute_step(const unsigned char* st, int k0, int qw0, int qrow,
                                              int N, int jq, int hf, int lane, const bf16x8* qf,
                                              float sc_log2, f32x16* oacc, float& m_i, float& l_i,
-                                             Scored scored = {}, VReady v_ready = {}) {
+                                             bool* odd = nullptr, Scored scored = {},
+                                             VReady v_ready = {}) {
   // S^T = K Q^T for the 64 keys (two 32-key tiles): every operand read is
   // issued before the first product, and the first V^T operands arrive during
   // the softmax.  Left to the scheduler, each product of the first key tile
@@ -409,8 +477,15 @@ __device__ __forceinline__ void compute_step(const unsigned char* st, int k0, in
   }
   l_i += lsum;
   // O^T += V^T P^T, the operands of the next head-dim tile read ahead
+  if constexpr (LATE_V) v_ready();
+  if constexpr (GUARD) {
+    if (need_mask && odd_values(st, lane)) {
+      add_finite_values(st, lane, pw, oacc);
+      *odd = true;
+      return;
+    }
+  }
   if constexpr (LATE_V) {
-    v_ready();
 #pragma unroll
     for (int s = 0; s < 4; ++s) vf[0][s] = read_vt(st, 0, s, lane);
   }
@@ -429,21 +504,44 @@ __device__ __forceinline__ void compute_step(const unsigned char* st, int k0, in
   }
 }
 
-// O = O^T / l for the lane's query row, bf16.
-__device__ __forceinline__ void store_rows(uint16_t* __restrict__ o, size_t row_base, int hf,
-                                           const f32x16* oacc, float l_i) {
+// Whether a lane of the workgroup has a NaN in `odd` (a barrier).
+__device__ __forceinline__ bool any_odd(float odd, bool (&waves)[kThreads / kWave]) {
+  const bool mine = __builtin_amdgcn_ballot_w64(odd != odd) != 0;
+  if (threadIdx.x % kWave == 0) waves[threadIdx.x / kWave] = mine;
+  __syncthreads();
+  bool any = false;
+#pragma unroll
+  for (int w = 0; w < kThreads / kWave; ++w) any |= waves[w];
+  return __builtin_amdgcn_readfirstlane(any) != 0;
+}
+__device__ __forceinline__ void clear_sums(f32x16* oacc, float& m_i, float& l_i) {
+#pragma unroll
+  for (int d = 0; d < 4; ++d)
+#pragma unroll
+    for (int r = 0; r < 16; ++r) oacc[d][r] = 0.0f;
+  m_i = -INFINITY;
+  l_i = 0.0f;
+}
+
+// O = O^T / l for the lane's query row, bf16.  Returns NaN if it holds an infinity or NaN.
+__device__ __forceinline__ float store_rows(uint16_t* __restrict__ o, size_t row_base, int hf,
+                                            const f32x16* oacc, float l_i) {
   const float l = l_i + __shfl_xor(l_i, 32);
   const float inv = l > 0.0f ? 1.0f / l : 0.0f;
   uint16_t* op = o + row_base * kHeadDim;
+  float odd = 0.0f;
 #pragma unroll
   for (int d = 0; d < 4; ++d)
 #pragma unroll
     for (int gq = 0; gq < 4; ++gq) {
       const int dim = 32 * d + 8 * gq + 4 * hf;
-      *(uint2*)(op + dim) =
+      const uint2 w =
           make_uint2(pack_bf16x2(oacc[d][4 * gq] * inv, oacc[d][4 * gq + 1] * inv),
                      pack_bf16x2(oacc[d][4 * gq + 2] * inv, oacc[d][4 * gq + 3] * inv));
+      odd = odd_or(w.y, odd_or(w.x, odd));
+      *(uint2*)(op + dim) = w;
     }
+  return odd;
 }
 
 template <int MODE, int SUB>
@@ -658,11 +756,12 @@ __device__ __forceinline__ void issue_tile(unsigned char* dst, const uint16_t* _
 struct SplitSmem {
   __attribute__((aligned(1024))) unsigned char stages[kSplitWaves][kStageBytes];
   float part_m[kSplitWaves][kSplitTileQ], part_l[kSplitWaves][kSplitTileQ];
+  bool odd[kSplitWaves];
 };
 
 // Tile `tile` of a sequence of N rows that starts at q, kh, vh and o; sparse:
 // its block list and count.
-template <int MODE, int SUB>
+template <int MODE, int SUB, bool GUARD = false>
 __device__ __forceinline__ void split_tile(SplitSmem& sm, const uint16_t* __restrict__ q,
                                            const uint16_t* __restrict__ kh,
                                            const uint16_t* __restrict__ vh,
@@ -717,80 +816,97 @@ __device__ __forceinline__ void split_tile(SplitSmem& sm, const uint16_t* __rest
     for (int r = 0; r < 16; ++r) oacc[d][r] = 0.0f;
   float m_i = -INFINITY, l_i = 0.0f;
 
-  EI_WAIT_VMCNT(0);   // the Q operands: no later wait covers copies in flight
-  int k0 = 0;
-  if (wave < n_steps) {
-    k0 = step_key0(wave);
-    issue_tile(st, kh, k0, N, lane, koff, false);
-    issue_tile(st + kTileBytes, vh, k0, N, lane, voff, true);
-  }
-  for (int i = wave; i < n_steps; i += kSplitWaves) {
-    const bool more = i + kSplitWaves < n_steps;
-    const int kn = more ? step_key0(i + kSplitWaves) : 0;
-    EI_WAIT_VMCNT(16);   // K has landed (V's 16 copies may be in flight)
-    asm volatile("" ::: "memory");
-    // (every LDS read of a tile has returned before its copies are issued)
-    auto next_k = [&]() {
-      EI_WAIT_LGKM0();
-      if (more) issue_tile(st, kh, kn, N, lane, koff, false);
-    };
-    auto wait_v = [&]() {
-      if (more) EI_WAIT_VMCNT(16); else EI_WAIT_VMCNT(0);
-      asm volatile("" ::: "memory");
-    };
-    if (MODE == kDenseFull || k0 <= q_last) {
-      compute_step<MODE, true>(st, k0, q0, qrow, N, jq, hf, lane, qf, sc_log2, oacc, m_i, l_i,
-                               next_k, wait_v);
-    } else {
-      next_k();
-      wait_v();
+  bool odd = false;   // the wave's masked step left values out
+  auto walk = [&](auto guard) {
+    EI_WAIT_VMCNT(0);   // the Q operands: no later wait covers copies in flight
+    int k0 = 0;
+    if (wave < n_steps) {
+      k0 = step_key0(wave);
+      issue_tile(st, kh, k0, N, lane, koff, false);
+      issue_tile(st + kTileBytes, vh, k0, N, lane, voff, true);
     }
-    EI_WAIT_LGKM0();
-    if (more) issue_tile(st + kTileBytes, vh, kn, N, lane, voff, true);
-    k0 = kn;
-  }
-
+    for (int i = wave; i < n_steps; i += kSplitWaves) {
+      const bool more = i + kSplitWaves < n_steps;
+      const int kn = more ? step_key0(i + kSplitWaves) : 0;
+      EI_WAIT_VMCNT(16);   // K has landed (V's 16 copies may be in flight)
+      asm volatile("" ::: "memory");
+      // (every LDS read of a tile has returned before its copies are issued)
+      auto next_k = [&]() {
+        EI_WAIT_LGKM0();
+        if (more) issue_tile(st, kh, kn, N, lane, koff, false);
+      };
+      auto wait_v = [&]() {
+        if (more) EI_WAIT_VMCNT(16); else EI_WAIT_VMCNT(0);
+        asm volatile("" ::: "memory");
+      };
+      if (MODE == kDenseFull || k0 <= q_last) {
+        compute_step<MODE, true, guard.value>(st, k0, q0, qrow, N, jq, hf, lane, qf, sc_log2, oacc,
+                                              m_i, l_i, &odd, next_k, wait_v);
+      } else {
+        next_k();
+        wait_v();
+      }
+      EI_WAIT_LGKM0();
+      if (more) issue_tile(st + kTileBytes, vh, kn, N, lane, voff, true);
+      k0 = kn;
+    }
+  };
   // Merge: each wave leaves its O in its own stage (every read and copy of
   // which is done), then takes 32 of the 128 dims of all four.
-  const float l = l_i + __shfl_xor(l_i, 32);
-  if (hf == 0) {
-    part_m[wave][jq] = m_i;
-    part_l[wave][jq] = l;
-  }
+  auto merge = [&]() -> float {
+    const float l = l_i + __shfl_xor(l_i, 32);
+    if (hf == 0) {
+      part_m[wave][jq] = m_i;
+      part_l[wave][jq] = l;
+    }
 #pragma unroll
-  for (int d = 0; d < 4; ++d)
+    for (int d = 0; d < 4; ++d)
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
-      *(float4*)(st + ((d * 4 + r) * kWave + lane) * 16) =
-          make_float4(oacc[d][4 * r], oacc[d][4 * r + 1], oacc[d][4 * r + 2], oacc[d][4 * r + 3]);
-  __syncthreads();
-  float m = part_m[0][jq];
+      for (int r = 0; r < 4; ++r)
+        *(float4*)(st + ((d * 4 + r) * kWave + lane) * 16) =
+            make_float4(oacc[d][4 * r], oacc[d][4 * r + 1], oacc[d][4 * r + 2], oacc[d][4 * r + 3]);
+    __syncthreads();
+    float m = part_m[0][jq];
 #pragma unroll
-  for (int w = 1; w < kSplitWaves; ++w) m = fmaxf(m, part_m[w][jq]);
-  float f[kSplitWaves], lsum = 0.0f;
-#pragma unroll
-  for (int w = 0; w < kSplitWaves; ++w) {
-    const float mw = part_m[w][jq];
-    f[w] = mw == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mw - m);
-    lsum += f[w] * part_l[w][jq];
-  }
-  const float inv = lsum > 0.0f ? 1.0f / lsum : 0.0f;
-  if (qrow >= N) return;
-  uint16_t* op = o + (size_t)qrow * kHeadDim + 32 * wave + 4 * hf;
-#pragma unroll
-  for (int r = 0; r < 4; ++r) {
-    float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    for (int w = 1; w < kSplitWaves; ++w) m = fmaxf(m, part_m[w][jq]);
+    float f[kSplitWaves], lsum = 0.0f;
 #pragma unroll
     for (int w = 0; w < kSplitWaves; ++w) {
-      const float4 x = *(const float4*)(stages[w] + ((wave * 4 + r) * kWave + lane) * 16);
-      a.x += f[w] * x.x;
-      a.y += f[w] * x.y;
-      a.z += f[w] * x.z;
-      a.w += f[w] * x.w;
+      const float mw = part_m[w][jq];
+      f[w] = mw == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(mw - m);
+      lsum += f[w] * part_l[w][jq];
     }
-    *(uint2*)(op + 8 * r) =
-        make_uint2(pack_bf16x2(a.x * inv, a.y * inv), pack_bf16x2(a.z * inv, a.w * inv));
-  }
+    const float inv = lsum > 0.0f ? 1.0f / lsum : 0.0f;
+    if (qrow >= N) return 0.0f;
+    float odd_row = 0.0f;   // becomes NaN where an infinity or NaN is stored
+    uint16_t* op = o + (size_t)qrow * kHeadDim + 32 * wave + 4 * hf;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+      float4 a = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+      for (int w = 0; w < kSplitWaves; ++w) {
+        const float4 x = *(const float4*)(stages[w] + ((wave * 4 + r) * kWave + lane) * 16);
+        a.x += f[w] * x.x;
+        a.y += f[w] * x.y;
+        a.z += f[w] * x.z;
+        a.w += f[w] * x.w;
+      }
+      const uint2 w =
+          make_uint2(pack_bf16x2(a.x * inv, a.y * inv), pack_bf16x2(a.z * inv, a.w * inv));
+      odd_row = odd_or(w.y, odd_or(w.x, odd_row));
+      *(uint2*)(op + 8 * r) = w;
+    }
+    return odd_row;
+  };
+  walk(std::false_type{});
+  const float bad = merge();
+  if constexpr (GUARD)
+    if (__builtin_expect(any_odd(bad, sm.odd), 0)) {   // (as in attn_packed_kernel)
+      clear_sums(oacc, m_i, l_i);
+      walk(std::true_type{});
+      if (odd) add_odd_values<MODE>(vh, q0, qrow, N, hf, oacc);
+      merge();
+    }
 }
 
 template <int MODE, int SUB>
@@ -1167,6 +1283,7 @@ __global__ __launch_bounds__(kThreads, 2) void attn_packed_kernel(
     const int32_t* __restrict__ cu, int S, float sc_log2) {
   __shared__ __attribute__((aligned(1024))) unsigned char stage0[kStageBytes];
   __shared__ __attribute__((aligned(1024))) unsigned char stage1[kStageBytes];
+  __shared__ bool odd_waves[kThreads / kWave];
   int h, rank;
   packed_item(blockIdx.x, Hq, Hkv, h, rank);
   const PackedTile pt = packed_tile<kTileQ>(cu, S, T, rank);
@@ -1201,25 +1318,39 @@ __global__ __launch_bounds__(kThreads, 2) void attn_packed_kernel(
   float m_i = -INFINITY, l_i = 0.0f;
 
   // the two-stage ring of attn_kernel
-  auto step = [&](const int i, unsigned char* st) {
-    if (i + 1 < n_steps) EI_WAIT_VMCNT(8); else EI_WAIT_VMCNT(0);
-    __syncthreads();
-    const int k0 = i * kSub;
-    if ((MODE == kDenseFull || k0 <= qw0 + 31) && qw0 < N)
-      compute_step<MODE>(st, k0, qw0, qrow, N, jq, hf, lane, qf, sc_log2, oacc, m_i, l_i);
-    if (i + 2 < n_steps) {
-      __syncthreads();   // every wave is done reading this stage
-      issue_stage<4>(st, kh, vh, (i + 2) * kSub, N, wave, lane, koff, voff);
+  bool odd = false;   // the wave's masked step left values out
+  auto walk = [&](auto guard) {
+    auto step = [&](const int i, unsigned char* st) {
+      if (i + 1 < n_steps) EI_WAIT_VMCNT(8); else EI_WAIT_VMCNT(0);
+      __syncthreads();
+      const int k0 = i * kSub;
+      if ((MODE == kDenseFull || k0 <= qw0 + 31) && qw0 < N)
+        compute_step<MODE, false, guard.value>(st, k0, qw0, qrow, N, jq, hf, lane, qf, sc_log2, oacc,
+                                               m_i, l_i, &odd);
+      if (i + 2 < n_steps) {
+        __syncthreads();   // every wave is done reading this stage
+        issue_stage<4>(st, kh, vh, (i + 2) * kSub, N, wave, lane, koff, voff);
+      }
+    };
+    EI_WAIT_VMCNT(0);
+    issue_stage<4>(stage0, kh, vh, 0, N, wave, lane, koff, voff);
+    if (n_steps > 1) issue_stage<4>(stage1, kh, vh, kSub, N, wave, lane, koff, voff);
+    for (int i = 0; i < n_steps; i += 2) {
+      step(i, stage0);
+      if (i + 1 < n_steps) step(i + 1, stage1);
     }
   };
-  EI_WAIT_VMCNT(0);
-  issue_stage<4>(stage0, kh, vh, 0, N, wave, lane, koff, voff);
-  if (n_steps > 1) issue_stage<4>(stage1, kh, vh, kSub, N, wave, lane, koff, voff);
-  for (int i = 0; i < n_steps; i += 2) {
-    step(i, stage0);
-    if (i + 1 < n_steps) step(i + 1, stage1);
+  walk(std::false_type{});
+  // Where the tile's rows hold an infinity or NaN, once more with GUARD (within 1%
+  // of a kernel without; the guard in the first loop cost every launch 9%).
+  float bad = 0.0f;
+  if (qrow < N) bad = store_rows(o, row_base, hf, oacc, l_i);
+  if (__builtin_expect(any_odd(bad, odd_waves), 0)) {
+    clear_sums(oacc, m_i, l_i);
+    walk(std::true_type{});
+    if (odd) add_odd_values<MODE>(vh, qw0, qrow, N, hf, oacc);
+    if (qrow < N) store_rows(o, row_base, hf, oacc, l_i);
   }
-  if (qrow < N) store_rows(o, row_base, hf, oacc, l_i);
 }
 
 // Small launches take the split by the rules of dense attention (split_tiles),
@@ -1248,8 +1379,8 @@ __global__ __launch_bounds__(kThreads, 1) void attn_packed_split_kernel(
   if (pt.tile < 0) return;
   const size_t kv = ((size_t)(h / (Hq / Hkv)) * T + pt.first) * kHeadDim;
   const size_t at = ((size_t)h * T + pt.first) * kHeadDim;
-  split_tile<MODE, 1>(sm, q + at, k + kv, v + kv, o + at, pt.N, pt.tile, 0, sc_log2, nullptr,
-                      nullptr, 0);
+  split_tile<MODE, 1, true>(sm, q + at, k + kv, v + kv, o + at, pt.N, pt.tile, 0, sc_log2, nullptr,
+                            nullptr, 0);
 }
 
 template <int MODE>

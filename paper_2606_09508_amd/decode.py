@@ -191,24 +191,43 @@ class PagedCache:
 
     def storing(self, seqs):
         """A ``store`` for prefill.prefill: keeps the keys and values of a batch
-        of new sequences, all of the prompt's length."""
-        seqs = list(seqs)
-        where = []
+        of new sequences, all of the prompt's length.  A prompt that fails
+        leaves them empty."""
+        return _Storing(self, list(seqs))
 
-        def store(layer: int, k, v):
-            B, _, N, _ = k.shape
-            if layer == 0:
-                if B != len(seqs) or any(self.length(s) for s in seqs):
-                    raise ValueError(f"storing a batch of {B} takes as many empty sequences")
-                self.extend(seqs, [N] * B)
-                table, lengths = self.table(seqs)
-                where[:] = (torch.from_numpy(np.ascontiguousarray(table)).to(k.device),
-                            torch.from_numpy(lengths).to(k.device))
-            table, lengths = where
-            for b in range(B):
-                eb.cache_store(k[b:b + 1], v[b:b + 1], self.layer(layer), table[b:b + 1],
-                               lengths[b:b + 1])
-        return store
+
+class _Storing:
+    """What PagedCache.storing returns: takes a prompt's layers, in order, and
+    gives back the room where the block around them fails."""
+
+    def __init__(self, cache: PagedCache, seqs):
+        self.cache, self.seqs = cache, seqs
+        self.where, self.took = None, False
+
+    def __call__(self, layer: int, k, v):
+        B, _, N, _ = k.shape
+        if layer == 0:
+            if B != len(self.seqs) or any(self.cache.length(s) for s in self.seqs):
+                raise ValueError(f"storing a batch of {B} takes as many empty sequences")
+            self.cache.extend(self.seqs, [N] * B)
+            self.took = True
+            table, lengths = self.cache.table(self.seqs)
+            self.where = (torch.from_numpy(np.ascontiguousarray(table)).to(k.device),
+                          torch.from_numpy(lengths).to(k.device))
+        table, lengths = self.where
+        for b in range(B):
+            eb.cache_store(k[b:b + 1], v[b:b + 1], self.cache.layer(layer), table[b:b + 1],
+                           lengths[b:b + 1])
+
+    def __enter__(self):
+        self.took = False
+        return self
+
+    def __exit__(self, error, *_):
+        if error is not None and self.took:
+            for s in self.seqs:
+                self.cache.truncate(s, 0)
+        self.took = False
 
 
 class _Batch:

@@ -18,6 +18,7 @@ carries no part of the method.
 from __future__ import annotations
 
 import argparse
+import contextlib
 import functools
 import math
 import sys
@@ -286,14 +287,16 @@ def prefill(x, layers, shape: DecoderShape, attn: Attention, lm_head=None, store
     final normed hidden state of the last token (and its logits when an LM
     head [hidden, vocab] is given) -- what the first generated token needs.
     ``store`` (optional) receives (layer index, keys, values) of every layer,
-    as decode.PagedCache.storing takes them."""
+    as decode.PagedCache.storing takes them; where it is a context manager, the
+    layers run inside it, so that it learns of a failure."""
     N = x.shape[1]
     cos, sin = rope_tables(N, shape.head_dim, shape.rope_theta, x.device)
     y = None
-    for i, w in enumerate(layers):
-        x, y = _layer(x, y, w, shape, attn, cos, sin,
-                      store=None if store is None else functools.partial(store, i))
-    return finish(x[:, -1:], None if y is None else y[:, -1:], layers, shape, lm_head)
+    with store if hasattr(store, "__exit__") else contextlib.nullcontext():
+        for i, w in enumerate(layers):
+            x, y = _layer(x, y, w, shape, attn, cos, sin,
+                          store=None if store is None else functools.partial(store, i))
+        return finish(x[:, -1:], None if y is None else y[:, -1:], layers, shape, lm_head)
 
 
 def ttft_table(lengths, shape: DecoderShape, n_layers: int, reps: int, cfg: SparseConfig,

@@ -144,7 +144,8 @@ class PagedCache:
     def truncate(self, seq: int, length: int) -> None:
         """Drops a sequence's tokens from `length` on.  The scales of the page it
         then ends in stay what the dropped tokens made them (NaN, and with it the
-        page's other tokens, where those were not finite)."""
+        page's other tokens, where those were not finite), and so do the codes
+        before them, which were rounded again where a scale grew."""
         old = self.length(seq)
         if not 0 <= length <= old:
             raise ValueError(f"cannot cut {old} tokens to {length}")
@@ -278,7 +279,8 @@ class Decoder:
     def step(self, x, seqs, counts=None):
         """New tokens of the sequences (counts[i] of seqs[i], one each without),
         packed in x: (normed hidden state of every token [tokens, hidden], their
-        logits or None)."""
+        logits or None).  Where a layer fails the sequences are cut back to what
+        they held."""
         counts = [1] * len(seqs) if counts is None else [int(c) for c in counts]
         ws = {}
 
@@ -317,7 +319,9 @@ class Decoder:
                 x, y = x[at], y[at]
             return pf.finish(x, y, self.layers, self.shape, self.lm_head)
         except BaseException:
-            for s, n in zip(seqs, held):   # (nothing was stored that counts)
+            # the room is given back; what the layers that ran made of a page's
+            # scale and older codes stays, as truncate says
+            for s, n in zip(seqs, held):
                 self.cache.truncate(s, n)
             raise
 

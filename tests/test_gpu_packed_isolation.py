@@ -1,7 +1,7 @@
 """What a query of packed prompts does not see never reaches it, whatever it
-holds: its own sequence's later values, and the places past a sequence's end in
-its last key block.  In both kernels: tiles of 128 rows, and tiles of 32 whose
-keys the waves share."""
+holds: its own sequence's later keys and values, those of the sequences before
+and behind it, and the places past a sequence's end in its last key block.  In
+both kernels: tiles of 128 rows, and tiles of 32 whose keys the waves share."""
 import math
 
 import pytest
@@ -82,3 +82,44 @@ def test_last_value_over_all_keys(kernel, n):
     x[:, :, n - 1, 3] = math.inf
     y[:, :, :n, 3] = math.inf
     _same(_run(q, k, x, cu, causal=False), y)
+
+
+@pytest.mark.parametrize("causal", [True, False])
+@pytest.mark.parametrize("kernel", HEADS)
+@pytest.mark.parametrize("lengths", [(150, 140, 170), (129, 300, 131), (200, 64, 330)])
+def test_sequences_before_and_behind(lengths, kernel, causal):
+    """The other sequences' keys and values are NaN and infinite."""
+    cu = [0, lengths[0], sum(lengths[:2]), sum(lengths)]
+    q, k, v = _tensors(HEADS[kernel], cu[-1])
+    want = _run(q, k, v, cu, causal)
+    for s in range(3):
+        for bad_k, bad_v in ((math.nan, math.inf), (math.inf, math.nan), (-math.inf, -math.inf)):
+            x, y = torch.full_like(k, bad_k), torch.full_like(v, bad_v)
+            x[:, :, cu[s]:cu[s + 1]] = k[:, :, cu[s]:cu[s + 1]]
+            y[:, :, cu[s]:cu[s + 1]] = v[:, :, cu[s]:cu[s + 1]]
+            got = _run(q, x, y, cu, causal)
+            assert torch.equal(got[:, :, cu[s]:cu[s + 1]], want[:, :, cu[s]:cu[s + 1]])
+
+
+@pytest.mark.parametrize("kernel", HEADS)
+@pytest.mark.parametrize("bad", BAD)
+def test_later_keys_of_the_sequence(kernel, bad):
+    """Queries before a key that is not finite stay finite and as they were, but
+    for the roundings of another running maximum: each of their probabilities
+    is rounded to bf16 once more (2^-8 of it) and the output too."""
+    n = 300
+    q, k, v = _tensors(HEADS[kernel], n)
+    want = _run(q, k, v, [0, n])
+    # the sum of a query's weights times |v|, head by head
+    c = 1.0 / math.sqrt(D)
+    x = (q[0].double() @ k[0].double().repeat_interleave(G, 0).transpose(1, 2)) * c
+    i = torch.arange(n, device="cuda")
+    w = torch.softmax(x.masked_fill(i > i[:, None], -math.inf), -1)
+    a = w @ v[0].double().repeat_interleave(G, 0).abs()
+    off = 1.01 * 2 * (2.0 ** -8 * want[0].double().abs() + (2.0 ** -8 + 1e-4) * a)
+    for j in (1, 33, 100, n - 1):
+        y = k.clone()
+        y[:, :, j] = bad
+        got = _run(q, y, v, [0, n])
+        err = (got[0].double() - want[0].double()).abs()[:, :j]
+        assert bool((err <= off[:, :j]).all())

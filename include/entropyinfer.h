@@ -432,9 +432,9 @@ ei_status ei_swiglu(const uint16_t* g, const uint16_t* u, int64_t n, uint16_t* o
  *   q, k, v, o   bf16 [Hq][T][D], [Hkv][T][D]; dims.batch must be 1 (else
  *                EI_ERR_SHAPE) and dims.seq_len is T
  *   cu_seqlens   i32 [n_seqs + 1], ascending, on the device.  Values are
- *                clamped to [0, T] and a sequence that does not end after it
- *                starts is empty, so no list leads out of the tensors; rows
- *                that two sequences share hold the result of either.
+ *                clamped to [0, T].  With a list that does not ascend nothing
+ *                outside the tensors is read or written; which rows of o are
+ *                written, and over which keys, is then not defined.
  *
  * Rows of o that belong to no sequence are left as they were.  Keys and values
  * that a query does not attend to reach no element of its row, whatever they
@@ -443,7 +443,9 @@ ei_status ei_swiglu(const uint16_t* g, const uint16_t* u, int64_t n, uint16_t* o
  * bits depend, by roundings, on T and n_seqs as the bits of
  * ei_dense_prefill_attn do on its launch.
  *
- * Errors: as ei_dense_prefill_attn; EI_ERR_SHAPE also for n_seqs < 0.
+ * Errors: as ei_dense_prefill_attn; EI_ERR_SHAPE also for n_seqs < 0;
+ * EI_ERR_SHAPE or EI_ERR_LAUNCH where (T / 128 + n_seqs) * Hq workgroups of 256
+ * threads are more than a launch takes.
  */
 ei_status ei_packed_prefill_attn(const uint16_t* q, const uint16_t* k, const uint16_t* v,
                                  ei_dims dims, const int32_t* cu_seqlens, int32_t n_seqs,
@@ -457,11 +459,13 @@ ei_status ei_packed_prefill_attn(const uint16_t* q, const uint16_t* k, const uin
  * page_table[s][p / page_len].
  *
  * New tokens come packed: bf16 [heads][T][D] (T = n_tokens), sequence s being
- * the rows cu_seqlens[s] .. cu_seqlens[s+1]-1 (clamped as in
- * ei_packed_prefill_attn), or, with cu_seqlens NULL, T / n_seqs rows of each
- * sequence (T must be a multiple, else EI_ERR_SHAPE).  lengths[s] is the number of
- * tokens of sequence s in the cache, its new ones included: the last of them
- * is at position lengths[s] - 1.
+ * the rows cu_seqlens[s] .. cu_seqlens[s+1]-1 (ascending and clamped as in
+ * ei_packed_prefill_attn; with a list that does not ascend nothing outside the
+ * tensors and the sequences' own pages is touched, and what in them is not
+ * defined), or, with cu_seqlens NULL, T / n_seqs rows of each sequence (T must be
+ * a multiple, else EI_ERR_SHAPE).  lengths[s] is the number of tokens of
+ * sequence s in the cache, its new ones included: the last of them is at
+ * position lengths[s] - 1.
  */
 typedef enum {
   EI_CACHE_E4M3 = 0, /* 8-bit floating point, 4 exponent and 3 fraction bits */

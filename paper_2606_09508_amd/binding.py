@@ -619,8 +619,9 @@ def packed_prefill_attn(q, k, v, cu_seqlens, softmax_scale: float | None = None,
                         causal: bool = True, out=None):
     """ei_packed_prefill_attn: dense attention within each of the sequences
     that lie one behind the other in q [1, Hq, T, D], k and v [1, Hkv, T, D];
-    sequence s is the rows cu_seqlens[s] .. cu_seqlens[s + 1] - 1 (int32, on the
-    device).  Rows of ``out`` outside every sequence are left as they were."""
+    sequence s is the rows cu_seqlens[s] .. cu_seqlens[s + 1] - 1 (int32,
+    ascending, on the device).  Rows of ``out`` outside every sequence are left as
+    they were."""
     dev, kv_shape = _tokens(k, v)
     _req_packed(q, "q", dev)
     _req_i32(cu_seqlens, "cu_seqlens", 1, dev)

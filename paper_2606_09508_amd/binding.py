@@ -621,7 +621,7 @@ def packed_prefill_attn(q, k, v, cu_seqlens, softmax_scale: float | None = None,
     that lie one behind the other in q [1, Hq, T, D], k and v [1, Hkv, T, D];
     sequence s is the rows cu_seqlens[s] .. cu_seqlens[s + 1] - 1 (int32,
     ascending, on the device).  Rows of ``out`` outside every sequence are left as
-    they were."""
+    they were (without ``out``: undefined, as torch.empty leaves them)."""
     dev, kv_shape = _tokens(k, v)
     _req_packed(q, "q", dev)
     _req_i32(cu_seqlens, "cu_seqlens", 1, dev)
@@ -774,8 +774,10 @@ def cache_attn(q, pages: CachePages, page_table, lengths, cu_seqlens=None,
                softmax_scale: float | None = None, out=None, workspace=None):
     """ei_cache_attn: attention of each sequence's newest tokens q [1, Hq, T, D]
     over the cache, which holds them already; page_table, lengths and
-    cu_seqlens as cache_store.  Returns bf16 [1, Hq, T, D].  ``workspace``
-    (optional, uint8, of cache_attn_workspace_bytes) is scratch of this call."""
+    cu_seqlens as cache_store.  Returns bf16 [1, Hq, T, D]; rows of ``out`` outside
+    every sequence are left as they were (without ``out``: undefined, as
+    torch.empty leaves them).  ``workspace`` (optional, uint8, of
+    cache_attn_workspace_bytes) is scratch of this call."""
     dev = _device_of(q)
     _req_packed(q, "q", dev)
     hkv, head_dim, cs, ptrs = _cache_args(pages, dev)

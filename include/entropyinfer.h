@@ -528,7 +528,9 @@ size_t ei_cache_attn_workspace_bytes(int32_t n_q_heads, int32_t n_tokens, int32_
  * at position lengths[s] - n_s + i and attends to the keys up to its own;
  * grouped heads as everywhere.  fp32 accumulation and online softmax, bf16
  * output; the probabilities times V's scale enter the second product with 16
- * significant bits (as the sum of two bf16 numbers).
+ * significant bits (as the sum of two bf16 numbers).  That holds for scales of V
+ * from 2^-90 to 2^64 (pages whose largest elements are 2^-83 to 2^70); with
+ * smaller ones bits are lost, with larger ones sums may overflow.
  *
  *   q, o        bf16 [n_q_heads][T][D]
  *   workspace   ei_cache_attn_workspace_bytes(), 16-byte aligned

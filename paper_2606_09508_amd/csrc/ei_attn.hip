@@ -1210,7 +1210,12 @@ hipError_t launch_union_t(const uint16_t* q, const uint16_t* k, const uint16_t* 
 // that starts cu[s] rows further on: attn_kernel's steps on shifted pointers,
 // and bound like it by power where the sequences are long (64k tokens in ten of
 // them, 32 heads: 7.25 ms, 1.13 PFLOP/s) and by a tile's start where they are
-// short (eight of 1 to 2100 tokens: 138 us, 0.77; 64 of 512: 255 us, 0.52).
+// short (eight of 1 to 2100 tokens: 127-138 us, 0.77-0.84; 64 of 512: 255 us, 0.54;
+// over all keys, of those eight 225-239 us, 0.90-0.95, of 8 x 4096 tokens 1.98 ms, 1.11).
+// As there, a probability enters the second product as one bf16 number (8 bits;
+// the sums are fp32): the result is then 0.0021 from 64 bits, relative, where its
+// own rounding alone makes 0.0016.  As two numbers, the sum of which has 16 bits, the
+// 64k tokens took 7.4 -> 10.6 ms, the eight 128 -> 175 us, 64 of 512 257 -> 303.
 // The host does not know the lengths: sequence s owns the ranks cu[s] / TILE + s
 // up to the next one's first, one for each of its tiles, heaviest first, and at
 // most one more (which leaves its workgroup nothing).  (Ranking the tiles by

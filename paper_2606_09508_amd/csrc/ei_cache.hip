@@ -679,8 +679,11 @@ constexpr int kShareLeast = 4;   // steps and costs a wave takes at least
 // third: 6 sequences of 13000, 32 rows, int8 40.7 / 38.9 / 36.6 us, e4m3 40.0 / 38.4 /
 // 36.4, 16 of 500 to 8000 33.6 / 32.9 / 30.9; 16 rows, equal / sixth: 40 of 300 to
 // 6000 18.1 / 17.5; 8 of up to 128k 245.4 / 244.2; 256 of 200 to 8000 188.7 / 187.6; an
-// eighth or a fifth within 1% of that), unless equal runs are whole items (as many
+// eighth or a fifth within 1% of that; the loser: 16 of 4000 to 16000, two tiles of
+// 32 rows each, a call 113.6 / - / 114.9), unless equal runs are whole items (as many
 // sequences of one length as make it so: 256 of 4096 and 8 KV heads 322 / 341).
+// That workgroups 0 .. 255 are the CUs' first is how the launch fills the chip, and
+// only the balance rests on it.
 constexpr int elder_share(int rt) { return rt == 1 ? 6 : 3; }
 
 // A value that all lanes share, in scalar registers.
@@ -1082,7 +1085,9 @@ Pages pages_of(const ei_cache_shape& c, const ei_cache_pages& p, const int32_t* 
 // A table of no more keys: one workgroup per item.  (It reads about 50 KB per us,
 // whatever its waves; dealt out, with the second kernel: 1 sequence of 1500 tokens
 // 13.7 / 10 + 4 us, 32 of 1900 21.8 / 26 + 5, 100 of up to 1900 49.5 / 41 + 5; tables
-// of 3900 here / dealt out: 1 28 / 10 + 4, 32 41 / 45 + 5, 100 of up to 3900 96 / 72 + 6.)
+// of 3900 here / dealt out: 1 28 / 10 + 4, 32 41 / 45 + 5, 100 of up to 3900 96 / 72 + 6.
+// The width alone decides, and is off by up to a fifth on either side of it: 100 of
+// up to 1900 lose 3 us by it, 32 of 3900 nine.)
 constexpr int kShortKeys = 2048;
 constexpr int kShortWaves = 4;     // (8 / 16: 1 of 1000 9.2 -> 9.2 / 10.8 us, 200 51 -> 59 / 72)
 

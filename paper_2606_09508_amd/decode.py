@@ -106,8 +106,8 @@ class PagedCache:
 
     def extend(self, seqs, counts) -> None:
         """Room for counts[i] more tokens of seqs[i] (their values come with the
-        next store).  Raises CacheFull, and changes nothing, where the pages do
-        not suffice."""
+        next store).  Raises CacheFull where the pages do not suffice; whatever it
+        raises, it has changed nothing."""
         seqs, counts = list(seqs), [int(c) for c in counts]
         if len(set(seqs)) != len(seqs) or len(counts) != len(seqs) or min(counts, default=0) < 0:
             raise ValueError("extend takes each sequence once, with a count of new tokens")
@@ -126,20 +126,30 @@ class PagedCache:
             plan.append((s, c, last if copy else -1, new))
         if need > len(self._free):
             raise CacheFull(f"{need} pages needed, {len(self._free)} of {self.n_pages} free")
-        src, dst = [], []
+        # the copies first: where they cannot be made, the pages go back
+        pages = [heapq.heappop(self._free) for _ in range(need)]
+        take, src, dst, found = iter(pages), [], [], []
         for s, c, shared, new in plan:
+            if shared >= 0:
+                src.append(shared)
+                dst.append(next(take))
+            found.append([next(take) for _ in range(new)])
+        try:
+            self._copy(src, dst)
+        except BaseException:
+            for page in pages:
+                heapq.heappush(self._free, page)
+            raise
+        self._refs[pages] = 1
+        own = iter(dst)
+        for (s, c, shared, new), fresh in zip(plan, found):
             old = int(self._length[s])
             if shared >= 0:
-                page = self._take()
-                src.append(shared)
-                dst.append(page)
                 self._drop(shared)
-                self._table[s, old // self.page_len] = page
+                self._table[s, old // self.page_len] = next(own)
             at = self._count(old)
-            for i in range(new):
-                self._table[s, at + i] = self._take()
+            self._table[s, at:at + new] = fresh
             self._length[s] = old + c
-        self._copy(src, dst)
 
     def truncate(self, seq: int, length: int) -> None:
         """Drops a sequence's tokens from `length` on.  The scales of the page it
@@ -172,11 +182,6 @@ class PagedCache:
             self._refs[src] = 0
         self._free = list(range(n, self.n_pages))
         return len(src)
-
-    def _take(self) -> int:
-        page = heapq.heappop(self._free)
-        self._refs[page] = 1
-        return page
 
     def _drop(self, page: int) -> None:
         self._refs[page] -= 1

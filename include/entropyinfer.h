@@ -318,8 +318,8 @@ ei_status ei_sparse_prefill_attn_gqa_union(const uint16_t* q, const uint16_t* k,
  * ei_dense_prefill_attn -- dense GQA attention (Section 2's A_h V), causal
  * (keys j <= i) when `causal` is non-zero, else over all N keys; same tile
  * code and numerics as ei_sparse_prefill_attn.
- * A value that is infinite or NaN makes NaN of the queries before it, too, that
- * share its 64 keys (ei_packed_prefill_attn's do not).
+ * In both, a value that is infinite or NaN makes NaN of the queries before it, too,
+ * that share its 64 keys (in ei_packed_prefill_attn it does not).
  *
  * Errors: EI_ERR_NULL, EI_ERR_SHAPE (also a softmax_scale that is not finite
  * and positive), EI_ERR_UNSUPPORTED, EI_ERR_LAUNCH.

@@ -18,6 +18,8 @@
  *   ei_cache_*              a paged 8-bit cache of keys and values: storing
  *                           into it, attention of new tokens over it, copies
  *                           of pages
+ *   ei_adapter_*            low-rank corrections of the projections, each
+ *                           request's own
  *
  * Conventions shared by every entry point
  *  - Tensors are contiguous, row-major, in device memory owned by the caller;
@@ -570,6 +572,71 @@ ei_status ei_cache_attn(const uint16_t* q, int32_t n_q_heads, int32_t n_tokens,
  */
 ei_status ei_cache_copy(ei_cache_shape shape, int32_t n_layers, ei_cache_pages pages,
                         const int32_t* src, const int32_t* dst, int32_t n, void* stream);
+
+/*
+ * Low-rank adapters: corrections that the requests of a batch, each with an
+ * adapter of its own choice, add to projections that all of them share,
+ *   y[t] += scale[a] (x[t] A_a^T) B_a^T,   a = index[the sequence of token t].
+ * Tokens are packed as in the cache: sequence s is the rows cu_seqlens[s] ..
+ * cu_seqlens[s+1]-1 of x and y (ascending and clamped to [0, n_tokens]), or, with
+ * cu_seqlens NULL, n_tokens / n_seqs rows of each sequence.
+ *
+ * ei_adapter_batch: n_tokens rows of n_seqs sequences, and how many adapters there
+ * are (8192 at most, else EI_ERR_UNSUPPORTED).
+ */
+typedef struct {
+  int32_t n_tokens, n_seqs, n_adapters;
+} ei_adapter_batch;
+
+/* One projection of x: a bf16 [n_adapters][rank][n_in], b bf16
+ * [n_adapters][n_out][rank], scale fp32 [n_adapters] or NULL (1), y bf16
+ * [n_tokens][n_out]; n_out a multiple of 8 (else EI_ERR_UNSUPPORTED). */
+typedef struct {
+  const uint16_t *a, *b;
+  const float* scale;
+  uint16_t* y;
+  int32_t n_out;
+} ei_adapter_target;
+
+/* Bytes of a batch's plan; 0: none needed, or invalid sizes. */
+size_t ei_adapter_plan_bytes(ei_adapter_batch batch);
+
+/*
+ * ei_adapter_plan -- the batch's tokens ordered by adapter, for every
+ * ei_adapter_add of the same batch (all projections of all layers of a step).
+ *
+ *   index   i32 [n_seqs]: the adapter of each sequence; one outside
+ *           [0, n_adapters) means none
+ *   plan    out, ei_adapter_plan_bytes() of device memory, 16-byte aligned
+ *
+ * Errors: EI_ERR_NULL, EI_ERR_SHAPE, EI_ERR_UNSUPPORTED, EI_ERR_WORKSPACE (plan
+ * missing or too small), EI_ERR_LAUNCH.
+ */
+ei_status ei_adapter_plan(const int32_t* index, const int32_t* cu_seqlens, ei_adapter_batch batch,
+                          void* plan, size_t plan_bytes, void* stream);
+
+/* Workspace bytes ei_adapter_add needs; 0: none, or invalid sizes. */
+size_t ei_adapter_add_workspace_bytes(ei_adapter_batch batch, int32_t n_in, int32_t rank,
+                                      int32_t n_targets);
+
+/*
+ * ei_adapter_add -- adds the corrections of up to four projections of the same x
+ * (bf16 [n_tokens][n_in]) to their y, in place.  rank is a multiple of 8 up to 128
+ * (smaller ones are padded with zeros), n_in a multiple of 8 (else
+ * EI_ERR_UNSUPPORTED).  x A^T is held in fp32, enters the second product with 16
+ * significant bits (as the sum of two bf16 numbers), and y is rounded once.
+ * `targets` is read on the host.  Rows of y whose sequence has no adapter, or that
+ * belong to no sequence, are left as they were; offsets that do not ascend leave
+ * the values of y undefined, and nothing outside the tensors is touched.  No y may
+ * overlap another or any input.  The workspace is scratch of one call.
+ *
+ * Errors: EI_ERR_NULL, EI_ERR_SHAPE, EI_ERR_UNSUPPORTED, EI_ERR_WORKSPACE (plan or
+ * workspace missing or too small), EI_ERR_LAUNCH.
+ */
+ei_status ei_adapter_add(const uint16_t* x, int32_t n_in, int32_t rank,
+                         const ei_adapter_target* targets, int32_t n_targets,
+                         ei_adapter_batch batch, const void* plan, size_t plan_bytes,
+                         void* workspace, size_t workspace_bytes, void* stream);
 
 #ifdef __cplusplus
 }

@@ -53,6 +53,16 @@ class CachePointers(ctypes.Structure):   # ei_cache_pages
                 ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p)]
 
 
+class AdapterBatch(ctypes.Structure):
+    _fields_ = [("n_tokens", ctypes.c_int32), ("n_seqs", ctypes.c_int32),
+                ("n_adapters", ctypes.c_int32)]
+
+
+class AdapterTarget(ctypes.Structure):
+    _fields_ = [("a", ctypes.c_void_p), ("b", ctypes.c_void_p), ("scale", ctypes.c_void_p),
+                ("y", ctypes.c_void_p), ("n_out", ctypes.c_int32)]
+
+
 class EIError(RuntimeError):
     def __init__(self, fn: str, status: int, text: str):
         super().__init__(f"{fn} returned {status} ({_STATUS.get(status, '?')}): {text}")
@@ -143,6 +153,15 @@ def lib() -> ctypes.CDLL:
         L.ei_cache_copy.restype = ctypes.c_int
         L.ei_cache_copy.argtypes = [CacheShape, ctypes.c_int32, CachePointers, _VP, _VP,
                                     ctypes.c_int32, _VP]
+        L.ei_adapter_plan_bytes.restype = ctypes.c_size_t
+        L.ei_adapter_plan_bytes.argtypes = [AdapterBatch]
+        L.ei_adapter_plan.restype = ctypes.c_int
+        L.ei_adapter_plan.argtypes = [_VP, _VP, AdapterBatch, _VP, ctypes.c_size_t, _VP]
+        L.ei_adapter_add_workspace_bytes.restype = ctypes.c_size_t
+        L.ei_adapter_add_workspace_bytes.argtypes = [AdapterBatch] + [ctypes.c_int32] * 3
+        L.ei_adapter_add.restype = ctypes.c_int
+        L.ei_adapter_add.argtypes = [_VP, ctypes.c_int32, ctypes.c_int32, _VP, ctypes.c_int32,
+                                     AdapterBatch, _VP, ctypes.c_size_t, _VP, ctypes.c_size_t, _VP]
         _LIB = L
     return _LIB
 
@@ -839,3 +858,114 @@ def cache_copy(pages: CachePages, src, dst) -> None:
                              _raw_stream(dev))
     if st:
         _check("ei_cache_copy", st)
+
+
+# --------------------------------------------------------------------------
+# Low-rank adapters
+# --------------------------------------------------------------------------
+
+class Adapters(NamedTuple):
+    """Low-rank corrections of one projection (ei_adapter_target): a [n, rank,
+    n_in] and b [n, n_out, rank] in bf16, scale fp32 [n] or None (1).  rank is a
+    multiple of 8 up to 128: fill up smaller ones with zeros."""
+    a: torch.Tensor
+    b: torch.Tensor
+    scale: torch.Tensor | None = None
+
+
+class AdapterPlan(NamedTuple):
+    """What adapter_plan returns: the tokens of a batch ordered by adapter."""
+    data: torch.Tensor
+    batch: AdapterBatch
+
+
+def adapter_plan(index, n_adapters: int, n_tokens: int, cu_seqlens=None) -> AdapterPlan:
+    """ei_adapter_plan: for n_tokens packed tokens of the sequences whose adapters
+    index (int32 [S], outside [0, n_adapters): none) names; cu_seqlens int32
+    [S + 1] as cache_store (None: n_tokens / S rows each).  One plan serves every
+    adapter_add of the batch."""
+    dev = _device_of(index)
+    if dev < 0:
+        _req(index, "index", torch.int32, 1)
+    _req_i32(index, "index", 1, dev)
+    S = index.size(0)
+    if cu_seqlens is not None:
+        _req_i32(cu_seqlens, "cu_seqlens", 1, dev)
+        if cu_seqlens.size(0) != S + 1:
+            raise ValueError(f"cu_seqlens has {cu_seqlens.size(0)} offsets for {S} sequences")
+    elif n_tokens and (not S or n_tokens % S):
+        raise ValueError(f"{n_tokens} tokens do not divide among {S} sequences: pass cu_seqlens")
+    if dev != _current_device():
+        with torch.cuda.device(dev):
+            return adapter_plan(index, n_adapters, n_tokens, cu_seqlens)
+    batch = AdapterBatch(n_tokens, S, n_adapters)
+    nb = lib().ei_adapter_plan_bytes(batch)
+    data = torch.empty((nb,), dtype=torch.uint8, device=index.device)
+    st = lib().ei_adapter_plan(index.data_ptr(), _ptr(cu_seqlens), batch, data.data_ptr(), nb,
+                               _raw_stream(dev))
+    if st:
+        _check("ei_adapter_plan", st)
+    return AdapterPlan(data, batch)
+
+
+def adapter_add(x, ys, adapters, plan: AdapterPlan, workspace=None) -> None:
+    """ei_adapter_add: ys[i] += the corrections adapters[i] (Adapters) of x, in
+    place, for up to four projections of the same x.  x [..., n_in] and ys[i]
+    [..., n_out] are bf16 with the plan's tokens in their leading dimensions.
+    ``workspace`` (optional, uint8, of adapter_add_workspace_bytes) is scratch of
+    this call."""
+    dev, bf16, T = _device_of(x), torch.bfloat16, plan.batch.n_tokens
+    if not (dev >= 0 and x.dtype is bf16 and x.dim() > 0 and x.is_contiguous()):
+        _req(x, "x", bf16, max(x.dim(), 1) if isinstance(x, torch.Tensor) else 1)
+    if plan.data.get_device() != dev:
+        raise ValueError(f"tensors on different devices: {x.device} and {plan.data.device}")
+    n_in = x.size(-1)
+    if x.numel() != T * n_in:
+        raise ValueError(f"x {tuple(x.shape)} does not hold the {T} tokens of the plan")
+    if not len(ys) == len(adapters) or not ys:
+        raise ValueError(f"{len(adapters)} sets of adapters for {len(ys)} projections")
+    n, rank = plan.batch.n_adapters, 0
+    targets = (AdapterTarget * len(ys))()
+    for i, (y, (a, b, scale)) in enumerate(zip(ys, adapters)):
+        for t, name, nd in ((y, "y", y.dim() if isinstance(y, torch.Tensor) else 1), (a, "a", 3),
+                            (b, "b", 3)):
+            if not (isinstance(t, torch.Tensor) and t.dtype is bf16 and t.get_device() == dev
+                    and t.dim() == nd and nd and t.is_contiguous()):
+                _req(t, f"{name} of projection {i}", bf16, max(nd, 1))
+                raise ValueError(f"tensors on different devices: {x.device} and {t.device}")
+        n_out = y.size(-1)
+        if i == 0:
+            rank = a.size(1)
+        if a.shape != (n, rank, n_in) or b.shape != (n, n_out, rank) or y.numel() != T * n_out:
+            raise ValueError(f"projection {i}: a {tuple(a.shape)}, b {tuple(b.shape)} and y "
+                             f"{tuple(y.shape)} are not [{n}, {rank}, {n_in}], [{n}, n_out, "
+                             f"{rank}] and {T} tokens of n_out")
+        if scale is not None:
+            _req(scale, f"scale of projection {i}", torch.float32, 1)
+            _same_device(x, scale)
+            if scale.size(0) != n:
+                raise ValueError(f"projection {i}: {scale.size(0)} scales for {n} adapters")
+        targets[i] = AdapterTarget(a.data_ptr(), b.data_ptr(), _ptr(scale), y.data_ptr(), n_out)
+    if dev != _current_device():
+        with torch.cuda.device(dev):
+            return adapter_add(x, ys, adapters, plan, workspace)
+    L = lib()
+    if workspace is None:
+        nb = L.ei_adapter_add_workspace_bytes(plan.batch, n_in, rank, len(ys))
+        if nb:
+            workspace = torch.empty((nb,), dtype=torch.uint8, device=x.device)
+    else:
+        _same_device(x, workspace)
+        if not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous")
+        nb = workspace.numel() * workspace.element_size()
+    st = L.ei_adapter_add(x.data_ptr(), n_in, rank, targets, len(ys), plan.batch,
+                          plan.data.data_ptr(), plan.data.numel(), _ptr(workspace), nb,
+                          _raw_stream(dev))
+    if st:
+        _check("ei_adapter_add", st)
+
+
+def adapter_add_workspace_bytes(plan: AdapterPlan, n_in: int, rank: int, n_targets: int) -> int:
+    """Bytes of the workspace that adapter_add takes for such a call."""
+    return int(lib().ei_adapter_add_workspace_bytes(plan.batch, n_in, rank, n_targets))

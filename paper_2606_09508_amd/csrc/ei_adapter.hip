@@ -1,0 +1,528 @@
+// Low-rank corrections of the projections that the requests of a batch share:
+//   y[t] += scale[a] (x[t] A_a^T) B_a^T,   a = the adapter of t's sequence,
+// A_a [rank][in], B_a [out][rank], for up to four projections of the same x.
+//
+//  plan_kernel    the tokens ordered by adapter, in tiles of one adapter each
+//  shrink_kernel  V = x A^T in fp32, the ranks of all projections side by side
+//  expand_kernel  y += (scale V) B^T
+//
+// Both products run on the matrix cores (16x16x32, weights on M, tokens on N)
+// and are bound by HBM: a tile's weights are read once and its x and y pass by.
+#include "../../include/entropyinfer.h"
+#include "ei_internal.h"
+
+#include <limits.h>
+
+namespace ei {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / kWave;
+constexpr int kMaxAdapters = 8192;   // their counts lie in LDS
+constexpr int kMaxRank = 128;
+constexpr int kMaxTargets = 4;
+
+__device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi) {
+  const f32x2 x = {lo, hi};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, bf16x2));
+}
+
+// ----------------------------------------------------------------------------
+// Plan.  [0] the number of tiles; from kPlanHead on the tiles; then the
+// tokens.  A tile is `count` tokens of one adapter, from place `begin` of the
+// list of tokens on.
+// ----------------------------------------------------------------------------
+struct Tile {
+  int adapter, begin, count, pad;
+};
+constexpr size_t kPlanHead = 64;
+constexpr int kPlanThreads = 1024;
+
+struct PlanShape {
+  int tokens, seqs, adapters;
+  int rows;        // of a tile, at most
+  int max_tiles;
+  size_t list_at, bytes;
+};
+// Tiles of 64 tokens where a sequence has 32 on average, else of 16.
+PlanShape plan_shape(const ei_adapter_batch& b) {
+  PlanShape p{b.n_tokens, b.n_seqs, b.n_adapters, 16, 0, 0, 0};
+  if (b.n_tokens / 32 >= b.n_seqs) p.rows = 64;
+  const int used = b.n_adapters < b.n_seqs ? b.n_adapters : b.n_seqs;
+  p.max_tiles = b.n_tokens / p.rows + (used < b.n_tokens ? used : b.n_tokens);
+  p.list_at = kPlanHead + (size_t)p.max_tiles * sizeof(Tile);
+  p.bytes = p.list_at + (size_t)b.n_tokens * sizeof(int32_t);
+  return p;
+}
+
+struct PlanArgs {
+  const int32_t *index, *cu;
+  int32_t* head;
+  Tile* tiles;
+  int32_t* list;
+  PlanShape p;
+};
+
+__device__ __forceinline__ void rows_of(const PlanArgs& a, int s, int& first, int& n) {
+  if (!a.cu) {
+    n = a.p.tokens / a.p.seqs;
+    first = s * n;
+    return;
+  }
+  first = min(max(a.cu[s], 0), a.p.tokens);
+  n = max(min(max(a.cu[s + 1], 0), a.p.tokens) - first, 0);
+}
+
+// One workgroup.  The counts are integers, and each sequence's place follows from
+// those before it, so the list does not depend on the order of the atomics.
+__global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
+  __shared__ int place[kMaxAdapters];          // an adapter's tokens; then its next place
+  __shared__ int first_tile[kMaxAdapters];
+  __shared__ int seq_a[kPlanThreads], seq_n[kPlanThreads];
+  __shared__ int wave_tokens[kPlanThreads / kWave], wave_tiles[kPlanThreads / kWave];
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  const int n = a.p.adapters;
+  for (int i = tid; i < n; i += kPlanThreads) place[i] = 0;
+  __syncthreads();
+  for (int s = tid; s < a.p.seqs; s += kPlanThreads) {
+    const int at = a.index[s];
+    int first, count;
+    rows_of(a, s, first, count);
+    if (at >= 0 && at < n && count > 0) atomicAdd(&place[at], count);
+  }
+  __syncthreads();
+  // the adapters' first places and tiles; a thread has `per` of them in a row
+  const int per = (n + kPlanThreads - 1) / kPlanThreads, i0 = tid * per;
+  int tokens = 0, tiles = 0;
+  for (int i = i0; i < min(i0 + per, n); ++i) {
+    tokens += place[i];
+    tiles += (place[i] + a.p.rows - 1) / a.p.rows;
+  }
+  const int up_tokens = (int)wave_incl_scan_u32((uint32_t)tokens);
+  const int up_tiles = (int)wave_incl_scan_u32((uint32_t)tiles);
+  if (lane == kWave - 1) {
+    wave_tokens[wave] = up_tokens;
+    wave_tiles[wave] = up_tiles;
+  }
+  __syncthreads();
+  int at = up_tokens - tokens, tile = up_tiles - tiles, all = 0;
+  for (int w = 0; w < kPlanThreads / kWave; ++w) {
+    if (w < wave) {
+      at += wave_tokens[w];
+      tile += wave_tiles[w];
+    }
+    all += wave_tiles[w];
+  }
+  for (int i = i0; i < min(i0 + per, n); ++i) {
+    const int count = place[i];
+    first_tile[i] = tile;
+    place[i] = at;
+    at += count;
+    tile += (count + a.p.rows - 1) / a.p.rows;
+  }
+  // (Offsets that do not ascend may count more tokens than there are, past 2^31 even:
+  // a tile then ends with the list or is empty.)
+  all = min(all, a.p.max_tiles);
+  if (tid == 0) a.head[0] = all;
+  if (tid == kPlanThreads - 1) seq_n[0] = at;
+  __syncthreads();
+  const int total = seq_n[0];
+  for (int t = tid; t < all; t += kPlanThreads) {
+    int lo = 0, hi = n - 1;      // the last adapter that starts at tile t or before
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) / 2;
+      if (first_tile[mid] <= t) lo = mid; else hi = mid - 1;
+    }
+    const int begin = place[lo] + (t - first_tile[lo]) * a.p.rows;
+    const int stop = min(lo + 1 < n ? place[lo + 1] : total, a.p.tokens);
+    a.tiles[t] = Tile{lo, begin, begin < 0 ? 0 : min(stop - begin, a.p.rows), 0};
+  }
+  __syncthreads();
+  // the sequences in their order, kPlanThreads at a time
+  for (int s0 = 0; s0 < a.p.seqs; s0 += kPlanThreads) {
+    const int s = s0 + tid, here = min(a.p.seqs - s0, kPlanThreads);
+    int first = 0, count = 0, ad = -1;
+    if (s < a.p.seqs) {
+      ad = a.index[s];
+      rows_of(a, s, first, count);
+      if (ad < 0 || ad >= n) ad = -1;
+    }
+    seq_a[tid] = ad;
+    seq_n[tid] = count;
+    __syncthreads();
+    int before = 0;
+    for (int i = 0; i < min(here, (wave + 1) * kWave); ++i)
+      before += i < tid && seq_a[i] == ad ? seq_n[i] : 0;
+    const int to = ad < 0 ? -1 : place[ad] + before;
+    __syncthreads();
+    if (ad >= 0) atomicAdd(&place[ad], count);
+    // a wave writes its 64 sequences' tokens, one sequence after the other
+    for (uint64_t todo = __builtin_amdgcn_ballot_w64(to >= 0 && count > 0); todo; todo &= todo - 1) {
+      const int l = (int)__builtin_ctzll(todo);
+      const int f = __builtin_amdgcn_readlane(first, l), c = __builtin_amdgcn_readlane(count, l);
+      const int p = __builtin_amdgcn_readlane(to, l);
+      for (int i = lane; i < c; i += kWave)
+        if ((unsigned)(p + i) < (unsigned)a.p.tokens) a.list[p + i] = f + i;
+    }
+    __syncthreads();
+  }
+}
+
+// ----------------------------------------------------------------------------
+// Shrink.  The ranks of all targets are rows 0 .. targets * rank - 1 of one
+// matrix.  A workgroup takes 16 MT of them, a tile's 16 NT tokens and a part of
+// the columns, which its waves share; their sums are added in LDS in the waves'
+// order, and the parts' by expand_kernel.  A lane's 16 columns of 64 are 32 bytes
+// of a row (the order of the columns is free as long as both operands share it).
+// ----------------------------------------------------------------------------
+struct Target {
+  const uint16_t *a, *b;
+  const float* scale;
+  uint16_t* y;
+  int n_out;
+  int block0;      // expand_kernel's first workgroup of it, per tile
+};
+struct AddArgs {
+  const uint16_t* x;
+  float* v;                    // [splits][tokens, in the plan's order][targets * rank]
+  const int32_t* head;
+  const Tile* tiles;
+  const int32_t* list;
+  int tokens, n_in, rank, targets, splits;
+  int blocks;                  // expand_kernel's workgroups per tile
+  Target t[kMaxTargets];
+};
+
+__device__ __forceinline__ const Target& target(const AddArgs& a, int i) {
+  return i == 0 ? a.t[0] : i == 1 ? a.t[1] : i == 2 ? a.t[2] : a.t[3];
+}
+
+// Token i of a tile (the last one where it has fewer).  Offsets that do not ascend
+// may leave places of the list unset.
+__device__ __forceinline__ int token_at(const AddArgs& a, const Tile& t, int i) {
+  return min(max(a.list[t.begin + min(i, t.count - 1)], 0), a.tokens - 1);
+}
+
+constexpr int kColumns = 64;   // of a step
+
+template <int MT, int NT>
+__global__ __launch_bounds__(kThreads) void shrink_kernel(AddArgs a, int row_tiles, int64_t unit0) {
+  constexpr int kRows = 16 * MT, kTokens = 16 * NT, kPitch = kRows + 4;
+  __shared__ __attribute__((aligned(16))) float sm[kWaves][kTokens * kPitch];
+  int64_t unit = unit0 + blockIdx.x;
+  const int split = (int)(unit % a.splits);
+  unit /= a.splits;
+  const int r0 = (int)(unit % row_tiles) * kRows;
+  const int tile = (int)(unit / row_tiles);
+  if (tile >= a.head[0]) return;
+  const Tile t = a.tiles[tile];
+  if (t.count <= 0) return;
+  const int R = a.targets * a.rank;
+  const int lane = threadIdx.x % kWave, j = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const uint16_t* wp[MT];
+  const uint16_t* xp[NT];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) {
+    const int row = min(r0 + 16 * m + j, R - 1), i = row / a.rank;
+    wp[m] = target(a, i).a + ((int64_t)t.adapter * a.rank + row % a.rank) * a.n_in + 16 * g;
+  }
+#pragma unroll
+  for (int k = 0; k < NT; ++k) {
+    xp[k] = a.x + (int64_t)token_at(a, t, 16 * k + j) * a.n_in + 16 * g;
+  }
+  f32x4 acc[MT][NT];
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int k = 0; k < NT; ++k) acc[m][k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  const int steps = (a.n_in + kColumns - 1) / kColumns;
+  const int per = (steps + a.splits - 1) / a.splits;
+  const int end = min((split + 1) * per, steps);
+  for (int s = split * per + wave; s < end; s += kWaves) {
+    const int c = s * kColumns, left = a.n_in - c - 16 * g;
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {
+      const bool in = 8 * half < left;       // (columns come in eights)
+      bf16x8 w[MT], x[NT];
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+        w[m] = __builtin_bit_cast(bf16x8, in ? *(const uint4*)(wp[m] + c + 8 * half)
+                                             : make_uint4(0u, 0u, 0u, 0u));
+#pragma unroll
+      for (int k = 0; k < NT; ++k)
+        x[k] = __builtin_bit_cast(bf16x8, in ? *(const uint4*)(xp[k] + c + 8 * half)
+                                             : make_uint4(0u, 0u, 0u, 0u));
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int k = 0; k < NT; ++k)
+          acc[m][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[m], x[k], acc[m][k], 0, 0, 0);
+    }
+  }
+  // lane: token j, rows 4g .. 4g + 3 of each tile
+#pragma unroll
+  for (int m = 0; m < MT; ++m)
+#pragma unroll
+    for (int k = 0; k < NT; ++k)
+      *(float4*)&sm[wave][(16 * k + j) * kPitch + 16 * m + 4 * g] =
+          make_float4(acc[m][k][0], acc[m][k][1], acc[m][k][2], acc[m][k][3]);
+  __syncthreads();
+  for (int e = threadIdx.x; e < kRows * kTokens; e += kThreads) {
+    const int tok = e / kRows, row = e % kRows;
+    if (tok >= t.count || r0 + row >= R) continue;
+    float sum = sm[0][tok * kPitch + row];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) sum += sm[w][tok * kPitch + row];
+    a.v[((int64_t)split * a.tokens + t.begin + tok) * R + r0 + row] = sum;
+  }
+}
+
+// ----------------------------------------------------------------------------
+// Expand.  V times the scale goes to the matrix cores as the sum of two bf16
+// numbers (16 bits; one alone would double the variance that y's rounding has):
+// they are columns 0 .. rank - 1 and rank .. 2 rank - 1 of one operand, each
+// against the same columns of B.  y is the accumulator's start and is rounded
+// once.  A wave takes 64 outputs; row i of its product m is output 16 (i / 4) +
+// 4 m + i % 4, so that a lane has 16 outputs in a row of its token.
+// ----------------------------------------------------------------------------
+constexpr int kWaveOuts = 64;
+constexpr int kBlockOuts = kWaveOuts * kWaves;
+
+template <int NT>
+__global__ __launch_bounds__(kThreads) void expand_kernel(AddArgs a, int64_t unit0) {
+  constexpr int kTokens = 16 * NT, kPad = 8;
+  __shared__ __attribute__((aligned(16))) uint16_t sm[kTokens * (2 * kMaxRank + kPad)];
+  const int64_t unit = unit0 + blockIdx.x;
+  const int block = (int)(unit % a.blocks), tile = (int)(unit / a.blocks);
+  if (tile >= a.head[0]) return;
+  int ti = 0;
+  for (int i = 1; i < a.targets; ++i)
+    if (block >= target(a, i).block0) ti = i;
+  const Target tg = target(a, ti);
+  const Tile t = a.tiles[tile];
+  if (t.count <= 0) return;
+  const int r = a.rank, pitch = 2 * r + kPad, R = a.targets * r;
+  const float scale = tg.scale ? tg.scale[t.adapter] : 1.0f;
+  // the tile's V, as pairs of bf16 numbers
+  for (int e = threadIdx.x; e < kTokens * (r / 2); e += kThreads) {
+    const int tok = e / (r / 2), c = e % (r / 2) * 2;
+    float x0 = 0.0f, x1 = 0.0f;
+    if (tok < t.count)
+      for (int s = 0; s < a.splits; ++s) {
+        const float* p = a.v + ((int64_t)s * a.tokens + t.begin + tok) * R + ti * r + c;
+        x0 += p[0];
+        x1 += p[1];
+      }
+    x0 *= scale;
+    x1 *= scale;
+    const uint32_t hi = pack_bf16x2(x0, x1);
+    *(uint32_t*)&sm[tok * pitch + c] = hi;
+    // (an infinity has no rest)
+    const float y0 = __builtin_isinf(x0) ? 0.0f : x0 - bf16_lo(hi);
+    const float y1 = __builtin_isinf(x1) ? 0.0f : x1 - bf16_hi(hi);
+    *(uint32_t*)&sm[tok * pitch + r + c] = pack_bf16x2(y0, y1);
+  }
+  __syncthreads();
+  const int lane = threadIdx.x % kWave, j = lane & 15, g = lane >> 4;
+  const int o0 = (block - tg.block0) * kBlockOuts + (int)(threadIdx.x / kWave) * kWaveOuts;
+  if (o0 >= tg.n_out) return;
+  const int chunks = (2 * r + 31) / 32;
+  const uint16_t* bp[4];
+#pragma unroll
+  for (int m = 0; m < 4; ++m) {
+    const int o = min(o0 + 16 * (j >> 2) + 4 * m + (j & 3), tg.n_out - 1);
+    bp[m] = tg.b + ((int64_t)t.adapter * tg.n_out + o) * r;
+  }
+  const int mine = o0 + 16 * g;     // this lane's outputs
+#pragma unroll
+  for (int k = 0; k < NT; ++k) {
+    if (16 * k >= t.count) break;
+    const int row = 16 * k + j;
+    uint16_t* yp = tg.y + (int64_t)token_at(a, t, row) * tg.n_out + mine;
+    uint4 w[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      w[h] = mine + 8 * h < tg.n_out ? *(const uint4*)(yp + 8 * h) : make_uint4(0u, 0u, 0u, 0u);
+    f32x4 acc[4];
+#pragma unroll
+    for (int m = 0; m < 4; ++m) {
+      const uint32_t u0 = m & 1 ? w[m >> 1].z : w[m >> 1].x, u1 = m & 1 ? w[m >> 1].w : w[m >> 1].y;
+      acc[m] = f32x4{bf16_lo(u0), bf16_hi(u0), bf16_lo(u1), bf16_hi(u1)};
+    }
+    for (int c = 0; c < chunks; ++c) {
+      const int col = 32 * c + 8 * g;     // (past 2 r: nothing, rank 8 alone)
+      const bool in = col < 2 * r;
+      const uint4 v = in ? *(const uint4*)&sm[row * pitch + col] : make_uint4(0u, 0u, 0u, 0u);
+      const int bc = col < r ? col : col - r;
+#pragma unroll
+      for (int m = 0; m < 4; ++m) {
+        const uint4 b = in ? *(const uint4*)(bp[m] + bc) : make_uint4(0u, 0u, 0u, 0u);
+        acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+            __builtin_bit_cast(bf16x8, b), __builtin_bit_cast(bf16x8, v), acc[m], 0, 0, 0);
+      }
+    }
+    if (row >= t.count) continue;
+#pragma unroll
+    for (int h = 0; h < 2; ++h)
+      if (mine + 8 * h < tg.n_out)
+        *(uint4*)(yp + 8 * h) = make_uint4(
+            pack_bf16x2(acc[2 * h][0], acc[2 * h][1]), pack_bf16x2(acc[2 * h][2], acc[2 * h][3]),
+            pack_bf16x2(acc[2 * h + 1][0], acc[2 * h + 1][1]),
+            pack_bf16x2(acc[2 * h + 1][2], acc[2 * h + 1][3]));
+  }
+}
+
+// ----------------------------------------------------------------------------
+// Host side
+// ----------------------------------------------------------------------------
+constexpr int64_t kMaxGrid = (1ll << 31) / kThreads;
+unsigned launch_grid(int64_t left) { return (unsigned)(left < kMaxGrid ? left : kMaxGrid); }
+bool aligned(const void* p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
+ei_status from_hip(hipError_t e) { return e == hipSuccess ? EI_OK : EI_ERR_LAUNCH; }
+
+ei_status check_batch(const ei_adapter_batch& b) {
+  if (b.n_tokens < 0 || b.n_seqs < 0 || b.n_adapters < 0) return EI_ERR_SHAPE;
+  if (b.n_adapters > kMaxAdapters) return EI_ERR_UNSUPPORTED;
+  return EI_OK;
+}
+bool nothing(const ei_adapter_batch& b) {
+  return b.n_tokens == 0 || b.n_seqs == 0 || b.n_adapters == 0;
+}
+
+struct AddPlan {
+  int row_tiles, splits, mt;
+  size_t bytes;
+};
+// Parts of the columns: as many as give the chip 512 workgroups, of 512 columns at
+// least (two steps a wave).
+AddPlan add_plan(const PlanShape& p, int n_in, int rank, int targets) {
+  AddPlan s{};
+  const int R = targets * rank;
+  s.mt = p.rows == 16 || R <= 16 ? 1 : R <= 32 ? 2 : R <= 48 ? 3 : 4;
+  s.row_tiles = (R + 16 * s.mt - 1) / (16 * s.mt);
+  const int64_t units = (int64_t)p.max_tiles * s.row_tiles;
+  int64_t splits = 512 / (units > 0 ? units : 1);
+  const int64_t most = n_in / 512;
+  if (splits > most) splits = most;
+  s.splits = splits < 1 ? 1 : (int)splits;
+  s.bytes = (size_t)s.splits * p.tokens * R * sizeof(float);
+  return s;
+}
+ei_status check_sizes(int32_t n_in, int32_t rank, int32_t n_targets) {
+  if (n_in <= 0 || rank <= 0 || n_targets < 0) return EI_ERR_SHAPE;
+  if (n_in % 8 || rank % 8 || rank > kMaxRank || n_targets > kMaxTargets) return EI_ERR_UNSUPPORTED;
+  return EI_OK;
+}
+
+}  // namespace
+}  // namespace ei
+
+extern "C" {
+
+size_t ei_adapter_plan_bytes(ei_adapter_batch batch) {
+  if (ei::check_batch(batch) != EI_OK || ei::nothing(batch)) return 0;
+  return ei::plan_shape(batch).bytes;
+}
+
+ei_status ei_adapter_plan(const int32_t* index, const int32_t* cu_seqlens, ei_adapter_batch batch,
+                          void* plan, size_t plan_bytes, void* stream) {
+  const ei_status st = ei::check_batch(batch);
+  if (st != EI_OK) return st;
+  if (!cu_seqlens && batch.n_seqs > 0 && batch.n_tokens % batch.n_seqs) return EI_ERR_SHAPE;
+  if (ei::nothing(batch)) return EI_OK;
+  if (!index) return EI_ERR_NULL;
+  if (!ei::aligned(index, 4) || !ei::aligned(cu_seqlens, 4)) return EI_ERR_UNSUPPORTED;
+  const ei::PlanShape p = ei::plan_shape(batch);
+  if (!plan || plan_bytes < p.bytes) return EI_ERR_WORKSPACE;
+  if (!ei::aligned(plan, 16)) return EI_ERR_UNSUPPORTED;
+  char* at = (char*)plan;
+  const ei::PlanArgs a{index, cu_seqlens, (int32_t*)at, (ei::Tile*)(at + ei::kPlanHead),
+                       (int32_t*)(at + p.list_at), p};
+  hipLaunchKernelGGL(ei::plan_kernel, dim3(1), dim3(ei::kPlanThreads), 0, (hipStream_t)stream, a);
+  return ei::from_hip(hipGetLastError());
+}
+
+size_t ei_adapter_add_workspace_bytes(ei_adapter_batch batch, int32_t n_in, int32_t rank,
+                                      int32_t n_targets) {
+  if (ei::check_batch(batch) != EI_OK || ei::nothing(batch) ||
+      ei::check_sizes(n_in, rank, n_targets) != EI_OK || n_targets == 0)
+    return 0;
+  return ei::add_plan(ei::plan_shape(batch), n_in, rank, n_targets).bytes;
+}
+
+ei_status ei_adapter_add(const uint16_t* x, int32_t n_in, int32_t rank,
+                         const ei_adapter_target* targets, int32_t n_targets,
+                         ei_adapter_batch batch, const void* plan, size_t plan_bytes,
+                         void* workspace, size_t workspace_bytes, void* stream) {
+  ei_status st = ei::check_batch(batch);
+  if (st != EI_OK) return st;
+  if ((st = ei::check_sizes(n_in, rank, n_targets)) != EI_OK) return st;
+  if (n_targets > 0 && !targets) return EI_ERR_NULL;
+  int64_t blocks = 0;
+  ei::AddArgs a{};
+  for (int i = 0; i < n_targets; ++i) {
+    const ei_adapter_target& t = targets[i];
+    if (t.n_out <= 0) return EI_ERR_SHAPE;
+    if (t.n_out % 8) return EI_ERR_UNSUPPORTED;
+    a.t[i] = ei::Target{t.a, t.b, t.scale, t.y, t.n_out, (int)blocks};
+    blocks += ((int64_t)t.n_out + ei::kBlockOuts - 1) / ei::kBlockOuts;
+  }
+  if (ei::nothing(batch) || n_targets == 0) return EI_OK;
+  const ei::PlanShape p = ei::plan_shape(batch);
+  if (!x) return EI_ERR_NULL;
+  if (!ei::aligned(x, 16)) return EI_ERR_UNSUPPORTED;
+  for (int i = 0; i < n_targets; ++i) {
+    const ei_adapter_target& t = targets[i];
+    if (!t.a || !t.b || !t.y) return EI_ERR_NULL;
+    if (!ei::aligned(t.a, 16) || !ei::aligned(t.b, 16) || !ei::aligned(t.y, 16) ||
+        !ei::aligned(t.scale, 4))
+      return EI_ERR_UNSUPPORTED;
+  }
+  const ei::AddPlan s = ei::add_plan(p, n_in, rank, n_targets);
+  if (!plan || plan_bytes < p.bytes || !workspace || workspace_bytes < s.bytes)
+    return EI_ERR_WORKSPACE;
+  if (!ei::aligned(plan, 16) || !ei::aligned(workspace, 16)) return EI_ERR_UNSUPPORTED;
+  const char* at = (const char*)plan;
+  a.x = x;
+  a.v = (float*)workspace;
+  a.head = (const int32_t*)at;
+  a.tiles = (const ei::Tile*)(at + ei::kPlanHead);
+  a.list = (const int32_t*)(at + p.list_at);
+  a.tokens = p.tokens;
+  a.n_in = n_in;
+  a.rank = rank;
+  a.targets = n_targets;
+  a.splits = s.splits;
+  a.blocks = (int)blocks;
+  hipStream_t s0 = (hipStream_t)stream;
+  const dim3 block(ei::kThreads);
+  const int64_t shrinks = (int64_t)p.max_tiles * s.row_tiles * s.splits;
+  for (int64_t u = 0; u < shrinks; u += ei::kMaxGrid) {
+    const dim3 grid(ei::launch_grid(shrinks - u));
+#define EI_SHRINK(MT, NT) \
+  hipLaunchKernelGGL((ei::shrink_kernel<MT, NT>), grid, block, 0, s0, a, s.row_tiles, u)
+    if (p.rows == 16) EI_SHRINK(1, 1);
+    else if (s.mt == 1) EI_SHRINK(1, 4);
+    else if (s.mt == 2) EI_SHRINK(2, 4);
+    else if (s.mt == 3) EI_SHRINK(3, 4);
+    else EI_SHRINK(4, 4);
+#undef EI_SHRINK
+  }
+  const int64_t expands = (int64_t)p.max_tiles * blocks;
+  for (int64_t u = 0; u < expands; u += ei::kMaxGrid) {
+    const dim3 grid(ei::launch_grid(expands - u));
+    if (p.rows == 16)
+      hipLaunchKernelGGL((ei::expand_kernel<1>), grid, block, 0, s0, a, u);
+    else
+      hipLaunchKernelGGL((ei::expand_kernel<4>), grid, block, 0, s0, a, u);
+  }
+  return ei::from_hip(hipGetLastError());
+}
+
+}  // extern "C"

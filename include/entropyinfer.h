@@ -18,6 +18,7 @@
  *   ei_cache_*              a paged 8-bit cache of keys and values: storing
  *                           into it, attention of new tokens over it, copies
  *                           of pages
+ *   ei_sample_tokens        the next token of each row of logits
  *   ei_adapter_*            low-rank corrections of the projections, each
  *                           request's own
  *
@@ -572,6 +573,57 @@ ei_status ei_cache_attn(const uint16_t* q, int32_t n_q_heads, int32_t n_tokens,
  */
 ei_status ei_cache_copy(ei_cache_shape shape, int32_t n_layers, ei_cache_pages pages,
                         const int32_t* src, const int32_t* dst, int32_t n, void* stream);
+
+typedef enum {
+  EI_LOGITS_BF16 = 0,
+  EI_LOGITS_FP32 = 1
+} ei_logits_format;
+
+/* Workspace bytes ei_sample_tokens needs (0: none, or invalid sizes).  The
+ * workspace is scratch of one call. */
+size_t ei_sample_workspace_bytes(int32_t rows, int32_t vocab, int32_t format);
+
+/*
+ * ei_sample_tokens -- the next token of each row of logits, drawn with the random
+ * number that the caller gives.
+ *
+ * With m the largest logit of a row and T its temperature, token i weighs w_i =
+ * exp((x_i - m) / T), rounded to a multiple of 2^-44 (the largest weighs 1).  In the
+ * order of falling logits, equal ones by rising index, kept are
+ *   top_k   the first k;
+ *   top_p   of them the shortest run from the first on whose weight is at least p
+ *           times theirs (one token at least);
+ *   min_p   of them those with w_i >= min_p (before the rounding).
+ * The token is the first kept one, by index, at which the kept weights summed up
+ * to it exceed u times their total.
+ *
+ *   logits       bf16 or fp32 (an ei_logits_format), row r at r * row_stride
+ *                elements, row_stride >= vocab; aligned to an element
+ *   u            fp32 [rows], meant for [0, 1): NaN and lesser values count as 0,
+ *                greater ones as 1 - 2^-24
+ *   temperature  fp32 [rows] or NULL (1).  One that is not > 0 takes the largest
+ *                logit, the lowest index of equal ones; infinity weighs all alike
+ *   top_k        i32 [rows] or NULL; values <= 0: no limit
+ *   top_p        fp32 [rows] or NULL; values >= 1 and NaN: no limit
+ *   min_p        fp32 [rows] or NULL; values <= 0 and NaN: no limit, > 1 as 1
+ *   tokens       out, i32 [rows]
+ *   logprobs     out, fp32 [rows] or NULL: ln of the token's share of the kept
+ *                weights (0 where temperature is not > 0)
+ *   workspace    ei_sample_workspace_bytes(), 16-byte aligned
+ *
+ * Logits of -inf and NaN are no tokens; a row of nothing else (or of vocab 0) gives
+ * -1 and -inf.  Logits of +inf weigh 1, all others beside them 0.  Sums of weights
+ * are whole numbers, so nothing depends on their order.  vocab is 2^19 at most
+ * (else EI_ERR_UNSUPPORTED).
+ *
+ * Errors: EI_ERR_NULL, EI_ERR_SHAPE, EI_ERR_UNSUPPORTED, EI_ERR_WORKSPACE,
+ * EI_ERR_LAUNCH.
+ */
+ei_status ei_sample_tokens(const void* logits, int32_t format, int32_t rows, int32_t vocab,
+                           int64_t row_stride, const float* u, const float* temperature,
+                           const int32_t* top_k, const float* top_p, const float* min_p,
+                           int32_t* tokens, float* logprobs, void* workspace,
+                           size_t workspace_bytes, void* stream);
 
 /*
  * Low-rank adapters: corrections that the requests of a batch, each with an

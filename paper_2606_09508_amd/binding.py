@@ -153,6 +153,12 @@ def lib() -> ctypes.CDLL:
         L.ei_cache_copy.restype = ctypes.c_int
         L.ei_cache_copy.argtypes = [CacheShape, ctypes.c_int32, CachePointers, _VP, _VP,
                                     ctypes.c_int32, _VP]
+        L.ei_sample_workspace_bytes.restype = ctypes.c_size_t
+        L.ei_sample_workspace_bytes.argtypes = [ctypes.c_int32] * 3
+        L.ei_sample_tokens.restype = ctypes.c_int
+        L.ei_sample_tokens.argtypes = [_VP, ctypes.c_int32, ctypes.c_int32, ctypes.c_int32,
+                                       ctypes.c_int64, _VP, _VP, _VP, _VP, _VP, _VP, _VP, _VP,
+                                       ctypes.c_size_t, _VP]
         L.ei_adapter_plan_bytes.restype = ctypes.c_size_t
         L.ei_adapter_plan_bytes.argtypes = [AdapterBatch]
         L.ei_adapter_plan.restype = ctypes.c_int
@@ -969,3 +975,81 @@ def adapter_add(x, ys, adapters, plan: AdapterPlan, workspace=None) -> None:
 def adapter_add_workspace_bytes(plan: AdapterPlan, n_in: int, rank: int, n_targets: int) -> int:
     """Bytes of the workspace that adapter_add takes for such a call."""
     return int(lib().ei_adapter_add_workspace_bytes(plan.batch, n_in, rank, n_targets))
+
+
+# --------------------------------------------------------------------------
+# Sampling
+# --------------------------------------------------------------------------
+
+LOGITS_FORMATS = {torch.bfloat16: 0, torch.float32: 1}   # ei_logits_format
+
+
+def _setting(t, name: str, dtype, rows: int, dev: int):
+    """A row setting's pointer: 0 for None."""
+    if t is None:
+        return None
+    if not (isinstance(t, torch.Tensor) and t.dtype is dtype and t.dim() == 1
+            and t.get_device() == dev and t.is_contiguous()):
+        _req(t, name, dtype, 1)
+        raise ValueError(f"tensors on different devices: {name} on {t.device}")
+    if t.size(0) != rows:
+        raise ValueError(f"{name} holds {t.size(0)} values for {rows} rows")
+    return t.data_ptr()
+
+
+def sample_tokens(logits, u, temperature=None, top_k=None, top_p=None, min_p=None, out=None,
+                  logprobs=None, workspace=None):
+    """ei_sample_tokens: the next token of each row of logits [rows, vocab] (bf16 or
+    fp32; the rows may lie apart), drawn with the random numbers u (fp32 [rows] in
+    [0, 1)).  temperature, top_p, min_p (fp32) and top_k (int32) hold a value for
+    each row; None: 1, or no limit.  Returns (tokens int32 [rows], the logarithms of
+    their shares fp32 [rows]); -1 and -inf for a row without tokens.  ``out`` and
+    ``logprobs`` (optional) are those two tensors, ``workspace`` (uint8, of
+    sample_workspace_bytes) is scratch of this call."""
+    dev = _device_of(logits)
+    fmt = LOGITS_FORMATS.get(logits.dtype) if dev >= 0 else None
+    if fmt is None or logits.dim() != 2:
+        if isinstance(logits, torch.Tensor) and logits.dtype not in LOGITS_FORMATS:
+            raise TypeError(f"logits are bfloat16 or float32, not {logits.dtype}")
+        _req(logits, "logits", getattr(logits, "dtype", None), 2)
+    rows, vocab = logits.shape
+    stride = logits.stride(0) if rows > 1 else vocab
+    if (vocab > 1 and logits.stride(1) != 1) or stride < vocab:
+        raise ValueError(f"the rows of logits {tuple(logits.shape)} with strides "
+                         f"{logits.stride()} do not lie one behind the other")
+    f32 = torch.float32
+    if u is None:
+        raise TypeError("u must be a torch.Tensor")
+    args = [_setting(u, "u", f32, rows, dev), _setting(temperature, "temperature", f32, rows, dev),
+            _setting(top_k, "top_k", torch.int32, rows, dev),
+            _setting(top_p, "top_p", f32, rows, dev), _setting(min_p, "min_p", f32, rows, dev)]
+    if out is None:
+        out = torch.empty((rows,), dtype=torch.int32, device=logits.device)
+    if logprobs is None:
+        logprobs = torch.empty((rows,), dtype=f32, device=logits.device)
+    args += [_setting(out, "out", torch.int32, rows, dev),
+             _setting(logprobs, "logprobs", f32, rows, dev)]
+    if dev != _current_device():
+        with torch.cuda.device(dev):
+            return sample_tokens(logits, u, temperature, top_k, top_p, min_p, out, logprobs,
+                                 workspace)
+    L = lib()
+    if workspace is None:
+        nb = L.ei_sample_workspace_bytes(rows, vocab, fmt)
+        if nb:
+            workspace = torch.empty((nb,), dtype=torch.uint8, device=logits.device)
+    else:
+        _same_device(logits, workspace)
+        if not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous")
+        nb = workspace.numel() * workspace.element_size()
+    st = L.ei_sample_tokens(logits.data_ptr(), fmt, rows, vocab, stride, *args, _ptr(workspace), nb,
+                            _raw_stream(dev))
+    if st:
+        _check("ei_sample_tokens", st)
+    return out, logprobs
+
+
+def sample_workspace_bytes(rows: int, vocab: int, dtype=torch.bfloat16) -> int:
+    """Bytes of the workspace that sample_tokens takes for such logits."""
+    return int(lib().ei_sample_workspace_bytes(rows, vocab, LOGITS_FORMATS[dtype]))

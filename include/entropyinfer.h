@@ -562,6 +562,46 @@ ei_status ei_cache_attn(const uint16_t* q, int32_t n_q_heads, int32_t n_tokens,
                         ei_cache_pages pages, float softmax_scale, uint16_t* o, void* workspace,
                         size_t workspace_bytes, void* stream);
 
+/* Workspace bytes ei_cache_attn_shared needs; 0: invalid sizes, or no tokens. */
+size_t ei_cache_attn_shared_workspace_bytes(int32_t n_q_heads, int32_t n_tokens, int32_t n_seqs,
+                                            int32_t n_groups, int32_t max_pages,
+                                            ei_cache_shape shape);
+
+/*
+ * ei_cache_attn_shared -- ei_cache_attn for sequences that share their first pages
+ * (continuations of one prompt, requests behind one system prompt): the keys there
+ * are read once for all of a group's new tokens.
+ *
+ *   group_seqs     i32 [n_groups + 1]: group g is the sequences group_seqs[g] ..
+ *                  group_seqs[g+1]-1 (ascending, clamped to [0, n_seqs]); sequences
+ *                  of no group attend by themselves, as those of a group of one
+ *                  that shares nothing
+ *   shared_pages   i32 [n_groups]: in so many first columns of the page table the
+ *                  group's sequences name the same pages; the first sequence's row
+ *                  is read for all of them
+ *   workspace      ei_cache_attn_shared_workspace_bytes(), 16-byte aligned; scratch
+ *                  of one call
+ *   the others     as ei_cache_attn
+ *
+ * Columns with a key that a new token of the group does not see (it lies in the page
+ * or before) are read for each sequence by itself, so shared_pages may be too large
+ * for the lengths, but not for the table.  The probabilities of shared keys enter
+ * the second product as fp16 numbers (11 bits) where a group has more than 32 rows
+ * (tokens times query heads of a KV head) on average, with 16 bits otherwise; all
+ * else is as in ei_cache_attn, zero rows and rows of no sequence included.  Lists that
+ * do not ascend leave o undefined, and nothing outside the tensors is touched.
+ * A sequence's bits depend, by roundings, on the others of the call.
+ *
+ * Errors: as ei_cache_attn; EI_ERR_SHAPE also for n_groups < 0.
+ */
+ei_status ei_cache_attn_shared(const uint16_t* q, int32_t n_q_heads, int32_t n_tokens,
+                               const int32_t* cu_seqlens, int32_t n_seqs, const int32_t* lengths,
+                               const int32_t* page_table, int32_t max_pages,
+                               const int32_t* group_seqs, const int32_t* shared_pages,
+                               int32_t n_groups, ei_cache_shape shape, ei_cache_pages pages,
+                               float softmax_scale, uint16_t* o, void* workspace,
+                               size_t workspace_bytes, void* stream);
+
 /*
  * ei_cache_copy -- page dst[i] = page src[i] (codes and scales of K and V) in
  * each of n_layers caches of the same shape that lie one behind the other

@@ -150,6 +150,13 @@ def lib() -> ctypes.CDLL:
         L.ei_cache_attn.argtypes = [_VP, ctypes.c_int32, ctypes.c_int32, _VP, ctypes.c_int32, _VP,
                                     _VP, ctypes.c_int32, CacheShape, CachePointers,
                                     ctypes.c_float, _VP, _VP, ctypes.c_size_t, _VP]
+        L.ei_cache_attn_shared_workspace_bytes.restype = ctypes.c_size_t
+        L.ei_cache_attn_shared_workspace_bytes.argtypes = [ctypes.c_int32] * 5 + [CacheShape]
+        L.ei_cache_attn_shared.restype = ctypes.c_int
+        L.ei_cache_attn_shared.argtypes = [_VP, ctypes.c_int32, ctypes.c_int32, _VP,
+                                           ctypes.c_int32, _VP, _VP, ctypes.c_int32, _VP, _VP,
+                                           ctypes.c_int32, CacheShape, CachePointers,
+                                           ctypes.c_float, _VP, _VP, ctypes.c_size_t, _VP]
         L.ei_cache_copy.restype = ctypes.c_int
         L.ei_cache_copy.argtypes = [CacheShape, ctypes.c_int32, CachePointers, _VP, _VP,
                                     ctypes.c_int32, _VP]
@@ -846,6 +853,64 @@ def cache_attn_workspace_bytes(n_q_heads: int, n_tokens: int, packed: bool, n_se
     shape = _cache_shape(*pages.k.shape[-4:], CACHE_FORMATS[pages.k.dtype])
     return int(lib().ei_cache_attn_workspace_bytes(n_q_heads, n_tokens, packed, n_seqs, max_pages,
                                                    shape))
+
+
+def cache_attn_shared(q, pages: CachePages, page_table, lengths, group_seqs, shared_pages,
+                      cu_seqlens=None, softmax_scale: float | None = None, out=None,
+                      workspace=None):
+    """ei_cache_attn_shared: cache_attn of sequences that share their first pages.
+    Group g is the sequences group_seqs[g] .. group_seqs[g + 1] - 1 (int32, ascending,
+    on the device); the first shared_pages[g] (int32) columns of their rows of the page
+    table are alike, and the keys there are read once for all of them.  ``workspace``
+    (optional, uint8, of cache_attn_shared_workspace_bytes) is scratch of this call."""
+    dev = _device_of(q)
+    _req_packed(q, "q", dev)
+    hkv, head_dim, cs, ptrs = _cache_args(pages, dev)
+    _, Hq, T, D = shape = q.shape
+    if D != head_dim or not hkv or Hq % hkv:
+        raise ValueError(f"q {tuple(shape)} does not match the pages {tuple(pages.k.shape)}")
+    S, cols = _sequences(T, page_table, lengths, cu_seqlens, dev)
+    _req_i32(group_seqs, "group_seqs", 1, dev)
+    _req_i32(shared_pages, "shared_pages", 1, dev)
+    n_groups = shared_pages.size(0)
+    if group_seqs.size(0) != n_groups + 1:
+        raise ValueError(f"group_seqs has {group_seqs.size(0)} offsets for {n_groups} groups")
+    if out is not None:
+        _req_packed(out, "out", dev)
+        if out.shape != shape:
+            raise ValueError(f"out {tuple(out.shape)} does not match q {tuple(shape)}")
+    if dev != _current_device():
+        with torch.cuda.device(dev):
+            return cache_attn_shared(q, pages, page_table, lengths, group_seqs, shared_pages,
+                                     cu_seqlens, softmax_scale, out, workspace)
+    if out is None:
+        out = torch.empty_like(q)
+    L = lib()
+    if workspace is None:
+        nb = L.ei_cache_attn_shared_workspace_bytes(Hq, T, S, n_groups, cols, cs)
+        if nb:
+            workspace = torch.empty((nb,), dtype=torch.uint8, device=q.device)
+    else:
+        _same_device(q, workspace)
+        if not workspace.is_contiguous():
+            raise ValueError("workspace must be contiguous")
+        nb = workspace.numel() * workspace.element_size()
+    sc = 1.0 / math.sqrt(D) if softmax_scale is None else float(softmax_scale)
+    st = L.ei_cache_attn_shared(q.data_ptr(), Hq, T, _ptr(cu_seqlens), S, lengths.data_ptr(),
+                                page_table.data_ptr(), cols, group_seqs.data_ptr(),
+                                shared_pages.data_ptr(), n_groups, cs, ptrs, sc, out.data_ptr(),
+                                _ptr(workspace), nb, _raw_stream(dev))
+    if st:
+        _check("ei_cache_attn_shared", st)
+    return out
+
+
+def cache_attn_shared_workspace_bytes(n_q_heads: int, n_tokens: int, n_seqs: int, n_groups: int,
+                                      max_pages: int, pages: CachePages) -> int:
+    """Bytes of the workspace that cache_attn_shared takes for such a call."""
+    shape = _cache_shape(*pages.k.shape[-4:], CACHE_FORMATS[pages.k.dtype])
+    return int(lib().ei_cache_attn_shared_workspace_bytes(n_q_heads, n_tokens, n_seqs, n_groups,
+                                                          max_pages, shape))
 
 
 def cache_copy(pages: CachePages, src, dst) -> None:

@@ -17,7 +17,7 @@ LIB = os.path.join(HERE, "libentropyinfer.so")
 ROOT = os.path.dirname(HERE)
 
 SOURCES = ["ei_api.hip", "ei_probe.hip", "ei_select.hip", "ei_attn.hip", "ei_noalloc.hip",
-           "ei_decoder.hip", "ei_cache.hip", "ei_adapter.hip", "ei_sample.hip"]
+           "ei_decoder.hip", "ei_cache.hip", "ei_shared.hip", "ei_adapter.hip", "ei_sample.hip"]
 ARCH = os.environ.get("EI_OFFLOAD_ARCH", "gfx950")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 

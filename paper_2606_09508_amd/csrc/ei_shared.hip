@@ -1,0 +1,775 @@
+// Attention over the paged cache for sequences that share their first pages.
+//
+// A group's sequences name the same pages in their first `shared` columns.  The
+// keys there are read once for all new tokens of the group, the keys behind them
+// for each sequence by itself, and the sums are joined.
+//
+//  shared_plan_kernel   how many pages a group shares in earnest (none that a new
+//                       token of it lies in or before), and where the work of
+//                       groups and sequences starts
+//  shared_wide_kernel   groups' keys, where a group has many rows: tiles of 64 or
+//                       128 rows against keys in LDS
+//  shared_steps_kernel  sequences' keys (and groups', where they have few rows):
+//                       16 or 32 rows against keys in registers, as cache attention
+//  shared_join_kernel   a row's parts joined
+//
+// Work is counted in units, the items (rows of a group or sequence and a KV head)
+// one behind the other, and dealt out in runs of equal length.  A worker leaves a
+// part of every item that its run touches at slot (item + worker): both only grow
+// along the units, so no two parts meet, and items + workers slots suffice.
+#include "ei_attend.h"
+
+namespace ei {
+namespace {
+
+constexpr int kPlanThreads = 1024;
+constexpr int kWideThreads = 512;
+constexpr int kWideWaves = kWideThreads / kWave;
+constexpr int kWideKeys = 128;        // of a step
+constexpr int kWideWorkers = 256;     // one a CU
+constexpr int kWideCost = 1;          // units of an item before its steps
+constexpr int kWideLeast = 2;         // units of a run, at least
+constexpr int kStepsGroups = 512;     // workgroups, two a CU
+constexpr int kStepsCost = 5;
+constexpr int kStepsLeast = 8;
+
+typedef _Float16 half8 __attribute__((ext_vector_type(8)));
+typedef _Float16 half2 __attribute__((ext_vector_type(2)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+
+struct Totals {
+  int64_t wide_per, steps_per;       // units of a run
+  int64_t group_units, seq_units;
+  int32_t bad, pad[7];               // lists that count more items than there is room for
+};
+struct GroupInfo {      // its shared keys; n = 0 where there are none
+  int first, n, pages, lead;
+  int64_t unit;
+  int item, pad;
+};
+struct SeqInfo {        // its own keys
+  int group, key0, item, pad;
+  int64_t unit;
+  int first, n;
+};
+
+struct SharedArgs {
+  AttendArgs a;             // (part_ml and part_o: the parts of shared_steps_kernel)
+  const int32_t *group_seqs, *shared_pages;
+  int n_groups;
+  int wide_rows;            // of a tile, 0: groups' keys go to shared_steps_kernel
+  int steps_rows;
+  int steps_workers;
+  int64_t wide_items, steps_items;   // slots there are, less the workers
+  Totals* totals;
+  GroupInfo* groups;
+  SeqInfo* seqs;
+  Part* wide_ml;
+  float* wide_o;
+};
+
+__device__ __forceinline__ int64_t block_before(int64_t* sums, int64_t v, int64_t& total) {
+  // the sum over the threads before this one, and over all
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  int64_t up = v;
+#pragma unroll
+  for (int o = 1; o < kWave; o <<= 1) {
+    const int64_t t = __shfl_up(up, o);
+    if (lane >= o) up += t;
+  }
+  __syncthreads();
+  if (lane == kWave - 1) sums[wave] = up;
+  __syncthreads();
+  int64_t before = up - v;
+  total = 0;
+  for (int w = 0; w < kPlanThreads / kWave; ++w) {
+    if (w < wave) before += sums[w];
+    total += sums[w];
+  }
+  return before;
+}
+
+__global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(SharedArgs x) {
+  __shared__ int64_t sums[kPlanThreads / kWave];
+  const AttendArgs& a = x.a;
+  const int S = a.tk.S, P = a.pg.P, G = a.Hq / a.pg.Hkv;
+  const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
+  for (int s = tid; s < S; s += kPlanThreads) {
+    SeqInfo q{};
+    q.group = -1;
+    seq_rows(a.tk, s, q.first, q.n);
+    x.seqs[s] = q;
+  }
+  __syncthreads();
+  for (int g = wave; g < x.n_groups; g += kPlanThreads / kWave) {
+    const int b = min(max(x.group_seqs[g], 0), S), e = min(max(x.group_seqs[g + 1], 0), S);
+    int pages = min(max(x.shared_pages[g], 0), a.pg.max_pages);
+    GroupInfo q{};
+    if (b < e) {
+      for (int s = b + lane; s < e; s += kWave) {
+        int first, n;
+        seq_rows(a.tk, s, first, n);
+        if (n > 0) pages = min(pages, max(a.lengths[s] - n, 0) / P);
+      }
+      pages = (int)wave_min_u32_f((uint32_t)pages);
+      int n0, end, n1;
+      seq_rows(a.tk, b, q.first, n0);
+      seq_rows(a.tk, e - 1, end, n1);
+      q.n = pages > 0 ? max(end + n1 - q.first, 0) : 0;
+      q.pages = pages;
+      q.lead = b;
+      if (q.n > 0)
+        for (int s = b + lane; s < e; s += kWave) {
+          x.seqs[s].group = g;
+          x.seqs[s].key0 = pages * P;
+        }
+    }
+    if (lane == 0) x.groups[g] = q;
+  }
+  __syncthreads();
+  const int tile = x.wide_rows ? x.wide_rows : x.steps_rows;
+  int64_t units = 0, items = 0;
+  for (int g0 = 0; g0 < x.n_groups; g0 += kPlanThreads) {
+    const int g = g0 + tid;
+    int64_t u = 0, it = 0, all_u, all_it;
+    if (g < x.n_groups && x.groups[g].n > 0) {
+      const int64_t keys = (int64_t)x.groups[g].pages * P;
+      it = ((int64_t)x.groups[g].n * G + tile - 1) / tile * a.pg.Hkv;
+      u = it * (x.wide_rows ? (keys + kWideKeys - 1) / kWideKeys + kWideCost
+                            : keys / kKeys + kStepsCost);
+    }
+    const int64_t bu = block_before(sums, u, all_u), bi = block_before(sums, it, all_it);
+    if (g < x.n_groups) {
+      x.groups[g].unit = units + bu;
+      x.groups[g].item = (int)(items + bi);
+    }
+    units += all_u;
+    items += all_it;
+  }
+  Totals t{};
+  t.group_units = units;
+  if (x.wide_rows) {
+    t.bad = items > x.wide_items;
+    units = items = 0;
+  }
+  for (int s0 = 0; s0 < S; s0 += kPlanThreads) {
+    const int s = s0 + tid;
+    int64_t u = 0, it = 0, all_u, all_it;
+    if (s < S) {
+      const int64_t keys = min((int64_t)max(a.lengths[s], 0), (int64_t)a.pg.max_pages * P);
+      it = ((int64_t)x.seqs[s].n * G + x.steps_rows - 1) / x.steps_rows * a.pg.Hkv;
+      u = it * ((max(keys - x.seqs[s].key0, (int64_t)0) + kKeys - 1) / kKeys + kStepsCost);
+    }
+    const int64_t bu = block_before(sums, u, all_u), bi = block_before(sums, it, all_it);
+    if (s < S) {
+      x.seqs[s].unit = units + bu;
+      x.seqs[s].item = (int)(items + bi);
+    }
+    units += all_u;
+    items += all_it;
+  }
+  if (tid == 0) {
+    t.seq_units = units;     // (with the groups' where shared_steps_kernel has those too)
+    // (Offsets that do not ascend may name tokens or sequences twice.)
+    t.bad |= items > x.steps_items;
+    if (t.bad) t.group_units = t.seq_units = units = 0;
+    const int64_t w = (t.group_units + kWideWorkers - 1) / kWideWorkers;
+    const int64_t n = (units + x.steps_workers - 1) / x.steps_workers;
+    t.wide_per = w > kWideLeast ? w : kWideLeast;
+    t.steps_per = n > kStepsLeast ? n : kStepsLeast;
+    *x.totals = t;
+  }
+}
+
+// The last of n elements of a list whose unit is at most u.
+template <class Info>
+__device__ __forceinline__ int at_unit(const Info* list, int n, int64_t u) {
+  int lo = 0, hi = n - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) / 2;
+    if (entry(&list->unit, (int64_t)mid * (sizeof(Info) / 8)) <= u) lo = mid; else hi = mid - 1;
+  }
+  return lo;
+}
+template <class Info>
+__device__ __forceinline__ Info info_at(const Info* list, int i) {
+  static_assert(sizeof(Info) == 32, "read as four words of 64 bits");
+  uint64_t w[4];
+#pragma unroll
+  for (int k = 0; k < 4; ++k) w[k] = entry((const uint64_t*)list, (int64_t)i * 4 + k);
+  return __builtin_bit_cast(Info, w);
+}
+
+// ----------------------------------------------------------------------------
+// Wide tiles.  8 waves: RW of them have 32 rows each, KW = 8 / RW share the 128
+// keys of a step.  K lies in LDS as bf16 [key][dim], V as fp16 [dim][key].
+//   S^T = K Q^T        MFMA 32x32x16 bf16 (keys on M, rows on N)
+//   O^T += V^T P^T     MFMA 32x32x16 f16 (dims on M)
+// Operand layouts (lane l, j = l % 32, h = l / 32): A[i][k]: i = j, k = 8h .. 8h+7;
+// B[k][n]: n = j, the same k; D[i][n]: n = j, i = 8 (r / 4) + 4h + r % 4, r < 16.  A
+// lane's scores of 16 keys are thus its B operand of the second product where V's
+// operand takes the keys 4h .. 4h+3 and 8+4h .. 8+4h+3 of them.
+//
+// Both formats' codes are exact in bf16 and in fp16.  The probabilities enter the
+// second product as one fp16 number each (11 bits, against 8 of bf16; rounding them
+// costs a tenth of what the output's rounding to bf16 does): e = 2^(x - M) with x the
+// score (base 2) plus the exponent of V's scale, and M a running maximum of x, less
+// 8, that may trail by 6 more: e is at most 2^14, and what fp16 loses lies 2^-32
+// below the row's largest.  l sums e / 2^exponent, so it and O are relative to the
+// same M.  A scale's significand, 1 from cache_store, is multiplied in where it is
+// not.
+// ----------------------------------------------------------------------------
+constexpr float kWideLimit = 0x1p14f;
+constexpr float kWideHead = 8.0f;
+
+template <int FMT, bool HI>
+__device__ __forceinline__ uint32_t half2_of(uint32_t x) {
+  if constexpr (FMT == EI_CACHE_E4M3) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(x, 1.0f, HI));
+  } else {
+    // 1024 + 128 + code, by the bits, less 1152
+    const uint32_t w = __builtin_amdgcn_perm(0x64646464u, x ^ 0x80808080u,
+                                             HI ? 0x04030402u : 0x04010400u);
+    const half2 d = __builtin_bit_cast(half2, w) - half2{(_Float16)1152.0f, (_Float16)1152.0f};
+    return __builtin_bit_cast(uint32_t, d);
+  }
+}
+__device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
+  const f32x2 x = {lo, hi};
+  return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, half2));
+}
+
+struct __attribute__((aligned(16))) WideSmem {
+  uint8_t k[2][kWideKeys * kHeadDim * 2];
+  uint8_t v[2][kWideKeys * kHeadDim * 2];
+};
+// Bytes of 16 (8 dims) of a key, and of 8 (4 keys) of a dim: rows of 256 bytes, the
+// pieces of neighbouring rows at other banks.
+__device__ __forceinline__ int k_at(int key, int piece) {
+  return key * (kHeadDim * 2) + ((piece ^ (key & 15)) << 4);
+}
+__device__ __forceinline__ int v_at(int dim, int piece) {
+  return dim * (kWideKeys * 2) + ((piece ^ (((dim ^ (dim >> 3)) & 15) | (dim & 16))) << 3);
+}
+
+template <int FMT, int P, int RW>
+__global__ __launch_bounds__(kWideThreads, 2) void shared_wide_kernel(SharedArgs x) {
+  constexpr int KW = kWideWaves / RW, KT = kWideKeys / KW / 32;   // key tiles of a wave
+  constexpr int kRowsOf = 32 * RW;
+  __shared__ WideSmem sm;
+  const AttendArgs& a = x.a;
+  const int G = a.Hq / a.pg.Hkv, lane = threadIdx.x % kWave, j = lane & 31, h = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int rw = wave % RW, kw = wave / RW;
+  const int64_t per = entry(&x.totals->wide_per, 0), total = entry(&x.totals->group_units, 0);
+  const int worker = (int)blockIdx.x;
+  int64_t u = worker * per;
+  const int64_t u1 = min(u + per, total);
+  if (u >= u1) return;
+  int g = at_unit(x.groups, x.n_groups, u);
+  for (; u < u1 && g < x.n_groups; ) {
+    const GroupInfo q = info_at(x.groups, g);
+    const int tiles = (q.n * G + kRowsOf - 1) / kRowsOf;
+    const int steps = (int)(((int64_t)q.pages * P + kWideKeys - 1) / kWideKeys);
+    const int whole = steps + kWideCost;
+    const int64_t off = u - q.unit;
+    const int item = (int)(off / whole), at = (int)(off % whole);
+    if (q.n == 0 || item >= tiles * a.pg.Hkv) {    // (a group without units, or behind this one)
+      ++g;
+      continue;
+    }
+    const int to = (int)min((int64_t)whole, at + (u1 - u));
+    u += to - at;
+    const int st0 = max(at - kWideCost, 0), st1 = max(to - kWideCost, 0);
+    const int kvh = item / tiles, row0 = item % tiles * kRowsOf, rows = q.n * G;
+    const int64_t table_row = (int64_t)q.lead * a.pg.max_pages;
+
+    bf16x8 qf[8];
+    {
+      const int row = min(row0 + 32 * rw + j, rows - 1);
+      const uint16_t* qp = a.q + ((int64_t)(kvh * G + row % G) * a.tk.T + q.first + row / G) * kHeadDim;
+#pragma unroll
+      for (int c = 0; c < 8; ++c)
+        qf[c] = __builtin_bit_cast(bf16x8, *(const uint4*)(qp + 16 * c + 8 * h));
+    }
+    float M = -INFINITY, l = 0.0f;
+    f32x16 o[4];
+#pragma unroll
+    for (int m = 0; m < 4; ++m)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) o[m][r] = 0.0f;
+
+    // the page of a step's 64 keys number `half`, -1 for none
+    auto page_of = [&](int st, int half) -> int {
+      const int key = st * kWideKeys + 64 * half;
+      if (st >= st1 || key >= q.pages * P) return -1;
+      const int p = entry(a.pg.table, table_row + key / P);
+      return (unsigned)p < (unsigned)a.pg.n_pages ? p : -1;
+    };
+    uint4 kr[2];
+    uint2 vr[4];
+    auto load = [&](int st, int p0, int p1) {
+      const int t = threadIdx.x;
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int page = half ? p1 : p0, key = 64 * half + t / 8;
+        kr[half] = make_uint4(0u, 0u, 0u, 0u);
+        if (page >= 0)
+          kr[half] = *(const uint4*)(a.pg.k + (((int64_t)page * a.pg.Hkv + kvh) * P +
+                                               (st * kWideKeys + key) % P) * kHeadDim + 16 * (t % 8));
+      }
+      const int piece = t / 16, page = piece / 16 ? p1 : p0;
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        vr[r] = make_uint2(0u, 0u);
+        if (page >= 0)
+          vr[r] = *(const uint2*)(a.pg.v + (((int64_t)page * a.pg.Hkv + kvh) * P +
+                                            (st * kWideKeys + 4 * piece + r) % P) * kHeadDim + 8 * (t % 16));
+      }
+    };
+    auto stage = [&](int buf) {
+      const int t = threadIdx.x;
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        const int key = 64 * half + t / 8;
+        *(bf16x8*)&sm.k[buf][k_at(key, 2 * (t % 8))] = widen8<FMT>(kr[half].x, kr[half].y);
+        *(bf16x8*)&sm.k[buf][k_at(key, 2 * (t % 8) + 1)] = widen8<FMT>(kr[half].z, kr[half].w);
+      }
+      const int piece = t / 16, d0 = 8 * (t % 16);
+#pragma unroll
+      for (int word = 0; word < 2; ++word) {
+        uint32_t pr[2][2];      // [keys 0-1, 2-3][dims 0-1, 2-3]: bytes of two keys side by side
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const uint32_t w0 = word ? vr[2 * c].y : vr[2 * c].x;
+          const uint32_t w1 = word ? vr[2 * c + 1].y : vr[2 * c + 1].x;
+          pr[c][0] = __builtin_amdgcn_perm(w1, w0, 0x05010400u);
+          pr[c][1] = __builtin_amdgcn_perm(w1, w0, 0x07030602u);
+        }
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int d = d0 + 4 * word + 2 * i;
+          *(uint2*)&sm.v[buf][v_at(d, piece)] =
+              make_uint2(half2_of<FMT, false>(pr[0][i]), half2_of<FMT, false>(pr[1][i]));
+          *(uint2*)&sm.v[buf][v_at(d + 1, piece)] =
+              make_uint2(half2_of<FMT, true>(pr[0][i]), half2_of<FMT, true>(pr[1][i]));
+        }
+      }
+    };
+
+    const int my_half = kw * (32 * KT) / 64;
+    auto compute = [&](int buf, int page) {
+      const int64_t sc = (int64_t)page * a.pg.Hkv + kvh;
+      const float kf = entry(a.pg.ks, sc) * a.sc_log2, vf = entry(a.pg.vs, sc);
+      // V's scale as significand * 2^exponent (zeros, infinities and NaN: 2^0)
+      const uint32_t vb = __float_as_uint(vf), ve = vb >> 23 & 0xffu;
+      const bool normal = ve != 0 && ve != 0xffu;
+      const float E = normal ? (float)((int)ve - 127) : 0.0f;
+      const float sig = normal ? __uint_as_float((vb & 0x807fffffu) | 0x3f800000u) : vf;
+      const float unit = normal ? __uint_as_float((ve == 254u ? 1u : 254u - ve) << 23) : 1.0f;
+      f32x16 s[KT];
+#pragma unroll
+      for (int t = 0; t < KT; ++t) {
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[t][r] = 0.0f;
+        const int key = 32 * (KT * kw + t) + j;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+          const bf16x8 kk = *(const bf16x8*)&sm.k[buf][k_at(key, 2 * c + h)];
+          s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kk, qf[c], s[t], 0, 0, 0);
+        }
+      }
+      float e[KT][16], sum;
+      auto probs = [&](float c) {
+        sum = 0.0f;
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) {
+            e[t][r] = __builtin_amdgcn_exp2f(fmaf(s[t][r], kf, c));
+            sum += e[t][r];
+          }
+      };
+      probs(E - M);
+      if (__builtin_amdgcn_ballot_w64(!(sum <= kWideLimit)) != 0) {
+        float mx = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[t][r] * kf);
+        mx = fmaxf(mx, __shfl_xor(mx, 32)) + E - kWideHead;
+        const float m_new = fmaxf(M, mx);
+        const float alpha = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(M - m_new);
+        l *= alpha;
+#pragma unroll
+        for (int m = 0; m < 4; ++m) o[m] *= alpha;
+        M = m_new;
+        probs(M == -INFINITY ? 0.0f : E - M);
+      }
+      l += sum * unit;
+      if (sig != 1.0f) {
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) e[t][r] *= sig;
+      }
+#pragma unroll
+      for (int t = 0; t < KT; ++t)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          const half8 p = __builtin_bit_cast(
+              half8, make_uint4(pack_half2(e[t][8 * c], e[t][8 * c + 1]),
+                                pack_half2(e[t][8 * c + 2], e[t][8 * c + 3]),
+                                pack_half2(e[t][8 * c + 4], e[t][8 * c + 5]),
+                                pack_half2(e[t][8 * c + 6], e[t][8 * c + 7])));
+          const int piece = 8 * (KT * kw + t) + 4 * c + h;
+#pragma unroll
+          for (int m = 0; m < 4; ++m) {
+            const uint2 lo = *(const uint2*)&sm.v[buf][v_at(32 * m + j, piece)];
+            const uint2 hi = *(const uint2*)&sm.v[buf][v_at(32 * m + j, piece + 2)];
+            o[m] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+                __builtin_bit_cast(half8, make_uint4(lo.x, lo.y, hi.x, hi.y)), p, o[m], 0, 0, 0);
+          }
+        }
+    };
+
+    int p0 = page_of(st0, 0), p1 = page_of(st0, 1), buf = 0;
+    load(st0, p0, p1);
+    for (int st = st0; st < st1; ++st, buf ^= 1) {
+      stage(buf);
+      const int mine = my_half ? p1 : p0;
+      p0 = page_of(st + 1, 0);
+      p1 = page_of(st + 1, 1);
+      load(st + 1, p0, p1);
+      // (the buffer before was read before the last barrier but one: two suffice)
+      __syncthreads();
+      if (mine >= 0) compute(buf, mine);
+    }
+    l += __shfl_xor(l, 32);
+    // the sums of the waves with the same rows, by halves
+    float* const ex = (float*)&sm;
+#pragma unroll
+    for (int half = KW / 2; half > 0; half >>= 1) {
+      __syncthreads();
+      float* const to_wave = ex + ((kw - half) * RW + rw) * (66 * kWave) + lane;
+      if (kw >= half && kw < 2 * half) {
+        to_wave[0] = M;
+        to_wave[kWave] = l;
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) to_wave[(2 + 16 * m + r) * kWave] = o[m][r];
+      }
+      __syncthreads();
+      if (kw < half) {
+        const float* from = ex + (kw * RW + rw) * (66 * kWave) + lane;
+        const float m2 = from[0], l2 = from[kWave], mm = fmaxf(M, m2);
+        const float f = M == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(M - mm);
+        const float f2 = m2 == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m2 - mm);
+        M = mm;
+        l = l * f + l2 * f2;
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+#pragma unroll
+          for (int r = 0; r < 16; ++r) o[m][r] = o[m][r] * f + from[(2 + 16 * m + r) * kWave] * f2;
+      }
+    }
+    __syncthreads();
+    const int row = 32 * rw + j;
+    if (kw == 0 && row0 + row < rows) {
+      const int64_t pr = ((int64_t)q.item + item + worker) * kRowsOf + row;
+      if (h == 0) x.wide_ml[pr] = Part{M, l};
+      float* to_row = x.wide_o + pr * kHeadDim + 4 * h;
+#pragma unroll
+      for (int m = 0; m < 4; ++m)
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+          *(float4*)(to_row + 32 * m + 8 * r) =
+              make_float4(o[m][4 * r], o[m][4 * r + 1], o[m][4 * r + 2], o[m][4 * r + 3]);
+    }
+  }
+}
+
+// ----------------------------------------------------------------------------
+// Steps of 32 keys in registers: a wave takes a run of the sequences' own keys,
+// behind the groups' where those have few rows.
+// ----------------------------------------------------------------------------
+template <int FMT, int P, int RT>
+__global__ __launch_bounds__(kThreads, attend_occupancy(RT)) void shared_steps_kernel(SharedArgs x) {
+  const AttendArgs& a = x.a;
+  const int G = a.Hq / a.pg.Hkv, lane = threadIdx.x % kWave, j = lane & 15, g4 = lane >> 4;
+  const int worker = (int)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  const int64_t per = entry(&x.totals->steps_per, 0), total = entry(&x.totals->seq_units, 0);
+  const int64_t groups = x.wide_rows ? 0 : entry(&x.totals->group_units, 0);
+  int64_t u = worker * per;
+  const int64_t u1 = min(u + per, total);
+  if (u >= u1) return;
+  int g = u < groups ? at_unit(x.groups, x.n_groups, u) : x.n_groups;
+  int s = u < groups ? 0 : at_unit(x.seqs, a.tk.S, u);
+  while (u < u1 && s < a.tk.S) {
+    const bool is_group = u < groups;
+    int first, n, lead, seq_len, key0, key1, item0;
+    int64_t start;
+    if (is_group) {
+      const GroupInfo q = info_at(x.groups, g);
+      first = q.first; n = q.n; lead = q.lead; key0 = 0; key1 = q.pages * P;
+      item0 = q.item; start = q.unit;
+      seq_len = INT_MAX / 2;      // (every row sees all of them)
+    } else {
+      const SeqInfo q = info_at(x.seqs, s);
+      first = q.first; n = q.n; lead = s; key0 = q.key0; seq_len = entry(a.lengths, s);
+      key1 = keys_of<P>(a, s);
+      item0 = q.item; start = q.unit;
+    }
+    const int tiles = (n * G + kRows * RT - 1) / (kRows * RT);
+    const int steps = (max(key1 - key0, 0) + kKeys - 1) / kKeys, whole = steps + kStepsCost;
+    const int64_t off = u - start;
+    const int item = (int)(off / whole), at = (int)(off % whole);
+    if (n == 0 || item >= tiles * a.pg.Hkv) {
+      if (is_group) ++g; else ++s;
+      if (is_group && g >= x.n_groups) break;      // (the units of groups end with the last one)
+      continue;
+    }
+    const int to = (int)min((int64_t)whole, at + (u1 - u));
+    u += to - at;
+    const int st0 = max(at - kStepsCost, 0), st1 = max(to - kStepsCost, 0);
+    const int kvh = item / tiles, row0 = item % tiles * kRows * RT;
+    WaveSums<RT> ws;
+    attend_steps<FMT, P, RT>(a, lead, kvh, row0, first, n, seq_len, key0 + kKeys * st0,
+                             min(key0 + kKeys * st1, max(key1, key0)), 0, 1, ws);
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      const int row = kRows * rt + j;
+      if (row0 + row >= n * G) continue;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = ws.o[rt][i][q];
+        store_part<RT>(a, item0 + item + worker, row, 8 * (4 * g4 + q), ws.m[rt], ws.l[rt], v);
+      }
+    }
+  }
+}
+
+// ----------------------------------------------------------------------------
+// A row's parts: 32 lanes, four dims each.  A workgroup has 8 heads of a token.
+// ----------------------------------------------------------------------------
+constexpr int kJoinRows = kThreads / 32;
+
+struct RowParts {       // parts `first` .. `first` + n - 1 of a row, `pitch` rows apart
+  const Part* ml;
+  const float* o;
+  int64_t first;
+  int pitch, n;
+};
+
+__global__ __launch_bounds__(kThreads) void shared_join_kernel(SharedArgs x, int64_t unit0) {
+  const AttendArgs& a = x.a;
+  const int G = a.Hq / a.pg.Hkv, blocks = (a.Hq + kJoinRows - 1) / kJoinRows;
+  const int64_t unit = unit0 + blockIdx.x;
+  const int t = (int)(unit / blocks), head = (int)(unit % blocks) * kJoinRows + threadIdx.x / 32;
+  int s = 0;
+  if (!a.tk.cu) {
+    s = t / a.tk.each;
+  } else {
+    int hi = a.tk.S - 1;
+    while (s < hi) {
+      const int mid = (s + hi + 1) / 2;
+      if (entry(a.tk.cu, mid) <= t) s = mid; else hi = mid - 1;
+    }
+  }
+  const SeqInfo q = info_at(x.seqs, s);
+  if (t < q.first || t >= q.first + q.n || entry(&x.totals->bad, 0)) return;
+  if (head >= a.Hq) return;
+  const int kvh = head / G, d = threadIdx.x % 32 * 4;
+  // the parts of an item whose units are [begin, begin + whole): its workers' slots
+  auto parts_of = [&](const Part* ml, const float* o, int tile_rows, int64_t unit, int item, int n,
+                      int row, int whole, int64_t per) {
+    const int tiles = (n * G + tile_rows - 1) / tile_rows, at = kvh * tiles + row / tile_rows;
+    const int64_t begin = unit + (int64_t)at * whole;
+    const int64_t w0 = begin / per, w1 = (begin + whole - 1) / per;
+    return RowParts{ml, o, (item + at + w0) * tile_rows + row % tile_rows, tile_rows,
+                    (int)(w1 - w0) + 1};
+  };
+  const int64_t keys = min((int64_t)max(entry(a.lengths, s), 0), (int64_t)a.pg.max_pages * a.pg.P);
+  const int own_steps = (int)((max(keys - q.key0, (int64_t)0) + kKeys - 1) / kKeys);
+  const int64_t steps_per = entry(&x.totals->steps_per, 0);
+  const RowParts own = parts_of(a.part_ml, a.part_o, x.steps_rows, q.unit, q.item, q.n,
+                                (t - q.first) * G + head % G, own_steps + kStepsCost, steps_per);
+  RowParts common{};
+  if (q.group >= 0) {
+    const GroupInfo g = info_at(x.groups, q.group);
+    const int row = (t - g.first) * G + head % G;
+    const int64_t gkeys = (int64_t)g.pages * a.pg.P;
+    if (t >= g.first && t < g.first + g.n)
+      common = x.wide_rows
+          ? parts_of(x.wide_ml, x.wide_o, x.wide_rows, g.unit, g.item, g.n, row,
+                     (int)((gkeys + kWideKeys - 1) / kWideKeys) + kWideCost,
+                     entry(&x.totals->wide_per, 0))
+          : parts_of(a.part_ml, a.part_o, x.steps_rows, g.unit, g.item, g.n, row,
+                     (int)(gkeys / kKeys) + kStepsCost, steps_per);
+  }
+  float m = -INFINITY, l = 0.0f;
+  float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+  constexpr int kAhead = 4;
+  const int all = common.n + own.n;
+  for (int p0 = 0; p0 < all; p0 += kAhead) {
+    Part ml[kAhead];
+    float4 v[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      const int p = min(p0 + k, all - 1);
+      const RowParts& r = p < common.n ? common : own;
+      const int64_t at = r.first + (int64_t)(p < common.n ? p : p - common.n) * r.pitch;
+      ml[k] = r.ml[at];
+      v[k] = *(const float4*)(r.o + at * kHeadDim + d);
+    }
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k) {
+      if (p0 + k >= all) break;
+      const float mn = fmaxf(m, ml[k].m);
+      const float f = m == mn ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
+      const float g = ml[k].m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml[k].m - mn);
+      l = l * f + ml[k].l * g;
+      acc.x = acc.x * f + v[k].x * g;
+      acc.y = acc.y * f + v[k].y * g;
+      acc.z = acc.z * f + v[k].z * g;
+      acc.w = acc.w * f + v[k].w * g;
+      m = mn;
+    }
+  }
+  const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+  *(uint2*)(a.o + ((int64_t)head * a.tk.T + t) * kHeadDim + d) =
+      make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
+}
+
+// ----------------------------------------------------------------------------
+// Host side
+// ----------------------------------------------------------------------------
+struct SharedPlan {
+  int wide_rows, rt, groups;       // workgroups of shared_steps_kernel
+  int64_t items, wide_items;
+  bool fits;
+  size_t at_groups, at_seqs, at_wide_ml, at_wide_o, at_ml, at_o, bytes;
+};
+SharedPlan shared_plan(int Hq, int n_tokens, int n_seqs, int n_groups, int max_pages,
+                       const ei_cache_shape& c) {
+  SharedPlan p{};
+  const int64_t G = Hq / c.n_kv_heads, rows = n_tokens * G;
+  // rows of a group and a KV head on average: tiles in LDS from 33 on
+  const int64_t of_group = n_groups ? rows / n_groups : 0;
+  p.wide_rows = of_group > 64 ? 128 : of_group > 32 ? 64 : 0;
+  p.rt = rows > (int64_t)kRows * n_seqs ||
+                 (!p.wide_rows && n_groups && rows > (int64_t)kRows * n_groups) ? 2 : 1;
+  const int64_t tile = kRows * p.rt, most_keys = (int64_t)max_pages * c.page_len;
+  int64_t items = (rows / tile + n_seqs) * c.n_kv_heads;
+  const int64_t cost = most_keys / kKeys + 1 + kStepsCost;
+  int64_t wide_items = 0;
+  if (p.wide_rows) wide_items = (rows / p.wide_rows + n_groups) * c.n_kv_heads;
+  else items += (rows / tile + n_groups) * c.n_kv_heads;
+  p.items = items;
+  p.wide_items = wide_items;
+  p.fits = items <= INT_MAX / 2 && wide_items <= INT_MAX / 2 && rows <= INT_MAX / 2;
+  if (!p.fits) return p;
+  const int64_t waves = items > INT64_MAX / cost ? INT64_MAX : (items * cost + kStepsLeast - 1) / kStepsLeast;
+  p.groups = (int)(waves / kWaves + 1 < kStepsGroups ? waves / kWaves + 1 : kStepsGroups);
+  auto up = [](size_t n) { return (n + 255) / 256 * 256; };
+  const size_t slots = ((size_t)items + (size_t)p.groups * kWaves) * tile;
+  const size_t wide = p.wide_rows ? ((size_t)wide_items + kWideWorkers) * p.wide_rows : 0;
+  p.at_groups = up(sizeof(Totals));
+  p.at_seqs = p.at_groups + up(n_groups * sizeof(GroupInfo));
+  p.at_wide_ml = p.at_seqs + up(n_seqs * sizeof(SeqInfo));
+  p.at_wide_o = p.at_wide_ml + up(wide * sizeof(Part));
+  p.at_ml = p.at_wide_o + wide * kHeadDim * sizeof(float);
+  p.at_o = p.at_ml + up(slots * sizeof(Part));
+  p.bytes = p.at_o + slots * kHeadDim * sizeof(float);
+  return p;
+}
+
+template <int FMT, int P>
+void launch_shared(const SharedPlan& pl, const SharedArgs& x, hipStream_t stream) {
+  hipLaunchKernelGGL(shared_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, x);
+  if (pl.wide_rows == 128)
+    hipLaunchKernelGGL((shared_wide_kernel<FMT, P, 4>), dim3(kWideWorkers), dim3(kWideThreads), 0,
+                       stream, x);
+  else if (pl.wide_rows == 64)
+    hipLaunchKernelGGL((shared_wide_kernel<FMT, P, 2>), dim3(kWideWorkers), dim3(kWideThreads), 0,
+                       stream, x);
+  if (pl.rt == 1)
+    hipLaunchKernelGGL((shared_steps_kernel<FMT, P, 1>), dim3((unsigned)pl.groups), dim3(kThreads),
+                       0, stream, x);
+  else
+    hipLaunchKernelGGL((shared_steps_kernel<FMT, P, 2>), dim3((unsigned)pl.groups), dim3(kThreads),
+                       0, stream, x);
+  const int64_t units = (int64_t)x.a.tk.T * ((x.a.Hq + kJoinRows - 1) / kJoinRows);
+  for (int64_t u = 0; u < units; u += kMaxGrid)
+    hipLaunchKernelGGL(shared_join_kernel, dim3(launch_grid(units - u)), dim3(kThreads), 0, stream,
+                       x, u);
+}
+
+}  // namespace
+}  // namespace ei
+
+extern "C" {
+
+size_t ei_cache_attn_shared_workspace_bytes(int32_t n_q_heads, int32_t n_tokens, int32_t n_seqs,
+                                            int32_t n_groups, int32_t max_pages,
+                                            ei_cache_shape shape) {
+  if (ei::check_shape(shape) != EI_OK || n_q_heads <= 0 || n_q_heads % shape.n_kv_heads ||
+      n_tokens <= 0 || n_seqs <= 0 || n_groups < 0 || max_pages < 0)
+    return 0;
+  if ((int64_t)n_tokens * n_q_heads > INT_MAX || (int64_t)max_pages * shape.page_len > INT_MAX)
+    return 0;
+  return ei::shared_plan(n_q_heads, n_tokens, n_seqs, n_groups, max_pages, shape).bytes;
+}
+
+ei_status ei_cache_attn_shared(const uint16_t* q, int32_t n_q_heads, int32_t n_tokens,
+                               const int32_t* cu_seqlens, int32_t n_seqs, const int32_t* lengths,
+                               const int32_t* page_table, int32_t max_pages,
+                               const int32_t* group_seqs, const int32_t* shared_pages,
+                               int32_t n_groups, ei_cache_shape shape, ei_cache_pages pages,
+                               float softmax_scale, uint16_t* o, void* workspace,
+                               size_t workspace_bytes, void* stream) {
+  ei_status st = ei::check_shape(shape);
+  if (st != EI_OK && st != EI_ERR_UNSUPPORTED) return st;
+  if (n_q_heads <= 0 || n_q_heads % shape.n_kv_heads || n_groups < 0) return EI_ERR_SHAPE;
+  if (!(softmax_scale > 0.0f && softmax_scale <= 3.402823466e38f)) return EI_ERR_SHAPE;
+  if (st != EI_OK) return st;
+  if ((st = ei::check_tokens(n_tokens, cu_seqlens, n_seqs, max_pages)) != EI_OK) return st;
+  if ((int64_t)n_tokens * n_q_heads > INT_MAX || (int64_t)max_pages * shape.page_len > INT_MAX)
+    return EI_ERR_SHAPE;
+  if (n_tokens == 0 || n_seqs == 0) return EI_OK;
+  const ei::SharedPlan pl = ei::shared_plan(n_q_heads, n_tokens, n_seqs, n_groups, max_pages, shape);
+  if (!pl.fits) return EI_ERR_SHAPE;
+  if (!q || !o || !lengths || (!page_table && max_pages > 0)) return EI_ERR_NULL;
+  if (n_groups > 0 && (!group_seqs || !shared_pages)) return EI_ERR_NULL;
+  if ((st = ei::check_pages(shape, pages)) != EI_OK) return st;
+  if (!ei::aligned(q, 16) || !ei::aligned(o, 16) || !ei::aligned(lengths, 4) ||
+      !ei::aligned(page_table, 4) || !ei::aligned(cu_seqlens, 4) || !ei::aligned(group_seqs, 4) ||
+      !ei::aligned(shared_pages, 4))
+    return EI_ERR_UNSUPPORTED;
+  if (!workspace || workspace_bytes < pl.bytes) return EI_ERR_WORKSPACE;
+  if (!ei::aligned(workspace, 16)) return EI_ERR_UNSUPPORTED;
+  char* ws = (char*)workspace;
+  const ei::Tokens tk{cu_seqlens, n_tokens, n_seqs, n_tokens / n_seqs};
+  const ei::Pages pg = ei::pages_of(shape, pages, page_table, max_pages);
+  const ei::AttendArgs a{q, o, tk, lengths, pg, n_q_heads,
+                         (float)((double)softmax_scale * 1.4426950408889634),
+                         (ei::Part*)(ws + pl.at_ml), (float*)(ws + pl.at_o), nullptr};
+  const ei::SharedArgs x{a, group_seqs, shared_pages, n_groups, pl.wide_rows, ei::kRows * pl.rt,
+                         pl.groups * ei::kWaves, pl.wide_items, pl.items, (ei::Totals*)ws,
+                         (ei::GroupInfo*)(ws + pl.at_groups), (ei::SeqInfo*)(ws + pl.at_seqs),
+                         (ei::Part*)(ws + pl.at_wide_ml), (float*)(ws + pl.at_wide_o)};
+  hipStream_t s0 = (hipStream_t)stream;
+  if (shape.format == EI_CACHE_E4M3) {
+    if (shape.page_len == 64) ei::launch_shared<EI_CACHE_E4M3, 64>(pl, x, s0);
+    else ei::launch_shared<EI_CACHE_E4M3, 128>(pl, x, s0);
+  } else {
+    if (shape.page_len == 64) ei::launch_shared<EI_CACHE_INT8, 64>(pl, x, s0);
+    else ei::launch_shared<EI_CACHE_INT8, 128>(pl, x, s0);
+  }
+  return ei::from_hip(hipGetLastError());
+}
+
+}  // extern "C"

@@ -633,7 +633,7 @@ size_t ei_sample_workspace_bytes(int32_t rows, int32_t vocab, int32_t format);
  *   top_k   the first k;
  *   top_p   of them the shortest run from the first on whose weight is at least p
  *           times theirs (one token at least);
- *   min_p   of them those with w_i >= min_p (before the rounding).
+ *   min_p   of them those with w_i >= min_p (rounded down to such a multiple).
  * The token is the first kept one, by index, at which the kept weights summed up
  * to it exceed u times their total.
  *

@@ -16,6 +16,10 @@ def _gen(seed):
     return torch.Generator().manual_seed(seed)
 
 
+def _i32(x):
+    return torch.tensor(x, dtype=torch.int32)
+
+
 def reference(x, u, t=1.0, k=0, p=1.0, least=0.0):
     """(token, log of its share, distance of u * total to the next sum, of the total)."""
     x = [float(v) for v in x.double()]
@@ -122,6 +126,38 @@ def test_min_p_and_all_together(vocab, dtype):
     check(x, us(6, vocab), None, None, None, [0.0, 0.05, 0.5, 1.0, 2.0, 1e-4])
     check(x, us(6, vocab + 5), [1.0, 0.8, 1.5, 0.0, 3.0, 1.0], [50, 20, 3, 5, 1000, 0],
           [0.9, 0.5, 0.99, 0.9, 0.8, 0.7], [0.01, 0.1, 0.0, 0.2, 0.3, 0.02])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("scale", [1e-3, 0.05, 1.0, 20.0, 1e4])
+def test_flat_and_steep_rows(scale, dtype):
+    """From nearly all tokens kept to next to none, cuts anywhere."""
+    x = logits(10, 6007, 31, F32, scale, 1).to(dtype)
+    x[8:, 1500:] = torch.finfo(dtype).min
+    x[9, 50:] = -1e30
+    u = us(10, 31)
+    p = [0.9, 0.999, 0.1, 0.5, 0.9999, 0.3, 0.95, 1.0, 0.9, 0.97]
+    k = [0, 0, 5000, 1500, 0, 30, 4097, 2999, 900, 1499]
+    for t in (1.0, 0.2, 6.0):
+        check(x, u, [t] * 10, None, p)
+        check(x, u, [t] * 10, k)
+        check(x, u, [t] * 10, k, p)
+        check(x, u, [t] * 10, k, p, [1e-3] * 10)
+        check(x, u, [t] * 10, None, None, [1e-3] * 10)
+
+
+def test_signaling_nan_is_no_token():
+    x = logits(1, 500, 2, F32)
+    x[0, 7] = 1e5
+    raw = x.clone().view(torch.int32)
+    raw[0, 7], raw[0, 100] = 0x7f800001, -0x7fffff
+    y = raw.view(F32)
+    assert y[0, 7].isnan() and y[0, 100].isnan()
+    x[0, 7] = x[0, 100] = -INF
+    for t, k in ((1.0, 0), (0.0, 0), (1.0, 10)):
+        a = eb.sample_tokens(y.cuda(), torch.tensor([0.4]).cuda(), torch.tensor([t]).cuda(),
+                             _i32([k]).cuda())
+        assert a[0].tolist() == check(x, [0.4], [t], [k])
 
 
 @pytest.mark.parametrize("vocab", [3, 130, 5000])

@@ -9,11 +9,13 @@
 // in it and how many tokens of that key it has (struct Cut).
 //
 //  sample_scan_kernel   each part of a row: its largest logit
-//  sample_weigh_kernel  each part: its weights by pieces of 512 tokens or, for a
-//                       row with top-k or top-p, counts and weights by distance
-//                       from the largest (bins)
-//  sample_pick_kernel   a workgroup a row: the bin that the cut lies in, the cut
-//                       among that bin's tokens, the token
+//  sample_bins_kernel   each part of a row with top-k or top-p: counts or weights by
+//                       distance from the largest logit
+//  sample_cut_kernel    a workgroup for each of those rows: the bin that the cut
+//                       lies in, the cut among that bin's tokens, and the token
+//                       where few are kept
+//  sample_weigh_kernel  each part: the kept weights of each 2048 tokens
+//  sample_pick_kernel   a workgroup a row: the 2048 that u lies in, the token
 #include "../../include/entropyinfer.h"
 #include "ei_internal.h"
 
@@ -25,13 +27,17 @@ namespace {
 
 constexpr int kPartThreads = 256;
 constexpr int kPartWaves = kPartThreads / kWave;
-constexpr int kThreads = 1024;       // of sample_pick_kernel
+constexpr int kThreads = 1024;       // of sample_cut_kernel
 constexpr int kWaves = kThreads / kWave;
 constexpr int kDigitBits = 11, kDigits = 1 << kDigitBits;
 constexpr int kMaxVocab = 1 << 19;   // sums of weights: 2^19 * 2^44 = 2^63
 constexpr double kOne = 0x1p44;
 constexpr int kPiece = 8 * kWave;    // tokens a wave takes at once
-constexpr int kMaxPieces = kMaxVocab / kPiece + 1;
+constexpr int kBlockPieces = 4;      // pieces whose weights are summed together
+constexpr int kMaxBlocks = (kMaxVocab / kPiece + 1 + kBlockPieces - 1) / kBlockPieces;
+constexpr int kPickThreads = 512;
+static_assert(kMaxBlocks <= kPickThreads, "a thread for each");
+constexpr int kFew = 256;            // kept tokens that sample_cut_kernel picks from
 constexpr int kMaxParts = 64;
 constexpr int kBins = 512;           // the last one: all that lies further off
 constexpr int kList = 4096;
@@ -49,12 +55,24 @@ struct SampleArgs {
   const float *top_p, *min_p;
   int32_t* tokens;
   float* logprobs;
-  int parts, part_pieces;      // of a row; pieces of a part
-  int pieces;                  // of a row
+  int parts, part_blocks;      // of a row; blocks of a part
+  int blocks;                  // of a row
   PartInfo* part;              // [rows][parts]
-  uint64_t* piece_sums;        // [rows][pieces]
+  struct RowCut* cut;          // [rows], of those with top-k or top-p
+  uint64_t* sums;              // [rows][blocks]: kept weights above the cut's key
+  uint32_t* equal;             // [rows][blocks]: tokens of that key
   uint64_t* bin_sums;          // [rows][kBins]
   uint32_t* bin_counts;        // [rows][kBins]
+};
+
+// The tokens above `key` and the first `count` of those that have it.
+struct Cut {
+  uint32_t key;
+  uint64_t count;
+};
+struct RowCut {
+  Cut cut;
+  int done, pad[3];
 };
 
 // Logits in their order as unsigned numbers: 0 for -inf and NaN (no token there),
@@ -68,98 +86,110 @@ __device__ __forceinline__ float logit_of(uint32_t key) {
   return __uint_as_float(key & 0x80000000u ? key & 0x7fffffffu : ~key);
 }
 
-// A row in pieces of 512 tokens; lane l has 8 of them in a row, 16 bytes aligned: piece
-// q's are the tokens 512 q - skip + 8 l .. + 7, skip being how far the row's first token
-// lies behind such a boundary.
+// A row in pieces of 512 tokens; lane l has the 8 from 512 q + 8 l on of piece q.  Loads
+// are of 16 bytes, aligned to an element only.
 template <int FMT>
 struct Row {
-  const char* at;      // of token -skip
-  int skip, vocab;
+  const char* at;
+  int vocab;
   __device__ __forceinline__ Row(const SampleArgs& a, int64_t row) {
-    constexpr int kSize = FMT == EI_LOGITS_BF16 ? 2 : 4;
-    const char* p = (const char*)a.logits + row * a.stride * kSize;
-    skip = (int)((uintptr_t)p % (8 * kSize)) / kSize;
-    at = p - skip * kSize;
+    at = (const char*)a.logits + row * a.stride * (FMT == EI_LOGITS_BF16 ? 2 : 4);
     vocab = a.vocab;
   }
-  // token number of element 0
-  __device__ __forceinline__ int index(int piece, int lane) const {
-    return piece * kPiece + 8 * lane - skip;
+  __device__ __forceinline__ static int index(int piece, int lane) { return piece * kPiece + 8 * lane; }
+  __device__ __forceinline__ static uint4 load16(const void* p) {
+    uint4 w;
+    __builtin_memcpy(&w, p, 16);
+    return w;
+  }
+  // (bf16 as it is)
+  __device__ __forceinline__ uint4 load_full(int piece, int lane) const {
+    return load16((const uint16_t*)at + index(piece, lane));
   }
   // -inf where there is none
-  __device__ __forceinline__ void load(int piece, int lane, float (&x)[8]) const {
+  __device__ __forceinline__ uint4 load_raw(int piece, int lane) const {
     const int i0 = index(piece, lane);
-    const int64_t e0 = (int64_t)piece * kPiece + 8 * lane;
-    if (i0 >= 0 && i0 + 8 <= vocab) {
-      if constexpr (FMT == EI_LOGITS_BF16) {
-        const uint4 w = *(const uint4*)(at + e0 * 2);
-        const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+    const uint16_t* p = (const uint16_t*)at + i0;
+    if (i0 + 8 <= vocab) return load16(p);
+    uint64_t w[2] = {0, 0};
+#pragma unroll 1
+    for (int e = 7; e >= 0; --e) {
+      const uint64_t v = i0 + e < vocab ? p[e] : 0xff80u;
+      w[1] = w[1] << 16 | w[0] >> 48;
+      w[0] = w[0] << 16 | v;
+    }
+    return make_uint4((uint32_t)w[0], (uint32_t)(w[0] >> 32), (uint32_t)w[1], (uint32_t)(w[1] >> 32));
+  }
+  __device__ __forceinline__ void load(int piece, int lane, float (&x)[8]) const {
+    if constexpr (FMT == EI_LOGITS_BF16) {
+      const uint4 w = load_raw(piece, lane);
+      const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          x[2 * e] = bf16_lo(ww[e]);
-          x[2 * e + 1] = bf16_hi(ww[e]);
-        }
+      for (int e = 0; e < 4; ++e) {
+        x[2 * e] = bf16_lo(ww[e]);
+        x[2 * e + 1] = bf16_hi(ww[e]);
+      }
+    } else {
+      const int i0 = index(piece, lane);
+      const float* p = (const float*)at + i0;
+      if (i0 + 8 <= vocab) {
+        const uint4 u = load16(p), v = load16(p + 4);
+        const uint32_t w[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(w[e]);
       } else {
-        const float4 u = ((const float4*)(at + e0 * 4))[0], v = ((const float4*)(at + e0 * 4))[1];
-        x[0] = u.x; x[1] = u.y; x[2] = u.z; x[3] = u.w;
-        x[4] = v.x; x[5] = v.y; x[6] = v.z; x[7] = v.w;
-      }
-      return;
-    }
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      x[e] = -INFINITY;
-      if (i0 + e >= 0 && i0 + e < vocab) {
-        if constexpr (FMT == EI_LOGITS_BF16)
-          x[e] = __uint_as_float((uint32_t)((const uint16_t*)at)[e0 + e] << 16);
-        else
-          x[e] = ((const float*)at)[e0 + e];
+        for (int e = 0; e < 8; ++e) x[e] = i0 + e < vocab ? p[e] : -INFINITY;
       }
     }
+  }
+  // four pieces one behind the other
+  __device__ __forceinline__ void load_block(int block, int lane, float (&x)[kBlockPieces][8]) const {
+#pragma unroll
+    for (int q = 0; q < kBlockPieces; ++q) load(block * kBlockPieces + q, lane, x[q]);
   }
 };
 
-// 2^y for y <= 0, as a whole multiple of 2^-44: y = n + f, |f| <= 1/2, and 2^f by its
-// power series up to f^12 (the rest is below 2^-52).
-__device__ __forceinline__ uint64_t steps_of_exp2(double y) {
-  y = fmax(y, -46.0);
-  const double big = 0x1.8p52;
-  const double z = y + big;
-  const double f = y - (z - big);
-  double p = 0x1.0p0;
-  constexpr double kLn2 = 0.693147180559945309417232121458;
-  constexpr double c1 = kLn2, c2 = c1 * kLn2 / 2, c3 = c2 * kLn2 / 3, c4 = c3 * kLn2 / 4,
-                   c5 = c4 * kLn2 / 5, c6 = c5 * kLn2 / 6, c7 = c6 * kLn2 / 7, c8 = c7 * kLn2 / 8,
-                   c9 = c8 * kLn2 / 9, c10 = c9 * kLn2 / 10, c11 = c10 * kLn2 / 11,
-                   c12 = c11 * kLn2 / 12;
-  p = fma(c12, f, c11);
-  p = fma(p, f, c10);
-  p = fma(p, f, c9);
-  p = fma(p, f, c8);
-  p = fma(p, f, c7);
-  p = fma(p, f, c6);
-  p = fma(p, f, c5);
-  p = fma(p, f, c4);
-  p = fma(p, f, c3);
-  p = fma(p, f, c2);
-  p = fma(p, f, c1);
-  p = fma(p, f, 1.0);
-  // times 2^n, then rounded to steps of 2^-44 by adding 2^8 (whose last place they are)
-  const uint64_t b = __builtin_bit_cast(uint64_t, p) +
-                     ((uint64_t)(uint32_t)__builtin_bit_cast(uint64_t, z) << 52);
-  return __builtin_bit_cast(uint64_t, __builtin_bit_cast(double, b) + 0x1p8) -
-         __builtin_bit_cast(uint64_t, 0x1p8);
-}
+// 2^y for y <= 0 (more counts as 0, NaN as -inf), as a whole multiple of 2^-44: y =
+// n + f, |f| <= 1/2, and 2^f by its power series up to f^12 (the rest is below 2^-52).
+// In 64 bits, which cost a lane as many cycles as 32; the series' factors lie in scalar
+// registers (as constants the compiler moves each to a vector register first).
+struct Series {
+  double c[13];
+  __device__ __forceinline__ Series() {
+    double f = 1.0;
+#pragma unroll
+    for (int i = 1; i <= 12; ++i) {
+      f *= 0.693147180559945309417232121458 / i;
+      c[i] = f;
+      asm("" : "+s"(c[i]));
+    }
+  }
+  __device__ __forceinline__ uint64_t steps_of_exp2(double y) const {
+    y = fmin(fmax(y, -46.0), 0.0);
+    const double big = 0x1.8p52;
+    const double z = y + big;
+    const double f = y - (z - big);
+    double p = fma(c[12], f, c[11]);
+#pragma unroll
+    for (int i = 10; i >= 1; --i) p = fma(p, f, c[i]);
+    p = fma(p, f, 1.0);
+    // times 2^n, then rounded to steps of 2^-44 by adding 2^8 (whose last place they are)
+    const uint64_t b = __builtin_bit_cast(uint64_t, p) +
+                       ((uint64_t)((uint32_t)__builtin_bit_cast(uint64_t, z) << 20) << 32);
+    return __builtin_bit_cast(uint64_t, __builtin_bit_cast(double, b) + 0x1p8) -
+           __builtin_bit_cast(uint64_t, 0x1p8);
+  }
+};
 
 struct Weights {
-  float top;             // the largest logit
-  double per_t;          // log2(e) / T
+  double top;            // the largest logit; an infinite one as 10^300
+  double per_t;          // log2(e) / T; beside an infinite logit 1
   uint64_t least;        // min_p in steps: lighter ones are not kept
+  Series series;
+  // (x = -inf: y is that or NaN; x = +inf: y is that)
   __device__ __forceinline__ uint64_t of(float x) const {
-    // (top is more than -inf; beside an infinite one all others weigh nothing)
-    if (!(x > -INFINITY)) return 0;
-    if (top == INFINITY) return x == top ? (uint64_t)kOne : 0;
-    return steps_of_exp2(((double)x - (double)top) * per_t);
+    return series.steps_of_exp2(((double)x - top) * per_t);
   }
   __device__ __forceinline__ uint64_t kept(float x) const {
     const uint64_t w = of(x);
@@ -183,8 +213,8 @@ __device__ __forceinline__ Settings settings_of(const SampleArgs& a, int64_t row
   s.p = p < 1.0f ? p : 1.0f;
   s.cuts = !s.greedy && (s.k > 0 || s.p < 1.0f);
   const float m = a.min_p ? a.min_p[row] : 0.0f;
-  s.w.top = top;
-  s.w.per_t = s.greedy || t == INFINITY ? 0.0 : 1.4426950408889634 / (double)t;
+  s.w.top = top == INFINITY ? 1e300 : (double)top;
+  s.w.per_t = s.greedy || top == INFINITY ? 1.0 : 1.4426950408889634 / (double)t;
   s.w.least = m > 0.0f ? (uint64_t)(fmin((double)m, 1.0) * kOne) : 0;
   return s;
 }
@@ -225,19 +255,21 @@ __global__ __launch_bounds__(kPartThreads) void sample_scan_kernel(SampleArgs a,
       a.bin_counts[row * kBins + b] = 0;
     }
   const Row<FMT> r(a, row);
-  const int q0 = part * a.part_pieces, q1 = min(q0 + a.part_pieces, a.pieces);
+  const int b0 = part * a.part_blocks, b1 = min(b0 + a.part_blocks, a.blocks);
   float top = -INFINITY, sum = 0.0f;
   int finite = 0;
-  for (int q = q0 + wave; q < q1; q += kPartWaves) {
-    float x[8];
-    r.load(q, lane, x);
+  for (int b = b0 + wave; b < b1; b += kPartWaves) {
+    float x[kBlockPieces][8];
+    r.load_block(b, lane, x);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      top = fmaxf(top, x[e]);
-      const bool in = fabsf(x[e]) < 0x1p64f;    // (masks of a type's lowest value apart)
-      sum += in ? x[e] : 0.0f;
-      finite += in ? 1 : 0;
-    }
+    for (int q = 0; q < kBlockPieces; ++q)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        top = fmaxf(top, x[q][e]);
+        const bool in = fabsf(x[q][e]) < 0x1p64f;    // (masks of a type's lowest value apart)
+        sum += in ? x[q][e] : 0.0f;
+        finite += in ? 1 : 0;
+      }
   }
   top = wave_max_f32_dpp(top);
   sum = wave_sum_f32(sum);
@@ -278,7 +310,7 @@ struct Bins {
     top = p.top;
     const float spread = p.finite > 0 ? top - p.sum / (float)p.finite : 0.0f;
     const float range = s.k > 0 ? spread : 16.0f * 1.4426950408889634f / (float)s.w.per_t;
-    scale = (float)(kBins - 1) / range;
+    scale = top < INFINITY ? (float)(kBins - 1) / range : 0.0f;
     if (!(scale > 0.0f && scale < 0x1p100f)) scale = 0.0f;    // (all in the last one)
   }
   __device__ __forceinline__ int of(float x) const {
@@ -288,10 +320,10 @@ struct Bins {
 };
 
 // ----------------------------------------------------------------------------
-// Weigh
+// Bins
 // ----------------------------------------------------------------------------
 template <int FMT>
-__global__ __launch_bounds__(kPartThreads) void sample_weigh_kernel(SampleArgs a, int64_t unit0) {
+__global__ __launch_bounds__(kPartThreads) void sample_bins_kernel(SampleArgs a, int64_t unit0) {
   __shared__ unsigned long long sums[kBins];
   __shared__ uint32_t counts[kBins];
   const int64_t unit = unit0 + blockIdx.x;
@@ -301,73 +333,63 @@ __global__ __launch_bounds__(kPartThreads) void sample_weigh_kernel(SampleArgs a
   const PartInfo info = row_info(a, row);
   if (info.top == -INFINITY) return;
   const Settings s = settings_of(a, row, info.top);
-  if (s.greedy) return;
+  if (!s.cuts) return;
   const Row<FMT> r(a, row);
-  const int q0 = part * a.part_pieces, q1 = min(q0 + a.part_pieces, a.pieces);
-  if (!s.cuts) {
-    for (int q = q0 + wave; q < q1; q += kPartWaves) {
-      float x[8];
-      r.load(q, lane, x);
-      uint64_t sum = 0;
-#pragma unroll
-      for (int e = 0; e < 8; ++e) sum += s.w.kept(x[e]);
-      sum = wave_sum_u64(sum);
-      if (lane == 0) a.piece_sums[row * a.pieces + q] = sum;
-    }
-    return;
-  }
+  const int b0 = part * a.part_blocks, b1 = min(b0 + a.part_blocks, a.blocks);
   for (int b = threadIdx.x; b < kBins; b += kPartThreads) {
     sums[b] = 0;
     counts[b] = 0;
   }
   __syncthreads();
   const Bins bins(s, info);
-  const bool weigh = s.p < 1.0f;
-  uint64_t far = 0;
-  uint32_t n_far = 0;
-  for (int q = q0 + wave; q < q1; q += kPartWaves) {
-    float x[8];
-    r.load(q, lane, x);
+  // top-k alone needs counts, top-p alone weights
+  auto pass = [&](auto weigh, auto count) {
+    uint64_t far = 0;
+    uint32_t n_far = 0;
+    for (int b = b0 + wave; b < b1; b += kPartWaves) {
+      float x[kBlockPieces][8];
+      r.load_block(b, lane, x);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      if (!(x[e] > -INFINITY)) continue;
-      const uint64_t w = weigh ? s.w.of(x[e]) : 0;
-      const int b = bins.of(x[e]);
-      if (b == kBins - 1) {
-        far += w;
-        ++n_far;
-      } else {
-        if (weigh) atomicAdd(&sums[b], (unsigned long long)w);
-        atomicAdd(&counts[b], 1u);
-      }
+      for (int q = 0; q < kBlockPieces; ++q)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+          const float v = x[q][e];
+          const uint64_t w = weigh() ? s.w.of(v) : 0;
+          const int bin = bins.of(v);
+          if (bin == kBins - 1) {
+            far += w;
+            n_far += v > -INFINITY ? 1 : 0;
+          } else {
+            if (weigh()) atomicAdd(&sums[bin], (unsigned long long)w);
+            if (count()) atomicAdd(&counts[bin], 1u);
+          }
+        }
     }
-  }
-  far = wave_sum_u64(far);
+    far = wave_sum_u64(far);
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) n_far += __shfl_xor(n_far, o);
-  if (lane == 0 && n_far) {
-    atomicAdd(&sums[kBins - 1], (unsigned long long)far);
-    atomicAdd(&counts[kBins - 1], n_far);
-  }
+    for (int o = 32; o > 0; o >>= 1) n_far += __shfl_xor(n_far, o);
+    if (lane == 0 && n_far) {
+      atomicAdd(&sums[kBins - 1], (unsigned long long)far);
+      atomicAdd(&counts[kBins - 1], n_far);
+    }
+  };
+  auto yes = []() { return true; };
+  auto no = []() { return false; };
+  if (s.k == 0) pass(yes, no);
+  else if (s.p < 1.0f) pass(yes, yes);
+  else pass(no, yes);
   __syncthreads();
-  for (int b = threadIdx.x; b < kBins; b += kPartThreads)
-    if (counts[b]) {
-      atomicAdd((unsigned long long*)&a.bin_sums[row * kBins + b], sums[b]);
-      atomicAdd(&a.bin_counts[row * kBins + b], counts[b]);
-    }
+  for (int b = threadIdx.x; b < kBins; b += kPartThreads) {
+    if (sums[b]) atomicAdd((unsigned long long*)&a.bin_sums[row * kBins + b], sums[b]);
+    if (counts[b]) atomicAdd(&a.bin_counts[row * kBins + b], counts[b]);
+  }
 }
 
 // ----------------------------------------------------------------------------
-// Pick
+// Cut
 // ----------------------------------------------------------------------------
-// The tokens above `key` and the first `count` of those that have it.
-struct Cut {
-  uint32_t key;
-  uint64_t count;
-};
-
 struct PickSmem {
-  uint64_t digits[kDigits];      // (pieces' sums, too)
+  uint64_t digits[kDigits];
   uint64_t bin_sum[kBins];       // of the bin and those before it
   uint32_t bin_count[kBins];
   uint32_t key[kList];
@@ -376,9 +398,7 @@ struct PickSmem {
   uint32_t wave_bits[2][kWaves];
   int found, listed, first_bin;
   uint64_t found_above;
-  uint32_t equal[kMaxPieces];
 };
-static_assert(kMaxPieces <= kDigits, "pieces' sums lie in `digits`");
 
 __device__ __forceinline__ uint64_t block_sum(PickSmem& sm, uint64_t v) {
   v = wave_sum_u64(v);
@@ -472,58 +492,58 @@ __device__ Cut find_cut(PickSmem& sm, Cut in, uint64_t want, Each each, Value va
   return c;
 }
 
+__device__ __forceinline__ void answer(const SampleArgs& a, int64_t row, int token, double logprob) {
+  a.tokens[row] = token;
+  if (a.logprobs) a.logprobs[row] = (float)logprob;
+}
+// The random number's place among the weights.
+__device__ __forceinline__ uint64_t want_of(const SampleArgs& a, int64_t row, uint64_t total) {
+  float u = a.u[row];
+  u = u > 0.0f ? fminf(u, 0x1.fffffep-1f) : 0.0f;
+  return (uint64_t)((double)u * (double)total);
+}
+__device__ __forceinline__ double log_share(const Settings& s, float x, uint64_t total) {
+  const double y = fmin(((double)x - s.w.top) * s.w.per_t, 0.0);
+  return y * 0.6931471805599453 - log((double)total * (1.0 / kOne));
+}
+
 template <int FMT>
-__global__ __launch_bounds__(kThreads) void sample_pick_kernel(SampleArgs a, int64_t row0) {
+__global__ __launch_bounds__(kThreads) void sample_cut_kernel(SampleArgs a, int64_t row0) {
   __shared__ PickSmem sm;
   const int64_t row = row0 + blockIdx.x;
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const Row<FMT> r(a, row);
   const PartInfo info = row_info(a, row);
-  auto answer = [&](int token, double logprob) {
-    a.tokens[row] = token;
-    if (a.logprobs) a.logprobs[row] = (float)logprob;
-  };
-  if (info.top == -INFINITY) {
-    if (threadIdx.x == 0) answer(-1, -INFINITY);
-    return;
-  }
+  if (info.top == -INFINITY) return;
   const Settings s = settings_of(a, row, info.top);
-  if (s.greedy) {
-    // the first part that has it
-    const float top = lane < a.parts ? a.part[row * a.parts + lane].top : -INFINITY;
-    const int part = __builtin_ctzll(__builtin_amdgcn_ballot_w64(top == info.top));
-    const int q0 = part * a.part_pieces, q1 = min(q0 + a.part_pieces, a.pieces);
-    uint32_t at = UINT_MAX;
-    for (int q = q0 + wave; q < q1; q += kWaves) {
-      float x[8];
-      r.load(q, lane, x);
+  if (!s.cuts) return;
+  // all of the row's logits, with their indexes
+  auto each_logit = [&](auto use) {
+    for (int b = wave; b < a.blocks; b += kWaves) {
+      float x[kBlockPieces][8];
+      r.load_block(b, lane, x);
 #pragma unroll
-      for (int e = 7; e >= 0; --e)
-        if (x[e] == info.top) at = min(at, (uint32_t)(r.index(q, lane) + e));
+      for (int q = 0; q < kBlockPieces; ++q)
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (x[q][e] > -INFINITY) use(x[q][e], r.index(b * kBlockPieces + q, lane) + e);
     }
-    at = wave_min_u32_f(at);
-    if (lane == 0) sm.wave_bits[0][wave] = at;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      for (int w = 0; w < kWaves; ++w) at = min(at, sm.wave_bits[0][w]);
-      answer((int)at, 0.0);
-    }
-    return;
-  }
-  float u = a.u[row];
-  u = u > 0.0f ? fminf(u, 0x1.fffffep-1f) : 0.0f;
-  auto log_share = [&](float x, uint64_t total) -> double {
-    const double y = x == s.w.top ? 0.0 : ((double)x - (double)s.w.top) * s.w.per_t;
-    return y * 0.6931471805599453 - log((double)total * (1.0 / kOne));
   };
 
   Cut cut{0, 0};
-  if (s.cuts) {
+  {
     const Bins bins(s, info);
     // sums over the bins from the largest logit on
     const int b = threadIdx.x;
-    const uint64_t own_count = b < kBins ? a.bin_counts[row * kBins + b] : 0;
     const uint64_t own_sum = b < kBins ? a.bin_sums[row * kBins + b] : 0;
+    uint64_t own_count = b < kBins ? a.bin_counts[row * kBins + b] : 0;
+    if (s.k == 0 && b < kBins - 1) {
+      // At most so many, by the least weight that a logit of the bin has (a hundredth
+      // of T further off is far more than its distance was rounded by).
+      const double y = ((double)(b + 1) / (double)bins.scale) * s.w.per_t + 0.015;
+      const uint64_t least = s.w.series.steps_of_exp2(-y);
+      own_count = least ? own_sum / least : own_sum ? kMaxVocab : 0;
+    }
     const uint64_t count_to = block_up_to(sm, own_count), sum_to = block_up_to(sm, own_sum);
     if (b < kBins) {
       sm.bin_count[b] = (uint32_t)count_to;
@@ -558,21 +578,15 @@ __global__ __launch_bounds__(kThreads) void sample_pick_kernel(SampleArgs a, int
       __syncthreads();
       first_listed = sm.first_bin;
       last_listed = bin;
-      for (int q = wave; q < a.pieces; q += kWaves) {
-        float x[8];
-        r.load(q, lane, x);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          if (!(x[e] > -INFINITY)) continue;
-          const int at = bins.of(x[e]);
-          if (at < first_listed || at > last_listed) continue;
-          const int to = atomicAdd(&sm.listed, 1);
-          if (to < kList) {        // (always)
-            sm.key[to] = key_of(x[e]);
-            sm.index[to] = r.index(q, lane) + e;
-          }
+      each_logit([&](float x, int index) {
+        const int at = bins.of(x);
+        if (at < first_listed || at > last_listed) return;
+        const int to = atomicAdd(&sm.listed, 1);
+        if (to < kList) {        // (always)
+          sm.key[to] = key_of(x);
+          sm.index[to] = index;
         }
-      }
+      });
       __syncthreads();
       return true;
     };
@@ -585,13 +599,9 @@ __global__ __launch_bounds__(kThreads) void sample_pick_kernel(SampleArgs a, int
         }, value);
       }
       return find_cut(sm, in, want, [&](auto use) {
-        for (int q = wave; q < a.pieces; q += kWaves) {
-          float x[8];
-          r.load(q, lane, x);
-#pragma unroll
-          for (int e = 0; e < 8; ++e)
-            if (x[e] > -INFINITY && bins.of(x[e]) == bin) use(key_of(x[e]));
-        }
+        each_logit([&](float x, int) {
+          if (bins.of(x) == bin) use(key_of(x));
+        });
       }, value);
     };
     int cut_bin = kBins;
@@ -611,14 +621,9 @@ __global__ __launch_bounds__(kThreads) void sample_pick_kernel(SampleArgs a, int
           for (int i = threadIdx.x; i < sm.listed; i += kThreads)
             if (sm.key[i] > cut.key && bins.of(logit_of(sm.key[i])) == cut_bin) sum += weight(sm.key[i]);
         } else {
-          for (int q = wave; q < a.pieces; q += kWaves) {
-            float x[8];
-            r.load(q, lane, x);
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-              if (x[e] > -INFINITY && bins.of(x[e]) == cut_bin && key_of(x[e]) > cut.key)
-                sum += s.w.of(x[e]);
-          }
+          each_logit([&](float x, int) {
+            if (bins.of(x) == cut_bin && key_of(x) > cut.key) sum += s.w.of(x);
+          });
         }
         total = before + block_sum(sm, sum) + cut.count * weight(cut.key);
       }
@@ -633,169 +638,651 @@ __global__ __launch_bounds__(kThreads) void sample_pick_kernel(SampleArgs a, int
     }
     // All kept ones in the list, and few: each thread has one, and adds up those of
     // lesser index.
-    if (first_listed == 0 && cut_bin < kBins && cut_bin <= last_listed &&
-        sm.bin_count[cut_bin] <= kThreads) {
+    if (first_listed == 0 && cut_bin <= last_listed) {
       const int n = sm.listed;
-      int mine = -1;
-      uint32_t key = 0;
-      uint64_t w = 0;
-      // (more are listed than the bins up to the cut's hold only where top-p cut again)
+      uint64_t same = 0;
       __syncthreads();
       if (threadIdx.x == 0) sm.found = 0;
       __syncthreads();
       for (int i = threadIdx.x; i < n; i += kThreads) {
-        const uint32_t have = sm.key[i];
-        bool in = have > cut.key;
-        if (have == cut.key) {
-          uint64_t rank = 0;
-          for (int j = 0; j < n; ++j) rank += sm.key[j] == have && sm.index[j] < sm.index[i];
-          in = rank < cut.count;
-        }
-        if (in) {
-          const int to = atomicAdd(&sm.found, 1);
-          sm.digits[to] = (uint64_t)(uint32_t)sm.index[i] << 32 | have;
-        }
+        const uint32_t key = sm.key[i];
+        if (key < cut.key) continue;
+        same += key == cut.key;
+        const int to = atomicAdd(&sm.found, 1);
+        if (to < kFew) sm.digits[to] = (uint64_t)(uint32_t)sm.index[i] << 32 | key;
       }
-      __syncthreads();
+      same = block_sum(sm, same);
       const int m = sm.found;
-      if ((int)threadIdx.x < m) {
-        mine = (int)(sm.digits[threadIdx.x] >> 32);
-        key = (uint32_t)sm.digits[threadIdx.x];
-        w = s.w.kept(logit_of(key));
+      if (m <= kFew) {
+        uint32_t key = 0;
+        int mine = 0;
+        uint64_t w = 0;
+        if ((int)threadIdx.x < m) {
+          mine = (int)(sm.digits[threadIdx.x] >> 32);
+          key = (uint32_t)sm.digits[threadIdx.x];
+          uint64_t rank = 0;
+          if (key == cut.key && same > cut.count)
+            for (int j = 0; j < m; ++j)
+              rank += (uint32_t)sm.digits[j] == key && (int)(sm.digits[j] >> 32) < mine;
+          if (key > cut.key || rank < cut.count) w = s.w.kept(logit_of(key));
+          sm.digits[kFew + threadIdx.x] = w;
+        }
+        const uint64_t total = block_sum(sm, w);
+        const uint64_t want = want_of(a, row, total);
+        if (w > 0) {
+          uint64_t before = 0;
+          for (int j = 0; j < m; ++j)
+            before += (int)(sm.digits[j] >> 32) < mine ? sm.digits[kFew + j] : 0;
+          if (before <= want && want < before + w)
+            answer(a, row, mine, log_share(s, logit_of(key), total));
+        }
+        if (threadIdx.x == 0) a.cut[row].done = 1;
+        return;
       }
-      const uint64_t total = block_sum(sm, w);
-      sm.digits[kThreads + threadIdx.x] = w;
-      __syncthreads();
-      const uint64_t want = (uint64_t)((double)u * (double)total);
-      if (w > 0) {
-        uint64_t before = 0;
-        for (int j = 0; j < m; ++j)
-          before += (int)(sm.digits[j] >> 32) < mine ? sm.digits[kThreads + j] : 0;
-        if (before <= want && want < before + w) answer(mine, log_share(logit_of(key), total));
-      }
-      return;
     }
   }
+  if (threadIdx.x == 0) a.cut[row] = RowCut{cut, 0, {}};
+}
 
-  // The pieces' kept weights, then the piece that u times their total lies in.
-  __syncthreads();
-  const uint64_t w_cut = cut.key ? s.w.kept(logit_of(cut.key)) : 0;
+// ----------------------------------------------------------------------------
+// Weigh
+// ----------------------------------------------------------------------------
+template <int FMT>
+__global__ __launch_bounds__(kPartThreads) void sample_weigh_kernel(SampleArgs a, int64_t unit0) {
+  const int64_t unit = unit0 + blockIdx.x;
+  const int64_t row = unit / a.parts;
+  const int part = (int)(unit % a.parts);
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const PartInfo info = row_info(a, row);
+  if (info.top == -INFINITY) return;
+  const Settings s = settings_of(a, row, info.top);
+  if (s.greedy) return;
+  const Row<FMT> r(a, row);
+  const int b0 = part * a.part_blocks, b1 = min(b0 + a.part_blocks, a.blocks);
   if (!s.cuts) {
-    for (int q = threadIdx.x; q < a.pieces; q += kThreads) {
-      sm.digits[q] = a.piece_sums[row * a.pieces + q];
-      sm.equal[q] = 0;
-    }
-  } else {
-    for (int q = wave; q < a.pieces; q += kWaves) {
-      float x[8];
-      r.load(q, lane, x);
+    for (int b = b0 + wave; b < b1; b += kPartWaves) {
+      float x[kBlockPieces][8];
+      r.load_block(b, lane, x);
       uint64_t sum = 0;
-      uint32_t equal = 0;
+#pragma unroll
+      for (int q = 0; q < kBlockPieces; ++q)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) sum += s.w.kept(x[q][e]);
+      sum = wave_sum_u64(sum);
+      if (lane == 0) a.sums[row * a.blocks + b] = sum;
+    }
+    return;
+  }
+  const RowCut rc = a.cut[row];
+  if (rc.done) return;
+  const uint32_t cut = rc.cut.key;
+  for (int b = b0 + wave; b < b1; b += kPartWaves) {
+    float x[kBlockPieces][8];
+    r.load_block(b, lane, x);
+    uint64_t sum = 0;
+    uint32_t equal = 0;
+#pragma unroll
+    for (int q = 0; q < kBlockPieces; ++q)
 #pragma unroll
       for (int e = 0; e < 8; ++e) {
-        const uint32_t key = key_of(x[e]);
-        if (key > cut.key) sum += s.w.kept(x[e]);
-        equal += key != 0 && key == cut.key;
+        const uint32_t key = key_of(x[q][e]);
+        if (key > cut) sum += s.w.kept(x[q][e]);
+        equal += key != 0 && key == cut;
       }
-      sum = wave_sum_u64(sum);
+    sum = wave_sum_u64(sum);
 #pragma unroll
-      for (int o = 32; o > 0; o >>= 1) equal += __shfl_xor(equal, o);
-      if (lane == 0) {
-        sm.digits[q] = sum;
-        sm.equal[q] = equal;
-      }
+    for (int o = 32; o > 0; o >>= 1) equal += __shfl_xor(equal, o);
+    if (lane == 0) {
+      a.sums[row * a.blocks + b] = sum;
+      a.equal[row * a.blocks + b] = equal;
     }
   }
-  __syncthreads();
+}
+
+// ----------------------------------------------------------------------------
+// Pick
+// ----------------------------------------------------------------------------
+constexpr int kPickWaves = kPickThreads / kWave;
+
+template <int FMT>
+__global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a, int64_t row0) {
+  __shared__ uint64_t wave_sum[2][kPickWaves];
+  __shared__ uint32_t wave_min[kPickWaves];
+  __shared__ uint64_t found_above, found_equal;
+  __shared__ int found;
+  const int64_t row = row0 + blockIdx.x;
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const Row<FMT> r(a, row);
+  const PartInfo info = row_info(a, row);
+  if (info.top == -INFINITY) {
+    if (threadIdx.x == 0) answer(a, row, -1, -INFINITY);
+    return;
+  }
+  const Settings s = settings_of(a, row, info.top);
+  if (s.greedy) {
+    // in the first part that has it
+    const float top = lane < a.parts ? a.part[row * a.parts + lane].top : -INFINITY;
+    const int part = __builtin_ctzll(__builtin_amdgcn_ballot_w64(top == info.top));
+    const int b0 = part * a.part_blocks, b1 = min(b0 + a.part_blocks, a.blocks);
+    uint32_t at = UINT_MAX;
+    for (int q = b0 * kBlockPieces + wave; q < b1 * kBlockPieces; q += kPickWaves) {
+      float x[8];
+      r.load(q, lane, x);
+#pragma unroll
+      for (int e = 7; e >= 0; --e)
+        if (x[e] == info.top) at = min(at, (uint32_t)(r.index(q, lane) + e));
+    }
+    at = wave_min_u32_f(at);
+    if (lane == 0) wave_min[wave] = at;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      for (int w = 0; w < kPickWaves; ++w) at = min(at, wave_min[w]);
+      answer(a, row, (int)at, 0.0);
+    }
+    return;
+  }
+  Cut cut{0, 0};
+  if (s.cuts) {
+    const RowCut rc = a.cut[row];
+    if (rc.done) return;
+    cut = rc.cut;
+  }
+  const uint64_t w_cut = cut.key ? s.w.kept(logit_of(cut.key)) : 0;
   auto kept = [&](uint64_t before) { return before < cut.count ? before : cut.count; };
-  // two pieces a thread (kMaxPieces of them at most)
-  const int qa = 2 * (int)threadIdx.x, qb = qa + 1;
-  const uint64_t ea = qa < a.pieces ? sm.equal[qa] : 0, eb = qb < a.pieces ? sm.equal[qb] : 0;
-  const uint64_t equal_end = block_up_to(sm, ea + eb), equal_mid = equal_end - eb;
-  const uint64_t equal_begin = equal_mid - ea;
-  const uint64_t ma = (qa < a.pieces ? sm.digits[qa] : 0) + (kept(equal_mid) - kept(equal_begin)) * w_cut;
-  const uint64_t mb = (qb < a.pieces ? sm.digits[qb] : 0) + (kept(equal_end) - kept(equal_mid)) * w_cut;
-  const uint64_t end = block_up_to(sm, ma + mb), mid = end - mb, begin = mid - ma;
-  const uint64_t total = block_sum(sm, ma + mb);
-  const uint64_t want = (uint64_t)((double)u * (double)total);
-  __syncthreads();
-  if (begin <= want && want < end) {
-    const bool second = mid <= want;
-    sm.found = second ? qb : qa;
-    sm.found_above = second ? mid : begin;
-    sm.digits[0] = second ? equal_mid : equal_begin;
+  // the sum over this thread and those before it
+  auto up_to = [&](int which, uint64_t v, uint64_t& total) -> uint64_t {
+    v = wave_up_to(v, lane);
+    if (lane == kWave - 1) wave_sum[which][wave] = v;
+    __syncthreads();
+    total = 0;
+    for (int w = 0; w < kPickWaves; ++w) {
+      if (w < wave) v += wave_sum[which][w];
+      total += wave_sum[which][w];
+    }
+    return v;
+  };
+  const bool in = (int)threadIdx.x < a.blocks;
+  const int64_t at = row * a.blocks + threadIdx.x;
+  const uint64_t equal = in && cut.key ? a.equal[at] : 0;
+  uint64_t total, equals;
+  const uint64_t equal_end = up_to(0, equal, equals), equal_begin = equal_end - equal;
+  const uint64_t sum = (in ? a.sums[at] : 0) + (kept(equal_end) - kept(equal_begin)) * w_cut;
+  const uint64_t end = up_to(1, sum, total), want = want_of(a, row, total);
+  if (end - sum <= want && want < end) {
+    found = (int)threadIdx.x;
+    found_above = end - sum;
+    found_equal = equal_begin;
   }
   __syncthreads();
   if (wave != 0) return;
-  const int q = sm.found;      // (of one wave)
-  float x[8];
-  r.load(q, lane, x);
-  uint32_t same = 0;
-  uint64_t sum = 0;
+  uint64_t run = found_above, same = found_equal;
+  const int b = found;
+  for (int q = b * kBlockPieces; q < (b + 1) * kBlockPieces; ++q) {
+    float x[8];
+    r.load(q, lane, x);
+    uint32_t n_same = 0;
+    uint64_t mine = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t key = key_of(x[e]);
+      if (key > cut.key) mine += s.w.kept(x[e]);
+      n_same += key != 0 && key == cut.key;
+    }
+    const uint64_t same_end = same + wave_up_to(n_same, lane), same_begin = same_end - n_same;
+    mine += (kept(same_end) - kept(same_begin)) * w_cut;
+    const uint64_t mine_end = run + wave_up_to(mine, lane);
+    uint64_t to = mine_end - mine;
+    if (to <= want && want < mine_end) {
+      uint64_t n = same_begin;
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t key = key_of(x[e]);
+        if (key > cut.key) to += s.w.kept(x[e]);
+        else if (key != 0 && key == cut.key && n++ < cut.count) to += w_cut;
+        if (to > want) {
+          answer(a, row, r.index(q, lane) + e, log_share(s, x[e], total));
+          break;
+        }
+      }
+    }
+    run = __shfl(mine_end, kWave - 1);
+    same = __shfl(same_end, kWave - 1);
+    if (want < run) return;
+  }
+}
+
+// ----------------------------------------------------------------------------
+// A row of bf16 in one workgroup
+//
+// bf16 has few values between the largest logit and where weights vanish, so the
+// weights come from a table in LDS by the bits of the logit: the 16 binades up to the
+// largest logit, and those up to the farthest negative one that weighs something.
+// The tokens counted by the same bits tell the cuts of top-k and top-p exactly, in
+// one scan over the table: its entries are single values.  Values nearer to 0 than
+// the tables reach (2^-16 of their ends) are rare: their weights are computed one by
+// one, and a cut among them is searched for in the row.
+// ----------------------------------------------------------------------------
+constexpr int kMaxPieces = kMaxVocab / kPiece + 1;
+constexpr int kSide = 2047;                        // table entries of a sign
+constexpr int kTable = 2 * (kSide + 1);            // (the last of each: weight 0)
+
+struct RowSmem {
+  PickSmem pick;
+  uint64_t weight[kTable];
+  uint32_t count[kTable];
+  uint64_t piece_sum[kMaxPieces];
+  uint32_t piece_equal[kMaxPieces];
+  float wave_top[kWaves];
+  int small_count, found;
+  uint64_t small_sum, found_before, found_weight, found_count;
+};
+
+__device__ __forceinline__ uint64_t wave_sum_u64_dpp(uint64_t v) {
+#define EI_ADD_DPP(ctrl)                                                              \
+  v += (uint64_t)EI_DPP_U32((uint32_t)(v >> 32), ctrl, 0xF, false) << 32 |            \
+       EI_DPP_U32((uint32_t)v, ctrl, 0xF, false)
+  EI_ADD_DPP(0xB1);     // quad_perm [1,0,3,2]
+  EI_ADD_DPP(0x4E);     // quad_perm [2,3,0,1]
+  EI_ADD_DPP(0x141);    // row_half_mirror
+  EI_ADD_DPP(0x140);    // row_mirror
+#undef EI_ADD_DPP
+  uint64_t s = 0;
+#pragma unroll
+  for (int l = 0; l < kWave; l += 16)
+    s += (uint64_t)rl_u32((uint32_t)(v >> 32), l) << 32 | rl_u32((uint32_t)v, l);
+  return s;
+}
+
+// The magnitude bits of a bf16 number, those of `x` (>= 0) rounded up.
+__device__ __forceinline__ int bits_above(double x) {
+  if (!(x < 3e38)) return 0x7f7f;
+  const uint32_t b = __float_as_uint((float)fmax(x, 0.0)) >> 16;
+  return min((int)b + 2, 0x7f7f);     // (the conversion may have rounded down)
+}
+
+__global__ __launch_bounds__(kThreads) void sample_row_kernel(SampleArgs a, int64_t row0) {
+  __shared__ RowSmem sm;
+  const int64_t row = row0 + blockIdx.x;
+  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
+  const Row<EI_LOGITS_BF16> r(a, row);
+
+  // A wave has `per` pieces in a row.  All of them: use(words, piece), four loads
+  // under way while four pieces are used.  (The row is read again for each pass, from
+  // the caches: in registers, 64 a thread, the passes have to be unrolled, and waiting
+  // for code that runs once took most of the time, 62 us for a row of 128256.)
+  const int pieces = (a.vocab + kPiece - 1) / kPiece, full = a.vocab / kPiece;
+  const int per = (pieces + kWaves - 1) / kWaves, q0 = wave * per, q1 = min(q0 + per, pieces);
+  auto each_piece = [&](auto use) {
+    constexpr int kAhead = 4;
+    uint4 next[kAhead];
+    const int qf = min(q1, full);
+    auto ask = [&](int q) {
+      if (q + kAhead <= qf)
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) next[i] = r.load_full(q + i, lane);
+    };
+    int q = q0;
+    ask(q);
+#pragma unroll 1
+    for (; q + kAhead <= qf; q += kAhead) {
+      uint4 now[kAhead];
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) now[i] = next[i];
+      ask(q + kAhead);
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        const uint32_t words[4] = {now[i].x, now[i].y, now[i].z, now[i].w};
+        use(words, q + i);
+      }
+    }
+#pragma unroll 1
+    for (; q < q1; ++q) {
+      const uint4 now = r.load_raw(q, lane);
+      const uint32_t words[4] = {now.x, now.y, now.z, now.w};
+      use(words, q);
+    }
+  };
+  auto bits_of = [](const uint32_t (&words)[4], int e) {
+    return e & 1 ? words[e / 2] >> 16 : words[e / 2] & 0xffffu;
+  };
+  auto value = [](uint32_t bits) { return __uint_as_float(bits << 16); };
+
+  float top = -INFINITY;
+  each_piece([&](const uint32_t (&words)[4], int) {
+#pragma unroll
+    for (int w = 0; w < 4; ++w) top = fmaxf(top, fmaxf(bf16_lo(words[w]), bf16_hi(words[w])));
+  });
+  top = wave_max_f32_dpp(top);
+  if (lane == 0) sm.wave_top[wave] = top;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sm.wave_top[w]);
+  if (top == -INFINITY) {
+    if (threadIdx.x == 0) answer(a, row, -1, -INFINITY);
+    return;
+  }
+  const Settings s = settings_of(a, row, top);
+  if (s.greedy) {
+    uint32_t at = UINT_MAX;
+    each_piece([&](const uint32_t (&words)[4], int q) {
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (value(bits_of(words, e)) == top) at = min(at, (uint32_t)(r.index(q, lane) + e));
+    });
+    at = wave_min_u32_f(at);
+    if (lane == 0) sm.pick.wave_bits[0][wave] = at;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      for (int w = 0; w < kWaves; ++w) at = min(at, sm.pick.wave_bits[0][w]);
+      answer(a, row, (int)at, 0.0);
+    }
+    return;
+  }
+
+  // The tables: entry i of a sign is the magnitude base - i.  Negative logits past
+  // 46 binary places below the top weigh nothing.
+  const int base_p = max(top > 0.0f ? (int)(__float_as_uint(top) >> 16) : 0, kSide);
+  const int base_n = max(bits_above(46.0 / s.w.per_t - s.w.top), kSide);
+  for (int i = threadIdx.x; i < kTable; i += kThreads) {
+    const int off = i & kSide, mag = (i > kSide ? base_n : base_p) - off;
+    const uint32_t bits = (uint32_t)mag | (i > kSide ? 0x8000u : 0u);
+    sm.weight[i] = off < kSide ? s.w.of(value(bits)) : 0;
+    sm.count[i] = 0;
+  }
+  if (threadIdx.x == 0) {
+    sm.small_count = 0;
+    sm.small_sum = 0;
+  }
+  __syncthreads();
+  // (off: the entry, as it is; kSide and more: nearer to 0 than the table, below zero:
+  // weighs nothing, NaN and -inf among them)
+  auto off_of = [&](uint32_t bits) -> int {
+    return (bits & 0x8000u ? base_n : base_p) - (int)(bits & 0x7fffu);
+  };
+  auto entry_of = [&](uint32_t bits, int off) -> int {
+    return (int)(bits >> 15) * (kSide + 1) + (int)min((uint32_t)off, (uint32_t)kSide);
+  };
+
+  // those nearer to 0 than the tables, of a thread's piece: use(bits, place)
+  auto each_small_of = [&](const uint32_t (&words)[4], auto use) {
+    const uint32_t w0 = words[0], w1 = words[1], w2 = words[2], w3 = words[3];
+#pragma unroll 1
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t w = e < 4 ? e < 2 ? w0 : w1 : e < 6 ? w2 : w3;
+      const uint32_t bits = e & 1 ? w >> 16 : w & 0xffffu;
+      if (off_of(bits) >= kSide) use(bits, e);
+    }
+  };
+
+  Cut cut{0, 0};
+  bool split = false;          // not all tokens of the cut's key are kept
+  if (s.cuts) {
+    uint64_t small_sum = 0;
+    int small_count = 0;
+    each_piece([&](const uint32_t (&words)[4], int) {
+      bool small = false;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t bits = bits_of(words, e);
+        const int off = off_of(bits);
+        small |= off >= kSide;
+        if ((uint32_t)off < (uint32_t)kSide) atomicAdd(&sm.count[entry_of(bits, off)], 1u);
+      }
+      if (small)
+        each_small_of(words, [&](uint32_t bits, int) {
+          ++small_count;
+          small_sum += s.w.of(value(bits));
+        });
+    });
+    if (small_count) {
+      atomicAdd(&sm.small_count, small_count);
+      atomicAdd((unsigned long long*)&sm.small_sum, (unsigned long long)small_sum);
+    }
+    __syncthreads();
+    // the values in their order, four a thread: positive, near 0, negative
+    constexpr int kEach = kTable / kThreads;
+    auto place_of = [](int at) { return at <= kSide ? at : kSide + 1 + (2 * kSide - at); };
+    auto counts_at = [&](int at) -> uint64_t {
+      return at == kSide ? (uint64_t)sm.small_count : at > 2 * kSide ? 0 : sm.count[place_of(at)];
+    };
+    auto weights_at = [&](int at) -> uint64_t {
+      return at == kSide ? sm.small_sum : counts_at(at) * sm.weight[place_of(min(at, 2 * kSide))];
+    };
+    uint64_t n_all = 0, w_all = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      n_all += counts_at((int)threadIdx.x * kEach + i);
+      w_all += weights_at((int)threadIdx.x * kEach + i);
+    }
+    const uint64_t n_to = block_up_to(sm.pick, n_all), w_to = block_up_to(sm.pick, w_all);
+    const uint64_t total_n = block_sum(sm.pick, n_all);
+    auto key_at = [&](int entry) {
+      const uint32_t bits = entry > kSide ? 0x8000u | (uint32_t)(base_n - (entry - kSide - 1))
+                                          : (uint32_t)(base_p - entry);
+      return key_of(value(bits));
+    };
+    auto each_small = [&](auto use) {
+#pragma unroll 1
+      for (int q = q0; q < q1; ++q) {
+        const uint4 again = r.load_raw(q, lane);
+        const uint32_t words[4] = {again.x, again.y, again.z, again.w};
+        each_small_of(words, [&](uint32_t bits, int) { use(key_of(value(bits))); });
+      }
+    };
+    auto weight = [&](uint32_t key) { return s.w.of(logit_of(key)); };
+    uint64_t total_w = block_sum(sm.pick, w_all), cut_before = 0;
+    int cut_at = -1;
+    uint64_t same = 0;         // tokens of the cut's key
+    // top-k by counts, then top-p by weights
+#pragma unroll 1
+    for (int stage = 0; stage < 2; ++stage) {
+      const bool by_count = stage == 0;
+      // (the tokens past all that weigh something need no cut)
+      if (by_count ? s.k == 0 || (uint64_t)s.k >= total_n : s.p >= 1.0f) continue;
+      uint64_t want = (uint64_t)s.k;
+      if (!by_count) {
+        if (cut_at >= 0) {       // the weight of top-k's tokens
+          uint64_t mine = 0;
+          if (cut_at == kSide)
+            each_small([&](uint32_t key) {
+              if (key > cut.key) mine += weight(key);
+            });
+          total_w = cut_before + block_sum(sm.pick, mine) + cut.count * weight(cut.key);
+        }
+        const double real = ceil((double)s.p * (double)total_w);
+        want = real < 1.0 ? 1 : (uint64_t)real;
+      }
+      Cut in{0, 0};
+      if (cut_at >= 0 && cut_before < want) {      // in the same entry
+        in = cut;
+        want -= cut_before;
+      } else {
+        // the entry at which the values reach `want`, and what lies before it
+        uint64_t before = by_count ? n_to - n_all : w_to - w_all;
+        uint64_t weight_before = w_to - w_all;
+        __syncthreads();
+#pragma unroll 1
+        for (int at = (int)threadIdx.x * kEach; at < ((int)threadIdx.x + 1) * kEach; ++at) {
+          const uint64_t n = counts_at(at), w = weights_at(at), v = by_count ? n : w;
+          if (before < want && want <= before + v) {
+            sm.found = place_of(at);
+            sm.found_before = before;
+            sm.found_weight = weight_before;
+            sm.found_count = n;
+          }
+          before += v;
+          weight_before += w;
+        }
+        __syncthreads();
+        cut_at = sm.found;
+        want -= sm.found_before;
+        cut_before = sm.found_weight;
+        same = sm.found_count;
+      }
+      if (cut_at == kSide) {
+        cut = find_cut(sm.pick, in, want, each_small,
+                       [&](uint32_t key) { return by_count ? (uint64_t)1 : weight(key); });
+      } else {
+        const uint64_t v = by_count ? 1 : sm.weight[cut_at];
+        cut = Cut{key_at(cut_at), (want + v - 1) / v};
+      }
+    }
+    if (cut.key) split = cut_at == kSide || cut.count < same;
+    __syncthreads();
+  }
+
+  // What is not kept weighs nothing from here on; nor does the cut's own key where its
+  // tokens are split (they are counted).
+  const uint64_t w_cut = split ? s.w.kept(logit_of(cut.key)) : 0;
+  for (int i = threadIdx.x; i < kTable; i += kThreads) {
+    const int off = i & kSide, mag = (i > kSide ? base_n : base_p) - off;
+    const uint32_t key = key_of(value((uint32_t)mag | (i > kSide ? 0x8000u : 0u)));
+    if (off < kSide && (sm.weight[i] < s.w.least || key < cut.key || (split && key == cut.key)))
+      sm.weight[i] = 0;
+  }
+  __syncthreads();
+  const float least = cut.key ? logit_of(cut.key) : -INFINITY;
+  auto kept = [&](uint64_t before) { return before < cut.count ? before : cut.count; };
+  auto small_weight = [&](uint32_t bits) -> uint64_t {
+    const uint32_t key = key_of(value(bits));
+    return (split ? key > cut.key : key >= cut.key) ? s.w.kept(value(bits)) : 0;
+  };
+  each_piece([&](const uint32_t (&words)[4], int q) {
+    uint64_t sum = 0;
+    uint32_t equal = 0;
+    bool some = true;
+    if (cut.key) {
+      float most = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) most = fmaxf(most, fmaxf(bf16_lo(words[w]), bf16_hi(words[w])));
+      some = __builtin_amdgcn_ballot_w64(most >= least) != 0;
+    }
+    if (some) {
+      bool small = false;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const uint32_t bits = bits_of(words, e);
+        const int off = off_of(bits);
+        sum += sm.weight[entry_of(bits, off)];
+        small |= off >= kSide;
+      }
+      if (small) each_small_of(words, [&](uint32_t bits, int) { sum += small_weight(bits); });
+      if (split) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) equal += value(bits_of(words, e)) == least ? 1 : 0;
+        equal = (uint32_t)wave_sum_u64_dpp(equal);
+      }
+      sum = wave_sum_u64_dpp(sum);
+    }
+    if (lane == 0) {
+      sm.piece_sum[q] = sum;
+      sm.piece_equal[q] = equal;
+    }
+  });
+  __syncthreads();
+  // two pieces a thread
+  const int qa = 2 * (int)threadIdx.x, qb = qa + 1;
+  const uint64_t ea = split && qa < pieces ? sm.piece_equal[qa] : 0;
+  const uint64_t eb = split && qb < pieces ? sm.piece_equal[qb] : 0;
+  const uint64_t equal_end = split ? block_up_to(sm.pick, ea + eb) : 0, equal_mid = equal_end - eb;
+  const uint64_t equal_begin = equal_mid - ea;
+  const uint64_t ma = (qa < pieces ? sm.piece_sum[qa] : 0) + (kept(equal_mid) - kept(equal_begin)) * w_cut;
+  const uint64_t mb = (qb < pieces ? sm.piece_sum[qb] : 0) + (kept(equal_end) - kept(equal_mid)) * w_cut;
+  const uint64_t end = block_up_to(sm.pick, ma + mb), mid = end - mb, begin = mid - ma;
+  uint64_t total = 0;
+#pragma unroll
+  for (int w = 0; w < kWaves; ++w) total += sm.pick.wave_sum[w];
+  const uint64_t want = want_of(a, row, total);
+  if (begin <= want && want < end) {
+    const bool second = mid <= want;
+    sm.found = second ? qb : qa;
+    sm.found_before = second ? mid : begin;
+    sm.found_count = second ? equal_mid : equal_begin;
+  }
+  __syncthreads();
+  if (wave != 0) return;
+  const int q = sm.found;
+  const uint4 again = r.load_raw(q, lane);
+  const uint32_t words[4] = {again.x, again.y, again.z, again.w};
+  uint64_t mine[8], all = 0;
+  uint32_t n_same = 0;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const uint32_t key = key_of(x[e]);
-    if (key > cut.key) sum += s.w.kept(x[e]);
-    same += key != 0 && key == cut.key;
+    const uint32_t bits = bits_of(words, e);
+    const int off = off_of(bits);
+    mine[e] = off >= kSide ? small_weight(bits) : sm.weight[entry_of(bits, off)];
+    n_same += split && value(bits) == least ? 1 : 0;
   }
-  const uint64_t same0 = sm.digits[0] + (wave_up_to(same, lane) - same);
-  sum += (kept(same0 + same) - kept(same0)) * w_cut;
-  uint64_t run = sm.found_above + wave_up_to(sum, lane) - sum;
-  if (!(run <= want && want < run + sum)) return;
-  uint64_t n_same = same0;
+  uint64_t same = sm.found_count + wave_up_to(n_same, lane) - n_same;
+#pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const uint32_t key = key_of(x[e]);
-    if (key > cut.key) run += s.w.kept(x[e]);
-    else if (key != 0 && key == cut.key && n_same++ < cut.count) run += w_cut;
-    if (run > want) {
-      answer(r.index(q, lane) + e, log_share(x[e], total));
-      return;
-    }
+    const uint32_t bits = bits_of(words, e);
+    if (split && value(bits) == least && same++ < cut.count) mine[e] = w_cut;
+    all += mine[e];
+  }
+  uint64_t run = sm.found_before + wave_up_to(all, lane) - all;
+  if (!(run <= want && want < run + all)) return;
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    const uint32_t bits = bits_of(words, e);
+    if (run <= want && want < run + mine[e])
+      answer(a, row, r.index(q, lane) + e, log_share(s, value(bits), total));
+    run += mine[e];
   }
 }
 
 // ----------------------------------------------------------------------------
 // Host side
 // ----------------------------------------------------------------------------
-constexpr int64_t kMaxGrid = (1ll << 31) / kThreads;
 bool aligned(const void* p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 
+bool in_one_workgroup(int format) { return format == EI_LOGITS_BF16; }
+
 struct SamplePlan {
-  int pieces, parts, part_pieces;
-  size_t at_bins, at_counts, at_pieces, bytes;
+  int blocks, parts, part_blocks;
+  size_t at_cuts, at_bins, at_counts, at_sums, at_equal, bytes;
 };
-// Parts of a row: as many as give the chip 1024 workgroups, of 4 pieces at least.
+// Parts of a row: as many as give the chip 1024 workgroups, of a block a wave at least.
 SamplePlan sample_plan(int rows, int vocab) {
   SamplePlan p{};
-  p.pieces = (vocab + 7 + kPiece - 1) / kPiece;      // (the first may start 7 tokens early)
+  const int tokens = kBlockPieces * kPiece;
+  p.blocks = (vocab + tokens - 1) / tokens;
+  if (p.blocks < 1) p.blocks = 1;
   int parts = 1024 / rows;
-  const int most = (p.pieces + kPartWaves - 1) / kPartWaves;
+  const int most = (p.blocks + kPartWaves - 1) / kPartWaves;
   parts = parts > kMaxParts ? kMaxParts : parts < 1 ? 1 : parts;
   parts = parts > most ? most : parts;
-  p.part_pieces = (p.pieces + parts - 1) / parts;
-  p.parts = (p.pieces + p.part_pieces - 1) / p.part_pieces;
+  p.part_blocks = (p.blocks + parts - 1) / parts;
+  p.parts = (p.blocks + p.part_blocks - 1) / p.part_blocks;
   auto up = [](size_t n) { return (n + 255) / 256 * 256; };
-  p.at_bins = up((size_t)rows * p.parts * sizeof(PartInfo));
+  p.at_cuts = up((size_t)rows * p.parts * sizeof(PartInfo));
+  p.at_bins = p.at_cuts + up((size_t)rows * sizeof(RowCut));
   p.at_counts = p.at_bins + (size_t)rows * kBins * sizeof(uint64_t);
-  p.at_pieces = p.at_counts + (size_t)rows * kBins * sizeof(uint32_t);
-  p.bytes = p.at_pieces + (size_t)rows * p.pieces * sizeof(uint64_t);
+  p.at_sums = p.at_counts + (size_t)rows * kBins * sizeof(uint32_t);
+  p.at_equal = p.at_sums + (size_t)rows * p.blocks * sizeof(uint64_t);
+  p.bytes = p.at_equal + (size_t)rows * p.blocks * sizeof(uint32_t);
   return p;
 }
 
 template <int FMT>
 void launch_sample(const SampleArgs& a, hipStream_t stream) {
+  auto launch = [&](auto kernel, int64_t groups, int threads) {
+    const int64_t most = (1ll << 31) / threads;
+    for (int64_t u = 0; u < groups; u += most)
+      hipLaunchKernelGGL(kernel, dim3((unsigned)(groups - u < most ? groups - u : most)),
+                         dim3((unsigned)threads), 0, stream, a, u);
+  };
+  if (in_one_workgroup(FMT)) {
+    launch(sample_row_kernel, a.rows, kThreads);
+    return;
+  }
   const int64_t units = (int64_t)a.rows * a.parts;
-  constexpr int64_t most = (1ll << 31) / kPartThreads;
-  for (int64_t u = 0; u < units; u += most)
-    hipLaunchKernelGGL((sample_scan_kernel<FMT>), dim3((unsigned)(units - u < most ? units - u : most)),
-                       dim3(kPartThreads), 0, stream, a, u);
-  for (int64_t u = 0; u < units; u += most)
-    hipLaunchKernelGGL((sample_weigh_kernel<FMT>), dim3((unsigned)(units - u < most ? units - u : most)),
-                       dim3(kPartThreads), 0, stream, a, u);
-  for (int64_t r = 0; r < a.rows; r += kMaxGrid)
-    hipLaunchKernelGGL((sample_pick_kernel<FMT>),
-                       dim3((unsigned)(a.rows - r < kMaxGrid ? a.rows - r : kMaxGrid)),
-                       dim3(kThreads), 0, stream, a, r);
+  launch(sample_scan_kernel<FMT>, units, kPartThreads);
+  if (a.top_k || a.top_p) {
+    launch(sample_bins_kernel<FMT>, units, kPartThreads);
+    launch(sample_cut_kernel<FMT>, a.rows, kThreads);
+  }
+  launch(sample_weigh_kernel<FMT>, units, kPartThreads);
+  launch(sample_pick_kernel<FMT>, a.rows, kPickThreads);
 }
 
 bool valid(int32_t rows, int32_t vocab, int32_t format) {
@@ -806,7 +1293,9 @@ bool valid(int32_t rows, int32_t vocab, int32_t format) {
 }  // namespace ei
 
 extern "C" size_t ei_sample_workspace_bytes(int32_t rows, int32_t vocab, int32_t format) {
-  if (!ei::valid(rows, vocab, format) || vocab > ei::kMaxVocab || rows == 0) return 0;
+  if (!ei::valid(rows, vocab, format) || vocab > ei::kMaxVocab || rows == 0 ||
+      ei::in_one_workgroup(format))
+    return 0;
   return ei::sample_plan(rows, vocab).bytes;
 }
 
@@ -826,12 +1315,14 @@ extern "C" ei_status ei_sample_tokens(const void* logits, int32_t format, int32_
       !ei::aligned(min_p, 4) || !ei::aligned(tokens, 4) || !ei::aligned(logprobs, 4))
     return EI_ERR_UNSUPPORTED;
   const ei::SamplePlan p = ei::sample_plan(rows, vocab);
-  if (!workspace || workspace_bytes < p.bytes) return EI_ERR_WORKSPACE;
+  if (!ei::in_one_workgroup(format) && (!workspace || workspace_bytes < p.bytes))
+    return EI_ERR_WORKSPACE;
   if (!ei::aligned(workspace, 16)) return EI_ERR_UNSUPPORTED;
   char* ws = (char*)workspace;
   const ei::SampleArgs a{logits, rows, vocab, row_stride, u, temperature, top_k, top_p, min_p,
-                         tokens, logprobs, p.parts, p.part_pieces, p.pieces, (ei::PartInfo*)ws,
-                         (uint64_t*)(ws + p.at_pieces), (uint64_t*)(ws + p.at_bins),
+                         tokens, logprobs, p.parts, p.part_blocks, p.blocks, (ei::PartInfo*)ws,
+                         (ei::RowCut*)(ws + p.at_cuts), (uint64_t*)(ws + p.at_sums),
+                         (uint32_t*)(ws + p.at_equal), (uint64_t*)(ws + p.at_bins),
                          (uint32_t*)(ws + p.at_counts)};
   if (format == EI_LOGITS_BF16) ei::launch_sample<EI_LOGITS_BF16>(a, (hipStream_t)stream);
   else ei::launch_sample<EI_LOGITS_FP32>(a, (hipStream_t)stream);

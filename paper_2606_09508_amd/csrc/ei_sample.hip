@@ -865,12 +865,14 @@ constexpr int kMaxPieces = kMaxVocab / kPiece + 1;
 constexpr int kSide = 2047;                        // table entries of a sign
 constexpr int kTable = 2 * (kSide + 1);            // (the last of each: weight 0)
 
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+
 struct RowSmem {
   PickSmem pick;
   uint64_t weight[kTable];
-  uint32_t count[kTable];
+  uint32_t count[kTable + kWave];      // (the last 64: of logits without an entry)
   uint64_t piece_sum[kMaxPieces];
-  uint32_t piece_equal[kMaxPieces];
   float wave_top[kWaves];
   int small_count, found;
   uint64_t small_sum, found_before, found_weight, found_count;
@@ -998,9 +1000,18 @@ __global__ __launch_bounds__(kThreads) void sample_row_kernel(SampleArgs a, int6
   auto off_of = [&](uint32_t bits) -> int {
     return (bits & 0x8000u ? base_n : base_p) - (int)(bits & 0x7fffu);
   };
-  auto entry_of = [&](uint32_t bits, int off) -> int {
-    return (int)(bits >> 15) * (kSide + 1) + (int)min((uint32_t)off, (uint32_t)kSide);
+  // The entries of two logits (the last of their sign where they have none), 8 times
+  // each, in 16-bit pairs; `off`: theirs.
+  const uint32_t base_p2 = (uint32_t)base_p * 0x10001u, base_n2 = (uint32_t)base_n * 0x10001u;
+  auto entries_of = [&](uint32_t word, s16x2& off) -> uint32_t {
+    const uint32_t sign = __builtin_bit_cast(uint32_t, __builtin_bit_cast(s16x2, word) >> 15);
+    const uint32_t base = (sign & base_n2) | (~sign & base_p2);
+    off = __builtin_bit_cast(s16x2, base) - __builtin_bit_cast(s16x2, word & 0x7fff7fffu);
+    const u16x2 at = __builtin_elementwise_min(__builtin_bit_cast(u16x2, off), u16x2{kSide, kSide});
+    const uint32_t entry = (sign & (uint32_t)((kSide + 1) * 0x10001)) | __builtin_bit_cast(uint32_t, at);
+    return entry << 3;
   };
+  auto any_small = [&](s16x2 most) { return most.x >= kSide || most.y >= kSide; };
 
   // those nearer to 0 than the tables, of a thread's piece: use(bits, place)
   auto each_small_of = [&](const uint32_t (&words)[4], auto use) {
@@ -1019,15 +1030,19 @@ __global__ __launch_bounds__(kThreads) void sample_row_kernel(SampleArgs a, int6
     uint64_t small_sum = 0;
     int small_count = 0;
     each_piece([&](const uint32_t (&words)[4], int) {
-      bool small = false;
+      s16x2 most = {-1, -1};
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const uint32_t bits = bits_of(words, e);
-        const int off = off_of(bits);
-        small |= off >= kSide;
-        if ((uint32_t)off < (uint32_t)kSide) atomicAdd(&sm.count[entry_of(bits, off)], 1u);
+      for (int w = 0; w < 4; ++w) {
+        s16x2 off;
+        const uint32_t at = entries_of(words[w], off);
+        most = __builtin_elementwise_max(most, off);
+        // (the lanes without an entry count apart, each for itself)
+        constexpr uint32_t kNone = 8 * kSide;
+        const uint32_t lo = at & 0xffffu, hi = at >> 16;
+        atomicAdd(&sm.count[(lo & kNone) == kNone ? kTable + lane : lo >> 3], 1u);
+        atomicAdd(&sm.count[(hi & kNone) == kNone ? kTable + lane : hi >> 3], 1u);
       }
-      if (small)
+      if (any_small(most))
         each_small_of(words, [&](uint32_t bits, int) {
           ++small_count;
           small_sum += s.w.of(value(bits));
@@ -1130,25 +1145,28 @@ __global__ __launch_bounds__(kThreads) void sample_row_kernel(SampleArgs a, int6
     __syncthreads();
   }
 
-  // What is not kept weighs nothing from here on; nor does the cut's own key where its
-  // tokens are split (they are counted).
+  // What is not kept weighs nothing from here on.  The cut's own key, where its tokens
+  // are split, weighs kSame: a piece's sum (2^53 at most) then counts them above it.
+  constexpr int kSameBit = 54;
+  constexpr uint64_t kSame = (uint64_t)1 << kSameBit;
+  static_assert((uint64_t)kPiece * kSame != 0 && kPiece <= 1 << (63 - kSameBit), "512 of them");
   const uint64_t w_cut = split ? s.w.kept(logit_of(cut.key)) : 0;
+  auto left_of = [&](uint32_t key, uint64_t w) -> uint64_t {
+    return split && key == cut.key ? kSame : key < cut.key || w < s.w.least ? 0 : w;
+  };
   for (int i = threadIdx.x; i < kTable; i += kThreads) {
     const int off = i & kSide, mag = (i > kSide ? base_n : base_p) - off;
-    const uint32_t key = key_of(value((uint32_t)mag | (i > kSide ? 0x8000u : 0u)));
-    if (off < kSide && (sm.weight[i] < s.w.least || key < cut.key || (split && key == cut.key)))
-      sm.weight[i] = 0;
+    const uint32_t bits = (uint32_t)mag | (i > kSide ? 0x8000u : 0u);
+    if (off < kSide) sm.weight[i] = left_of(key_of(value(bits)), sm.weight[i]);
   }
   __syncthreads();
   const float least = cut.key ? logit_of(cut.key) : -INFINITY;
   auto kept = [&](uint64_t before) { return before < cut.count ? before : cut.count; };
-  auto small_weight = [&](uint32_t bits) -> uint64_t {
-    const uint32_t key = key_of(value(bits));
-    return (split ? key > cut.key : key >= cut.key) ? s.w.kept(value(bits)) : 0;
+  auto small_weight = [&](uint32_t bits) {
+    return left_of(key_of(value(bits)), s.w.of(value(bits)));
   };
   each_piece([&](const uint32_t (&words)[4], int q) {
     uint64_t sum = 0;
-    uint32_t equal = 0;
     bool some = true;
     if (cut.key) {
       float most = -INFINITY;
@@ -1157,36 +1175,30 @@ __global__ __launch_bounds__(kThreads) void sample_row_kernel(SampleArgs a, int6
       some = __builtin_amdgcn_ballot_w64(most >= least) != 0;
     }
     if (some) {
-      bool small = false;
+      s16x2 most = {-1, -1};
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const uint32_t bits = bits_of(words, e);
-        const int off = off_of(bits);
-        sum += sm.weight[entry_of(bits, off)];
-        small |= off >= kSide;
+      for (int w = 0; w < 4; ++w) {
+        s16x2 off;
+        const uint32_t at = entries_of(words[w], off);
+        most = __builtin_elementwise_max(most, off);
+        sum += *(const uint64_t*)((const char*)sm.weight + (at & 0xffffu));
+        sum += *(const uint64_t*)((const char*)sm.weight + (at >> 16));
       }
-      if (small) each_small_of(words, [&](uint32_t bits, int) { sum += small_weight(bits); });
-      if (split) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) equal += value(bits_of(words, e)) == least ? 1 : 0;
-        equal = (uint32_t)wave_sum_u64_dpp(equal);
-      }
+      if (any_small(most))
+        each_small_of(words, [&](uint32_t bits, int) { sum += small_weight(bits); });
       sum = wave_sum_u64_dpp(sum);
     }
-    if (lane == 0) {
-      sm.piece_sum[q] = sum;
-      sm.piece_equal[q] = equal;
-    }
+    if (lane == 0) sm.piece_sum[q] = sum;
   });
   __syncthreads();
   // two pieces a thread
   const int qa = 2 * (int)threadIdx.x, qb = qa + 1;
-  const uint64_t ea = split && qa < pieces ? sm.piece_equal[qa] : 0;
-  const uint64_t eb = split && qb < pieces ? sm.piece_equal[qb] : 0;
+  const uint64_t pa = qa < pieces ? sm.piece_sum[qa] : 0, pb = qb < pieces ? sm.piece_sum[qb] : 0;
+  const uint64_t ea = pa >> kSameBit, eb = pb >> kSameBit;
   const uint64_t equal_end = split ? block_up_to(sm.pick, ea + eb) : 0, equal_mid = equal_end - eb;
   const uint64_t equal_begin = equal_mid - ea;
-  const uint64_t ma = (qa < pieces ? sm.piece_sum[qa] : 0) + (kept(equal_mid) - kept(equal_begin)) * w_cut;
-  const uint64_t mb = (qb < pieces ? sm.piece_sum[qb] : 0) + (kept(equal_end) - kept(equal_mid)) * w_cut;
+  const uint64_t ma = (pa & (kSame - 1)) + (kept(equal_mid) - kept(equal_begin)) * w_cut;
+  const uint64_t mb = (pb & (kSame - 1)) + (kept(equal_end) - kept(equal_mid)) * w_cut;
   const uint64_t end = block_up_to(sm.pick, ma + mb), mid = end - mb, begin = mid - ma;
   uint64_t total = 0;
 #pragma unroll
@@ -1209,14 +1221,14 @@ __global__ __launch_bounds__(kThreads) void sample_row_kernel(SampleArgs a, int6
   for (int e = 0; e < 8; ++e) {
     const uint32_t bits = bits_of(words, e);
     const int off = off_of(bits);
-    mine[e] = off >= kSide ? small_weight(bits) : sm.weight[entry_of(bits, off)];
-    n_same += split && value(bits) == least ? 1 : 0;
+    const int entry = (int)(bits >> 15) * (kSide + 1) + (int)min((uint32_t)off, (uint32_t)kSide);
+    mine[e] = off >= kSide ? small_weight(bits) : sm.weight[entry];
+    n_same += (uint32_t)(mine[e] >> kSameBit);
   }
   uint64_t same = sm.found_count + wave_up_to(n_same, lane) - n_same;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
-    const uint32_t bits = bits_of(words, e);
-    if (split && value(bits) == least && same++ < cut.count) mine[e] = w_cut;
+    if (mine[e] >> kSameBit) mine[e] = same++ < cut.count ? w_cut : 0;
     all += mine[e];
   }
   uint64_t run = sm.found_before + wave_up_to(all, lane) - all;

@@ -89,6 +89,20 @@ __device__ __forceinline__ int64_t block_before(int64_t* sums, int64_t v, int64_
   return before;
 }
 
+// units, items: of shared_steps_kernel (with the groups' where it has those too).
+__device__ __forceinline__ void finish_totals(const SharedArgs& x, Totals t, int64_t units,
+                                              int64_t items) {
+  // (Offsets that do not ascend may name tokens or sequences twice.)
+  t.bad |= items > x.steps_items;
+  if (t.bad) t.group_units = units = 0;
+  t.seq_units = units;
+  const int64_t w = (t.group_units + kWideWorkers - 1) / kWideWorkers;
+  const int64_t n = (units + x.steps_workers - 1) / x.steps_workers;
+  t.wide_per = w > kWideLeast ? w : kWideLeast;
+  t.steps_per = n > kStepsLeast ? n : kStepsLeast;
+  *x.totals = t;
+}
+
 __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(SharedArgs x) {
   __shared__ int64_t sums[kPlanThreads / kWave];
   const AttendArgs& a = x.a;
@@ -168,17 +182,125 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(SharedArgs x)
     units += all_u;
     items += all_it;
   }
-  if (tid == 0) {
-    t.seq_units = units;     // (with the groups' where shared_steps_kernel has those too)
-    // (Offsets that do not ascend may name tokens or sequences twice.)
-    t.bad |= items > x.steps_items;
-    if (t.bad) t.group_units = t.seq_units = units = 0;
-    const int64_t w = (t.group_units + kWideWorkers - 1) / kWideWorkers;
-    const int64_t n = (units + x.steps_workers - 1) / x.steps_workers;
-    t.wide_per = w > kWideLeast ? w : kWideLeast;
-    t.steps_per = n > kStepsLeast ? n : kStepsLeast;
-    *x.totals = t;
+  if (tid == 0) finish_totals(x, t, units, items);
+}
+
+// The same for up to 256 sequences and groups, a thread each, with one round trip to
+// memory and back (of 8.4 us, the other's, most is its seven).
+constexpr int kFewThreads = 256;
+__global__ __launch_bounds__(kFewThreads) void shared_plan_few_kernel(SharedArgs x) {
+  constexpr int W = kFewThreads / kWave;
+  __shared__ int g_first[kFewThreads + 1], g_pages[kFewThreads];
+  __shared__ int s_first[kFewThreads], s_end[kFewThreads];
+  __shared__ int64_t units_of[W];
+  __shared__ int64_t items_of[W];
+  const AttendArgs& a = x.a;
+  const int S = a.tk.S, P = a.pg.P, G = a.Hq / a.pg.Hkv, n_groups = x.n_groups;
+  const int t = threadIdx.x, lane = t % kWave, wave = t / kWave;
+  int first = 0, n = 0, length = 0;
+  if (t < S) {
+    length = a.lengths[t];
+    if (a.tk.cu) {
+      first = min(max(a.tk.cu[t], 0), a.tk.T);
+      n = max(min(max(a.tk.cu[t + 1], 0), a.tk.T) - first, 0);
+    } else {
+      n = a.tk.each;
+      first = t * n;
+    }
   }
+  s_first[t] = first;
+  s_end[t] = first + n;
+  if (n_groups > 0) {
+    if (t <= n_groups) g_first[t] = min(max(x.group_seqs[t], 0), S);
+    if (t == 0 && n_groups == kFewThreads) g_first[n_groups] = min(max(x.group_seqs[n_groups], 0), S);
+    if (t < n_groups) g_pages[t] = min(max(x.shared_pages[t], 0), a.pg.max_pages);
+  }
+  __syncthreads();
+  // a sequence's group, if any
+  int group = -1;
+  if (t < S && n_groups > 0) {
+    int lo = 0, hi = n_groups - 1;
+    while (lo < hi) {
+      const int mid = (lo + hi + 1) / 2;
+      if (g_first[mid] <= t) lo = mid; else hi = mid - 1;
+    }
+    if (g_first[lo] <= t && t < g_first[lo + 1]) group = lo;
+    if (group >= 0 && n > 0) atomicMin(&g_pages[group], max(length - n, 0) / P);
+  }
+  __syncthreads();
+  GroupInfo gi{};
+  if (t < n_groups) {
+    const int b = g_first[t], e = g_first[t + 1];
+    if (b < e) {
+      gi.first = s_first[b];
+      gi.pages = g_pages[t];
+      gi.lead = b;
+      gi.n = gi.pages > 0 ? max(s_end[e - 1] - gi.first, 0) : 0;
+    }
+  }
+  SeqInfo si{};
+  si.group = group >= 0 && g_pages[group] > 0 ? group : -1;
+  si.key0 = si.group >= 0 ? g_pages[group] * P : 0;
+  si.first = first;
+  si.n = n;
+  auto sum_before = [&](int64_t& u, int64_t& it, int64_t& all_u, int64_t& all_it) {
+    int64_t uu = u, ii = it;
+#pragma unroll
+    for (int o = 1; o < kWave; o <<= 1) {
+      const int64_t a1 = __shfl_up(uu, o), a2 = __shfl_up(ii, o);
+      if (lane >= o) {
+        uu += a1;
+        ii += a2;
+      }
+    }
+    __syncthreads();
+    if (lane == kWave - 1) {
+      units_of[wave] = uu;
+      items_of[wave] = ii;
+    }
+    __syncthreads();
+    u = uu - u;
+    it = ii - it;
+    all_u = all_it = 0;
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+      if (w < wave) {
+        u += units_of[w];
+        it += items_of[w];
+      }
+      all_u += units_of[w];
+      all_it += items_of[w];
+    }
+  };
+  const int tile = x.wide_rows ? x.wide_rows : x.steps_rows;
+  int64_t units, items, all_u, all_it;
+  {
+    const int64_t keys = (int64_t)gi.pages * P;
+    items = ((int64_t)gi.n * G + tile - 1) / tile * a.pg.Hkv;
+    units = items * (x.wide_rows ? (keys + kWideKeys - 1) / kWideKeys + kWideCost
+                                 : keys / kKeys + kStepsCost);
+  }
+  sum_before(units, items, all_u, all_it);
+  gi.unit = units;
+  gi.item = (int)items;
+  Totals total{};
+  total.group_units = all_u;
+  int64_t base_u = all_u, base_it = all_it;
+  if (x.wide_rows) {
+    total.bad = all_it > x.wide_items;
+    base_u = base_it = 0;
+  }
+  {
+    const int64_t keys = min((int64_t)max(length, 0), (int64_t)a.pg.max_pages * P);
+    items = ((int64_t)n * G + x.steps_rows - 1) / x.steps_rows * a.pg.Hkv;
+    units = items * ((max(keys - si.key0, (int64_t)0) + kKeys - 1) / kKeys + kStepsCost);
+  }
+  sum_before(units, items, all_u, all_it);
+  si.unit = base_u + units;
+  si.item = (int)(base_it + items);
+  if (t < n_groups) x.groups[t] = gi;
+  if (t < S) x.seqs[t] = si;
+  if (t == 0) finish_totals(x, total, base_u + all_u, base_it + all_it);
 }
 
 // The last of n elements of a list whose unit is at most u.
@@ -239,18 +361,14 @@ __device__ __forceinline__ uint32_t pack_half2(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, __builtin_convertvector(x, half2));
 }
 
+// Rows of 272 bytes for a key, of 264 for a dim: the lanes of a read, a row each, then
+// lie at banks of their own, and all of a wave's reads have one address and constant
+// offsets from it.
+constexpr int kKeyPitch = kHeadDim * 2 + 16, kDimPitch = kWideKeys * 2 + 8;
 struct __attribute__((aligned(16))) WideSmem {
-  uint8_t k[2][kWideKeys * kHeadDim * 2];
-  uint8_t v[2][kWideKeys * kHeadDim * 2];
+  uint8_t k[2][kWideKeys * kKeyPitch];
+  uint8_t v[2][kHeadDim * kDimPitch];
 };
-// Bytes of 16 (8 dims) of a key, and of 8 (4 keys) of a dim: rows of 256 bytes, the
-// pieces of neighbouring rows at other banks.
-__device__ __forceinline__ int k_at(int key, int piece) {
-  return key * (kHeadDim * 2) + ((piece ^ (key & 15)) << 4);
-}
-__device__ __forceinline__ int v_at(int dim, int piece) {
-  return dim * (kWideKeys * 2) + ((piece ^ (((dim ^ (dim >> 3)) & 15) | (dim & 16))) << 3);
-}
 
 template <int FMT, int P, int RW>
 __global__ __launch_bounds__(kWideThreads, 2) void shared_wide_kernel(SharedArgs x) {
@@ -299,43 +417,43 @@ __global__ __launch_bounds__(kWideThreads, 2) void shared_wide_kernel(SharedArgs
 #pragma unroll
       for (int r = 0; r < 16; ++r) o[m][r] = 0.0f;
 
-    // the page of a step's 64 keys number `half`, -1 for none
-    auto page_of = [&](int st, int half) -> int {
-      const int key = st * kWideKeys + 64 * half;
-      if (st >= st1 || key >= q.pages * P) return -1;
-      const int p = entry(a.pg.table, table_row + key / P);
-      return (unsigned)p < (unsigned)a.pg.n_pages ? p : -1;
+    // the page of a step's 64 keys number `half`, -1 for none; its first of those keys
+    const int keys = q.pages * P;
+    auto number_of = [&](int st, int half) -> int {
+      const int64_t key = min((int64_t)st * kWideKeys + 64 * half, (int64_t)keys - 64);
+      return entry(a.pg.table, table_row + key / P);
     };
-    uint4 kr[2];
-    uint2 vr[4];
-    auto load = [&](int st, int p0, int p1) {
-      const int t = threadIdx.x;
+    auto page_of = [&](int number, int st, int half) -> int {
+      const bool in = st < st1 && st * kWideKeys + 64 * half < keys;
+      return in && (unsigned)number < (unsigned)a.pg.n_pages ? number : -1;
+    };
+    auto rows_of = [&](const uint8_t* base, int page, int half) -> const uint8_t* {
+      const int first = P == kWideKeys ? 64 * half : 0;
+      return base + (((int64_t)page * a.pg.Hkv + kvh) * P + first) * kHeadDim;
+    };
+    // K: a thread has 16 dims of a key of each half; V: 8 dims of 4 keys of its wave's half
+    const uint32_t k_off = threadIdx.x * 16, v_off = (uint32_t)(lane / 16 * 4 * kHeadDim + 8 * (lane % 16));
+    const int v_half = wave / 4;
+    uint4 kr[2] = {};
+    uint2 vr[4] = {};
+    auto load = [&](int p0, int p1) {
+      if (p0 >= 0) kr[0] = *(const uint4*)(rows_of(a.pg.k, p0, 0) + k_off);
+      if (p1 >= 0) kr[1] = *(const uint4*)(rows_of(a.pg.k, p1, 1) + k_off);
+      const int page = v_half ? p1 : p0;
+      if (page >= 0) {
+        const uint8_t* v = rows_of(a.pg.v, page, v_half) + wave % 4 * 16 * kHeadDim;
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        const int page = half ? p1 : p0, key = 64 * half + t / 8;
-        kr[half] = make_uint4(0u, 0u, 0u, 0u);
-        if (page >= 0)
-          kr[half] = *(const uint4*)(a.pg.k + (((int64_t)page * a.pg.Hkv + kvh) * P +
-                                               (st * kWideKeys + key) % P) * kHeadDim + 16 * (t % 8));
-      }
-      const int piece = t / 16, page = piece / 16 ? p1 : p0;
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        vr[r] = make_uint2(0u, 0u);
-        if (page >= 0)
-          vr[r] = *(const uint2*)(a.pg.v + (((int64_t)page * a.pg.Hkv + kvh) * P +
-                                            (st * kWideKeys + 4 * piece + r) % P) * kHeadDim + 8 * (t % 16));
+        for (int r = 0; r < 4; ++r) vr[r] = *(const uint2*)(v + v_off + r * kHeadDim);
       }
     };
     auto stage = [&](int buf) {
-      const int t = threadIdx.x;
+      uint8_t* k_to = sm.k[buf] + threadIdx.x / 8 * kKeyPitch + threadIdx.x % 8 * 32;
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        const int key = 64 * half + t / 8;
-        *(bf16x8*)&sm.k[buf][k_at(key, 2 * (t % 8))] = widen8<FMT>(kr[half].x, kr[half].y);
-        *(bf16x8*)&sm.k[buf][k_at(key, 2 * (t % 8) + 1)] = widen8<FMT>(kr[half].z, kr[half].w);
+        *(bf16x8*)(k_to + 64 * half * kKeyPitch) = widen8<FMT>(kr[half].x, kr[half].y);
+        *(bf16x8*)(k_to + 64 * half * kKeyPitch + 16) = widen8<FMT>(kr[half].z, kr[half].w);
       }
-      const int piece = t / 16, d0 = 8 * (t % 16);
+      uint8_t* v_to = sm.v[buf] + threadIdx.x % 16 * 8 * kDimPitch + threadIdx.x / 16 * 8;
 #pragma unroll
       for (int word = 0; word < 2; ++word) {
         uint32_t pr[2][2];      // [keys 0-1, 2-3][dims 0-1, 2-3]: bytes of two keys side by side
@@ -348,47 +466,50 @@ __global__ __launch_bounds__(kWideThreads, 2) void shared_wide_kernel(SharedArgs
         }
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          const int d = d0 + 4 * word + 2 * i;
-          *(uint2*)&sm.v[buf][v_at(d, piece)] =
-              make_uint2(half2_of<FMT, false>(pr[0][i]), half2_of<FMT, false>(pr[1][i]));
-          *(uint2*)&sm.v[buf][v_at(d + 1, piece)] =
+          uint8_t* to = v_to + (4 * word + 2 * i) * kDimPitch;
+          *(uint2*)to = make_uint2(half2_of<FMT, false>(pr[0][i]), half2_of<FMT, false>(pr[1][i]));
+          *(uint2*)(to + kDimPitch) =
               make_uint2(half2_of<FMT, true>(pr[0][i]), half2_of<FMT, true>(pr[1][i]));
         }
       }
     };
 
     const int my_half = kw * (32 * KT) / 64;
-    auto compute = [&](int buf, int page) {
-      const int64_t sc = (int64_t)page * a.pg.Hkv + kvh;
-      const float kf = entry(a.pg.ks, sc) * a.sc_log2, vf = entry(a.pg.vs, sc);
-      // V's scale as significand * 2^exponent (zeros, infinities and NaN: 2^0)
-      const uint32_t vb = __float_as_uint(vf), ve = vb >> 23 & 0xffu;
-      const bool normal = ve != 0 && ve != 0xffu;
-      const float E = normal ? (float)((int)ve - 127) : 0.0f;
-      const float sig = normal ? __uint_as_float((vb & 0x807fffffu) | 0x3f800000u) : vf;
-      const float unit = normal ? __uint_as_float((ve == 254u ? 1u : 254u - ve) << 23) : 1.0f;
+    auto scale_at = [&](int page) { return page < 0 ? 0 : (int64_t)page * a.pg.Hkv + kvh; };
+    // (where there is no page any scale will do, but a cache of none has no scales)
+    const float* const some = (const float*)a.lengths;
+    const float* const k_scales = a.pg.n_pages ? a.pg.ks : some;
+    const float* const v_scales = a.pg.n_pages ? a.pg.vs : some;
+    auto compute = [&](int buf, float k_scale, float vf) {
+      const float kf = k_scale * a.sc_log2;
+      // V's scale as sig * 2^E (E = 0 for zeros, infinities and NaN), unit = 2^-E
+      const int ve = (int)(__float_as_uint(vf) >> 23 & 0xffu);
+      const int ce = ve == 0 || ve == 0xff ? 127 : min(ve, 253);
+      const float E = (float)(ce - 127), unit = __uint_as_float((uint32_t)(254 - ce) << 23);
+      const float sig = vf * unit;
       f32x16 s[KT];
 #pragma unroll
-      for (int t = 0; t < KT; ++t) {
+      for (int t = 0; t < KT; ++t)
 #pragma unroll
         for (int r = 0; r < 16; ++r) s[t][r] = 0.0f;
-        const int key = 32 * (KT * kw + t) + j;
+      const uint8_t* k_at = sm.k[buf] + (32 * KT * kw + j) * kKeyPitch + 16 * h;
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {
-          const bf16x8 kk = *(const bf16x8*)&sm.k[buf][k_at(key, 2 * c + h)];
-          s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kk, qf[c], s[t], 0, 0, 0);
-        }
-      }
+      for (int c = 0; c < 8; ++c)
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+          s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+              *(const bf16x8*)(k_at + 32 * t * kKeyPitch + 32 * c), qf[c], s[t], 0, 0, 0);
       float e[KT][16], sum;
       auto probs = [&](float c) {
-        sum = 0.0f;
+        float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
 #pragma unroll
         for (int t = 0; t < KT; ++t)
 #pragma unroll
           for (int r = 0; r < 16; ++r) {
             e[t][r] = __builtin_amdgcn_exp2f(fmaf(s[t][r], kf, c));
-            sum += e[t][r];
+            part[r % 4] += e[t][r];
           }
+        sum = (part[0] + part[1]) + (part[2] + part[3]);
       };
       probs(E - M);
       if (__builtin_amdgcn_ballot_w64(!(sum <= kWideLimit)) != 0) {
@@ -413,6 +534,7 @@ __global__ __launch_bounds__(kWideThreads, 2) void shared_wide_kernel(SharedArgs
 #pragma unroll
           for (int r = 0; r < 16; ++r) e[t][r] *= sig;
       }
+      const uint8_t* v_at = sm.v[buf] + j * kDimPitch + 64 * KT * kw + 8 * h;
 #pragma unroll
       for (int t = 0; t < KT; ++t)
 #pragma unroll
@@ -422,28 +544,32 @@ __global__ __launch_bounds__(kWideThreads, 2) void shared_wide_kernel(SharedArgs
                                 pack_half2(e[t][8 * c + 2], e[t][8 * c + 3]),
                                 pack_half2(e[t][8 * c + 4], e[t][8 * c + 5]),
                                 pack_half2(e[t][8 * c + 6], e[t][8 * c + 7])));
-          const int piece = 8 * (KT * kw + t) + 4 * c + h;
 #pragma unroll
           for (int m = 0; m < 4; ++m) {
-            const uint2 lo = *(const uint2*)&sm.v[buf][v_at(32 * m + j, piece)];
-            const uint2 hi = *(const uint2*)&sm.v[buf][v_at(32 * m + j, piece + 2)];
+            const uint2 lo = *(const uint2*)(v_at + 32 * m * kDimPitch + 64 * t + 32 * c);
+            const uint2 hi = *(const uint2*)(v_at + 32 * m * kDimPitch + 64 * t + 32 * c + 16);
             o[m] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
                 __builtin_bit_cast(half8, make_uint4(lo.x, lo.y, hi.x, hi.y)), p, o[m], 0, 0, 0);
           }
         }
     };
 
-    int p0 = page_of(st0, 0), p1 = page_of(st0, 1), buf = 0;
-    load(st0, p0, p1);
+    // Pages are looked up two steps ahead, scales one.
+    int p0 = page_of(number_of(st0, 0), st0, 0), p1 = page_of(number_of(st0, 1), st0, 1), buf = 0;
+    int n0 = number_of(st0 + 1, 0), n1 = number_of(st0 + 1, 1);
+    load(p0, p1);
     for (int st = st0; st < st1; ++st, buf ^= 1) {
-      stage(buf);
       const int mine = my_half ? p1 : p0;
-      p0 = page_of(st + 1, 0);
-      p1 = page_of(st + 1, 1);
-      load(st + 1, p0, p1);
+      const float ks = entry(k_scales, scale_at(mine)), vs = entry(v_scales, scale_at(mine));
+      p0 = page_of(n0, st + 1, 0);
+      p1 = page_of(n1, st + 1, 1);
+      n0 = number_of(st + 2, 0);
+      n1 = number_of(st + 2, 1);
+      stage(buf);
+      load(p0, p1);
       // (the buffer before was read before the last barrier but one: two suffice)
       __syncthreads();
-      if (mine >= 0) compute(buf, mine);
+      if (mine >= 0) compute(buf, ks, vs);
     }
     l += __shfl_xor(l, 32);
     // the sums of the waves with the same rows, by halves
@@ -553,9 +679,10 @@ __global__ __launch_bounds__(kThreads, attend_occupancy(RT)) void shared_steps_k
 }
 
 // ----------------------------------------------------------------------------
-// A row's parts: 32 lanes, four dims each.  A workgroup has 8 heads of a token.
+// A row's parts: a wave, 16 lanes with eight dims each for every fourth part, the
+// fours then joined in order.  A workgroup has 4 heads of a token.
 // ----------------------------------------------------------------------------
-constexpr int kJoinRows = kThreads / 32;
+constexpr int kJoinRows = kWaves;
 
 struct RowParts {       // parts `first` .. `first` + n - 1 of a row, `pitch` rows apart
   const Part* ml;
@@ -568,7 +695,9 @@ __global__ __launch_bounds__(kThreads) void shared_join_kernel(SharedArgs x, int
   const AttendArgs& a = x.a;
   const int G = a.Hq / a.pg.Hkv, blocks = (a.Hq + kJoinRows - 1) / kJoinRows;
   const int64_t unit = unit0 + blockIdx.x;
-  const int t = (int)(unit / blocks), head = (int)(unit % blocks) * kJoinRows + threadIdx.x / 32;
+  const int t = (int)(unit / blocks);
+  const int head = (int)(unit % blocks) * kJoinRows +
+                   __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   int s = 0;
   if (!a.tk.cu) {
     s = t / a.tk.each;
@@ -582,7 +711,7 @@ __global__ __launch_bounds__(kThreads) void shared_join_kernel(SharedArgs x, int
   const SeqInfo q = info_at(x.seqs, s);
   if (t < q.first || t >= q.first + q.n || entry(&x.totals->bad, 0)) return;
   if (head >= a.Hq) return;
-  const int kvh = head / G, d = threadIdx.x % 32 * 4;
+  const int kvh = head / G, lane = threadIdx.x % kWave, d = lane % 16 * 8, stripe = lane / 16;
   // the parts of an item whose units are [begin, begin + whole): its workers' slots
   auto parts_of = [&](const Part* ml, const float* o, int tile_rows, int64_t unit, int item, int n,
                       int row, int whole, int64_t per) {
@@ -610,38 +739,53 @@ __global__ __launch_bounds__(kThreads) void shared_join_kernel(SharedArgs x, int
           : parts_of(a.part_ml, a.part_o, x.steps_rows, g.unit, g.item, g.n, row,
                      (int)(gkeys / kKeys) + kStepsCost, steps_per);
   }
-  float m = -INFINITY, l = 0.0f;
-  float4 acc = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-  constexpr int kAhead = 4;
+  float m = -INFINITY, l = 0.0f, acc[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) acc[i] = 0.0f;
+  auto add = [&](float m2, float l2, const float (&v)[8]) {
+    const float mn = fmaxf(m, m2);
+    const float f = m == mn ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
+    const float g = m2 == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m2 - mn);
+    l = l * f + l2 * g;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) acc[i] = acc[i] * f + v[i] * g;
+    m = mn;
+  };
+  constexpr int kAhead = 3;
   const int all = common.n + own.n;
-  for (int p0 = 0; p0 < all; p0 += kAhead) {
+  for (int p0 = stripe; p0 < all; p0 += 4 * kAhead) {
     Part ml[kAhead];
-    float4 v[kAhead];
+    float4 v[kAhead][2];
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
-      const int p = min(p0 + k, all - 1);
+      const int p = min(p0 + 4 * k, all - 1);
       const RowParts& r = p < common.n ? common : own;
       const int64_t at = r.first + (int64_t)(p < common.n ? p : p - common.n) * r.pitch;
       ml[k] = r.ml[at];
-      v[k] = *(const float4*)(r.o + at * kHeadDim + d);
+      v[k][0] = *(const float4*)(r.o + at * kHeadDim + d);
+      v[k][1] = *(const float4*)(r.o + at * kHeadDim + d + 4);
     }
 #pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      if (p0 + k >= all) break;
-      const float mn = fmaxf(m, ml[k].m);
-      const float f = m == mn ? 1.0f : __builtin_amdgcn_exp2f(m - mn);
-      const float g = ml[k].m == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(ml[k].m - mn);
-      l = l * f + ml[k].l * g;
-      acc.x = acc.x * f + v[k].x * g;
-      acc.y = acc.y * f + v[k].y * g;
-      acc.z = acc.z * f + v[k].z * g;
-      acc.w = acc.w * f + v[k].w * g;
-      m = mn;
-    }
+    for (int k = 0; k < kAhead; ++k)
+      if (p0 + 4 * k < all) {
+        const float x[8] = {v[k][0].x, v[k][0].y, v[k][0].z, v[k][0].w,
+                            v[k][1].x, v[k][1].y, v[k][1].z, v[k][1].w};
+        add(ml[k].m, ml[k].l, x);
+      }
+  }
+#pragma unroll
+  for (int o = 16; o <= 32; o <<= 1) {
+    const float m2 = __shfl_xor(m, o), l2 = __shfl_xor(l, o);
+    float v[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = __shfl_xor(acc[i], o);
+    add(m2, l2, v);
   }
   const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-  *(uint2*)(a.o + ((int64_t)head * a.tk.T + t) * kHeadDim + d) =
-      make_uint2(pack_bf16x2(acc.x * inv, acc.y * inv), pack_bf16x2(acc.z * inv, acc.w * inv));
+  if (stripe == 0)
+    *(uint4*)(a.o + ((int64_t)head * a.tk.T + t) * kHeadDim + d) =
+        make_uint4(pack_bf16x2(acc[0] * inv, acc[1] * inv), pack_bf16x2(acc[2] * inv, acc[3] * inv),
+                   pack_bf16x2(acc[4] * inv, acc[5] * inv), pack_bf16x2(acc[6] * inv, acc[7] * inv));
 }
 
 // ----------------------------------------------------------------------------
@@ -689,7 +833,10 @@ SharedPlan shared_plan(int Hq, int n_tokens, int n_seqs, int n_groups, int max_p
 
 template <int FMT, int P>
 void launch_shared(const SharedPlan& pl, const SharedArgs& x, hipStream_t stream) {
-  hipLaunchKernelGGL(shared_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, x);
+  if (x.a.tk.S <= kFewThreads && x.n_groups <= kFewThreads)
+    hipLaunchKernelGGL(shared_plan_few_kernel, dim3(1), dim3(kFewThreads), 0, stream, x);
+  else
+    hipLaunchKernelGGL(shared_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, x);
   if (pl.wide_rows == 128)
     hipLaunchKernelGGL((shared_wide_kernel<FMT, P, 4>), dim3(kWideWorkers), dim3(kWideThreads), 0,
                        stream, x);

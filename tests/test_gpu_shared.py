@@ -148,6 +148,17 @@ def test_lengths_of_the_shared_part(pages):
     Batch([3], [pages], [70] * 3, [1] * 3, 4, 1, 64, E4M3, seed=pages).check()
 
 
+@pytest.mark.parametrize("groups,size", [(1, 257), (256, 1), (257, 1), (300, 4), (255, 1), (2, 128)])
+def test_many_sequences_and_groups(groups, size):
+    """More than a thread each of the smaller plan has, and as many."""
+    S = groups * size
+    b = Batch([size] * groups, [1 + g % 2 for g in range(groups)], [1 + i % 70 for i in range(S)],
+              [1] * S, 2, 1, 64, E4M3, seed=groups)
+    b.check()
+    b.group_seqs, b.shared = b.group_seqs[:groups // 2 + 1], b.shared[:groups // 2]
+    b.check()
+
+
 def test_many_rows_of_one_sequence():
     """A group of one: its new tokens read what lies before them once."""
     Batch([1, 1], [20, 0], [300, 64], [257, 64], 8, 2, 64, E4M3, seed=3).check()

@@ -409,6 +409,9 @@ __global__ __launch_bounds__(kWideThreads, 2) void shared_wide_kernel(SharedArgs
 #pragma unroll
       for (int c = 0; c < 8; ++c)
         qf[c] = __builtin_bit_cast(bf16x8, *(const uint4*)(qp + 16 * c + 8 * h));
+      // (waited for here: in the loop a wait for them is one for the codes on their way)
+#pragma unroll
+      for (int c = 0; c < 8; ++c) asm volatile("" : "+v"(qf[c]));
     }
     float M = -INFINITY, l = 0.0f;
     f32x16 o[4];
@@ -431,9 +434,14 @@ __global__ __launch_bounds__(kWideThreads, 2) void shared_wide_kernel(SharedArgs
       const int first = P == kWideKeys ? 64 * half : 0;
       return base + (((int64_t)page * a.pg.Hkv + kvh) * P + first) * kHeadDim;
     };
-    // K: a thread has 16 dims of a key of each half; V: 8 dims of 4 keys of its wave's half
-    const uint32_t k_off = threadIdx.x * 16, v_off = (uint32_t)(lane / 16 * 4 * kHeadDim + 8 * (lane % 16));
-    const int v_half = wave / 4;
+    // K: a thread has 16 dims of a key of each half.  V: 8 dims (number v_dims) of 4 keys
+    // (number v_keys); a wave has 32 keys and 64 dims, the 32 lanes that write together
+    // 4 by 8 of them, each at banks of its own (with 2 by 16 a step took 1500 of 6500
+    // cycles more).
+    const uint32_t k_off = threadIdx.x * 16;
+    const int v_dims = 8 * (wave & 1) + (lane & 3) + 4 * (lane >> 5), v_half = wave / 4;
+    const int v_keys = 8 * (wave >> 1) + (lane >> 2 & 7);
+    const uint32_t v_off = (uint32_t)((v_keys & 15) * 4 * kHeadDim + 8 * v_dims);
     uint4 kr[2] = {};
     uint2 vr[4] = {};
     auto load = [&](int p0, int p1) {
@@ -441,7 +449,7 @@ __global__ __launch_bounds__(kWideThreads, 2) void shared_wide_kernel(SharedArgs
       if (p1 >= 0) kr[1] = *(const uint4*)(rows_of(a.pg.k, p1, 1) + k_off);
       const int page = v_half ? p1 : p0;
       if (page >= 0) {
-        const uint8_t* v = rows_of(a.pg.v, page, v_half) + wave % 4 * 16 * kHeadDim;
+        const uint8_t* v = rows_of(a.pg.v, page, v_half);
 #pragma unroll
         for (int r = 0; r < 4; ++r) vr[r] = *(const uint2*)(v + v_off + r * kHeadDim);
       }
@@ -453,7 +461,7 @@ __global__ __launch_bounds__(kWideThreads, 2) void shared_wide_kernel(SharedArgs
         *(bf16x8*)(k_to + 64 * half * kKeyPitch) = widen8<FMT>(kr[half].x, kr[half].y);
         *(bf16x8*)(k_to + 64 * half * kKeyPitch + 16) = widen8<FMT>(kr[half].z, kr[half].w);
       }
-      uint8_t* v_to = sm.v[buf] + threadIdx.x % 16 * 8 * kDimPitch + threadIdx.x / 16 * 8;
+      uint8_t* v_to = sm.v[buf] + v_dims * 8 * kDimPitch + v_keys * 8;
 #pragma unroll
       for (int word = 0; word < 2; ++word) {
         uint32_t pr[2][2];      // [keys 0-1, 2-3][dims 0-1, 2-3]: bytes of two keys side by side
@@ -480,25 +488,36 @@ __global__ __launch_bounds__(kWideThreads, 2) void shared_wide_kernel(SharedArgs
     const float* const some = (const float*)a.lengths;
     const float* const k_scales = a.pg.n_pages ? a.pg.ks : some;
     const float* const v_scales = a.pg.n_pages ? a.pg.vs : some;
-    auto compute = [&](int buf, float k_scale, float vf) {
+    f32x16 s[KT];
+    auto scores = [&](int buf) {
+#pragma unroll
+      for (int t = 0; t < KT; ++t)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) s[t][r] = 0.0f;
+      const uint8_t* k_at = sm.k[buf] + (32 * KT * kw + j) * kKeyPitch + 16 * h;
+      bf16x8 kk[2][KT];
+      auto read = [&](int c) {
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+          kk[c & 1][t] = *(const bf16x8*)(k_at + 32 * t * kKeyPitch + 32 * c);
+      };
+      read(0);
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        if (c + 1 < 8) read(c + 1);
+        __builtin_amdgcn_sched_barrier(0);      // (an operand is on its way while one is used)
+#pragma unroll
+        for (int t = 0; t < KT; ++t)
+          s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kk[c & 1][t], qf[c], s[t], 0, 0, 0);
+      }
+    };
+    auto sums = [&](int buf, float k_scale, float vf) {
       const float kf = k_scale * a.sc_log2;
       // V's scale as sig * 2^E (E = 0 for zeros, infinities and NaN), unit = 2^-E
       const int ve = (int)(__float_as_uint(vf) >> 23 & 0xffu);
       const int ce = ve == 0 || ve == 0xff ? 127 : min(ve, 253);
       const float E = (float)(ce - 127), unit = __uint_as_float((uint32_t)(254 - ce) << 23);
       const float sig = vf * unit;
-      f32x16 s[KT];
-#pragma unroll
-      for (int t = 0; t < KT; ++t)
-#pragma unroll
-        for (int r = 0; r < 16; ++r) s[t][r] = 0.0f;
-      const uint8_t* k_at = sm.k[buf] + (32 * KT * kw + j) * kKeyPitch + 16 * h;
-#pragma unroll
-      for (int c = 0; c < 8; ++c)
-#pragma unroll
-        for (int t = 0; t < KT; ++t)
-          s[t] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-              *(const bf16x8*)(k_at + 32 * t * kKeyPitch + 32 * c), qf[c], s[t], 0, 0, 0);
       float e[KT][16], sum;
       auto probs = [&](float c) {
         float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -535,41 +554,69 @@ __global__ __launch_bounds__(kWideThreads, 2) void shared_wide_kernel(SharedArgs
           for (int r = 0; r < 16; ++r) e[t][r] *= sig;
       }
       const uint8_t* v_at = sm.v[buf] + j * kDimPitch + 64 * KT * kw + 8 * h;
+      uint2 vv[2][4][2];
+      auto read = [&](int i) {
 #pragma unroll
-      for (int t = 0; t < KT; ++t)
-#pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          const half8 p = __builtin_bit_cast(
-              half8, make_uint4(pack_half2(e[t][8 * c], e[t][8 * c + 1]),
-                                pack_half2(e[t][8 * c + 2], e[t][8 * c + 3]),
-                                pack_half2(e[t][8 * c + 4], e[t][8 * c + 5]),
-                                pack_half2(e[t][8 * c + 6], e[t][8 * c + 7])));
-#pragma unroll
-          for (int m = 0; m < 4; ++m) {
-            const uint2 lo = *(const uint2*)(v_at + 32 * m * kDimPitch + 64 * t + 32 * c);
-            const uint2 hi = *(const uint2*)(v_at + 32 * m * kDimPitch + 64 * t + 32 * c + 16);
-            o[m] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
-                __builtin_bit_cast(half8, make_uint4(lo.x, lo.y, hi.x, hi.y)), p, o[m], 0, 0, 0);
-          }
+        for (int m = 0; m < 4; ++m) {
+          vv[i & 1][m][0] = *(const uint2*)(v_at + 32 * m * kDimPitch + 32 * i);
+          vv[i & 1][m][1] = *(const uint2*)(v_at + 32 * m * kDimPitch + 32 * i + 16);
         }
+      };
+      read(0);
+#pragma unroll
+      for (int i = 0; i < 2 * KT; ++i) {       // 16 keys each
+        const float(&x)[16] = e[i / 2];
+        const int r = 8 * (i & 1);
+        const half8 p = __builtin_bit_cast(
+            half8, make_uint4(pack_half2(x[r], x[r + 1]), pack_half2(x[r + 2], x[r + 3]),
+                              pack_half2(x[r + 4], x[r + 5]), pack_half2(x[r + 6], x[r + 7])));
+        if (i + 1 < 2 * KT) read(i + 1);
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+          const uint2 lo = vv[i & 1][m][0], hi = vv[i & 1][m][1];
+          o[m] = __builtin_amdgcn_mfma_f32_32x32x16_f16(
+              __builtin_bit_cast(half8, make_uint4(lo.x, lo.y, hi.x, hi.y)), p, o[m], 0, 0, 0);
+        }
+      }
     };
 
-    // Pages are looked up two steps ahead, scales one.
+    // While the matrix cores multiply a step's K, its successor's codes, asked for one
+    // step earlier, are converted into the other buffer: that costs as much as the
+    // step's softmax (a step 6200 cycles with it before the barrier, not beside).  Pages
+    // are looked up two steps ahead, scales one.
     int p0 = page_of(number_of(st0, 0), st0, 0), p1 = page_of(number_of(st0, 1), st0, 1), buf = 0;
     int n0 = number_of(st0 + 1, 0), n1 = number_of(st0 + 1, 1);
     load(p0, p1);
-    for (int st = st0; st < st1; ++st, buf ^= 1) {
-      const int mine = my_half ? p1 : p0;
-      const float ks = entry(k_scales, scale_at(mine)), vs = entry(v_scales, scale_at(mine));
-      p0 = page_of(n0, st + 1, 0);
-      p1 = page_of(n1, st + 1, 1);
-      n0 = number_of(st + 2, 0);
-      n1 = number_of(st + 2, 1);
-      stage(buf);
+    int mine = my_half ? p1 : p0;
+    float ks = entry(k_scales, scale_at(mine)), vs = entry(v_scales, scale_at(mine));
+    p0 = page_of(n0, st0 + 1, 0);
+    p1 = page_of(n1, st0 + 1, 1);
+    n0 = number_of(st0 + 2, 0);
+    n1 = number_of(st0 + 2, 1);
+    if (st0 < st1) {
+      stage(0);
       load(p0, p1);
-      // (the buffer before was read before the last barrier but one: two suffice)
-      __syncthreads();
-      if (mine >= 0) compute(buf, ks, vs);
+    }
+    for (int st = st0; st < st1; ++st, buf ^= 1) {
+      __syncthreads();      // (this step's codes are there; the other buffer has been read)
+      const int next = my_half ? p1 : p0;
+      const float ks_next = entry(k_scales, scale_at(next)), vs_next = entry(v_scales, scale_at(next));
+      p0 = page_of(n0, st + 2, 0);
+      p1 = page_of(n1, st + 2, 1);
+      n0 = number_of(st + 3, 0);
+      n1 = number_of(st + 3, 1);
+      const bool early = wave < kWideWaves / 2;
+      if (mine >= 0 && early) scores(buf);
+      if (st + 1 < st1) {
+        stage(buf ^ 1);
+        load(p0, p1);
+      }
+      if (mine >= 0 && !early) scores(buf);
+      if (mine >= 0) sums(buf, ks, vs);
+      mine = next;
+      ks = ks_next;
+      vs = vs_next;
     }
     l += __shfl_xor(l, 32);
     // the sums of the waves with the same rows, by halves

@@ -7,10 +7,10 @@
 //  shared_plan_kernel   how many pages a group shares in earnest (none that a new
 //                       token of it lies in or before), and where the work of
 //                       groups and sequences starts
-//  shared_wide_kernel   groups' keys, where a group has many rows: tiles of 64 or
-//                       128 rows against keys in LDS
-//  shared_steps_kernel  sequences' keys (and groups', where they have few rows):
-//                       16 or 32 rows against keys in registers, as cache attention
+//  shared_wide_kernel   where a group has many rows: the groups' keys, tiles of 64
+//                       or 128 rows against keys in LDS, then the sequences' own keys
+//  shared_steps_kernel  where they have few, both: 16 or 32 rows against keys in
+//                       registers, as cache attention
 //  shared_join_kernel   a row's parts joined
 //
 // Work is counted in units, the items (rows of a group or sequence and a KV head)
@@ -27,11 +27,12 @@ constexpr int kWideThreads = 512;
 constexpr int kWideWaves = kWideThreads / kWave;
 constexpr int kWideKeys = 128;        // of a step
 constexpr int kWideWorkers = 256;     // one a CU
-constexpr int kWideCost = 1;          // units of an item before its steps
+constexpr int kWideCost = 1;          // units of an item before its steps, unless runs are whole
 constexpr int kWideLeast = 2;         // units of a run, at least
 constexpr int kStepsGroups = 512;     // workgroups, two a CU
+static_assert(kStepsGroups * kWaves == kWideWorkers * kWideWaves, "the same waves");
 constexpr int kStepsCost = 5;
-constexpr int kStepsLeast = 8;
+constexpr int kStepsLeast = 8;        // half of it where not a quarter of the waves would have one
 
 typedef _Float16 half8 __attribute__((ext_vector_type(8)));
 typedef _Float16 half2 __attribute__((ext_vector_type(2)));
@@ -40,7 +41,8 @@ typedef float f32x16 __attribute__((ext_vector_type(16)));
 struct Totals {
   int64_t wide_per, steps_per;       // units of a run
   int64_t group_units, seq_units;
-  int32_t bad, pad[7];               // lists that count more items than there is room for
+  int32_t bad;                       // lists that count more items than there is room for
+  int32_t wide_cost, pad[6];         // units of a wide item before its steps
 };
 struct GroupInfo {      // its shared keys; n = 0 where there are none
   int first, n, pages, lead;
@@ -67,6 +69,21 @@ struct SharedArgs {
   Part* wide_ml;
   float* wide_o;
 };
+
+// Steps of a group's items.
+__device__ __forceinline__ int64_t group_steps(const SharedArgs& x, int pages) {
+  const int64_t keys = (int64_t)pages * x.a.pg.P;
+  return x.wide_rows ? (keys + kWideKeys - 1) / kWideKeys : keys / kKeys;
+}
+// Whether items of so many steps are whole runs when all workers have the same: an item's
+// cost in units would then only push the runs off the items' ends.
+__device__ __forceinline__ bool whole_runs(int64_t units, int64_t steps) {
+  const int64_t per = units / kWideWorkers;
+  return per >= kWideLeast && units % kWideWorkers == 0 && steps % per == 0;
+}
+__device__ __forceinline__ int group_cost(const SharedArgs& x, bool whole) {
+  return !x.wide_rows ? kStepsCost : whole ? 0 : kWideCost;
+}
 
 __device__ __forceinline__ int64_t block_before(int64_t* sums, int64_t v, int64_t& total) {
   // the sum over the threads before this one, and over all
@@ -99,7 +116,10 @@ __device__ __forceinline__ void finish_totals(const SharedArgs& x, Totals t, int
   const int64_t w = (t.group_units + kWideWorkers - 1) / kWideWorkers;
   const int64_t n = (units + x.steps_workers - 1) / x.steps_workers;
   t.wide_per = w > kWideLeast ? w : kWideLeast;
-  t.steps_per = n > kStepsLeast ? n : kStepsLeast;
+  // (half: 16 sequences of about 250 keys of their own 35.0 -> 32.5 us a call; always
+  // half: 32 of about 1000, 32 rows each, 79 -> 84)
+  const int least = units < (int64_t)x.steps_workers * kStepsLeast / 4 ? kStepsLeast / 2 : kStepsLeast;
+  t.steps_per = n > least ? n : least;
   *x.totals = t;
 }
 
@@ -147,10 +167,8 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(SharedArgs x)
     const int g = g0 + tid;
     int64_t u = 0, it = 0, all_u, all_it;
     if (g < x.n_groups && x.groups[g].n > 0) {
-      const int64_t keys = (int64_t)x.groups[g].pages * P;
       it = ((int64_t)x.groups[g].n * G + tile - 1) / tile * a.pg.Hkv;
-      u = it * (x.wide_rows ? (keys + kWideKeys - 1) / kWideKeys + kWideCost
-                            : keys / kKeys + kStepsCost);
+      u = it * group_steps(x, x.groups[g].pages);
     }
     const int64_t bu = block_before(sums, u, all_u), bi = block_before(sums, it, all_it);
     if (g < x.n_groups) {
@@ -160,8 +178,16 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(SharedArgs x)
     units += all_u;
     items += all_it;
   }
+  // (each thread has its own groups' units: the ones it wrote)
+  bool whole = true;
+  for (int g = tid; g < x.n_groups; g += kPlanThreads)
+    whole &= x.groups[g].n == 0 || whole_runs(units, group_steps(x, x.groups[g].pages));
+  const int cost = group_cost(x, __syncthreads_and(whole));
+  for (int g = tid; g < x.n_groups; g += kPlanThreads)
+    x.groups[g].unit += (int64_t)cost * x.groups[g].item;
   Totals t{};
-  t.group_units = units;
+  t.wide_cost = cost;
+  t.group_units = units += cost * items;
   if (x.wide_rows) {
     t.bad = items > x.wide_items;
     units = items = 0;
@@ -275,15 +301,17 @@ __global__ __launch_bounds__(kFewThreads) void shared_plan_few_kernel(SharedArgs
   const int tile = x.wide_rows ? x.wide_rows : x.steps_rows;
   int64_t units, items, all_u, all_it;
   {
-    const int64_t keys = (int64_t)gi.pages * P;
     items = ((int64_t)gi.n * G + tile - 1) / tile * a.pg.Hkv;
-    units = items * (x.wide_rows ? (keys + kWideKeys - 1) / kWideKeys + kWideCost
-                                 : keys / kKeys + kStepsCost);
+    units = items * group_steps(x, gi.pages);
   }
   sum_before(units, items, all_u, all_it);
-  gi.unit = units;
+  const int cost =
+      group_cost(x, __syncthreads_and(gi.n == 0 || whole_runs(all_u, group_steps(x, gi.pages))));
+  gi.unit = units + cost * items;
   gi.item = (int)items;
+  all_u += cost * all_it;
   Totals total{};
+  total.wide_cost = cost;
   total.group_units = all_u;
   int64_t base_u = all_u, base_it = all_it;
   if (x.wide_rows) {
@@ -320,6 +348,73 @@ __device__ __forceinline__ Info info_at(const Info* list, int i) {
 #pragma unroll
   for (int k = 0; k < 4; ++k) w[k] = entry((const uint64_t*)list, (int64_t)i * 4 + k);
   return __builtin_bit_cast(Info, w);
+}
+
+// ----------------------------------------------------------------------------
+// Steps of 32 keys in registers: a wave takes a run of the sequences' own keys,
+// behind the groups' where those have few rows (then in a launch of their own).
+// ----------------------------------------------------------------------------
+template <int FMT, int P, int RT>
+__device__ __forceinline__ void steps_run(const SharedArgs& x, int worker) {
+  const AttendArgs& a = x.a;
+  const int G = a.Hq / a.pg.Hkv, lane = threadIdx.x % kWave, j = lane & 15, g4 = lane >> 4;
+  const int64_t per = entry(&x.totals->steps_per, 0), total = entry(&x.totals->seq_units, 0);
+  const int64_t groups = x.wide_rows ? 0 : entry(&x.totals->group_units, 0);
+  int64_t u = worker * per;
+  const int64_t u1 = min(u + per, total);
+  if (u >= u1) return;
+  int g = u < groups ? at_unit(x.groups, x.n_groups, u) : x.n_groups;
+  int s = u < groups ? 0 : at_unit(x.seqs, a.tk.S, u);
+  while (u < u1 && s < a.tk.S) {
+    const bool is_group = u < groups;
+    int first, n, lead, seq_len, key0, key1, item0;
+    int64_t start;
+    if (is_group) {
+      const GroupInfo q = info_at(x.groups, g);
+      first = q.first; n = q.n; lead = q.lead; key0 = 0; key1 = q.pages * P;
+      item0 = q.item; start = q.unit;
+      seq_len = INT_MAX / 2;      // (every row sees all of them)
+    } else {
+      const SeqInfo q = info_at(x.seqs, s);
+      first = q.first; n = q.n; lead = s; key0 = q.key0; seq_len = entry(a.lengths, s);
+      key1 = keys_of<P>(a, s);
+      item0 = q.item; start = q.unit;
+    }
+    const int tiles = (n * G + kRows * RT - 1) / (kRows * RT);
+    const int steps = (max(key1 - key0, 0) + kKeys - 1) / kKeys, whole = steps + kStepsCost;
+    const int64_t off = u - start;
+    const int item = (int)(off / whole), at = (int)(off % whole);
+    if (n == 0 || item >= tiles * a.pg.Hkv) {
+      if (is_group) ++g; else ++s;
+      if (is_group && g >= x.n_groups) break;      // (the units of groups end with the last one)
+      continue;
+    }
+    const int to = (int)min((int64_t)whole, at + (u1 - u));
+    u += to - at;
+    const int st0 = max(at - kStepsCost, 0), st1 = max(to - kStepsCost, 0);
+    const int kvh = item / tiles, row0 = item % tiles * kRows * RT;
+    WaveSums<RT> ws;
+    attend_steps<FMT, P, RT>(a, lead, kvh, row0, first, n, seq_len, key0 + kKeys * st0,
+                             min(key0 + kKeys * st1, max(key1, key0)), 0, 1, ws);
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      const int row = kRows * rt + j;
+      if (row0 + row >= n * G) continue;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        float v[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = ws.o[rt][i][q];
+        store_part<RT>(a, item0 + item + worker, row, 8 * (4 * g4 + q), ws.m[rt], ws.l[rt], v);
+      }
+    }
+  }
+}
+
+template <int FMT, int P, int RT>
+__global__ __launch_bounds__(kThreads, attend_occupancy(RT)) void shared_steps_kernel(SharedArgs x) {
+  steps_run<FMT, P, RT>(x, __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) * (int)gridDim.x +
+                               (int)blockIdx.x);
 }
 
 // ----------------------------------------------------------------------------
@@ -371,15 +466,15 @@ struct __attribute__((aligned(16))) WideSmem {
 };
 
 template <int FMT, int P, int RW>
-__global__ __launch_bounds__(kWideThreads, 2) void shared_wide_kernel(SharedArgs x) {
+__device__ __forceinline__ void wide_run(const SharedArgs& x, WideSmem& sm) {
   constexpr int KW = kWideWaves / RW, KT = kWideKeys / KW / 32;   // key tiles of a wave
   constexpr int kRowsOf = 32 * RW;
-  __shared__ WideSmem sm;
   const AttendArgs& a = x.a;
   const int G = a.Hq / a.pg.Hkv, lane = threadIdx.x % kWave, j = lane & 31, h = lane >> 5;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
   const int rw = wave % RW, kw = wave / RW;
   const int64_t per = entry(&x.totals->wide_per, 0), total = entry(&x.totals->group_units, 0);
+  const int cost = entry(&x.totals->wide_cost, 0);
   const int worker = (int)blockIdx.x;
   int64_t u = worker * per;
   const int64_t u1 = min(u + per, total);
@@ -389,7 +484,7 @@ __global__ __launch_bounds__(kWideThreads, 2) void shared_wide_kernel(SharedArgs
     const GroupInfo q = info_at(x.groups, g);
     const int tiles = (q.n * G + kRowsOf - 1) / kRowsOf;
     const int steps = (int)(((int64_t)q.pages * P + kWideKeys - 1) / kWideKeys);
-    const int whole = steps + kWideCost;
+    const int whole = steps + cost;
     const int64_t off = u - q.unit;
     const int item = (int)(off / whole), at = (int)(off % whole);
     if (q.n == 0 || item >= tiles * a.pg.Hkv) {    // (a group without units, or behind this one)
@@ -398,7 +493,7 @@ __global__ __launch_bounds__(kWideThreads, 2) void shared_wide_kernel(SharedArgs
     }
     const int to = (int)min((int64_t)whole, at + (u1 - u));
     u += to - at;
-    const int st0 = max(at - kWideCost, 0), st1 = max(to - kWideCost, 0);
+    const int st0 = max(at - cost, 0), st1 = max(to - cost, 0);
     const int kvh = item / tiles, row0 = item % tiles * kRowsOf, rows = q.n * G;
     const int64_t table_row = (int64_t)q.lead * a.pg.max_pages;
 
@@ -663,66 +758,17 @@ __global__ __launch_bounds__(kWideThreads, 2) void shared_wide_kernel(SharedArgs
   }
 }
 
-// ----------------------------------------------------------------------------
-// Steps of 32 keys in registers: a wave takes a run of the sequences' own keys,
-// behind the groups' where those have few rows.
-// ----------------------------------------------------------------------------
-template <int FMT, int P, int RT>
-__global__ __launch_bounds__(kThreads, attend_occupancy(RT)) void shared_steps_kernel(SharedArgs x) {
-  const AttendArgs& a = x.a;
-  const int G = a.Hq / a.pg.Hkv, lane = threadIdx.x % kWave, j = lane & 15, g4 = lane >> 4;
-  const int worker = (int)blockIdx.x * kWaves + __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
-  const int64_t per = entry(&x.totals->steps_per, 0), total = entry(&x.totals->seq_units, 0);
-  const int64_t groups = x.wide_rows ? 0 : entry(&x.totals->group_units, 0);
-  int64_t u = worker * per;
-  const int64_t u1 = min(u + per, total);
-  if (u >= u1) return;
-  int g = u < groups ? at_unit(x.groups, x.n_groups, u) : x.n_groups;
-  int s = u < groups ? 0 : at_unit(x.seqs, a.tk.S, u);
-  while (u < u1 && s < a.tk.S) {
-    const bool is_group = u < groups;
-    int first, n, lead, seq_len, key0, key1, item0;
-    int64_t start;
-    if (is_group) {
-      const GroupInfo q = info_at(x.groups, g);
-      first = q.first; n = q.n; lead = q.lead; key0 = 0; key1 = q.pages * P;
-      item0 = q.item; start = q.unit;
-      seq_len = INT_MAX / 2;      // (every row sees all of them)
-    } else {
-      const SeqInfo q = info_at(x.seqs, s);
-      first = q.first; n = q.n; lead = s; key0 = q.key0; seq_len = entry(a.lengths, s);
-      key1 = keys_of<P>(a, s);
-      item0 = q.item; start = q.unit;
-    }
-    const int tiles = (n * G + kRows * RT - 1) / (kRows * RT);
-    const int steps = (max(key1 - key0, 0) + kKeys - 1) / kKeys, whole = steps + kStepsCost;
-    const int64_t off = u - start;
-    const int item = (int)(off / whole), at = (int)(off % whole);
-    if (n == 0 || item >= tiles * a.pg.Hkv) {
-      if (is_group) ++g; else ++s;
-      if (is_group && g >= x.n_groups) break;      // (the units of groups end with the last one)
-      continue;
-    }
-    const int to = (int)min((int64_t)whole, at + (u1 - u));
-    u += to - at;
-    const int st0 = max(at - kStepsCost, 0), st1 = max(to - kStepsCost, 0);
-    const int kvh = item / tiles, row0 = item % tiles * kRows * RT;
-    WaveSums<RT> ws;
-    attend_steps<FMT, P, RT>(a, lead, kvh, row0, first, n, seq_len, key0 + kKeys * st0,
-                             min(key0 + kKeys * st1, max(key1, key0)), 0, 1, ws);
-#pragma unroll
-    for (int rt = 0; rt < RT; ++rt) {
-      const int row = kRows * rt + j;
-      if (row0 + row >= n * G) continue;
-#pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        float v[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) v[i] = ws.o[rt][i][q];
-        store_part<RT>(a, item0 + item + worker, row, 8 * (4 * g4 + q), ws.m[rt], ws.l[rt], v);
-      }
-    }
-  }
+// A workgroup's run of the groups' keys, then its waves' runs of the sequences' own.
+// (Two launches instead: the second one's start, and the first one's uneven end, come
+// on top.)
+template <int FMT, int P, int RW, int RT>
+__global__ __launch_bounds__(kWideThreads, 2) void shared_wide_kernel(SharedArgs x) {
+  __shared__ WideSmem sm;
+  wide_run<FMT, P, RW>(x, sm);
+  // (where the runs are fewer than the waves: over the CUs, from the one without groups'
+  // keys on)
+  steps_run<FMT, P, RT>(x, __builtin_amdgcn_readfirstlane(threadIdx.x / kWave) * kWideWorkers +
+                               kWideWorkers - 1 - (int)blockIdx.x);
 }
 
 // ----------------------------------------------------------------------------
@@ -781,7 +827,7 @@ __global__ __launch_bounds__(kThreads) void shared_join_kernel(SharedArgs x, int
     if (t >= g.first && t < g.first + g.n)
       common = x.wide_rows
           ? parts_of(x.wide_ml, x.wide_o, x.wide_rows, g.unit, g.item, g.n, row,
-                     (int)((gkeys + kWideKeys - 1) / kWideKeys) + kWideCost,
+                     (int)((gkeys + kWideKeys - 1) / kWideKeys) + entry(&x.totals->wide_cost, 0),
                      entry(&x.totals->wide_per, 0))
           : parts_of(a.part_ml, a.part_o, x.steps_rows, g.unit, g.item, g.n, row,
                      (int)(gkeys / kKeys) + kStepsCost, steps_per);
@@ -839,7 +885,7 @@ __global__ __launch_bounds__(kThreads) void shared_join_kernel(SharedArgs x, int
 // Host side
 // ----------------------------------------------------------------------------
 struct SharedPlan {
-  int wide_rows, rt, groups;       // workgroups of shared_steps_kernel
+  int wide_rows, rt, groups;       // workgroups of four waves that take the steps
   int64_t items, wide_items;
   bool fits;
   size_t at_groups, at_seqs, at_wide_ml, at_wide_o, at_ml, at_o, bytes;
@@ -863,8 +909,9 @@ SharedPlan shared_plan(int Hq, int n_tokens, int n_seqs, int n_groups, int max_p
   p.wide_items = wide_items;
   p.fits = items <= INT_MAX / 2 && wide_items <= INT_MAX / 2 && rows <= INT_MAX / 2;
   if (!p.fits) return p;
-  const int64_t waves = items > INT64_MAX / cost ? INT64_MAX : (items * cost + kStepsLeast - 1) / kStepsLeast;
+  const int64_t waves = items > INT64_MAX / cost ? INT64_MAX : items * cost / (kStepsLeast / 2) + 1;
   p.groups = (int)(waves / kWaves + 1 < kStepsGroups ? waves / kWaves + 1 : kStepsGroups);
+  if (p.wide_rows) p.groups = kStepsGroups;      // (as many waves as shared_wide_kernel has)
   auto up = [](size_t n) { return (n + 255) / 256 * 256; };
   const size_t slots = ((size_t)items + (size_t)p.groups * kWaves) * tile;
   const size_t wide = p.wide_rows ? ((size_t)wide_items + kWideWorkers) * p.wide_rows : 0;
@@ -884,18 +931,19 @@ void launch_shared(const SharedPlan& pl, const SharedArgs& x, hipStream_t stream
     hipLaunchKernelGGL(shared_plan_few_kernel, dim3(1), dim3(kFewThreads), 0, stream, x);
   else
     hipLaunchKernelGGL(shared_plan_kernel, dim3(1), dim3(kPlanThreads), 0, stream, x);
-  if (pl.wide_rows == 128)
-    hipLaunchKernelGGL((shared_wide_kernel<FMT, P, 4>), dim3(kWideWorkers), dim3(kWideThreads), 0,
-                       stream, x);
-  else if (pl.wide_rows == 64)
-    hipLaunchKernelGGL((shared_wide_kernel<FMT, P, 2>), dim3(kWideWorkers), dim3(kWideThreads), 0,
-                       stream, x);
-  if (pl.rt == 1)
-    hipLaunchKernelGGL((shared_steps_kernel<FMT, P, 1>), dim3((unsigned)pl.groups), dim3(kThreads),
-                       0, stream, x);
-  else
-    hipLaunchKernelGGL((shared_steps_kernel<FMT, P, 2>), dim3((unsigned)pl.groups), dim3(kThreads),
-                       0, stream, x);
+#define EI_WIDE(RW, RT) \
+  hipLaunchKernelGGL((shared_wide_kernel<FMT, P, RW, RT>), dim3(kWideWorkers), dim3(kWideThreads), 0, stream, x)
+#define EI_STEPS(RT) \
+  hipLaunchKernelGGL((shared_steps_kernel<FMT, P, RT>), dim3((unsigned)pl.groups), dim3(kThreads), 0, stream, x)
+  if (pl.wide_rows == 128) {
+    if (pl.rt == 1) EI_WIDE(4, 1); else EI_WIDE(4, 2);
+  } else if (pl.wide_rows == 64) {
+    if (pl.rt == 1) EI_WIDE(2, 1); else EI_WIDE(2, 2);
+  } else {
+    if (pl.rt == 1) EI_STEPS(1); else EI_STEPS(2);
+  }
+#undef EI_WIDE
+#undef EI_STEPS
   const int64_t units = (int64_t)x.a.tk.T * ((x.a.Hq + kJoinRows - 1) / kJoinRows);
   for (int64_t u = 0; u < units; u += kMaxGrid)
     hipLaunchKernelGGL(shared_join_kernel, dim3(launch_grid(units - u)), dim3(kThreads), 0, stream,

@@ -83,7 +83,8 @@ __device__ __forceinline__ void rows_of(const PlanArgs& a, int s, int& first, in
 __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
   __shared__ int place[kMaxAdapters];          // an adapter's tokens; then its next place
   __shared__ int first_tile[kMaxAdapters];
-  __shared__ int seq_a[kPlanThreads], seq_n[kPlanThreads];
+  __shared__ __attribute__((aligned(16))) int seq_a[kPlanThreads], seq_n[kPlanThreads];
+  __shared__ int seq_first[kPlanThreads];
   __shared__ int wave_tokens[kPlanThreads / kWave], wave_tiles[kPlanThreads / kWave];
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   const int n = a.p.adapters;
@@ -156,19 +157,31 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
     seq_n[tid] = count;
     __syncthreads();
     int before = 0;
-    for (int i = 0; i < min(here, (wave + 1) * kWave); ++i)
-      before += i < tid && seq_a[i] == ad ? seq_n[i] : 0;
+    // (four at a time: those behind the last sequence count 0)
+    for (int i = 0; i < min(here, (wave + 1) * kWave); i += 4) {
+      const int4 ia = *(const int4*)&seq_a[i], in = *(const int4*)&seq_n[i];
+      before += (i < tid && ia.x == ad ? in.x : 0) + (i + 1 < tid && ia.y == ad ? in.y : 0) +
+                (i + 2 < tid && ia.z == ad ? in.z : 0) + (i + 3 < tid && ia.w == ad ? in.w : 0);
+    }
     const int to = ad < 0 ? -1 : place[ad] + before;
     __syncthreads();
     if (ad >= 0) atomicAdd(&place[ad], count);
-    // a wave writes its 64 sequences' tokens, one sequence after the other
-    for (uint64_t todo = __builtin_amdgcn_ballot_w64(to >= 0 && count > 0); todo; todo &= todo - 1) {
-      const int l = (int)__builtin_ctzll(todo);
-      const int f = __builtin_amdgcn_readlane(first, l), c = __builtin_amdgcn_readlane(count, l);
-      const int p = __builtin_amdgcn_readlane(to, l);
-      for (int i = lane; i < c; i += kWave)
+    // their tokens: of short sequences by a lane each, of longer ones by a wave, of long
+    // ones by all
+    constexpr int kShort = 8, kLong = 512;
+    auto write = [&](int p, int f, int c, int i0, int step) {
+      for (int i = i0; i < c; i += step)
         if ((unsigned)(p + i) < (unsigned)a.p.tokens) a.list[p + i] = f + i;
-    }
+    };
+    if (ad >= 0 && count <= kShort) write(to, first, count, 0, 1);
+    seq_a[tid] = to;
+    seq_first[tid] = first;
+    if (ad < 0) seq_n[tid] = 0;
+    __syncthreads();
+    for (int i = wave; i < here; i += kPlanThreads / kWave)
+      if (seq_n[i] > kShort && seq_n[i] <= kLong) write(seq_a[i], seq_first[i], seq_n[i], lane, kWave);
+    for (int i = 0; i < here; ++i)
+      if (seq_n[i] > kLong) write(seq_a[i], seq_first[i], seq_n[i], tid, kPlanThreads);
     __syncthreads();
   }
 }
@@ -177,8 +190,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
 // Shrink.  The ranks of all targets are rows 0 .. targets * rank - 1 of one
 // matrix.  A workgroup takes 16 MT of them, a tile's 16 NT tokens and a part of
 // the columns, which its waves share; their sums are added in LDS in the waves'
-// order, and the parts' by expand_kernel.  A lane's 16 columns of 64 are 32 bytes
-// of a row (the order of the columns is free as long as both operands share it).
+// order, and the parts' by expand_kernel.
 // ----------------------------------------------------------------------------
 struct Target {
   const uint16_t *a, *b;
@@ -194,7 +206,7 @@ struct AddArgs {
   const Tile* tiles;
   const int32_t* list;
   int tokens, n_in, rank, targets, splits;
-  int blocks;                  // expand_kernel's workgroups per tile
+  int blocks, spans;           // expand_kernel's workgroups per tile; 256 outputs of each
   Target t[kMaxTargets];
 };
 
@@ -219,9 +231,8 @@ __global__ __launch_bounds__(kThreads) void shrink_kernel(AddArgs a, int row_til
   unit /= a.splits;
   const int r0 = (int)(unit % row_tiles) * kRows;
   const int tile = (int)(unit / row_tiles);
-  if (tile >= a.head[0]) return;
   const Tile t = a.tiles[tile];
-  if (t.count <= 0) return;
+  if (tile >= a.head[0] || t.count <= 0) return;
   const int R = a.targets * a.rank;
   const int lane = threadIdx.x % kWave, j = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
@@ -230,11 +241,11 @@ __global__ __launch_bounds__(kThreads) void shrink_kernel(AddArgs a, int row_til
 #pragma unroll
   for (int m = 0; m < MT; ++m) {
     const int row = min(r0 + 16 * m + j, R - 1), i = row / a.rank;
-    wp[m] = target(a, i).a + ((int64_t)t.adapter * a.rank + row % a.rank) * a.n_in + 16 * g;
+    wp[m] = target(a, i).a + ((int64_t)t.adapter * a.rank + row % a.rank) * a.n_in + 8 * g;
   }
 #pragma unroll
   for (int k = 0; k < NT; ++k) {
-    xp[k] = a.x + (int64_t)token_at(a, t, 16 * k + j) * a.n_in + 16 * g;
+    xp[k] = a.x + (int64_t)token_at(a, t, 16 * k + j) * a.n_in + 8 * g;
   }
   f32x4 acc[MT][NT];
 #pragma unroll
@@ -242,28 +253,35 @@ __global__ __launch_bounds__(kThreads) void shrink_kernel(AddArgs a, int row_til
 #pragma unroll
     for (int k = 0; k < NT; ++k) acc[m][k] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
   const int steps = (a.n_in + kColumns - 1) / kColumns;
-  const int per = (steps + a.splits - 1) / a.splits;
-  const int end = min((split + 1) * per, steps);
-  for (int s = split * per + wave; s < end; s += kWaves) {
-    const int c = s * kColumns, left = a.n_in - c - 16 * g;
+  const int per = (steps + a.splits - 1) / a.splits, split_end = min((split + 1) * per, steps);
+  // a wave's steps are neighbours; U steps' operands are asked for, then used
+  const int mine = (per + kWaves - 1) / kWaves;
+  const int begin = split * per + wave * mine, end = min(begin + mine, split_end);
+  constexpr int U = NT == 1 ? 4 : 1;
+  for (int s = begin; s < end; s += U) {
+    uint4 w[U][2][MT], x[U][2][NT];
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const bool in = 8 * half < left;       // (columns come in eights)
-      bf16x8 w[MT], x[NT];
+    for (int u = 0; u < U; ++u)
 #pragma unroll
-      for (int m = 0; m < MT; ++m)
-        w[m] = __builtin_bit_cast(bf16x8, in ? *(const uint4*)(wp[m] + c + 8 * half)
-                                             : make_uint4(0u, 0u, 0u, 0u));
+      for (int half = 0; half < 2; ++half) {
+        const int c = (s + u) * kColumns + 32 * half;
+        const bool in = s + u < end && c + 8 * g < a.n_in;       // (columns come in eights)
 #pragma unroll
-      for (int k = 0; k < NT; ++k)
-        x[k] = __builtin_bit_cast(bf16x8, in ? *(const uint4*)(xp[k] + c + 8 * half)
-                                             : make_uint4(0u, 0u, 0u, 0u));
+        for (int m = 0; m < MT; ++m) w[u][half][m] = in ? *(const uint4*)(wp[m] + c) : make_uint4(0u, 0u, 0u, 0u);
 #pragma unroll
-      for (int m = 0; m < MT; ++m)
+        for (int k = 0; k < NT; ++k) x[u][half][k] = in ? *(const uint4*)(xp[k] + c) : make_uint4(0u, 0u, 0u, 0u);
+      }
 #pragma unroll
-        for (int k = 0; k < NT; ++k)
-          acc[m][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w[m], x[k], acc[m][k], 0, 0, 0);
-    }
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int half = 0; half < 2; ++half)
+#pragma unroll
+        for (int m = 0; m < MT; ++m)
+#pragma unroll
+          for (int k = 0; k < NT; ++k)
+            acc[m][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                __builtin_bit_cast(bf16x8, w[u][half][m]), __builtin_bit_cast(bf16x8, x[u][half][k]),
+                acc[m][k], 0, 0, 0);
   }
   // lane: token j, rows 4g .. 4g + 3 of each tile
 #pragma unroll
@@ -288,8 +306,10 @@ __global__ __launch_bounds__(kThreads) void shrink_kernel(AddArgs a, int row_til
 // numbers (16 bits; one alone would double the variance that y's rounding has):
 // they are columns 0 .. rank - 1 and rank .. 2 rank - 1 of one operand, each
 // against the same columns of B.  y is the accumulator's start and is rounded
-// once.  A wave takes 64 outputs; row i of its product m is output 16 (i / 4) +
-// 4 m + i % 4, so that a lane has 16 outputs in a row of its token.
+// once.  A wave takes 64 outputs at a time; row i of its product m is output
+// 16 (i / 4) + 4 m + i % 4, so that a lane has 16 outputs in a row of its token.
+// A workgroup brings its tile's V into LDS once for `a.spans` times 256 outputs;
+// each wave asks for its first outputs' y and B before that.
 // ----------------------------------------------------------------------------
 constexpr int kWaveOuts = 64;
 constexpr int kBlockOuts = kWaveOuts * kWaves;
@@ -300,81 +320,115 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(AddArgs a, int64_t uni
   __shared__ __attribute__((aligned(16))) uint16_t sm[kTokens * (2 * kMaxRank + kPad)];
   const int64_t unit = unit0 + blockIdx.x;
   const int block = (int)(unit % a.blocks), tile = (int)(unit / a.blocks);
-  if (tile >= a.head[0]) return;
+  const Tile t = a.tiles[tile];
+  if (tile >= a.head[0] || t.count <= 0) return;
   int ti = 0;
   for (int i = 1; i < a.targets; ++i)
     if (block >= target(a, i).block0) ti = i;
   const Target tg = target(a, ti);
-  const Tile t = a.tiles[tile];
-  if (t.count <= 0) return;
   const int r = a.rank, pitch = 2 * r + kPad, R = a.targets * r;
-  const float scale = tg.scale ? tg.scale[t.adapter] : 1.0f;
-  // the tile's V, as pairs of bf16 numbers
-  for (int e = threadIdx.x; e < kTokens * (r / 2); e += kThreads) {
-    const int tok = e / (r / 2), c = e % (r / 2) * 2;
-    float x0 = 0.0f, x1 = 0.0f;
-    if (tok < t.count)
-      for (int s = 0; s < a.splits; ++s) {
-        const float* p = a.v + ((int64_t)s * a.tokens + t.begin + tok) * R + ti * r + c;
-        x0 += p[0];
-        x1 += p[1];
-      }
-    x0 *= scale;
-    x1 *= scale;
-    const uint32_t hi = pack_bf16x2(x0, x1);
-    *(uint32_t*)&sm[tok * pitch + c] = hi;
-    // (an infinity has no rest)
-    const float y0 = __builtin_isinf(x0) ? 0.0f : x0 - bf16_lo(hi);
-    const float y1 = __builtin_isinf(x1) ? 0.0f : x1 - bf16_hi(hi);
-    *(uint32_t*)&sm[tok * pitch + r + c] = pack_bf16x2(y0, y1);
-  }
-  __syncthreads();
   const int lane = threadIdx.x % kWave, j = lane & 15, g = lane >> 4;
-  const int o0 = (block - tg.block0) * kBlockOuts + (int)(threadIdx.x / kWave) * kWaveOuts;
-  if (o0 >= tg.n_out) return;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x / kWave);
+  uint16_t* yp[NT];
+#pragma unroll
+  for (int k = 0; k < NT; ++k)
+    yp[k] = tg.y + (int64_t)token_at(a, t, 16 * k + j) * tg.n_out + 16 * g;
+  // outputs o0 .. o0 + 63 (of the wave), this lane's from o0 + 16 g on
+  uint4 y[NT][2];
+  auto load_y = [&](int o0) {
+#pragma unroll
+    for (int k = 0; k < NT; ++k)
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        if (16 * k < t.count && o0 + 16 * g + 8 * h < tg.n_out)
+          y[k][h] = *(const uint4*)(yp[k] + o0 + 8 * h);
+  };
   const int chunks = (2 * r + 31) / 32;
-  const uint16_t* bp[4];
-#pragma unroll
-  for (int m = 0; m < 4; ++m) {
-    const int o = min(o0 + 16 * (j >> 2) + 4 * m + (j & 3), tg.n_out - 1);
-    bp[m] = tg.b + ((int64_t)t.adapter * tg.n_out + o) * r;
-  }
-  const int mine = o0 + 16 * g;     // this lane's outputs
-#pragma unroll
-  for (int k = 0; k < NT; ++k) {
-    if (16 * k >= t.count) break;
-    const int row = 16 * k + j;
-    uint16_t* yp = tg.y + (int64_t)token_at(a, t, row) * tg.n_out + mine;
-    uint4 w[2];
-#pragma unroll
-    for (int h = 0; h < 2; ++h)
-      w[h] = mine + 8 * h < tg.n_out ? *(const uint4*)(yp + 8 * h) : make_uint4(0u, 0u, 0u, 0u);
-    f32x4 acc[4];
+  auto load_b = [&](int o0, int c, uint4 (&b)[4]) {
+    const int col = 32 * c + 8 * g;     // (past 2 r: nothing, rank 8 and the like)
+    const int bc = col < r ? col : col - r;
 #pragma unroll
     for (int m = 0; m < 4; ++m) {
-      const uint32_t u0 = m & 1 ? w[m >> 1].z : w[m >> 1].x, u1 = m & 1 ? w[m >> 1].w : w[m >> 1].y;
-      acc[m] = f32x4{bf16_lo(u0), bf16_hi(u0), bf16_lo(u1), bf16_hi(u1)};
+      const int o = min(o0 + 16 * (j >> 2) + 4 * m + (j & 3), tg.n_out - 1);
+      b[m] = make_uint4(0u, 0u, 0u, 0u);
+      if (col < 2 * r) b[m] = *(const uint4*)(tg.b + ((int64_t)t.adapter * tg.n_out + o) * r + bc);
     }
-    for (int c = 0; c < chunks; ++c) {
-      const int col = 32 * c + 8 * g;     // (past 2 r: nothing, rank 8 alone)
-      const bool in = col < 2 * r;
-      const uint4 v = in ? *(const uint4*)&sm[row * pitch + col] : make_uint4(0u, 0u, 0u, 0u);
-      const int bc = col < r ? col : col - r;
+  };
+  const int first = ((block - tg.block0) * a.spans * kWaves + wave) * kWaveOuts;
+  uint4 b0[4];
+  if (first < tg.n_out) {
+    load_y(first);
+    load_b(first, 0, b0);
+  }
+  const float scale = tg.scale ? tg.scale[t.adapter] : 1.0f;
+  // the tile's V, as pairs of bf16 numbers
+  for (int e = threadIdx.x; e < kTokens * (r / 4); e += kThreads) {
+    const int tok = e / (r / 4), c = e % (r / 4) * 4;
+    float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+    if (tok < t.count)
+      for (int s = 0; s < a.splits; ++s) {
+        const float4 p = *(const float4*)(a.v + ((int64_t)s * a.tokens + t.begin + tok) * R + ti * r + c);
+        x.x += p.x;
+        x.y += p.y;
+        x.z += p.z;
+        x.w += p.w;
+      }
+    const float v[4] = {x.x * scale, x.y * scale, x.z * scale, x.w * scale};
+    float rest[4];
+    const uint32_t hi[2] = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)      // (an infinity has no rest)
+      rest[i] = __builtin_isinf(v[i]) ? 0.0f : v[i] - (i & 1 ? bf16_hi(hi[i / 2]) : bf16_lo(hi[i / 2]));
+    *(uint2*)&sm[tok * pitch + c] = make_uint2(hi[0], hi[1]);
+    *(uint2*)&sm[tok * pitch + r + c] = make_uint2(pack_bf16x2(rest[0], rest[1]), pack_bf16x2(rest[2], rest[3]));
+  }
+  __syncthreads();
+  for (int i = 0; i < a.spans; ++i) {
+    const int o0 = first + i * kBlockOuts, mine = o0 + 16 * g;
+    if (o0 >= tg.n_out) break;
+    f32x4 acc[NT][4];
+#pragma unroll
+    for (int k = 0; k < NT; ++k)
 #pragma unroll
       for (int m = 0; m < 4; ++m) {
-        const uint4 b = in ? *(const uint4*)(bp[m] + bc) : make_uint4(0u, 0u, 0u, 0u);
-        acc[m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-            __builtin_bit_cast(bf16x8, b), __builtin_bit_cast(bf16x8, v), acc[m], 0, 0, 0);
+        const uint4 w = y[k][m >> 1];
+        const uint32_t u0 = m & 1 ? w.z : w.x, u1 = m & 1 ? w.w : w.y;
+        acc[k][m] = f32x4{bf16_lo(u0), bf16_hi(u0), bf16_lo(u1), bf16_hi(u1)};
       }
-    }
-    if (row >= t.count) continue;
+    uint4 b[4] = {b0[0], b0[1], b0[2], b0[3]};
+    const bool more = i + 1 < a.spans && o0 + kBlockOuts < tg.n_out;
+    if (more) load_y(o0 + kBlockOuts);
+    for (int c = 0; c < chunks; ++c) {
+      const int col = 32 * c + 8 * g;
+      uint4 next[4];
+      if (c + 1 < chunks) load_b(o0, c + 1, next);
+      else if (more) load_b(o0 + kBlockOuts, 0, next);
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-      if (mine + 8 * h < tg.n_out)
-        *(uint4*)(yp + 8 * h) = make_uint4(
-            pack_bf16x2(acc[2 * h][0], acc[2 * h][1]), pack_bf16x2(acc[2 * h][2], acc[2 * h][3]),
-            pack_bf16x2(acc[2 * h + 1][0], acc[2 * h + 1][1]),
-            pack_bf16x2(acc[2 * h + 1][2], acc[2 * h + 1][3]));
+      for (int k = 0; k < NT; ++k) {
+        if (16 * k >= t.count) break;
+        const uint4 v = col < 2 * r ? *(const uint4*)&sm[(16 * k + j) * pitch + col]
+                                    : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+        for (int m = 0; m < 4; ++m)
+          acc[k][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+              __builtin_bit_cast(bf16x8, b[m]), __builtin_bit_cast(bf16x8, v), acc[k][m], 0, 0, 0);
+      }
+#pragma unroll
+      for (int m = 0; m < 4; ++m) b[m] = next[m];
+    }
+#pragma unroll
+    for (int m = 0; m < 4; ++m) b0[m] = b[m];
+#pragma unroll
+    for (int k = 0; k < NT; ++k) {
+      if (16 * k + j >= t.count) continue;
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        if (mine + 8 * h < tg.n_out)
+          *(uint4*)(yp[k] + o0 + 8 * h) = make_uint4(
+              pack_bf16x2(acc[k][2 * h][0], acc[k][2 * h][1]), pack_bf16x2(acc[k][2 * h][2], acc[k][2 * h][3]),
+              pack_bf16x2(acc[k][2 * h + 1][0], acc[k][2 * h + 1][1]),
+              pack_bf16x2(acc[k][2 * h + 1][2], acc[k][2 * h + 1][3]));
+    }
   }
 }
 
@@ -413,6 +467,13 @@ AddPlan add_plan(const PlanShape& p, int n_in, int rank, int targets) {
   s.splits = splits < 1 ? 1 : (int)splits;
   s.bytes = (size_t)s.splits * p.tokens * R * sizeof(float);
   return s;
+}
+// Times 256 outputs of a workgroup of expand_kernel: up to 4 while 1024 workgroups are left.
+int spans_of(const PlanShape& p, const ei_adapter_target* t, int n) {
+  int64_t blocks = 0;
+  for (int i = 0; i < n; ++i) blocks += ((int64_t)t[i].n_out + kBlockOuts - 1) / kBlockOuts;
+  const int64_t s = blocks * p.max_tiles / 1024;
+  return s < 1 ? 1 : s > 4 ? 4 : (int)s;
 }
 ei_status check_sizes(int32_t n_in, int32_t rank, int32_t n_targets) {
   if (n_in <= 0 || rank <= 0 || n_targets < 0) return EI_ERR_SHAPE;
@@ -464,14 +525,9 @@ ei_status ei_adapter_add(const uint16_t* x, int32_t n_in, int32_t rank,
   if (st != EI_OK) return st;
   if ((st = ei::check_sizes(n_in, rank, n_targets)) != EI_OK) return st;
   if (n_targets > 0 && !targets) return EI_ERR_NULL;
-  int64_t blocks = 0;
-  ei::AddArgs a{};
   for (int i = 0; i < n_targets; ++i) {
-    const ei_adapter_target& t = targets[i];
-    if (t.n_out <= 0) return EI_ERR_SHAPE;
-    if (t.n_out % 8) return EI_ERR_UNSUPPORTED;
-    a.t[i] = ei::Target{t.a, t.b, t.scale, t.y, t.n_out, (int)blocks};
-    blocks += ((int64_t)t.n_out + ei::kBlockOuts - 1) / ei::kBlockOuts;
+    if (targets[i].n_out <= 0) return EI_ERR_SHAPE;
+    if (targets[i].n_out % 8) return EI_ERR_UNSUPPORTED;
   }
   if (ei::nothing(batch) || n_targets == 0) return EI_OK;
   const ei::PlanShape p = ei::plan_shape(batch);
@@ -489,6 +545,15 @@ ei_status ei_adapter_add(const uint16_t* x, int32_t n_in, int32_t rank,
     return EI_ERR_WORKSPACE;
   if (!ei::aligned(plan, 16) || !ei::aligned(workspace, 16)) return EI_ERR_UNSUPPORTED;
   const char* at = (const char*)plan;
+  ei::AddArgs a{};
+  a.spans = ei::spans_of(p, targets, n_targets);
+  int64_t blocks = 0;
+  for (int i = 0; i < n_targets; ++i) {
+    const ei_adapter_target& t = targets[i];
+    const int64_t outs = (int64_t)ei::kBlockOuts * a.spans;
+    a.t[i] = ei::Target{t.a, t.b, t.scale, t.y, t.n_out, (int)blocks};
+    blocks += (t.n_out + outs - 1) / outs;
+  }
   a.x = x;
   a.v = (float*)workspace;
   a.head = (const int32_t*)at;

@@ -12,6 +12,16 @@ together.  ``Decoder`` runs the decoder layers of ``prefill`` over it:
     last, logits = dec.prompts(x, lengths, seqs)      # x [1, sum(lengths), hidden]
     last, logits = dec.step(x_new, seqs)              # x_new [1, len(seqs), hidden]
 
+Sequences that were forked from one prompt share its pages; a ``Decoder`` with
+``shared_prefixes`` reads them once for all.  With ``adapters`` (low-rank
+corrections of the projections, prefill.check_adapters) each sequence of a call
+names its own, and ``Sampler`` draws tokens by each request's settings:
+
+    dec = Decoder(layers, shape, cache, lm_head, adapters, shared_prefixes=True)
+    sampler = Sampler([dict(temperature=0.7, top_p=0.9), dict(top_k=40)], device="cuda")
+    tokens, logprobs = sampler(logits)
+    tokens, logprobs = dec.generate(logits, embed, seqs, 100, sampler, adapter=[0, 3])
+
 A prompt that goes through the entropy-guided attention instead fills the cache
 with ``prefill.prefill(x, ..., store=cache.storing(seqs))`` (or of many at once,
 their lengths alike).
@@ -236,35 +246,87 @@ class _Storing:
         self.took = False
 
 
+def prefix_groups(table, shared):
+    """Sequences whose first pages are the same, from their rows of the page table
+    [S, columns] and the number of pages of each that all its new tokens see:
+    (order, group_seqs, shared_pages), the sequences so ordered that a group's lie
+    one behind the other, the groups' first places in that order (and its end),
+    and how many pages each group shares.
+
+    In the order of their rows, neighbours share most.  A sequence joins the
+    group before it unless leaving the group as it is and beginning another with
+    the sequence behind saves more reads of pages than joining, alone or with
+    that one, does."""
+    n = len(table)
+    rows = np.ascontiguousarray(table)
+    order = sorted(range(n), key=lambda s: rows[s].tobytes())
+    rows, most = rows[order], np.asarray(shared)[order]
+    alike = np.zeros(n, dtype=np.int64)      # of pages, with the sequence before
+    if n > 1:
+        differ = rows[1:] != rows[:-1]
+        same = np.where(differ.any(1), differ.argmax(1), rows.shape[1])
+        alike[1:] = np.minimum(same, np.minimum(most[1:], most[:-1]))
+    alike = alike.tolist() + [0]
+    first, pages = [], []
+    size, held = 0, 0
+    for i in range(n):
+        joined = alike[i] if size == 1 else min(held, alike[i])
+        saved = (size - 1) * held
+        if not i or not joined or saved + alike[i + 1] > max(
+                size * joined, (size + 1) * min(joined, alike[i + 1])):
+            first.append(i)
+            pages.append(0)
+            size, held = 1, 0
+        else:
+            size, held = size + 1, joined
+            pages[-1] = held
+    return order, first + [n], pages
+
+
 class _Batch:
     """What the layers need to know of a packed batch, copied to the device at
-    once: the sequences' pages and lengths, their rows, the tokens' positions."""
+    once: the sequences' pages and lengths, their rows, the tokens' positions,
+    and their adapters and groups where there are any."""
 
-    def __init__(self, cache: PagedCache, seqs, counts):
+    def __init__(self, cache: PagedCache, seqs, counts, adapter=None, groups=None):
         table, lengths = cache.table(seqs)
         S, T = len(counts), sum(counts)
         cu = np.concatenate([[0], np.cumsum(counts)]).astype(np.int32)
         pos = np.concatenate([np.arange(n - c, n) for n, c in zip(lengths.tolist(), counts)])
-        flat = np.concatenate([table.ravel(), lengths, cu, pos.astype(np.int32)])
-        dev = torch.from_numpy(flat).to(cache.device)
-        a, b = table.size, table.size + S
-        self.table, self.lengths = dev[:a].view(S, -1), dev[a:b]
-        self.cu = dev[b:b + S + 1]
-        self.positions = dev[b + S + 1:]
+        parts = [table.ravel(), lengths, cu, pos]
+        if adapter is not None:
+            parts.append(adapter)
+        if groups is not None:
+            parts += groups
+        flat = np.concatenate([np.asarray(p, dtype=np.int32) for p in parts])
+        at = np.cumsum([len(p) for p in parts])[:-1].tolist()
+        table, self.lengths, self.cu, self.positions, *rest = \
+            torch.from_numpy(flat).to(cache.device).tensor_split(at)
+        self.table = table.view(S, -1)
+        self.adapter = None if adapter is None else rest.pop(0)
+        self.groups = rest or None       # [first sequences, shared pages]
         self.uniform = T == S * counts[0] and len(set(counts)) == 1
 
 
 class Decoder:
     """The decoder layers over a cache.  Hidden states in and out are packed,
-    [1, tokens, hidden] bf16."""
+    [1, tokens, hidden] bf16.
 
-    def __init__(self, layers, shape: pf.DecoderShape, cache: PagedCache, lm_head=None):
+    ``adapters`` (optional) is what prefill.check_adapters takes; prompts, step and
+    generate then take ``adapter``, each sequence's number (-1: none).  With
+    ``shared_prefixes`` the steps read pages that sequences share once for all of
+    them (binding.cache_attn_shared); its results differ by roundings."""
+
+    def __init__(self, layers, shape: pf.DecoderShape, cache: PagedCache, lm_head=None,
+                 adapters=None, shared_prefixes: bool = False):
         self.layers, self.shape, self.cache, self.lm_head = layers, shape, cache, lm_head
+        self.adapters, self.shared_prefixes = adapters, shared_prefixes
+        self.n_adapters = 0 if adapters is None else pf.check_adapters(adapters, layers)
         self.scale = 1.0 / math.sqrt(shape.head_dim)
         self.cos, self.sin = pf.rope_tables(cache.max_len, shape.head_dim, shape.rope_theta,
                                             cache.device)
 
-    def prompts(self, x, lengths, seqs):
+    def prompts(self, x, lengths, seqs, adapter=None):
         """Prompts of empty sequences, one behind the other in x [1, sum(lengths),
         hidden]: (normed hidden state of each one's last token [len(seqs),
         hidden], their logits or None)."""
@@ -279,9 +341,9 @@ class Decoder:
                 eb.cache_store(k, v, pages, b.table, b.lengths, b.cu)
                 return eb.packed_prefill_attn(q, k, v, b.cu, self.scale)
             return attn
-        return self._run(x, seqs, lengths, attend, last_only=True)
+        return self._run(x, seqs, lengths, attend, True, adapter)
 
-    def step(self, x, seqs, counts=None):
+    def step(self, x, seqs, counts=None, adapter=None):
         """New tokens of the sequences (counts[i] of seqs[i], one each without),
         packed in x: (normed hidden state of every token [tokens, hidden], their
         logits or None).  Where a layer fails the sequences are cut back to what
@@ -295,30 +357,83 @@ class Decoder:
 
             def attn(q, k, v):
                 eb.cache_store(k, v, pages, b.table, b.lengths, cu)
+                S, cols = b.table.shape
                 if not ws:   # (the layers come one after the other: one workspace)
-                    nb = eb.cache_attn_workspace_bytes(q.shape[1], q.shape[2], cu is not None,
-                                                       b.lengths.shape[0], b.table.shape[1], pages)
+                    if b.groups is None:
+                        nb = eb.cache_attn_workspace_bytes(q.shape[1], q.shape[2], cu is not None,
+                                                           S, cols, pages)
+                    else:
+                        nb = eb.cache_attn_shared_workspace_bytes(
+                            q.shape[1], q.shape[2], S, b.groups[1].shape[0], cols, pages)
                     ws["ws"] = torch.empty((max(nb, 1),), dtype=torch.uint8, device=q.device)
-                return eb.cache_attn(q, pages, b.table, b.lengths, cu, self.scale,
-                                     workspace=ws["ws"])
+                if b.groups is None:
+                    return eb.cache_attn(q, pages, b.table, b.lengths, cu, self.scale,
+                                         workspace=ws["ws"])
+                return eb.cache_attn_shared(q, pages, b.table, b.lengths, *b.groups, cu, self.scale,
+                                            workspace=ws["ws"])
             return attn
-        return self._run(x, seqs, counts, attend, last_only=False)
+        return self._run(x, seqs, counts, attend, False, adapter, self.shared_prefixes)
 
-    def _run(self, x, seqs, counts, attend, last_only):
+    def generate(self, logits, embed, seqs, n: int, sampler, adapter=None):
+        """n tokens of each sequence from the logits [len(seqs), vocab] of its last
+        token on: each is drawn by the sampler and its row of embed [vocab, hidden]
+        put through a step, the last one too, so that the sequences hold them all:
+        (tokens int32 [len(seqs), n], their log probabilities)."""
+        if self.lm_head is None:
+            raise ValueError("generate draws from logits: the decoder has no LM head")
+        tokens, logprobs = [], []
+        for _ in range(n):
+            t, p = sampler(logits)
+            # (a row without tokens has -1: it goes on from the first)
+            x = embed.index_select(0, t.clamp(min=0))
+            _, logits = self.step(x[None], seqs, adapter=adapter)
+            tokens.append(t)
+            logprobs.append(p)
+        if not n:
+            dev = logits.device
+            return (torch.empty((len(seqs), 0), dtype=torch.int32, device=dev),
+                    torch.empty((len(seqs), 0), device=dev))
+        return torch.stack(tokens, 1), torch.stack(logprobs, 1)
+
+    def _run(self, x, seqs, counts, attend, last_only, adapter=None, share=False):
         seqs = list(seqs)
         if x.dim() != 3 or x.shape[0] != 1 or x.shape[1] != sum(counts) or not seqs \
                 or len(counts) != len(seqs):
             raise ValueError(f"x {tuple(x.shape)} is not [1, {sum(counts)}, hidden] of "
                              f"{len(counts)} counts for {len(seqs)} sequences")
-        held = [self.cache.length(s) for s in seqs]
+        if adapter is not None:
+            if self.adapters is None:
+                raise ValueError("the decoder has no adapters to choose from")
+            adapter = [int(i) for i in adapter]
+            if len(adapter) != len(seqs):
+                raise ValueError(f"{len(adapter)} adapters for {len(seqs)} sequences")
+            if any(not -1 <= i < self.n_adapters for i in adapter):
+                raise ValueError(f"adapters {adapter} of {self.n_adapters}")
+        held = {s: self.cache.length(s) for s in seqs}
         self.cache.extend(seqs, counts)
         try:
-            b = _Batch(self.cache, seqs, counts)
+            groups, back = None, None
+            if share:
+                order, groups = self._groups(seqs, counts)
+                if order is not None:        # a group's sequences one behind the other
+                    rows = np.split(np.arange(sum(counts)), np.cumsum(counts)[:-1])
+                    at = np.concatenate([rows[s] for s in order])
+                    at = torch.from_numpy(np.stack([at, np.argsort(at)])).to(x.device)
+                    x, back = x.index_select(1, at[0]), at[1]
+                    seqs, counts = [seqs[s] for s in order], [counts[s] for s in order]
+                    adapter = adapter and [adapter[s] for s in order]
+            b = _Batch(self.cache, seqs, counts, adapter, groups)
+            own = None if adapter is None else pf.BatchAdapters(
+                self.adapters, self.n_adapters, b.adapter, sum(counts),
+                None if b.uniform else b.cu)
             cos, sin = (t.index_select(0, b.positions) for t in (self.cos, self.sin))
             y = None
             for i, w in enumerate(self.layers):
-                x, y = pf._layer(x, y, w, self.shape, attend(i, b), cos, sin)
+                x, y = pf._layer(x, y, w, self.shape, attend(i, b), cos, sin,
+                                 correct=None if own is None else own.layer(i))
             x, y = x[0], y[0]
+            if back is not None:
+                x, y = x.index_select(0, back), y.index_select(0, back)
             if last_only:
                 at = (b.cu[1:] - 1).long()
                 x, y = x[at], y[at]
@@ -326,9 +441,51 @@ class Decoder:
         except BaseException:
             # the room is given back; what the layers that ran made of a page's
             # scale and older codes stays, as truncate says
-            for s, n in zip(seqs, held):
+            for s, n in held.items():
                 self.cache.truncate(s, n)
             raise
+
+    def _groups(self, seqs, counts):
+        """(the order of the sequences, None: as they are; the lists of their groups,
+        None: none worth it)."""
+        table, lengths = self.cache.table(seqs)
+        seen = (lengths - np.asarray(counts)) // self.cache.page_len
+        order, first, pages = prefix_groups(table, seen)
+        saved = sum((b - a - 1) * n for a, b, n in zip(first, first[1:], pages))
+        if not saved:
+            return None, None
+        return None if order == list(range(len(seqs))) else order, [first, pages]
+
+
+class Sampler:
+    """Draws each row's next token by its settings (binding.sample_tokens): a dict
+    for each row with any of temperature, top_k, top_p and min_p, or one number of
+    rows for plain draws.  The random numbers come from a generator of its own."""
+
+    SETTINGS = {"temperature": (1.0, torch.float32), "top_k": (0, torch.int32),
+                "top_p": (1.0, torch.float32), "min_p": (0.0, torch.float32)}
+
+    def __init__(self, requests, device="cuda", seed: int = 0):
+        if isinstance(requests, int):
+            requests = [{}] * requests
+        unknown = {k for r in requests for k in r} - set(self.SETTINGS)
+        if unknown:
+            raise ValueError(f"no settings of a request: {sorted(unknown)}")
+        self.rows = len(requests)
+        self.settings = {
+            name: torch.tensor([r.get(name, none) for r in requests], dtype=dtype).to(device)
+            for name, (none, dtype) in self.SETTINGS.items() if any(name in r for r in requests)}
+        self.generator = torch.Generator(device=device)
+        self.generator.manual_seed(seed)
+
+    def __call__(self, logits):
+        """(tokens int32 [rows], their log probabilities fp32 [rows])."""
+        if logits.shape[0] != self.rows:
+            raise ValueError(f"logits of {logits.shape[0]} rows for {self.rows} requests")
+        if self.rows > 1 and logits.stride(0) < logits.shape[1]:   # (one row, expanded)
+            logits = logits.contiguous()
+        u = torch.rand((self.rows,), generator=self.generator, device=logits.device)
+        return eb.sample_tokens(logits, u, **self.settings)
 
 
 def step_table(batches, contexts, shape: pf.DecoderShape, n_layers: int, reps: int,

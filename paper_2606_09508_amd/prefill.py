@@ -223,11 +223,115 @@ def _one_pass(x, w, shape: DecoderShape, cos, sin, quiet: bool | None = None) ->
             and cos.shape == sin.shape == (x.shape[1], 64) and _dense16(w["norm2"], cos, sin))
 
 
-def _layer(x, y, w, shape: DecoderShape, attn, cos, sin, trace=None, store=None):
+PROJECTIONS = ("wq", "wk", "wv", "wo", "w_gate", "w_up", "w_down")
+
+
+def check_adapters(adapters, layers) -> int:
+    """Adapters of a decoder: for each layer a dict of projections' names (those
+    of PROJECTIONS that have any) and their binding.Adapters, all for the same
+    number of adapters, which is returned."""
+    if len(adapters) != len(layers):
+        raise ValueError(f"adapters of {len(adapters)} layers for {len(layers)}")
+    count = None
+    for i, (mine, w) in enumerate(zip(adapters, layers)):
+        for name, t in mine.items():
+            if name not in PROJECTIONS:
+                raise ValueError(f"layer {i} has no projection {name!r}")
+            a, b, scale = t
+            n = a.shape[0]
+            count = n if count is None else count
+            if a.dim() != 3 or b.dim() != 3 or tuple(a.shape) != (count, a.shape[1], w[name].shape[0]) \
+                    or tuple(b.shape) != (count, w[name].shape[1], a.shape[1]) \
+                    or (scale is not None and tuple(scale.shape) != (count,)):
+                raise ValueError(f"{name} of layer {i}: adapters {tuple(a.shape)} and "
+                                 f"{tuple(b.shape)} do not correct {count} times a product of "
+                                 f"{tuple(w[name].shape)}")
+    return 0 if count is None else count
+
+
+def adapter_index(adapter, n_seqs: int, adapters, device):
+    """int32 [n_seqs] on the device of a list of adapters' numbers."""
+    if adapters is None:
+        raise ValueError("there are no adapters to choose from")
+    if len(adapter) != n_seqs:
+        raise ValueError(f"{len(adapter)} adapters for {n_seqs} sequences")
+    return torch.tensor([int(i) for i in adapter], dtype=torch.int32).to(device)
+
+
+class BatchAdapters:
+    """The adapters of a batch's sequences: of `count` adapters (what
+    check_adapters returned) those that index names (int32 [sequences], on the
+    device; outside of [0, count): none), for n_tokens packed tokens, cu as
+    binding.adapter_plan takes it.  layer(i) corrects that layer's products."""
+
+    def __init__(self, adapters, count: int, index, n_tokens: int, cu=None):
+        self.adapters, self.n = adapters, count
+        self.index, self.n_tokens, self.cu = index, n_tokens, cu
+        self._plan = None
+
+    def layer(self, i: int):
+        return functools.partial(self._correct, self.adapters[i])
+
+    def _correct(self, mine, h, names, ys):
+        """The products ys of h with the projections of these names, corrected:
+        in place by the kernel, those of one rank in one call, where that computes
+        all that the tensor operations would."""
+        ranks = {}
+        for i, name in enumerate(names):
+            if name in mine and self.n and self.n_tokens:
+                ranks.setdefault(mine[name].a.shape[1], []).append(i)
+        if not ranks:
+            return ys
+        ys, quiet = list(ys), _quiet(h.device)
+        for rank, at in ranks.items():
+            of = [mine[names[i]] for i in at]
+            if quiet and self._fits(h, rank, [ys[i] for i in at], of):
+                if self._plan is None:
+                    self._plan = eb.adapter_plan(self.index, self.n, self.n_tokens, self.cu)
+                eb.adapter_add(h, [ys[i] for i in at], of, self._plan)
+            else:
+                for i, t in zip(at, of):
+                    ys[i] = self._tensors(h, ys[i], t)
+        return ys
+
+    @staticmethod
+    def _fits(h, rank, ys, of) -> bool:
+        """Sizes, types and layout ei_adapter_add takes."""
+        ts = [t for a, b, _ in of for t in (a, b)]
+        scales = [s for _, _, s in of if s is not None]
+        return (rank % 8 == 0 and 0 < rank <= 128 and _ordinary(h, *ys, *ts, *scales)
+                and all(t.dtype == torch.bfloat16 and t.shape[-1] % 8 == 0 and _dense16(t)
+                        for t in (h, *ys, *ts))
+                and all(s.dtype == torch.float32 and s.is_contiguous() for s in scales))
+
+    def _tensors(self, h, y, t):
+        """The same by tensor operations: fp32, and one rounding to y's type."""
+        if self.cu is None:
+            which = self.index.repeat_interleave(self.n_tokens // self.index.shape[0])
+        else:
+            at = torch.arange(self.n_tokens, dtype=torch.int32, device=self.index.device)
+            which = self.index[torch.searchsorted(self.cu[1:].contiguous(), at, right=True)]
+        a, b, scale = t
+        hf, out = h.flatten(0, -2).float(), torch.zeros_like(y.flatten(0, -2), dtype=torch.float32)
+        for i in range(self.n):
+            d = (hf @ a[i].float().t()) @ b[i].float().t()
+            d = d if scale is None else d * scale[i]
+            out = torch.where((which == i)[:, None], d, out)
+        return (y.float() + out.view(y.shape)).to(y.dtype)
+
+
+def _products(h, w, names, correct):
+    """h times the weights of these names, each with its adapters' correction."""
+    ys = [h @ w[n] for n in names]
+    return ys if correct is None else correct(h, names, ys)
+
+
+def _layer(x, y, w, shape: DecoderShape, attn, cos, sin, trace=None, store=None, correct=None):
     """One decoder layer on the hidden state x + y (y None: x itself); returns
     the new hidden state as two summands, so that a following layer's norm
     takes their sum in the pass that reads it.  ``store`` (optional) receives
-    the rotated keys and the values."""
+    the rotated keys and the values, ``correct`` (optional, BatchAdapters.layer)
+    each product with the weights."""
     B, N, _ = x.shape
     Hq, Hkv, D = shape.n_q_heads, shape.n_kv_heads, shape.head_dim
     quiet = _quiet(x.device)   # once a layer: each look costs a small prompt ~2 us
@@ -239,9 +343,9 @@ def _layer(x, y, w, shape: DecoderShape, attn, cos, sin, trace=None, store=None)
     else:
         x = x if y is None else x + y
         h = _rmsnorm(x, w["norm1"], shape.rms_eps)
-    q, k, v = ((h @ w[n]).view(B, N, heads, D)
-               for n, heads in (("wq", Hq), ("wk", Hkv), ("wv", Hkv)))
-    if one_pass:
+    q, k, v = (t.view(B, N, heads, D) for t, heads in
+               zip(_products(h, w, ("wq", "wk", "wv"), correct), (Hq, Hkv, Hkv)))
+    if one_pass and (correct is None or _ordinary(q, k, v)):   # (adapters may have gradients)
         q, k, v = eb.rope_heads(q, k, v, cos, sin)
     else:
         q, k, v = (t.transpose(1, 2).contiguous() for t in (q, k, v))
@@ -251,16 +355,18 @@ def _layer(x, y, w, shape: DecoderShape, attn, cos, sin, trace=None, store=None)
     o = attn(q, k, v)
     if trace is not None:
         trace.update(q=q.clone(), k=k.clone(), v=v.clone(), o=o.clone())
-    y = o.transpose(1, 2).reshape(B, N, Hq * D) @ w["wo"]
+    y, = _products(o.transpose(1, 2).reshape(B, N, Hq * D), w, ("wo",), correct)
     if one_pass and _adds(x, y):   # (the attention may be a caller's own, with gradients)
         x, h = eb.add_rmsnorm(x, y, w["norm2"], shape.rms_eps)
-        g = h @ w["w_gate"]
-        m = eb.swiglu(g, h @ w["w_up"], out=g)
     else:
-        x = x + y
+        x, one_pass = x + y, False
         h = _rmsnorm(x, w["norm2"], shape.rms_eps)
-        m = torch.nn.functional.silu(h @ w["w_gate"]) * (h @ w["w_up"])
-    return x, m @ w["w_down"]
+    g, u = _products(h, w, ("w_gate", "w_up"), correct)
+    if one_pass and (correct is None or _ordinary(g, u)):
+        m = eb.swiglu(g, u, out=g)
+    else:
+        m = torch.nn.functional.silu(g) * u
+    return x, _products(m, w, ("w_down",), correct)[0]
 
 
 def layer_forward(x, w, shape: DecoderShape, attn: Attention, cos, sin, trace=None):
@@ -282,20 +388,28 @@ def finish(x, y, layers, shape: DecoderShape, lm_head=None):
     return last, (last @ lm_head if lm_head is not None else None)
 
 
-def prefill(x, layers, shape: DecoderShape, attn: Attention, lm_head=None, store=None):
+def prefill(x, layers, shape: DecoderShape, attn: Attention, lm_head=None, store=None,
+            adapters=None, adapter=None):
     """All layers over the prompt's hidden states x [B, N, hidden]; returns the
     final normed hidden state of the last token (and its logits when an LM
     head [hidden, vocab] is given) -- what the first generated token needs.
     ``store`` (optional) receives (layer index, keys, values) of every layer,
     as decode.PagedCache.storing takes them; where it is a context manager, the
-    layers run inside it, so that it learns of a failure."""
-    N = x.shape[1]
+    layers run inside it, so that it learns of a failure.  ``adapters``
+    (optional, as check_adapters takes them) correct the projections' products
+    of sequence b with adapter[b] (an integer; -1: none)."""
+    B, N, _ = x.shape
+    own = None
+    if adapter is not None:
+        index = adapter_index(adapter, B, adapters, x.device)
+        own = BatchAdapters(adapters, check_adapters(adapters, layers), index, B * N)
     cos, sin = rope_tables(N, shape.head_dim, shape.rope_theta, x.device)
     y = None
     with store if hasattr(store, "__exit__") else contextlib.nullcontext():
         for i, w in enumerate(layers):
             x, y = _layer(x, y, w, shape, attn, cos, sin,
-                          store=None if store is None else functools.partial(store, i))
+                          store=None if store is None else functools.partial(store, i),
+                          correct=None if own is None else own.layer(i))
         return finish(x[:, -1:], None if y is None else y[:, -1:], layers, shape, lm_head)
 
 

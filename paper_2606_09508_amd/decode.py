@@ -315,7 +315,14 @@ class Decoder:
     ``adapters`` (optional) is what prefill.check_adapters takes; prompts, step and
     generate then take ``adapter``, each sequence's number (-1: none).  With
     ``shared_prefixes`` the steps read pages that sequences share once for all of
-    them (binding.cache_attn_shared); its results differ by roundings."""
+    them (binding.cache_attn_shared) where that saves enough; its results differ
+    by roundings."""
+
+    # cache_attn_shared takes the place of cache_attn from so many keys on (times KV
+    # heads) that it does not read again: its plan and join cost 10 to 18 us, which
+    # so many keys take (32/8 heads, us of the one and the other: 4 x 4096 shared 29,
+    # 30; 16 x 4096 29, 29; 8 x 16384 49, 35; 64 x 4096 84, 36; but 64 x 1024 17, 32)
+    shared_least = 5 << 17
 
     def __init__(self, layers, shape: pf.DecoderShape, cache: PagedCache, lm_head=None,
                  adapters=None, shared_prefixes: bool = False):
@@ -452,7 +459,7 @@ class Decoder:
         seen = (lengths - np.asarray(counts)) // self.cache.page_len
         order, first, pages = prefix_groups(table, seen)
         saved = sum((b - a - 1) * n for a, b, n in zip(first, first[1:], pages))
-        if not saved:
+        if saved * self.cache.page_len * self.shape.n_kv_heads < self.shared_least:
             return None, None
         return None if order == list(range(len(seqs))) else order, [first, pages]
 

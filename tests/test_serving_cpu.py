@@ -67,6 +67,7 @@ def test_decoder_groups_follow_forks(monkeypatch):
     monkeypatch.setattr(eb, "cache_copy", lambda pages, src, dst: None)
     cache = decode.PagedCache(SHAPE, 2, 40, 8, 640, 64, torch.int8, "cpu")
     dec = decode.Decoder([], SHAPE, cache, shared_prefixes=True)
+    dec.shared_least = 1
     a, other = cache.add(), cache.add()
     cache.extend([a, other], [150, 200])
     b, c = cache.fork(a), cache.fork(a)
@@ -77,6 +78,12 @@ def test_decoder_groups_follow_forks(monkeypatch):
     assert sorted(order) == [0, 1, 2, 3]
     order, groups = dec._groups([a, other], [1, 1])
     assert order is None and groups is None
+    # two times two pages of 64 keys of one head are saved
+    dec.shared_least = 256
+    assert dec._groups(seqs, [1, 1, 1, 1])[1] is not None
+    dec.shared_least = 257
+    assert dec._groups(seqs, [1, 1, 1, 1]) == (None, None)
+    dec.shared_least = 1
     # in order already: left so, or put in another
     order, groups = dec._groups([a, b, c], [1, 1, 1])
     assert groups == [[0, 3], [2]] and (order is None or sorted(order) == [0, 1, 2])

@@ -220,22 +220,37 @@ __device__ __forceinline__ Settings settings_of(const SampleArgs& a, int64_t row
 }
 
 __device__ __forceinline__ uint64_t wave_sum_u64(uint64_t v) {
+#define EI_ADD_DPP(ctrl)                                                              \
+  v += (uint64_t)EI_DPP_U32((uint32_t)(v >> 32), ctrl, 0xF, false) << 32 |            \
+       EI_DPP_U32((uint32_t)v, ctrl, 0xF, false)
+  EI_ADD_DPP(0xB1);     // quad_perm [1,0,3,2]
+  EI_ADD_DPP(0x4E);     // quad_perm [2,3,0,1]
+  EI_ADD_DPP(0x141);    // row_half_mirror
+  EI_ADD_DPP(0x140);    // row_mirror
+#undef EI_ADD_DPP
+  uint64_t s = 0;
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
-  return v;
+  for (int l = 0; l < kWave; l += 16)
+    s += (uint64_t)rl_u32((uint32_t)(v >> 32), l) << 32 | rl_u32((uint32_t)v, l);
+  return s;
 }
 __device__ __forceinline__ float wave_sum_f32(float v) {
 #pragma unroll
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
   return v;
 }
-template <class T>
-__device__ __forceinline__ T wave_up_to(T v, int lane) {
-#pragma unroll
-  for (int o = 1; o < kWave; o <<= 1) {
-    const T t = __shfl_up(v, o);
-    if (lane >= o) v += t;
-  }
+// The sum over this lane and those before it.
+__device__ __forceinline__ uint64_t wave_up_to(uint64_t v) {
+#define EI_ADD_DPP(ctrl, rows)                                                        \
+  v += (uint64_t)EI_DPP_U32((uint32_t)(v >> 32), ctrl, rows, true) << 32 |            \
+       EI_DPP_U32((uint32_t)v, ctrl, rows, true)
+  EI_ADD_DPP(0x111, 0xF);   // row_shr:1
+  EI_ADD_DPP(0x112, 0xF);
+  EI_ADD_DPP(0x114, 0xF);
+  EI_ADD_DPP(0x118, 0xF);
+  EI_ADD_DPP(0x142, 0xA);   // row_bcast:15 into rows 1, 3
+  EI_ADD_DPP(0x143, 0xC);   // row_bcast:31 into rows 2, 3
+#undef EI_ADD_DPP
   return v;
 }
 
@@ -413,7 +428,7 @@ __device__ __forceinline__ uint64_t block_sum(PickSmem& sm, uint64_t v) {
 // The sum over this thread and those before it.
 __device__ __forceinline__ uint64_t block_up_to(PickSmem& sm, uint64_t v) {
   const int wave = threadIdx.x / kWave;
-  v = wave_up_to(v, threadIdx.x % kWave);
+  v = wave_up_to(v);
   __syncthreads();
   if (threadIdx.x % kWave == kWave - 1) sm.wave_sum[wave] = v;
   __syncthreads();
@@ -791,7 +806,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a,
   auto kept = [&](uint64_t before) { return before < cut.count ? before : cut.count; };
   // the sum over this thread and those before it
   auto up_to = [&](int which, uint64_t v, uint64_t& total) -> uint64_t {
-    v = wave_up_to(v, lane);
+    v = wave_up_to(v);
     if (lane == kWave - 1) wave_sum[which][wave] = v;
     __syncthreads();
     total = 0;
@@ -828,9 +843,9 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a,
       if (key > cut.key) mine += s.w.kept(x[e]);
       n_same += key != 0 && key == cut.key;
     }
-    const uint64_t same_end = same + wave_up_to(n_same, lane), same_begin = same_end - n_same;
+    const uint64_t same_end = same + wave_incl_scan_u32(n_same), same_begin = same_end - n_same;
     mine += (kept(same_end) - kept(same_begin)) * w_cut;
-    const uint64_t mine_end = run + wave_up_to(mine, lane);
+    const uint64_t mine_end = run + wave_up_to(mine);
     uint64_t to = mine_end - mine;
     if (to <= want && want < mine_end) {
       uint64_t n = same_begin;
@@ -877,22 +892,6 @@ struct RowSmem {
   int small_count, found;
   uint64_t small_sum, found_before, found_weight, found_count;
 };
-
-__device__ __forceinline__ uint64_t wave_sum_u64_dpp(uint64_t v) {
-#define EI_ADD_DPP(ctrl)                                                              \
-  v += (uint64_t)EI_DPP_U32((uint32_t)(v >> 32), ctrl, 0xF, false) << 32 |            \
-       EI_DPP_U32((uint32_t)v, ctrl, 0xF, false)
-  EI_ADD_DPP(0xB1);     // quad_perm [1,0,3,2]
-  EI_ADD_DPP(0x4E);     // quad_perm [2,3,0,1]
-  EI_ADD_DPP(0x141);    // row_half_mirror
-  EI_ADD_DPP(0x140);    // row_mirror
-#undef EI_ADD_DPP
-  uint64_t s = 0;
-#pragma unroll
-  for (int l = 0; l < kWave; l += 16)
-    s += (uint64_t)rl_u32((uint32_t)(v >> 32), l) << 32 | rl_u32((uint32_t)v, l);
-  return s;
-}
 
 // The magnitude bits of a bf16 number, those of `x` (>= 0) rounded up.
 __device__ __forceinline__ int bits_above(double x) {
@@ -1186,7 +1185,7 @@ __global__ __launch_bounds__(kThreads) void sample_row_kernel(SampleArgs a, int6
       }
       if (any_small(most))
         each_small_of(words, [&](uint32_t bits, int) { sum += small_weight(bits); });
-      sum = wave_sum_u64_dpp(sum);
+      sum = wave_sum_u64(sum);
     }
     if (lane == 0) sm.piece_sum[q] = sum;
   });
@@ -1225,13 +1224,13 @@ __global__ __launch_bounds__(kThreads) void sample_row_kernel(SampleArgs a, int6
     mine[e] = off >= kSide ? small_weight(bits) : sm.weight[entry];
     n_same += (uint32_t)(mine[e] >> kSameBit);
   }
-  uint64_t same = sm.found_count + wave_up_to(n_same, lane) - n_same;
+  uint64_t same = sm.found_count + wave_incl_scan_u32(n_same) - n_same;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     if (mine[e] >> kSameBit) mine[e] = same++ < cut.count ? w_cut : 0;
     all += mine[e];
   }
-  uint64_t run = sm.found_before + wave_up_to(all, lane) - all;
+  uint64_t run = sm.found_before + wave_up_to(all) - all;
   if (!(run <= want && want < run + all)) return;
 #pragma unroll
   for (int e = 0; e < 8; ++e) {

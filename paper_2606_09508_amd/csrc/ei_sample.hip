@@ -41,6 +41,8 @@ constexpr int kFew = 256;            // kept tokens that sample_cut_kernel picks
 constexpr int kMaxParts = 64;
 constexpr int kBins = 512;           // the last one: all that lies further off
 constexpr int kList = 4096;
+constexpr int kCUs = 256;
+constexpr int kLeastParts = 2;
 
 struct PartInfo {
   float top, sum;      // the largest logit; the sum of the finite ones, and how many
@@ -59,10 +61,14 @@ struct SampleArgs {
   int blocks;                  // of a row
   PartInfo* part;              // [rows][parts]
   struct RowCut* cut;          // [rows], of those with top-k or top-p
-  uint64_t* sums;              // [rows][blocks]: kept weights above the cut's key
+  uint64_t* sums;              // [rows][blocks]: kept weights above the cut's key (bf16: of pieces)
   uint32_t* equal;             // [rows][blocks]: tokens of that key
   uint64_t* bin_sums;          // [rows][kBins]
   uint32_t* bin_counts;        // [rows][kBins]
+  // of bf16 rows in several workgroups
+  float* tops;                 // [rows][parts]
+  struct RowState* state;      // [rows]
+  uint32_t* counts;            // [rows][kTable]
 };
 
 // The tokens above `key` and the first `count` of those that have it.
@@ -257,7 +263,6 @@ __device__ __forceinline__ uint64_t wave_up_to(uint64_t v) {
 // ----------------------------------------------------------------------------
 // Scan
 // ----------------------------------------------------------------------------
-template <int FMT>
 __global__ __launch_bounds__(kPartThreads) void sample_scan_kernel(SampleArgs a, int64_t unit0) {
   __shared__ PartInfo sm[kPartWaves];
   const int64_t unit = unit0 + blockIdx.x;
@@ -269,7 +274,7 @@ __global__ __launch_bounds__(kPartThreads) void sample_scan_kernel(SampleArgs a,
       a.bin_sums[row * kBins + b] = 0;
       a.bin_counts[row * kBins + b] = 0;
     }
-  const Row<FMT> r(a, row);
+  const Row<EI_LOGITS_FP32> r(a, row);
   const int b0 = part * a.part_blocks, b1 = min(b0 + a.part_blocks, a.blocks);
   float top = -INFINITY, sum = 0.0f;
   int finite = 0;
@@ -337,7 +342,6 @@ struct Bins {
 // ----------------------------------------------------------------------------
 // Bins
 // ----------------------------------------------------------------------------
-template <int FMT>
 __global__ __launch_bounds__(kPartThreads) void sample_bins_kernel(SampleArgs a, int64_t unit0) {
   __shared__ unsigned long long sums[kBins];
   __shared__ uint32_t counts[kBins];
@@ -349,7 +353,7 @@ __global__ __launch_bounds__(kPartThreads) void sample_bins_kernel(SampleArgs a,
   if (info.top == -INFINITY) return;
   const Settings s = settings_of(a, row, info.top);
   if (!s.cuts) return;
-  const Row<FMT> r(a, row);
+  const Row<EI_LOGITS_FP32> r(a, row);
   const int b0 = part * a.part_blocks, b1 = min(b0 + a.part_blocks, a.blocks);
   for (int b = threadIdx.x; b < kBins; b += kPartThreads) {
     sums[b] = 0;
@@ -522,12 +526,11 @@ __device__ __forceinline__ double log_share(const Settings& s, float x, uint64_t
   return y * 0.6931471805599453 - log((double)total * (1.0 / kOne));
 }
 
-template <int FMT>
 __global__ __launch_bounds__(kThreads) void sample_cut_kernel(SampleArgs a, int64_t row0) {
   __shared__ PickSmem sm;
   const int64_t row = row0 + blockIdx.x;
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const Row<FMT> r(a, row);
+  const Row<EI_LOGITS_FP32> r(a, row);
   const PartInfo info = row_info(a, row);
   if (info.top == -INFINITY) return;
   const Settings s = settings_of(a, row, info.top);
@@ -702,7 +705,6 @@ __global__ __launch_bounds__(kThreads) void sample_cut_kernel(SampleArgs a, int6
 // ----------------------------------------------------------------------------
 // Weigh
 // ----------------------------------------------------------------------------
-template <int FMT>
 __global__ __launch_bounds__(kPartThreads) void sample_weigh_kernel(SampleArgs a, int64_t unit0) {
   const int64_t unit = unit0 + blockIdx.x;
   const int64_t row = unit / a.parts;
@@ -712,7 +714,7 @@ __global__ __launch_bounds__(kPartThreads) void sample_weigh_kernel(SampleArgs a
   if (info.top == -INFINITY) return;
   const Settings s = settings_of(a, row, info.top);
   if (s.greedy) return;
-  const Row<FMT> r(a, row);
+  const Row<EI_LOGITS_FP32> r(a, row);
   const int b0 = part * a.part_blocks, b1 = min(b0 + a.part_blocks, a.blocks);
   if (!s.cuts) {
     for (int b = b0 + wave; b < b1; b += kPartWaves) {
@@ -759,7 +761,6 @@ __global__ __launch_bounds__(kPartThreads) void sample_weigh_kernel(SampleArgs a
 // ----------------------------------------------------------------------------
 constexpr int kPickWaves = kPickThreads / kWave;
 
-template <int FMT>
 __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a, int64_t row0) {
   __shared__ uint64_t wave_sum[2][kPickWaves];
   __shared__ uint32_t wave_min[kPickWaves];
@@ -767,7 +768,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a,
   __shared__ int found;
   const int64_t row = row0 + blockIdx.x;
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const Row<FMT> r(a, row);
+  const Row<EI_LOGITS_FP32> r(a, row);
   const PartInfo info = row_info(a, row);
   if (info.top == -INFINITY) {
     if (threadIdx.x == 0) answer(a, row, -1, -INFINITY);
@@ -891,6 +892,7 @@ struct RowSmem {
   float wave_top[kWaves];
   int small_count, found;
   uint64_t small_sum, found_before, found_weight, found_count;
+  uint64_t wave_sums[kWaves][2];
 };
 
 // The magnitude bits of a bf16 number, those of `x` (>= 0) rounded up.
@@ -900,19 +902,45 @@ __device__ __forceinline__ int bits_above(double x) {
   return min((int)b + 2, 0x7f7f);     // (the conversion may have rounded down)
 }
 
-__global__ __launch_bounds__(kThreads) void sample_row_kernel(SampleArgs a, int64_t row0) {
-  __shared__ RowSmem sm;
-  const int64_t row = row0 + blockIdx.x;
-  const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  const Row<EI_LOGITS_BF16> r(a, row);
+// What several workgroups of a row have in common.
+struct RowState {
+  Cut cut;
+  uint64_t small_sum;
+  uint32_t small_count;
+  uint32_t split;
+};
 
-  // A wave has `per` pieces in a row.  All of them: use(words, piece), four loads
-  // under way while four pieces are used.  (The row is read again for each pass, from
-  // the caches: in registers, 64 a thread, the passes have to be unrolled, and waiting
-  // for code that runs once took most of the time, 62 us for a row of 128256.)
-  const int pieces = (a.vocab + kPiece - 1) / kPiece, full = a.vocab / kPiece;
-  const int per = (pieces + kWaves - 1) / kWaves, q0 = wave * per, q1 = min(q0 + per, pieces);
-  auto each_piece = [&](auto use) {
+struct RowWork {
+  const SampleArgs& a;
+  RowSmem& sm;
+  const int64_t row;
+  const Row<EI_LOGITS_BF16> r;
+  const int lane, wave, full, pieces;
+  int q0, q1;                  // this wave's pieces
+  Settings s;
+  int base_p, base_n;
+  Cut cut;
+  bool split;                  // not all tokens of the cut's key are kept
+
+  __device__ __forceinline__ RowWork(const SampleArgs& a_, RowSmem& sm_, int64_t row_)
+      : a(a_), sm(sm_), row(row_), r(a_, row_), lane(threadIdx.x % kWave), wave(threadIdx.x / kWave),
+        full(a_.vocab / kPiece), pieces((a_.vocab + kPiece - 1) / kPiece), cut{0, 0}, split(false) {
+    take(0, 1);
+  }
+  // The workgroup's are part `part` of `parts`; a wave's lie one behind the other.
+  __device__ __forceinline__ void take(int part, int parts) {
+    const int of_part = (pieces + parts - 1) / parts, per = (of_part + kWaves - 1) / kWaves;
+    const int p0 = min(part * of_part, pieces), p1 = min(p0 + of_part, pieces);
+    q0 = min(p0 + wave * per, p1);
+    q1 = min(q0 + per, p1);
+  }
+
+  // All of them: use(words, piece), four loads under way while four pieces are used.
+  // (The row is read again for each pass, from the caches: in registers, 64 a thread,
+  // the passes have to be unrolled, and waiting for code that runs once took most of
+  // the time, 62 us for a row of 128256.)
+  template <class Use>
+  __device__ __forceinline__ void each_piece(Use use) const {
     constexpr int kAhead = 4;
     uint4 next[kAhead];
     const int qf = min(q1, full);
@@ -941,28 +969,28 @@ __global__ __launch_bounds__(kThreads) void sample_row_kernel(SampleArgs a, int6
       const uint32_t words[4] = {now.x, now.y, now.z, now.w};
       use(words, q);
     }
-  };
-  auto bits_of = [](const uint32_t (&words)[4], int e) {
-    return e & 1 ? words[e / 2] >> 16 : words[e / 2] & 0xffffu;
-  };
-  auto value = [](uint32_t bits) { return __uint_as_float(bits << 16); };
-
-  float top = -INFINITY;
-  each_piece([&](const uint32_t (&words)[4], int) {
-#pragma unroll
-    for (int w = 0; w < 4; ++w) top = fmaxf(top, fmaxf(bf16_lo(words[w]), bf16_hi(words[w])));
-  });
-  top = wave_max_f32_dpp(top);
-  if (lane == 0) sm.wave_top[wave] = top;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sm.wave_top[w]);
-  if (top == -INFINITY) {
-    if (threadIdx.x == 0) answer(a, row, -1, -INFINITY);
-    return;
   }
-  const Settings s = settings_of(a, row, top);
-  if (s.greedy) {
+  __device__ __forceinline__ static uint32_t bits_of(const uint32_t (&words)[4], int e) {
+    return e & 1 ? words[e / 2] >> 16 : words[e / 2] & 0xffffu;
+  }
+  __device__ __forceinline__ static float value(uint32_t bits) { return __uint_as_float(bits << 16); }
+
+  __device__ __forceinline__ float largest() {
+    float top = -INFINITY;
+    each_piece([&](const uint32_t (&words)[4], int) {
+#pragma unroll
+      for (int w = 0; w < 4; ++w) top = fmaxf(top, fmaxf(bf16_lo(words[w]), bf16_hi(words[w])));
+    });
+    top = wave_max_f32_dpp(top);
+    if (lane == 0) sm.wave_top[wave] = top;
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) top = fmaxf(top, sm.wave_top[w]);
+    return top;
+  }
+
+  // The first token of the largest logit.
+  __device__ __forceinline__ void take_largest(float top) {
     uint32_t at = UINT_MAX;
     each_piece([&](const uint32_t (&words)[4], int q) {
 #pragma unroll
@@ -976,56 +1004,62 @@ __global__ __launch_bounds__(kThreads) void sample_row_kernel(SampleArgs a, int6
       for (int w = 0; w < kWaves; ++w) at = min(at, sm.pick.wave_bits[0][w]);
       answer(a, row, (int)at, 0.0);
     }
-    return;
   }
 
   // The tables: entry i of a sign is the magnitude base - i.  Negative logits past
   // 46 binary places below the top weigh nothing.
-  const int base_p = max(top > 0.0f ? (int)(__float_as_uint(top) >> 16) : 0, kSide);
-  const int base_n = max(bits_above(46.0 / s.w.per_t - s.w.top), kSide);
-  for (int i = threadIdx.x; i < kTable; i += kThreads) {
-    const int off = i & kSide, mag = (i > kSide ? base_n : base_p) - off;
-    const uint32_t bits = (uint32_t)mag | (i > kSide ? 0x8000u : 0u);
-    sm.weight[i] = off < kSide ? s.w.of(value(bits)) : 0;
-    sm.count[i] = 0;
+  __device__ __forceinline__ void place_tables(const Settings& settings, float top) {
+    s = settings;
+    base_p = max(top > 0.0f ? (int)(__float_as_uint(top) >> 16) : 0, kSide);
+    base_n = max(bits_above(46.0 / s.w.per_t - s.w.top), kSide);
   }
-  if (threadIdx.x == 0) {
-    sm.small_count = 0;
-    sm.small_sum = 0;
+  __device__ __forceinline__ uint32_t bits_at(int entry) const {
+    return entry > kSide ? 0x8000u | (uint32_t)(base_n - (entry - kSide - 1))
+                         : (uint32_t)(base_p - entry);
   }
-  __syncthreads();
-  // (off: the entry, as it is; kSide and more: nearer to 0 than the table, below zero:
+  __device__ __forceinline__ void clear_counts() {
+    for (int i = threadIdx.x; i < kTable; i += kThreads) sm.count[i] = 0;
+    if (threadIdx.x == 0) {
+      sm.small_count = 0;
+      sm.small_sum = 0;
+    }
+  }
+  __device__ __forceinline__ void fill_weights() {
+    for (int i = threadIdx.x; i < kTable; i += kThreads)
+      sm.weight[i] = (i & kSide) < kSide ? s.w.of(value(bits_at(i))) : 0;
+  }
+
+  // (the entry, as it is; kSide and more: nearer to 0 than the table, below zero:
   // weighs nothing, NaN and -inf among them)
-  auto off_of = [&](uint32_t bits) -> int {
+  __device__ __forceinline__ int off_of(uint32_t bits) const {
     return (bits & 0x8000u ? base_n : base_p) - (int)(bits & 0x7fffu);
-  };
+  }
   // The entries of two logits (the last of their sign where they have none), 8 times
   // each, in 16-bit pairs; `off`: theirs.
-  const uint32_t base_p2 = (uint32_t)base_p * 0x10001u, base_n2 = (uint32_t)base_n * 0x10001u;
-  auto entries_of = [&](uint32_t word, s16x2& off) -> uint32_t {
+  __device__ __forceinline__ uint32_t entries_of(uint32_t word, s16x2& off) const {
+    const uint32_t base_p2 = (uint32_t)base_p * 0x10001u, base_n2 = (uint32_t)base_n * 0x10001u;
     const uint32_t sign = __builtin_bit_cast(uint32_t, __builtin_bit_cast(s16x2, word) >> 15);
     const uint32_t base = (sign & base_n2) | (~sign & base_p2);
     off = __builtin_bit_cast(s16x2, base) - __builtin_bit_cast(s16x2, word & 0x7fff7fffu);
     const u16x2 at = __builtin_elementwise_min(__builtin_bit_cast(u16x2, off), u16x2{kSide, kSide});
     const uint32_t entry = (sign & (uint32_t)((kSide + 1) * 0x10001)) | __builtin_bit_cast(uint32_t, at);
     return entry << 3;
-  };
-  auto any_small = [&](s16x2 most) { return most.x >= kSide || most.y >= kSide; };
-
-  // those nearer to 0 than the tables, of a thread's piece: use(bits, place)
-  auto each_small_of = [&](const uint32_t (&words)[4], auto use) {
+  }
+  __device__ __forceinline__ static bool any_small(s16x2 most) { return most.x >= kSide || most.y >= kSide; }
+  // those nearer to 0 than the tables, of a thread's piece: use(bits)
+  template <class Use>
+  __device__ __forceinline__ void each_small_of(const uint32_t (&words)[4], Use use) const {
     const uint32_t w0 = words[0], w1 = words[1], w2 = words[2], w3 = words[3];
 #pragma unroll 1
     for (int e = 0; e < 8; ++e) {
       const uint32_t w = e < 4 ? e < 2 ? w0 : w1 : e < 6 ? w2 : w3;
       const uint32_t bits = e & 1 ? w >> 16 : w & 0xffffu;
-      if (off_of(bits) >= kSide) use(bits, e);
+      if (off_of(bits) >= kSide) use(bits);
     }
-  };
+  }
 
-  Cut cut{0, 0};
-  bool split = false;          // not all tokens of the cut's key are kept
-  if (s.cuts) {
+  // The tokens of each entry.
+  __device__ __forceinline__ void count() {
     uint64_t small_sum = 0;
     int small_count = 0;
     each_piece([&](const uint32_t (&words)[4], int) {
@@ -1042,7 +1076,7 @@ __global__ __launch_bounds__(kThreads) void sample_row_kernel(SampleArgs a, int6
         atomicAdd(&sm.count[(hi & kNone) == kNone ? kTable + lane : hi >> 3], 1u);
       }
       if (any_small(most))
-        each_small_of(words, [&](uint32_t bits, int) {
+        each_small_of(words, [&](uint32_t bits) {
           ++small_count;
           small_sum += s.w.of(value(bits));
         });
@@ -1051,7 +1085,11 @@ __global__ __launch_bounds__(kThreads) void sample_row_kernel(SampleArgs a, int6
       atomicAdd(&sm.small_count, small_count);
       atomicAdd((unsigned long long*)&sm.small_sum, (unsigned long long)small_sum);
     }
-    __syncthreads();
+  }
+
+  // The cut of top-k and top-p, from the counts and weights; the pieces taken are the
+  // whole row's.
+  __device__ __forceinline__ void find() {
     // the values in their order, four a thread: positive, near 0, negative
     constexpr int kEach = kTable / kThreads;
     auto place_of = [](int at) { return at <= kSide ? at : kSide + 1 + (2 * kSide - at); };
@@ -1067,23 +1105,31 @@ __global__ __launch_bounds__(kThreads) void sample_row_kernel(SampleArgs a, int6
       n_all += counts_at((int)threadIdx.x * kEach + i);
       w_all += weights_at((int)threadIdx.x * kEach + i);
     }
-    const uint64_t n_to = block_up_to(sm.pick, n_all), w_to = block_up_to(sm.pick, w_all);
-    const uint64_t total_n = block_sum(sm.pick, n_all);
-    auto key_at = [&](int entry) {
-      const uint32_t bits = entry > kSide ? 0x8000u | (uint32_t)(base_n - (entry - kSide - 1))
-                                          : (uint32_t)(base_p - entry);
-      return key_of(value(bits));
-    };
+    // (both sums at once)
+    uint64_t n_to = wave_up_to(n_all), w_to = wave_up_to(w_all), total_n = 0, total_w = 0;
+    if (lane == kWave - 1) {
+      sm.wave_sums[wave][0] = n_to;
+      sm.wave_sums[wave][1] = w_to;
+    }
+    __syncthreads();
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const uint64_t n = sm.wave_sums[w][0], v = sm.wave_sums[w][1];
+      n_to += w < wave ? n : 0;
+      w_to += w < wave ? v : 0;
+      total_n += n;
+      total_w += v;
+    }
     auto each_small = [&](auto use) {
 #pragma unroll 1
       for (int q = q0; q < q1; ++q) {
         const uint4 again = r.load_raw(q, lane);
         const uint32_t words[4] = {again.x, again.y, again.z, again.w};
-        each_small_of(words, [&](uint32_t bits, int) { use(key_of(value(bits))); });
+        each_small_of(words, [&](uint32_t bits) { use(key_of(value(bits))); });
       }
     };
     auto weight = [&](uint32_t key) { return s.w.of(logit_of(key)); };
-    uint64_t total_w = block_sum(sm.pick, w_all), cut_before = 0;
+    uint64_t cut_before = 0;
     int cut_at = -1;
     uint64_t same = 0;         // tokens of the cut's key
     // top-k by counts, then top-p by weights
@@ -1137,108 +1183,249 @@ __global__ __launch_bounds__(kThreads) void sample_row_kernel(SampleArgs a, int6
                        [&](uint32_t key) { return by_count ? (uint64_t)1 : weight(key); });
       } else {
         const uint64_t v = by_count ? 1 : sm.weight[cut_at];
-        cut = Cut{key_at(cut_at), (want + v - 1) / v};
+        cut = Cut{key_of(value(bits_at(cut_at))), (want + v - 1) / v};
       }
     }
     if (cut.key) split = cut_at == kSide || cut.count < same;
     __syncthreads();
   }
 
-  // What is not kept weighs nothing from here on.  The cut's own key, where its tokens
-  // are split, weighs kSame: a piece's sum (2^53 at most) then counts them above it.
-  constexpr int kSameBit = 54;
-  constexpr uint64_t kSame = (uint64_t)1 << kSameBit;
-  static_assert((uint64_t)kPiece * kSame != 0 && kPiece <= 1 << (63 - kSameBit), "512 of them");
-  const uint64_t w_cut = split ? s.w.kept(logit_of(cut.key)) : 0;
-  auto left_of = [&](uint32_t key, uint64_t w) -> uint64_t {
+  // What is not kept weighs nothing.  The cut's own key, where its tokens are split,
+  // weighs kSame: a piece's sum (2^53 at most) then counts them above it.
+  static constexpr int kSameBit = 54;
+  static constexpr uint64_t kSame = (uint64_t)1 << kSameBit;
+  static_assert(kPiece <= 1 << (63 - kSameBit), "512 of them");
+  __device__ __forceinline__ uint64_t left_of(uint32_t key, uint64_t w) const {
     return split && key == cut.key ? kSame : key < cut.key || w < s.w.least ? 0 : w;
-  };
-  for (int i = threadIdx.x; i < kTable; i += kThreads) {
-    const int off = i & kSide, mag = (i > kSide ? base_n : base_p) - off;
-    const uint32_t bits = (uint32_t)mag | (i > kSide ? 0x8000u : 0u);
-    if (off < kSide) sm.weight[i] = left_of(key_of(value(bits)), sm.weight[i]);
   }
-  __syncthreads();
-  const float least = cut.key ? logit_of(cut.key) : -INFINITY;
-  auto kept = [&](uint64_t before) { return before < cut.count ? before : cut.count; };
-  auto small_weight = [&](uint32_t bits) {
+  __device__ __forceinline__ uint64_t small_weight(uint32_t bits) const {
     return left_of(key_of(value(bits)), s.w.of(value(bits)));
-  };
-  each_piece([&](const uint32_t (&words)[4], int q) {
-    uint64_t sum = 0;
-    bool some = true;
-    if (cut.key) {
-      float most = -INFINITY;
+  }
+  __device__ __forceinline__ void keep() {
+    for (int i = threadIdx.x; i < kTable; i += kThreads)
+      if ((i & kSide) < kSide) sm.weight[i] = left_of(key_of(value(bits_at(i))), sm.weight[i]);
+  }
+
+  // The kept weights of each piece.
+  __device__ __forceinline__ void weigh(uint64_t* piece_sum) const {
+    const float least = cut.key ? logit_of(cut.key) : -INFINITY;
+    each_piece([&](const uint32_t (&words)[4], int q) {
+      uint64_t sum = 0;
+      bool some = true;
+      if (cut.key) {
+        float most = -INFINITY;
 #pragma unroll
-      for (int w = 0; w < 4; ++w) most = fmaxf(most, fmaxf(bf16_lo(words[w]), bf16_hi(words[w])));
-      some = __builtin_amdgcn_ballot_w64(most >= least) != 0;
-    }
-    if (some) {
-      s16x2 most = {-1, -1};
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        s16x2 off;
-        const uint32_t at = entries_of(words[w], off);
-        most = __builtin_elementwise_max(most, off);
-        sum += *(const uint64_t*)((const char*)sm.weight + (at & 0xffffu));
-        sum += *(const uint64_t*)((const char*)sm.weight + (at >> 16));
+        for (int w = 0; w < 4; ++w) most = fmaxf(most, fmaxf(bf16_lo(words[w]), bf16_hi(words[w])));
+        some = __builtin_amdgcn_ballot_w64(most >= least) != 0;
       }
-      if (any_small(most))
-        each_small_of(words, [&](uint32_t bits, int) { sum += small_weight(bits); });
-      sum = wave_sum_u64(sum);
+      if (some) {
+        s16x2 most = {-1, -1};
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          s16x2 off;
+          const uint32_t at = entries_of(words[w], off);
+          most = __builtin_elementwise_max(most, off);
+          sum += *(const uint64_t*)((const char*)sm.weight + (at & 0xffffu));
+          sum += *(const uint64_t*)((const char*)sm.weight + (at >> 16));
+        }
+        if (any_small(most))
+          each_small_of(words, [&](uint32_t bits) { sum += small_weight(bits); });
+        sum = wave_sum_u64(sum);
+      }
+      if (lane == 0) piece_sum[q] = sum;
+    });
+  }
+
+  // The token, from the pieces' sums.
+  template <bool TABLE>        // whether the table of weights is there
+  __device__ __forceinline__ void pick(const uint64_t* piece_sum) {
+    const uint64_t w_cut = split ? s.w.kept(logit_of(cut.key)) : 0;
+    auto kept = [&](uint64_t before) { return before < cut.count ? before : cut.count; };
+    // two pieces a thread
+    const int qa = 2 * (int)threadIdx.x, qb = qa + 1;
+    const uint64_t pa = qa < pieces ? piece_sum[qa] : 0, pb = qb < pieces ? piece_sum[qb] : 0;
+    const uint64_t ea = pa >> kSameBit, eb = pb >> kSameBit;
+    const uint64_t equal_end = split ? block_up_to(sm.pick, ea + eb) : 0, equal_mid = equal_end - eb;
+    const uint64_t equal_begin = equal_mid - ea;
+    const uint64_t ma = (pa & (kSame - 1)) + (kept(equal_mid) - kept(equal_begin)) * w_cut;
+    const uint64_t mb = (pb & (kSame - 1)) + (kept(equal_end) - kept(equal_mid)) * w_cut;
+    const uint64_t end = block_up_to(sm.pick, ma + mb), mid = end - mb, begin = mid - ma;
+    uint64_t total = 0;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) total += sm.pick.wave_sum[w];
+    const uint64_t want = want_of(a, row, total);
+    if (begin <= want && want < end) {
+      const bool second = mid <= want;
+      sm.found = second ? qb : qa;
+      sm.found_before = second ? mid : begin;
+      sm.found_count = second ? equal_mid : equal_begin;
     }
-    if (lane == 0) sm.piece_sum[q] = sum;
-  });
+    __syncthreads();
+    if (wave != 0) return;
+    const int q = sm.found;
+    const uint4 again = r.load_raw(q, lane);
+    const uint32_t words[4] = {again.x, again.y, again.z, again.w};
+    uint64_t mine[8], all = 0;
+    uint32_t n_same = 0;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t bits = bits_of(words, e);
+      const int off = off_of(bits);
+      const int entry = (int)(bits >> 15) * (kSide + 1) + (int)min((uint32_t)off, (uint32_t)kSide);
+      mine[e] = !TABLE || off >= kSide ? small_weight(bits) : sm.weight[entry];
+      n_same += (uint32_t)(mine[e] >> kSameBit);
+    }
+    uint64_t same = sm.found_count + wave_incl_scan_u32(n_same) - n_same;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      if (mine[e] >> kSameBit) mine[e] = same++ < cut.count ? w_cut : 0;
+      all += mine[e];
+    }
+    uint64_t run = sm.found_before + wave_up_to(all) - all;
+    if (!(run <= want && want < run + all)) return;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const uint32_t bits = bits_of(words, e);
+      if (run <= want && want < run + mine[e])
+        answer(a, row, r.index(q, lane) + e, log_share(s, value(bits), total));
+      run += mine[e];
+    }
+  }
+};
+
+__global__ __launch_bounds__(kThreads) void sample_row_kernel(SampleArgs a, int64_t row0) {
+  __shared__ RowSmem sm;
+  const int64_t row = row0 + blockIdx.x;
+  RowWork work(a, sm, row);
+  const float top = work.largest();
+  if (top == -INFINITY) {
+    if (threadIdx.x == 0) answer(a, row, -1, -INFINITY);
+    return;
+  }
+  const Settings s = settings_of(a, row, top);
+  if (s.greedy) {
+    work.take_largest(top);
+    return;
+  }
+  work.place_tables(s, top);
+  work.fill_weights();
+  work.clear_counts();
   __syncthreads();
-  // two pieces a thread
-  const int qa = 2 * (int)threadIdx.x, qb = qa + 1;
-  const uint64_t pa = qa < pieces ? sm.piece_sum[qa] : 0, pb = qb < pieces ? sm.piece_sum[qb] : 0;
-  const uint64_t ea = pa >> kSameBit, eb = pb >> kSameBit;
-  const uint64_t equal_end = split ? block_up_to(sm.pick, ea + eb) : 0, equal_mid = equal_end - eb;
-  const uint64_t equal_begin = equal_mid - ea;
-  const uint64_t ma = (pa & (kSame - 1)) + (kept(equal_mid) - kept(equal_begin)) * w_cut;
-  const uint64_t mb = (pb & (kSame - 1)) + (kept(equal_end) - kept(equal_mid)) * w_cut;
-  const uint64_t end = block_up_to(sm.pick, ma + mb), mid = end - mb, begin = mid - ma;
-  uint64_t total = 0;
-#pragma unroll
-  for (int w = 0; w < kWaves; ++w) total += sm.pick.wave_sum[w];
-  const uint64_t want = want_of(a, row, total);
-  if (begin <= want && want < end) {
-    const bool second = mid <= want;
-    sm.found = second ? qb : qa;
-    sm.found_before = second ? mid : begin;
-    sm.found_count = second ? equal_mid : equal_begin;
+  if (s.cuts) {
+    work.count();
+    __syncthreads();
+    work.find();
   }
+  work.keep();
   __syncthreads();
-  if (wave != 0) return;
-  const int q = sm.found;
-  const uint4 again = r.load_raw(q, lane);
-  const uint32_t words[4] = {again.x, again.y, again.z, again.w};
-  uint64_t mine[8], all = 0;
-  uint32_t n_same = 0;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const uint32_t bits = bits_of(words, e);
-    const int off = off_of(bits);
-    const int entry = (int)(bits >> 15) * (kSide + 1) + (int)min((uint32_t)off, (uint32_t)kSide);
-    mine[e] = off >= kSide ? small_weight(bits) : sm.weight[entry];
-    n_same += (uint32_t)(mine[e] >> kSameBit);
+  work.weigh(sm.piece_sum);
+  __syncthreads();
+  work.pick<true>(sm.piece_sum);
+}
+
+// ----------------------------------------------------------------------------
+// A row of bf16 in several workgroups: the same steps, a launch up to each result that
+// all of them need.  (The cut and the token by the last workgroup of a row to be done,
+// in the launches before, took 270 us for 64 rows: its fences write back and discard
+// an XCD's L2 for each wave.)
+// ----------------------------------------------------------------------------
+__device__ __forceinline__ float row_top(const SampleArgs& a, int64_t row) {
+  const int lane = threadIdx.x % kWave;
+  return wave_max_f32_dpp(lane < a.parts ? a.tops[row * a.parts + lane] : -INFINITY);
+}
+
+__global__ __launch_bounds__(kThreads) void sample_tops_kernel(SampleArgs a, int64_t unit0) {
+  __shared__ RowSmem sm;
+  const int64_t unit = unit0 + blockIdx.x, row = unit / a.parts;
+  const int part = (int)(unit % a.parts);
+  RowWork work(a, sm, row);
+  work.take(part, a.parts);
+  for (int i = part * kThreads + threadIdx.x; i < kTable; i += a.parts * kThreads)
+    a.counts[row * kTable + i] = 0;
+  if (part == 0 && threadIdx.x == 0) a.state[row] = RowState{};
+  const float top = work.largest();
+  if (threadIdx.x == 0) a.tops[unit] = top;
+}
+
+__global__ __launch_bounds__(kThreads) void sample_counts_kernel(SampleArgs a, int64_t unit0) {
+  __shared__ RowSmem sm;
+  const int64_t unit = unit0 + blockIdx.x, row = unit / a.parts;
+  const float top = row_top(a, row);
+  if (top == -INFINITY) return;
+  const Settings s = settings_of(a, row, top);
+  if (!s.cuts) return;
+  RowState& state = a.state[row];
+  RowWork work(a, sm, row);
+  work.take((int)(unit % a.parts), a.parts);
+  work.place_tables(s, top);
+  work.clear_counts();
+  __syncthreads();
+  work.count();
+  __syncthreads();
+  uint32_t* counts = a.counts + row * kTable;
+  for (int i = threadIdx.x; i < kTable; i += kThreads)
+    if (sm.count[i]) atomicAdd(&counts[i], sm.count[i]);
+  if (threadIdx.x == 0 && sm.small_count) {
+    atomicAdd(&state.small_count, (uint32_t)sm.small_count);
+    atomicAdd((unsigned long long*)&state.small_sum, (unsigned long long)sm.small_sum);
   }
-  uint64_t same = sm.found_count + wave_incl_scan_u32(n_same) - n_same;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    if (mine[e] >> kSameBit) mine[e] = same++ < cut.count ? w_cut : 0;
-    all += mine[e];
+}
+
+__global__ __launch_bounds__(kThreads) void sample_weights_kernel(SampleArgs a, int64_t unit0) {
+  __shared__ RowSmem sm;
+  const int64_t unit = unit0 + blockIdx.x, row = unit / a.parts;
+  const int part = (int)(unit % a.parts);
+  const float top = row_top(a, row);
+  if (top == -INFINITY) {
+    if (part == 0 && threadIdx.x == 0) answer(a, row, -1, -INFINITY);
+    return;
   }
-  uint64_t run = sm.found_before + wave_up_to(all) - all;
-  if (!(run <= want && want < run + all)) return;
-#pragma unroll
-  for (int e = 0; e < 8; ++e) {
-    const uint32_t bits = bits_of(words, e);
-    if (run <= want && want < run + mine[e])
-      answer(a, row, r.index(q, lane) + e, log_share(s, value(bits), total));
-    run += mine[e];
+  const Settings s = settings_of(a, row, top);
+  RowWork work(a, sm, row);
+  if (s.greedy) {
+    // in the first part that has it
+    const float mine = work.lane < a.parts ? a.tops[row * a.parts + work.lane] : -INFINITY;
+    if (part != (int)__builtin_ctzll(__builtin_amdgcn_ballot_w64(mine == top))) return;
+    work.take(part, a.parts);
+    work.take_largest(top);
+    return;
   }
+  work.place_tables(s, top);
+  work.fill_weights();
+  if (s.cuts) {        // each workgroup finds the cut by itself
+    RowState& state = a.state[row];
+    for (int i = threadIdx.x; i < kTable; i += kThreads) sm.count[i] = a.counts[row * kTable + i];
+    if (threadIdx.x == 0) {
+      sm.small_count = (int)state.small_count;
+      sm.small_sum = state.small_sum;
+    }
+    __syncthreads();
+    work.find();
+    if (part == 0 && threadIdx.x == 0) {
+      state.cut = work.cut;
+      state.split = work.split;
+    }
+  }
+  work.take(part, a.parts);
+  work.keep();         // (a thread's entries are those that it filled)
+  __syncthreads();
+  work.weigh(a.sums + row * (int64_t)work.pieces);
+}
+
+__global__ __launch_bounds__(kThreads) void sample_token_kernel(SampleArgs a, int64_t row0) {
+  __shared__ RowSmem sm;
+  const int64_t row = row0 + blockIdx.x;
+  const float top = row_top(a, row);
+  if (top == -INFINITY) return;
+  const Settings s = settings_of(a, row, top);
+  if (s.greedy) return;
+  RowWork work(a, sm, row);
+  work.place_tables(s, top);
+  if (s.cuts) {
+    work.cut = a.state[row].cut;
+    work.split = a.state[row].split != 0;
+  }
+  work.pick<false>(a.sums + row * (int64_t)work.pieces);
 }
 
 // ----------------------------------------------------------------------------
@@ -1246,14 +1433,14 @@ __global__ __launch_bounds__(kThreads) void sample_row_kernel(SampleArgs a, int6
 // ----------------------------------------------------------------------------
 bool aligned(const void* p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 
-bool in_one_workgroup(int format) { return format == EI_LOGITS_BF16; }
-
 struct SamplePlan {
   int blocks, parts, part_blocks;
-  size_t at_cuts, at_bins, at_counts, at_sums, at_equal, bytes;
+  size_t at_cuts, at_bins, at_counts, at_sums, at_equal, at_state, bytes;
 };
-// Parts of a row: as many as give the chip 1024 workgroups, of a block a wave at least.
-SamplePlan sample_plan(int rows, int vocab) {
+size_t up(size_t n) { return (n + 255) / 256 * 256; }
+// fp32.  Parts of a row: as many as give the chip 1024 workgroups, of a block a wave at
+// least.
+SamplePlan fp32_plan(int rows, int vocab) {
   SamplePlan p{};
   const int tokens = kBlockPieces * kPiece;
   p.blocks = (vocab + tokens - 1) / tokens;
@@ -1264,7 +1451,6 @@ SamplePlan sample_plan(int rows, int vocab) {
   parts = parts > most ? most : parts;
   p.part_blocks = (p.blocks + parts - 1) / parts;
   p.parts = (p.blocks + p.part_blocks - 1) / p.part_blocks;
-  auto up = [](size_t n) { return (n + 255) / 256 * 256; };
   p.at_cuts = up((size_t)rows * p.parts * sizeof(PartInfo));
   p.at_bins = p.at_cuts + up((size_t)rows * sizeof(RowCut));
   p.at_counts = p.at_bins + (size_t)rows * kBins * sizeof(uint64_t);
@@ -1273,27 +1459,56 @@ SamplePlan sample_plan(int rows, int vocab) {
   p.bytes = p.at_equal + (size_t)rows * p.blocks * sizeof(uint32_t);
   return p;
 }
+// bf16.  A workgroup a row, or as many as the chip has CUs for, of a piece a wave at
+// least.
+SamplePlan bf16_plan(int rows, int vocab) {
+  SamplePlan p{};
+  const int pieces = (vocab + kPiece - 1) / kPiece;
+  const int most = pieces / kWaves;
+  p.parts = kCUs / rows;
+  p.parts = p.parts > most ? most : p.parts;
+  p.parts = p.parts > kMaxParts ? kMaxParts : p.parts;
+  if (p.parts < kLeastParts) {
+    p.parts = 1;
+    return p;
+  }
+  p.at_sums = up((size_t)rows * p.parts * sizeof(float));
+  p.at_state = p.at_sums + (size_t)rows * pieces * sizeof(uint64_t);
+  p.at_counts = p.at_state + (size_t)rows * sizeof(RowState);
+  p.bytes = p.at_counts + (size_t)rows * kTable * sizeof(uint32_t);
+  return p;
+}
+SamplePlan sample_plan(int rows, int vocab, int format) {
+  return format == EI_LOGITS_BF16 ? bf16_plan(rows, vocab) : fp32_plan(rows, vocab);
+}
 
-template <int FMT>
-void launch_sample(const SampleArgs& a, hipStream_t stream) {
-  auto launch = [&](auto kernel, int64_t groups, int threads) {
-    const int64_t most = (1ll << 31) / threads;
-    for (int64_t u = 0; u < groups; u += most)
-      hipLaunchKernelGGL(kernel, dim3((unsigned)(groups - u < most ? groups - u : most)),
-                         dim3((unsigned)threads), 0, stream, a, u);
-  };
-  if (in_one_workgroup(FMT)) {
-    launch(sample_row_kernel, a.rows, kThreads);
+template <class Kernel>
+void launch(Kernel kernel, const SampleArgs& a, int64_t groups, int threads, hipStream_t stream) {
+  const int64_t most = (1ll << 31) / threads;
+  for (int64_t u = 0; u < groups; u += most)
+    hipLaunchKernelGGL(kernel, dim3((unsigned)(groups - u < most ? groups - u : most)),
+                       dim3((unsigned)threads), 0, stream, a, u);
+}
+void launch_bf16(const SampleArgs& a, hipStream_t stream) {
+  if (a.parts == 1) {
+    launch(sample_row_kernel, a, a.rows, kThreads, stream);
     return;
   }
   const int64_t units = (int64_t)a.rows * a.parts;
-  launch(sample_scan_kernel<FMT>, units, kPartThreads);
+  launch(sample_tops_kernel, a, units, kThreads, stream);
+  if (a.top_k || a.top_p) launch(sample_counts_kernel, a, units, kThreads, stream);
+  launch(sample_weights_kernel, a, units, kThreads, stream);
+  launch(sample_token_kernel, a, a.rows, kThreads, stream);
+}
+void launch_fp32(const SampleArgs& a, hipStream_t stream) {
+  const int64_t units = (int64_t)a.rows * a.parts;
+  launch(sample_scan_kernel, a, units, kPartThreads, stream);
   if (a.top_k || a.top_p) {
-    launch(sample_bins_kernel<FMT>, units, kPartThreads);
-    launch(sample_cut_kernel<FMT>, a.rows, kThreads);
+    launch(sample_bins_kernel, a, units, kPartThreads, stream);
+    launch(sample_cut_kernel, a, a.rows, kThreads, stream);
   }
-  launch(sample_weigh_kernel<FMT>, units, kPartThreads);
-  launch(sample_pick_kernel<FMT>, a.rows, kPickThreads);
+  launch(sample_weigh_kernel, a, units, kPartThreads, stream);
+  launch(sample_pick_kernel, a, a.rows, kPickThreads, stream);
 }
 
 bool valid(int32_t rows, int32_t vocab, int32_t format) {
@@ -1304,10 +1519,8 @@ bool valid(int32_t rows, int32_t vocab, int32_t format) {
 }  // namespace ei
 
 extern "C" size_t ei_sample_workspace_bytes(int32_t rows, int32_t vocab, int32_t format) {
-  if (!ei::valid(rows, vocab, format) || vocab > ei::kMaxVocab || rows == 0 ||
-      ei::in_one_workgroup(format))
-    return 0;
-  return ei::sample_plan(rows, vocab).bytes;
+  if (!ei::valid(rows, vocab, format) || vocab > ei::kMaxVocab || rows == 0) return 0;
+  return ei::sample_plan(rows, vocab, format).bytes;
 }
 
 extern "C" ei_status ei_sample_tokens(const void* logits, int32_t format, int32_t rows,
@@ -1325,17 +1538,17 @@ extern "C" ei_status ei_sample_tokens(const void* logits, int32_t format, int32_
       !ei::aligned(temperature, 4) || !ei::aligned(top_k, 4) || !ei::aligned(top_p, 4) ||
       !ei::aligned(min_p, 4) || !ei::aligned(tokens, 4) || !ei::aligned(logprobs, 4))
     return EI_ERR_UNSUPPORTED;
-  const ei::SamplePlan p = ei::sample_plan(rows, vocab);
-  if (!ei::in_one_workgroup(format) && (!workspace || workspace_bytes < p.bytes))
-    return EI_ERR_WORKSPACE;
+  const ei::SamplePlan p = ei::sample_plan(rows, vocab, format);
+  if (p.bytes && (!workspace || workspace_bytes < p.bytes)) return EI_ERR_WORKSPACE;
   if (!ei::aligned(workspace, 16)) return EI_ERR_UNSUPPORTED;
   char* ws = (char*)workspace;
   const ei::SampleArgs a{logits, rows, vocab, row_stride, u, temperature, top_k, top_p, min_p,
                          tokens, logprobs, p.parts, p.part_blocks, p.blocks, (ei::PartInfo*)ws,
                          (ei::RowCut*)(ws + p.at_cuts), (uint64_t*)(ws + p.at_sums),
                          (uint32_t*)(ws + p.at_equal), (uint64_t*)(ws + p.at_bins),
+                         (uint32_t*)(ws + p.at_counts), (float*)ws, (ei::RowState*)(ws + p.at_state),
                          (uint32_t*)(ws + p.at_counts)};
-  if (format == EI_LOGITS_BF16) ei::launch_sample<EI_LOGITS_BF16>(a, (hipStream_t)stream);
-  else ei::launch_sample<EI_LOGITS_FP32>(a, (hipStream_t)stream);
+  if (format == EI_LOGITS_BF16) ei::launch_bf16(a, (hipStream_t)stream);
+  else ei::launch_fp32(a, (hipStream_t)stream);
   return hipGetLastError() == hipSuccess ? EI_OK : EI_ERR_LAUNCH;
 }

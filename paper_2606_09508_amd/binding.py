@@ -979,6 +979,15 @@ def adapter_plan(index, n_adapters: int, n_tokens: int, cu_seqlens=None) -> Adap
     return AdapterPlan(data, batch)
 
 
+def _req_projection(i: int, y, a, b, device) -> None:
+    """The error of tensors that adapter_add does not take."""
+    for t, name, nd in ((y, "y", 0), (a, "a", 3), (b, "b", 3)):
+        _req(t, f"{name} of projection {i}", torch.bfloat16,
+             nd or (max(t.dim(), 1) if isinstance(t, torch.Tensor) else 1))
+        if t.device != device:
+            raise ValueError(f"tensors on different devices: {device} and {t.device}")
+
+
 def adapter_add(x, ys, adapters, plan: AdapterPlan, workspace=None) -> None:
     """ei_adapter_add: ys[i] += the corrections adapters[i] (Adapters) of x, in
     place, for up to four projections of the same x.  x [..., n_in] and ys[i]
@@ -995,34 +1004,38 @@ def adapter_add(x, ys, adapters, plan: AdapterPlan, workspace=None) -> None:
         raise ValueError(f"x {tuple(x.shape)} does not hold the {T} tokens of the plan")
     if not len(ys) == len(adapters) or not ys:
         raise ValueError(f"{len(adapters)} sets of adapters for {len(ys)} projections")
-    n, rank = plan.batch.n_adapters, 0
-    targets = (AdapterTarget * len(ys))()
-    for i, (y, (a, b, scale)) in enumerate(zip(ys, adapters)):
-        for t, name, nd in ((y, "y", y.dim() if isinstance(y, torch.Tensor) else 1), (a, "a", 3),
-                            (b, "b", 3)):
-            if not (isinstance(t, torch.Tensor) and t.dtype is bf16 and t.get_device() == dev
-                    and t.dim() == nd and nd and t.is_contiguous()):
-                _req(t, f"{name} of projection {i}", bf16, max(nd, 1))
-                raise ValueError(f"tensors on different devices: {x.device} and {t.device}")
-        n_out = y.size(-1)
-        if i == 0:
-            rank = a.size(1)
-        if a.shape != (n, rank, n_in) or b.shape != (n, n_out, rank) or y.numel() != T * n_out:
-            raise ValueError(f"projection {i}: a {tuple(a.shape)}, b {tuple(b.shape)} and y "
-                             f"{tuple(y.shape)} are not [{n}, {rank}, {n_in}], [{n}, n_out, "
+    n, rank, targets, TT = plan.batch.n_adapters, 0, [], torch.Tensor
+    for y, (a, b, scale) in zip(ys, adapters):
+        if not (isinstance(y, TT) and isinstance(a, TT) and isinstance(b, TT)
+                and y.dtype is bf16 and a.dtype is bf16 and b.dtype is bf16
+                and y.get_device() == dev and a.get_device() == dev and b.get_device() == dev
+                and y.is_contiguous() and a.is_contiguous() and b.is_contiguous()):
+            _req_projection(len(targets), y, a, b, x.device)
+        a_shape, n_out = a.shape, y.shape[-1] if y.dim() else 0
+        if not targets and len(a_shape) == 3:
+            rank = a_shape[1]
+        if a_shape != (n, rank, n_in) or b.shape != (n, n_out, rank) or y.numel() != T * n_out:
+            _req_projection(len(targets), y, a, b, x.device)
+            raise ValueError(f"projection {len(targets)}: a {tuple(a.shape)}, b {tuple(b.shape)} "
+                             f"and y {tuple(y.shape)} are not [{n}, {rank}, {n_in}], [{n}, n_out, "
                              f"{rank}] and {T} tokens of n_out")
+        sp = None
         if scale is not None:
-            _req(scale, f"scale of projection {i}", torch.float32, 1)
-            _same_device(x, scale)
+            if not (isinstance(scale, TT) and scale.dtype is torch.float32 and scale.dim() == 1
+                    and scale.get_device() == dev and scale.is_contiguous()):
+                _req(scale, f"scale of projection {len(targets)}", torch.float32, 1)
+                _same_device(x, scale)
             if scale.size(0) != n:
-                raise ValueError(f"projection {i}: {scale.size(0)} scales for {n} adapters")
-        targets[i] = AdapterTarget(a.data_ptr(), b.data_ptr(), _ptr(scale), y.data_ptr(), n_out)
+                raise ValueError(f"projection {len(targets)}: {scale.size(0)} scales for {n} "
+                                 f"adapters")
+            sp = scale.data_ptr()
+        targets.append((a.data_ptr(), b.data_ptr(), sp, y.data_ptr(), n_out))
     if dev != _current_device():
         with torch.cuda.device(dev):
             return adapter_add(x, ys, adapters, plan, workspace)
     L = lib()
     if workspace is None:
-        nb = L.ei_adapter_add_workspace_bytes(plan.batch, n_in, rank, len(ys))
+        nb = L.ei_adapter_add_workspace_bytes(plan.batch, n_in, rank, len(targets))
         if nb:
             workspace = torch.empty((nb,), dtype=torch.uint8, device=x.device)
     else:
@@ -1030,9 +1043,9 @@ def adapter_add(x, ys, adapters, plan: AdapterPlan, workspace=None) -> None:
         if not workspace.is_contiguous():
             raise ValueError("workspace must be contiguous")
         nb = workspace.numel() * workspace.element_size()
-    st = L.ei_adapter_add(x.data_ptr(), n_in, rank, targets, len(ys), plan.batch,
-                          plan.data.data_ptr(), plan.data.numel(), _ptr(workspace), nb,
-                          _raw_stream(dev))
+    st = L.ei_adapter_add(x.data_ptr(), n_in, rank, (AdapterTarget * len(targets))(*targets),
+                          len(targets), plan.batch, plan.data.data_ptr(), plan.data.numel(),
+                          _ptr(workspace), nb, _raw_stream(dev))
     if st:
         _check("ei_adapter_add", st)
 

@@ -84,17 +84,31 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
   __shared__ int place[kMaxAdapters];          // an adapter's tokens; then its next place
   __shared__ int first_tile[kMaxAdapters];
   __shared__ __attribute__((aligned(16))) int seq_a[kPlanThreads], seq_n[kPlanThreads];
-  __shared__ int seq_first[kPlanThreads];
+  __shared__ int seq_first[kPlanThreads], longest;
   __shared__ int wave_tokens[kPlanThreads / kWave], wave_tiles[kPlanThreads / kWave];
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   const int n = a.p.adapters;
+  // a sequence's adapter (-1: none), first token and how many
+  int ad = -1, first = 0, count = 0;
+  auto look = [&](int s) {
+    ad = -1;
+    first = count = 0;
+    if (s < a.p.seqs) {
+      ad = a.index[s];
+      rows_of(a, s, first, count);
+      if (ad < 0 || ad >= n) ad = -1;
+    }
+  };
+  look(tid);
   for (int i = tid; i < n; i += kPlanThreads) place[i] = 0;
   __syncthreads();
-  for (int s = tid; s < a.p.seqs; s += kPlanThreads) {
-    const int at = a.index[s];
-    int first, count;
-    rows_of(a, s, first, count);
-    if (at >= 0 && at < n && count > 0) atomicAdd(&place[at], count);
+  if (ad >= 0) atomicAdd(&place[ad], count);
+  if (a.p.seqs > kPlanThreads) {
+    for (int s = tid + kPlanThreads; s < a.p.seqs; s += kPlanThreads) {
+      look(s);
+      if (ad >= 0) atomicAdd(&place[ad], count);
+    }
+    look(tid);
   }
   __syncthreads();
   // the adapters' first places and tiles; a thread has `per` of them in a row
@@ -146,13 +160,9 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
   __syncthreads();
   // the sequences in their order, kPlanThreads at a time
   for (int s0 = 0; s0 < a.p.seqs; s0 += kPlanThreads) {
-    const int s = s0 + tid, here = min(a.p.seqs - s0, kPlanThreads);
-    int first = 0, count = 0, ad = -1;
-    if (s < a.p.seqs) {
-      ad = a.index[s];
-      rows_of(a, s, first, count);
-      if (ad < 0 || ad >= n) ad = -1;
-    }
+    const int here = min(a.p.seqs - s0, kPlanThreads);
+    if (s0 > 0) look(s0 + tid);
+    if (tid == 0) longest = 0;
     seq_a[tid] = ad;
     seq_n[tid] = count;
     __syncthreads();
@@ -165,10 +175,11 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
     }
     const int to = ad < 0 ? -1 : place[ad] + before;
     __syncthreads();
+    constexpr int kShort = 8, kLong = 512;
     if (ad >= 0) atomicAdd(&place[ad], count);
+    if (ad >= 0 && count > kShort) atomicMax(&longest, count);
     // their tokens: of short sequences by a lane each, of longer ones by a wave, of long
     // ones by all
-    constexpr int kShort = 8, kLong = 512;
     auto write = [&](int p, int f, int c, int i0, int step) {
       for (int i = i0; i < c; i += step)
         if ((unsigned)(p + i) < (unsigned)a.p.tokens) a.list[p + i] = f + i;
@@ -178,10 +189,13 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
     seq_first[tid] = first;
     if (ad < 0) seq_n[tid] = 0;
     __syncthreads();
-    for (int i = wave; i < here; i += kPlanThreads / kWave)
-      if (seq_n[i] > kShort && seq_n[i] <= kLong) write(seq_a[i], seq_first[i], seq_n[i], lane, kWave);
-    for (int i = 0; i < here; ++i)
-      if (seq_n[i] > kLong) write(seq_a[i], seq_first[i], seq_n[i], tid, kPlanThreads);
+    const int most = longest;
+    if (most > kShort)
+      for (int i = wave; i < here; i += kPlanThreads / kWave)
+        if (seq_n[i] > kShort && seq_n[i] <= kLong) write(seq_a[i], seq_first[i], seq_n[i], lane, kWave);
+    if (most > kLong)
+      for (int i = 0; i < here; ++i)
+        if (seq_n[i] > kLong) write(seq_a[i], seq_first[i], seq_n[i], tid, kPlanThreads);
     __syncthreads();
   }
 }

@@ -537,14 +537,16 @@ __global__ __launch_bounds__(kThreads) void sample_cut_kernel(SampleArgs a, int6
   if (!s.cuts) return;
   // all of the row's logits, with their indexes
   auto each_logit = [&](auto use) {
-    for (int b = wave; b < a.blocks; b += kWaves) {
-      float x[kBlockPieces][8];
-      r.load_block(b, lane, x);
+    // (a piece at a time: four of them, unrolled, spend 57 us instead of 39 on 12 rows of
+    // 32001, mostly waiting for code)
+    const int pieces = (a.vocab + kPiece - 1) / kPiece;
+#pragma unroll 1
+    for (int q = wave; q < pieces; q += kWaves) {
+      float x[8];
+      r.load(q, lane, x);
 #pragma unroll
-      for (int q = 0; q < kBlockPieces; ++q)
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (x[q][e] > -INFINITY) use(x[q][e], r.index(b * kBlockPieces + q, lane) + e);
+      for (int e = 0; e < 8; ++e)
+        if (x[e] > -INFINITY) use(x[e], r.index(q, lane) + e);
     }
   };
 

@@ -379,14 +379,24 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(AddArgs a, int64_t uni
   for (int e = threadIdx.x; e < kTokens * (r / 4); e += kThreads) {
     const int tok = e / (r / 4), c = e % (r / 4) * 4;
     float4 x = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-    if (tok < t.count)
-      for (int s = 0; s < a.splits; ++s) {
-        const float4 p = *(const float4*)(a.v + ((int64_t)s * a.tokens + t.begin + tok) * R + ti * r + c);
-        x.x += p.x;
-        x.y += p.y;
-        x.z += p.z;
-        x.w += p.w;
+    if (tok < t.count) {
+      const float* from = a.v + ((int64_t)t.begin + tok) * R + ti * r + c;
+      const int64_t part = (int64_t)a.tokens * R;
+      constexpr int kAtOnce = 8;
+      for (int s = 0; s < a.splits; s += kAtOnce) {
+        float4 p[kAtOnce];
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i)
+          p[i] = s + i < a.splits ? *(const float4*)(from + (s + i) * part) : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+#pragma unroll
+        for (int i = 0; i < kAtOnce; ++i) {
+          x.x += p[i].x;
+          x.y += p[i].y;
+          x.z += p[i].z;
+          x.w += p[i].w;
+        }
       }
+    }
     const float v[4] = {x.x * scale, x.y * scale, x.z * scale, x.w * scale};
     float rest[4];
     const uint32_t hi[2] = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
@@ -417,16 +427,16 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(AddArgs a, int64_t uni
       uint4 next[4];
       if (c + 1 < chunks) load_b(o0, c + 1, next);
       else if (more) load_b(o0 + kBlockOuts, 0, next);
+      uint4 v[NT];
 #pragma unroll
-      for (int k = 0; k < NT; ++k) {
-        if (16 * k >= t.count) break;
-        const uint4 v = col < 2 * r ? *(const uint4*)&sm[(16 * k + j) * pitch + col]
-                                    : make_uint4(0u, 0u, 0u, 0u);
+      for (int k = 0; k < NT; ++k)
+        v[k] = col < 2 * r ? *(const uint4*)&sm[(16 * k + j) * pitch + col] : make_uint4(0u, 0u, 0u, 0u);
+#pragma unroll
+      for (int k = 0; k < NT; ++k)
 #pragma unroll
         for (int m = 0; m < 4; ++m)
           acc[k][m] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-              __builtin_bit_cast(bf16x8, b[m]), __builtin_bit_cast(bf16x8, v), acc[k][m], 0, 0, 0);
-      }
+              __builtin_bit_cast(bf16x8, b[m]), __builtin_bit_cast(bf16x8, v[k]), acc[k][m], 0, 0, 0);
 #pragma unroll
       for (int m = 0; m < 4; ++m) b[m] = next[m];
     }
@@ -467,15 +477,17 @@ struct AddPlan {
   int row_tiles, splits, mt;
   size_t bytes;
 };
-// Parts of the columns: as many as give the chip 512 workgroups, of 512 columns at
-// least (two steps a wave).
+// Parts of the columns, of 512 at least (two steps a wave): as many as give the chip 512
+// workgroups, or 256 with tiles of 64 tokens, each of whose V is read again by every
+// workgroup of expand_kernel (the four inputs of a layer, us a call: 64 single tokens 46
+// with 256 and 43 with 512; 1677 tokens, rank 64, 209 and 217, with 128 245).
 AddPlan add_plan(const PlanShape& p, int n_in, int rank, int targets) {
   AddPlan s{};
   const int R = targets * rank;
   s.mt = p.rows == 16 || R <= 16 ? 1 : R <= 32 ? 2 : R <= 48 ? 3 : 4;
   s.row_tiles = (R + 16 * s.mt - 1) / (16 * s.mt);
   const int64_t units = (int64_t)p.max_tiles * s.row_tiles;
-  int64_t splits = 512 / (units > 0 ? units : 1);
+  int64_t splits = (p.rows == 16 ? 512 : 256) / (units > 0 ? units : 1);
   const int64_t most = n_in / 512;
   if (splits > most) splits = most;
   s.splits = splits < 1 ? 1 : (int)splits;

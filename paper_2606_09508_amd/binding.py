@@ -1030,6 +1030,8 @@ def adapter_add(x, ys, adapters, plan: AdapterPlan, workspace=None) -> None:
                                  f"adapters")
             sp = scale.data_ptr()
         targets.append((a.data_ptr(), b.data_ptr(), sp, y.data_ptr(), n_out))
+    if T and len({t[3] for t in targets}) != len(targets):
+        raise ValueError("a projection's y is given twice")
     if dev != _current_device():
         with torch.cuda.device(dev):
             return adapter_add(x, ys, adapters, plan, workspace)

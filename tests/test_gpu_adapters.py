@@ -282,3 +282,13 @@ def test_leading_dimensions_and_refusals():
         eb.adapter_plan(_i32([0, 1, 1]).cuda(), 2, 7, _i32([0, 7]).cuda())
     with pytest.raises(eb.EIError, match="UNSUPPORTED"):
         eb.adapter_plan(_i32([0]).cuda(), 9000, 1)
+
+
+def test_a_projection_given_twice_is_refused():
+    x = torch.zeros((2, 16), dtype=BF16).cuda()
+    y = torch.zeros((2, 8), dtype=BF16).cuda()
+    ad = eb.Adapters(torch.zeros((1, 8, 16), dtype=BF16).cuda(), torch.zeros((1, 8, 8), dtype=BF16).cuda())
+    plan = eb.adapter_plan(_i32([0]).cuda(), 1, 2)
+    with pytest.raises(ValueError, match="twice"):
+        eb.adapter_add(x, [y, y], [ad, ad], plan)
+    eb.adapter_add(x, [y, y.clone()], [ad, ad], plan)

@@ -328,3 +328,87 @@ def test_binding_refusals():
         eb.sample_tokens(x, u.cpu())
     assert eb.sample_tokens(x[:0], u[:0])[0].shape == (0,)
     assert eb.sample_tokens(x[:, :0], u)[0].tolist() == [-1, -1, -1]
+
+
+def _in_many_rows(x, u, t, k, p, m):
+    """The same rows many times over: as many as get a workgroup each."""
+    n = -(-200 // x.shape[0])
+    got = eb.sample_tokens(x.cuda().repeat(n, 1), *(torch.tensor(v, dtype=d).cuda().repeat(n)
+                           for v, d in ((u, F32), (t, F32), (k, torch.int32), (p, F32), (m, F32))))
+    got = [v.view(n, -1) for v in got]
+    assert all(torch.equal(v, v[:1].expand_as(v)) for v in got)
+    return [v[0] for v in got]
+
+
+def _rows_of_all_kinds(vocab):
+    g = _gen(vocab)
+    x = logits(12, vocab, vocab, F32)
+    x[1] *= 1e-3                                   # near 0, flat
+    x[2] = -x[2].abs() - 30                        # all below 0
+    x[3] = -INF
+    x[4, ::2] = NAN
+    x[5, [7, vocab // 2, vocab - 1]] = INF
+    x[6] = torch.randint(-3, 4, (vocab,), generator=g)            # ties over the whole row
+    x[7] = -INF
+    x[7, vocab - 1] = -3.0                         # one token, the last
+    x[8] = torch.rand((vocab,), generator=g) * 2.0 ** -40         # all nearer to 0 than 2^-30
+    x[8, ::3] *= -1
+    x[8, vocab // 3] = 8.0                         # (and far below the largest)
+    x[9, : vocab // 2] = torch.finfo(BF16).min
+    x[10] *= 1e30
+    x[11] = 0.0
+    return x.to(BF16)
+
+
+@pytest.mark.parametrize("vocab", [16384, 16385, 32001, 70000, 524288])
+def test_a_row_is_the_same_in_one_workgroup_and_in_several(vocab):
+    """Sums of weights are whole numbers: every bit is the same, however a row is
+    divided, in any company."""
+    x = _rows_of_all_kinds(vocab)
+    n = x.shape[0]
+    settings = [([1.0] * n, [0] * n, [1.0] * n, [0.0] * n),
+                ([0.7] * n, [0] * n, [0.9] * n, [0.0] * n),
+                ([1.0] * n, [vocab // 3] * n, [1.0] * n, [0.0] * n),
+                ([1.3] * n, [1000 + i for i in range(n)], [0.5 + 0.04 * i for i in range(n)], [1e-3] * n),
+                ([0.0] * n, [0] * n, [1.0] * n, [0.0] * n),
+                ([INF, 1.0, 0.0, 2.0] * 3, [0, 1, 0, 50] * 3, [0.9, 1.0, 1.0, 0.3] * 3,
+                 [0.0, 0.0, 0.0, 0.2] * 3)]
+    for i, (t, k, p, m) in enumerate(settings):
+        u = us(n, vocab + i)
+        want = _in_many_rows(x, u, t, k, p, m)
+        got = eb.sample_tokens(x.cuda(), *(torch.tensor(v, dtype=d).cuda() for v, d in
+                               ((u, F32), (t, F32), (k, torch.int32), (p, F32), (m, F32))))
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1]), i
+        for r in (0, 6, 9):
+            one = eb.sample_tokens(x[r:r + 1].cuda(), *(torch.tensor(v[r:r + 1], dtype=d).cuda()
+                                   for v, d in ((u, F32), (t, F32), (k, torch.int32), (p, F32),
+                                                (m, F32))))
+            assert torch.equal(one[0], want[0][r:r + 1]) and torch.equal(one[1], want[1][r:r + 1])
+
+
+def test_rows_in_several_workgroups_against_the_definition():
+    x = _rows_of_all_kinds(16385)
+    n = x.shape[0]
+    check(x, us(n, 1), [1.0] * n, [0] * n, [0.9] * n)
+    check(x, us(n, 2), [0.8] * n, [700] * n, [0.95] * n, [1e-3] * n)
+    check(x, us(n, 3))
+
+
+def test_two_calls_at_once_with_a_workspace_each():
+    x, u = logits(4, 40000, 5).cuda(), torch.tensor(us(4, 5), dtype=F32).cuda()
+    p = torch.full((4,), 0.8).cuda()
+    want = eb.sample_tokens(x, u, top_p=p)
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    ws = [torch.empty(eb.sample_workspace_bytes(4, 40000), dtype=torch.uint8, device="cuda")
+          for _ in range(2)]
+    assert ws[0].numel() > 0
+    for _ in range(5):
+        here = eb.sample_tokens(x, u, top_p=p, workspace=ws[0])
+        with torch.cuda.stream(side):
+            there = eb.sample_tokens(x, u, top_p=p, workspace=ws[1])
+        torch.cuda.synchronize()
+        for got in (here, there):
+            assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    with pytest.raises(eb.EIError):
+        eb.sample_tokens(x, u, workspace=ws[0][:-256])

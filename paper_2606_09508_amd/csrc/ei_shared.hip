@@ -894,7 +894,11 @@ SharedPlan shared_plan(int Hq, int n_tokens, int n_seqs, int n_groups, int max_p
                        const ei_cache_shape& c) {
   SharedPlan p{};
   const int64_t G = Hq / c.n_kv_heads, rows = n_tokens * G;
-  // rows of a group and a KV head on average: tiles in LDS from 33 on
+  // Rows of a group and a KV head on average: tiles in LDS from 33 on, of 128 rows from
+  // 65 on.  Without, with 64, with 128, us a call: 8 groups of 4096 keys, 32 rows 44, 45,
+  // 50; 48 rows 56, 51, 54; 96 rows 82, 77, 70; 4 groups of 16384, 64 rows 75, 56, 63; 96
+  // rows 100, 87, 70; one group of 8192, 16 rows 26, 28, 28; 64 rows 35, 33, 33; 128 rows
+  // 41, 37, 37.
   const int64_t of_group = n_groups ? rows / n_groups : 0;
   p.wide_rows = of_group > 64 ? 128 : of_group > 32 ? 64 : 0;
   p.rt = rows > (int64_t)kRows * n_seqs ||

@@ -27,6 +27,7 @@ with ``prefill.prefill(x, ..., store=cache.storing(seqs))`` (or of many at once,
 their lengths alike).
 
     python -m paper_2606_09508_amd.decode --steps     # markdown table of step times
+    python -m paper_2606_09508_amd.decode --serving   # and of steps of one prompt's forks
 """
 from __future__ import annotations
 
@@ -545,24 +546,100 @@ def step_table(batches, contexts, shape: pf.DecoderShape, n_layers: int, reps: i
             torch.cuda.empty_cache()
 
 
+def random_adapters(layers, count: int, rank: int, seed: int = 0):
+    """Adapters for all projections of the layers, random bf16, whose corrections
+    are about as large as a tenth of the products."""
+    dev = layers[0]["wq"].device
+    g = torch.Generator(device=dev)
+    g.manual_seed(seed)
+
+    def bf16(*shape, scale):
+        return (torch.randn(shape, generator=g, device=dev) * scale).to(torch.bfloat16)
+    return [{name: eb.Adapters(bf16(count, rank, w[name].shape[0], scale=w[name].shape[0] ** -0.5),
+                               bf16(count, w[name].shape[1], rank, scale=0.1 * rank ** -0.5))
+             for name in pf.PROJECTIONS} for w in layers]
+
+
+def serving_table(batches, contexts, shape: pf.DecoderShape, n_layers: int, reps: int,
+                  dtype=torch.float8_e4m3fn, own: int = 200, count: int = 8, rank: int = 16,
+                  file=sys.stdout):
+    """Times of a step of one token per sequence, for forks of one sequence of
+    `context` tokens (random pages) that hold `own` more each: plain, with the
+    shared pages read once, with adapters too, and with the draw of the next tokens
+    (top-p) behind it."""
+    dev = torch.device("cuda:0")
+    layers = pf.make_weights(shape, n_layers, 0, dev)
+    adapters = random_adapters(layers, count, rank)
+    g = torch.Generator(device=dev)
+    g.manual_seed(1)
+    head = (torch.randn((shape.hidden, shape.vocab), generator=g, device=dev)
+            / math.sqrt(shape.hidden)).to(torch.bfloat16)
+    print(f"Decoder: {n_layers} layers, hidden {shape.hidden}, {shape.n_q_heads}/"
+          f"{shape.n_kv_heads} heads of {shape.head_dim}, MLP {shape.intermediate}, vocabulary "
+          f"{shape.vocab}, random bf16 weights; forks of one sequence with {own} tokens of their "
+          f"own, {count} adapters of rank {rank} on all projections; cache of {dtype} pages of 64 "
+          f"tokens; {reps} timed steps, ms.\n", file=file)
+    print("| forks | shared tokens | step | shared prefix | + adapters | + draw (top-p) |", file=file)
+    print("|---:|---:|---:|---:|---:|---:|", file=file)
+    for B in batches:
+        for N in contexts:
+            per = -(-(own + 4 * (reps + 4)) // 64) + 1
+            cache = PagedCache(shape, n_layers, -(-N // 64) + B * per, B, N + per * 64, dtype=dtype,
+                               device=dev)
+            for t in cache.pages[:2]:
+                for i in range(n_layers):
+                    t[i].view(torch.uint8).random_(0, 0x60)
+            for t in cache.pages[2:]:
+                t.fill_(2.0 ** -7)
+            seqs = [cache.add()]
+            cache.extend(seqs, [N])
+            seqs += [cache.fork(seqs[0]) for _ in range(B - 1)]
+            cache.extend(seqs, [own] * B)
+            x = torch.randn((1, B, shape.hidden), device=dev).to(torch.bfloat16)
+            sampler = Sampler([dict(temperature=0.8, top_p=0.95)] * B, dev)
+            adapter = [i % (count + 1) - 1 for i in range(B)]
+            times = []
+            for share, which, draw in ((False, None, False), (True, None, False),
+                                       (True, adapter, False), (True, adapter, True)):
+                dec = Decoder(layers, shape, cache, head, adapters, share)
+                e = [torch.cuda.Event(enable_timing=True) for _ in range(2)]
+                for i in range(reps + 3):
+                    if i == 3:
+                        e[0].record()
+                    _, logits = dec.step(x, seqs, adapter=which)
+                    if draw:
+                        sampler(logits)
+                e[1].record()
+                torch.cuda.synchronize()
+                times.append(e[0].elapsed_time(e[1]) / reps)
+            print(f"| {B} | {N} | " + " | ".join(f"{t:.2f}" for t in times) + " |", file=file,
+                  flush=True)
+            del cache, dec
+            torch.cuda.empty_cache()
+
+
 def main():
     ap = argparse.ArgumentParser(description=__doc__.split("\n\n")[0])
     ap.add_argument("--steps", action="store_true", help="time steps of one token per sequence")
+    ap.add_argument("--serving", action="store_true",
+                    help="time steps of forks of one sequence, with adapters and draws")
     ap.add_argument("--layers", type=int, default=pf.LLAMA3_8B.n_layers)
     ap.add_argument("--reps", type=int, default=20)
     ap.add_argument("--batches", default="1,16,64")
     ap.add_argument("--contexts", default="1024,8192,32768")
     ap.add_argument("--int8", action="store_true", help="pages in int8 (e4m3 without)")
     args = ap.parse_args()
-    if not args.steps:
+    if not (args.steps or args.serving):
         ap.print_help()
         return
     if not torch.cuda.is_available():
         print("a ROCm GPU is needed", file=sys.stderr)
         sys.exit(1)
-    step_table([int(n) for n in args.batches.split(",")],
-               [int(n) for n in args.contexts.split(",")], pf.LLAMA3_8B, args.layers, args.reps,
-               torch.int8 if args.int8 else torch.float8_e4m3fn)
+    for wanted, table in ((args.steps, step_table), (args.serving, serving_table)):
+        if wanted:
+            table([int(n) for n in args.batches.split(",")],
+                  [int(n) for n in args.contexts.split(",")], pf.LLAMA3_8B, args.layers, args.reps,
+                  torch.int8 if args.int8 else torch.float8_e4m3fn)
 
 
 if __name__ == "__main__":

@@ -297,12 +297,19 @@ class BatchAdapters:
     @staticmethod
     def _fits(h, rank, ys, of) -> bool:
         """Sizes, types and layout ei_adapter_add takes."""
-        ts = [t for a, b, _ in of for t in (a, b)]
-        scales = [s for _, _, s in of if s is not None]
-        return (rank % 8 == 0 and 0 < rank <= 128 and _ordinary(h, *ys, *ts, *scales)
-                and all(t.dtype == torch.bfloat16 and t.shape[-1] % 8 == 0 and _dense16(t)
-                        for t in (h, *ys, *ts))
-                and all(s.dtype == torch.float32 and s.is_contiguous() for s in scales))
+        if rank % 8 or not 0 < rank <= 128:
+            return False
+        ts = [h, *ys]
+        for a, b, scale in of:
+            ts += a, b
+            if scale is not None and not (scale.dtype is torch.float32 and scale.is_contiguous()
+                                          and _ordinary(h, scale)):
+                return False
+        for t in ts:      # (four such calls a layer: one loop over what they hold)
+            if t.dtype is not torch.bfloat16 or t.shape[-1] % 8 or not t.is_contiguous() \
+                    or t.data_ptr() % 16:
+                return False
+        return _ordinary(*ts)
 
     def _tensors(self, h, y, t):
         """The same by tensor operations: fp32, and one rounding to y's type."""

@@ -72,6 +72,10 @@ SHAPES = [
     ([130], 2, [1], 1032, [128, 128, 64], 40),
     ([31] * 4, 2, [0, 1, 1, 0], 64, [64], 8), ([32] * 4, 2, [0, 1, 1, 0], 64, [64], 8),
     ([1] * 2500, 700, [(i * i) % 703 for i in range(2500)], 64, [64], 8),
+    ([400, 1, 300, 65, 2], 3, [0, 1, 0, 2, 1], 136, [72, 1000, 256], 24),
+    ([1] * 900, 2, [i % 3 for i in range(900)], 72, [520], 16),
+    ([768], 4, [3], 1032, [512, 8, 16, 264], 128), ([767], 1, [0], 64, [64], 64),
+    ([40] * 30, 30, list(range(29)) + [-1], 64, [128, 64], 8),
     ([3] * 1100, 8192, [(i * 7919) % 8192 for i in range(1100)], 8, [16], 8),
 ]
 

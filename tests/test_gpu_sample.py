@@ -360,7 +360,7 @@ def _rows_of_all_kinds(vocab):
     return x.to(BF16)
 
 
-@pytest.mark.parametrize("vocab", [16384, 16385, 32001, 70000, 524288])
+@pytest.mark.parametrize("vocab", [73728, 73729, 128256, 524288])
 def test_a_row_is_the_same_in_one_workgroup_and_in_several(vocab):
     """Sums of weights are whole numbers: every bit is the same, however a row is
     divided, in any company."""
@@ -387,7 +387,7 @@ def test_a_row_is_the_same_in_one_workgroup_and_in_several(vocab):
 
 
 def test_rows_in_several_workgroups_against_the_definition():
-    x = _rows_of_all_kinds(16385)
+    x = _rows_of_all_kinds(73729)
     n = x.shape[0]
     check(x, us(n, 1), [1.0] * n, [0] * n, [0.9] * n)
     check(x, us(n, 2), [0.8] * n, [700] * n, [0.95] * n, [1e-3] * n)
@@ -395,12 +395,12 @@ def test_rows_in_several_workgroups_against_the_definition():
 
 
 def test_two_calls_at_once_with_a_workspace_each():
-    x, u = logits(4, 40000, 5).cuda(), torch.tensor(us(4, 5), dtype=F32).cuda()
+    x, u = logits(4, 80000, 5).cuda(), torch.tensor(us(4, 5), dtype=F32).cuda()
     p = torch.full((4,), 0.8).cuda()
     want = eb.sample_tokens(x, u, top_p=p)
     torch.cuda.synchronize()
     side = torch.cuda.Stream()
-    ws = [torch.empty(eb.sample_workspace_bytes(4, 40000), dtype=torch.uint8, device="cuda")
+    ws = [torch.empty(eb.sample_workspace_bytes(4, 80000), dtype=torch.uint8, device="cuda")
           for _ in range(2)]
     assert ws[0].numel() > 0
     for _ in range(5):
@@ -412,3 +412,28 @@ def test_two_calls_at_once_with_a_workspace_each():
             assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
     with pytest.raises(eb.EIError):
         eb.sample_tokens(x, u, workspace=ws[0][:-256])
+
+
+def test_captured_rows_in_several_workgroups():
+    """A graph of such a call, replayed with other settings and numbers between eager
+    calls; its workspace is its own."""
+    x = logits(5, 80000, 8).cuda()
+    u, p, k = torch.zeros(5).cuda(), torch.ones(5).cuda(), torch.zeros(5, dtype=torch.int32).cuda()
+    t = torch.ones(5).cuda()
+    for _ in range(2):
+        eb.sample_tokens(x, u, t, k, p)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out, logs = eb.sample_tokens(x, u, t, k, p)
+    for i in range(4):
+        u.copy_(torch.tensor(us(5, i), dtype=F32))
+        p.fill_((1.0, 0.9, 0.5, 0.99)[i])
+        k.fill_((0, 100, 0, 20000)[i])
+        t.copy_(torch.tensor([1.0, 0.0, 0.5, 3.0, 1.0]))
+        x[i] = -INF if i == 3 else x[i]
+        want = eb.sample_tokens(x, u, t, k, p)
+        graph.replay()
+        again = eb.sample_tokens(x, u, t, k, p)
+        torch.cuda.synchronize()
+        assert torch.equal(out, want[0]) and torch.equal(logs, want[1])
+        assert torch.equal(again[0], want[0])

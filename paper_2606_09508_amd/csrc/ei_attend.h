@@ -12,8 +12,8 @@
 namespace ei {
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kWaves = kThreads / kWave;
+constexpr int kAttendThreads = 256;
+constexpr int kAttendWaves = kAttendThreads / kWave;
 
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
@@ -118,8 +118,8 @@ __device__ __forceinline__ int page_at(const Pages& pg, int s, int c) {
 // K multiplies the fp32 scores, V's the fp32 probabilities, which go to the
 // matrix cores as the sum of two bf16 numbers (16 bits).
 // ----------------------------------------------------------------------------
-constexpr int kRows = 16;
-constexpr int kKeys = 32;
+constexpr int kAttendRows = 16;
+constexpr int kAttendKeys = 32;
 constexpr float kFastLimit = 0x1p32f;
 constexpr float kRescaleThreshold = 8.0f;
 
@@ -146,7 +146,7 @@ struct Part {          // of a row: sums against the maximum m (base 2)
 // An item (16 RT rows of a sequence and KV head) whose keys several waves
 // share, left for combine_kernel by the one with its first key.  Its parts in
 // the order of the keys: at first_slot and at 2 (worker + 1) ..: n_waves of
-// them (waves of the first workgroup); n_groups at 2 kWaves group ..
+// them (waves of the first workgroup); n_groups at 2 kAttendWaves group ..
 // (workgroups after it); the rest at 2 last .. (waves of the last one).
 // parts = 0: none.
 struct SplitItem {
@@ -190,7 +190,7 @@ __device__ __forceinline__ void attend_steps(const AttendArgs& a, int s, int kvh
   int pos[RT];
 #pragma unroll
   for (int rt = 0; rt < RT; ++rt) {
-    const int row = min(row0 + kRows * rt + j, rows - 1);
+    const int row = min(row0 + kAttendRows * rt + j, rows - 1);
     pos[rt] = max(max(seq_len, 0) - n + row / G, -1);
     const uint16_t* qp =
         a.q + ((int64_t)(kvh * G + row % G) * a.tk.T + first + row / G) * kHeadDim + 16 * g;
@@ -222,7 +222,7 @@ __device__ __forceinline__ void attend_steps(const AttendArgs& a, int s, int kvh
   constexpr int kOnce = 2;   // nontemporal
   auto rows_of = [&](uint8_t* base, int page, int k0, bool real) {
     const int64_t at = real ? (((int64_t)page * a.pg.Hkv + kvh) * P + k0 % P) * kHeadDim : 0;
-    return __builtin_amdgcn_make_buffer_rsrc(base + at, 0, real ? kKeys * kHeadDim : 0, 0x00027000);
+    return __builtin_amdgcn_make_buffer_rsrc(base + at, 0, real ? kAttendKeys * kHeadDim : 0, 0x00027000);
   };
   auto load_k = [&](int page, int k0, bool real) {
     const auto rsrc = rows_of(a.pg.k, page, k0, real);
@@ -264,8 +264,8 @@ __device__ __forceinline__ void attend_steps(const AttendArgs& a, int s, int kvh
     k_read();
     // steps that reach past a row's last key (the others see every key); the
     // asm statements keep the compiler from doing their work in every step
-    const bool edge = k0 + kKeys - 1 > pos_min || k0 + kKeys > key1;
-    if (k0 + kKeys > key1) {
+    const bool edge = k0 + kAttendKeys - 1 > pos_min || k0 + kAttendKeys > key1;
+    if (k0 + kAttendKeys > key1) {
       int left = key1 - k0 - 4 * g;
       asm volatile("" : "+v"(left));
       // rows behind the sequence's end hold anything, NaN codes included
@@ -364,10 +364,10 @@ __device__ __forceinline__ void attend_steps(const AttendArgs& a, int s, int kvh
   };
 
   // The wave's steps.  Pages are looked up two steps ahead, scales one.
-  const int steps = (key1 - key0 + kKeys - 1) / kKeys;
+  const int steps = (key1 - key0 + kAttendKeys - 1) / kAttendKeys;
   const int mine = (steps - w + stride - 1) / stride;
   if (mine > 0) {
-    auto key_of = [&](int i) { return key0 + kKeys * (w + stride * min(i, mine - 1)); };
+    auto key_of = [&](int i) { return key0 + kAttendKeys * (w + stride * min(i, mine - 1)); };
     // (the table has room for the keys: a step's column is one of it)
     const int64_t row = (int64_t)s * a.pg.max_pages;
     auto number_of = [&](int i) { return entry(a.pg.table, row + key_of(i) / P); };
@@ -389,7 +389,7 @@ __device__ __forceinline__ void attend_steps(const AttendArgs& a, int s, int kvh
       const float kf_next = entry(k_scales, scale_at(next)), vf_next = entry(v_scales, scale_at(next));
       const bool real = i + 1 < mine && next >= 0;
       // (keys on no page: zeros at places that no row sees)
-      compute(page >= 0 ? key_of(i) : INT_MAX - 2 * kKeys, page >= 0 ? kf * a.sc_log2 : 0.0f,
+      compute(page >= 0 ? key_of(i) : INT_MAX - 2 * kAttendKeys, page >= 0 ? kf * a.sc_log2 : 0.0f,
               page >= 0 ? vf : 0.0f, [&]() { load_k(next, key_of(i + 1), real); },
               [&]() { load_v(next, key_of(i + 1), real); });
       page = next;
@@ -425,8 +425,8 @@ __device__ __forceinline__ int keys_of(const AttendArgs& a, int s) {
 template <int WAVES>
 struct MergeSmem {
   static constexpr int kPitch = kHeadDim + 4;   // (a row's start moves on by 4 banks)
-  float m[WAVES][kRows], l[WAVES][kRows];
-  __attribute__((aligned(16))) float o[WAVES][kRows * kPitch];
+  float m[WAVES][kAttendRows], l[WAVES][kAttendRows];
+  __attribute__((aligned(16))) float o[WAVES][kAttendRows * kPitch];
 };
 template <int RT, int WAVES, class Out>
 __device__ __forceinline__ void merge_waves(MergeSmem<WAVES>& sm, const WaveSums<RT>& ws, int rows,
@@ -448,7 +448,7 @@ __device__ __forceinline__ void merge_waves(MergeSmem<WAVES>& sm, const WaveSums
     }
     __syncthreads();
     const int mr = threadIdx.x >> 4, md = (threadIdx.x & 15) * 8;   // row, dims
-    if (mr < kRows && kRows * rt + mr < rows) {
+    if (mr < kAttendRows && kAttendRows * rt + mr < rows) {
       float m = sm.m[0][mr];
 #pragma unroll
       for (int w = 1; w < WAVES; ++w) m = fmaxf(m, sm.m[w][mr]);
@@ -462,7 +462,7 @@ __device__ __forceinline__ void merge_waves(MergeSmem<WAVES>& sm, const WaveSums
 #pragma unroll
         for (int e = 0; e < 8; ++e) acc[e] += f * sm.o[w][mr * kPitch + md + e];
       }
-      out(kRows * rt + mr, md, m, l, acc);
+      out(kAttendRows * rt + mr, md, m, l, acc);
     }
   }
 }
@@ -471,7 +471,7 @@ __device__ __forceinline__ void merge_waves(MergeSmem<WAVES>& sm, const WaveSums
 template <int RT>
 __device__ __forceinline__ void store_part(const AttendArgs& a, int slot, int row, int d, float m,
                                            float l, const float (&x)[8]) {
-  const int64_t pr = (int64_t)slot * (kRows * RT) + row;
+  const int64_t pr = (int64_t)slot * (kAttendRows * RT) + row;
   if (d == 0) a.part_ml[pr] = Part{m, l};
   float* at = a.part_o + pr * kHeadDim + d;
   *(float4*)at = make_float4(x[0], x[1], x[2], x[3]);
@@ -483,7 +483,7 @@ constexpr int attend_occupancy(int rt) { return rt == 1 ? 3 : 2; }   // waves a 
 // ----------------------------------------------------------------------------
 // Host side
 // ----------------------------------------------------------------------------
-constexpr int64_t kMaxGrid = (1ll << 31) / kThreads;   // threads of a launch: 32 bits
+constexpr int64_t kMaxGrid = (1ll << 31) / kAttendThreads;   // threads of a launch: 32 bits
 unsigned launch_grid(int64_t left) { return (unsigned)(left < kMaxGrid ? left : kMaxGrid); }
 
 bool aligned(const void* p, uintptr_t a) { return ((uintptr_t)p & (a - 1)) == 0; }

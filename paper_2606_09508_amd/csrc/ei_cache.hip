@@ -26,6 +26,13 @@
 namespace ei {
 namespace {
 
+constexpr int kThreads = 256;
+constexpr int kWaves = kThreads / kWave;
+constexpr int kRows = 16;      // of a tile
+constexpr int kKeys = 32;      // of a step
+static_assert(kThreads == kAttendThreads && kRows == kAttendRows && kKeys == kAttendKeys,
+              "as the code that they share takes them");
+
 // ----------------------------------------------------------------------------
 // Store.  One workgroup takes a page of one KV head, K and V: the largest
 // magnitude of the new rows (as integers: bf16 magnitudes are ordered like

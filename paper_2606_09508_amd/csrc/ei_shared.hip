@@ -22,6 +22,8 @@
 namespace ei {
 namespace {
 
+constexpr int kThreads = kAttendThreads, kWaves = kAttendWaves;
+constexpr int kRows = kAttendRows, kKeys = kAttendKeys;
 constexpr int kPlanThreads = 1024;
 constexpr int kWideThreads = 512;
 constexpr int kWideWaves = kWideThreads / kWave;

@@ -410,13 +410,7 @@ class Decoder:
             raise ValueError(f"x {tuple(x.shape)} is not [1, {sum(counts)}, hidden] of "
                              f"{len(counts)} counts for {len(seqs)} sequences")
         if adapter is not None:
-            if self.adapters is None:
-                raise ValueError("the decoder has no adapters to choose from")
-            adapter = [int(i) for i in adapter]
-            if len(adapter) != len(seqs):
-                raise ValueError(f"{len(adapter)} adapters for {len(seqs)} sequences")
-            if any(not -1 <= i < self.n_adapters for i in adapter):
-                raise ValueError(f"adapters {adapter} of {self.n_adapters}")
+            adapter = pf.check_choice(adapter, len(seqs), self.adapters, self.n_adapters)
         held = {s: self.cache.length(s) for s in seqs}
         self.cache.extend(seqs, counts)
         try:

@@ -249,13 +249,16 @@ def check_adapters(adapters, layers) -> int:
     return 0 if count is None else count
 
 
-def adapter_index(adapter, n_seqs: int, adapters, device):
-    """int32 [n_seqs] on the device of a list of adapters' numbers."""
+def check_choice(adapter, n_seqs: int, adapters, count: int) -> list[int]:
+    """Each sequence's adapter (-1: none) of `count`, as integers."""
     if adapters is None:
         raise ValueError("there are no adapters to choose from")
+    adapter = [int(i) for i in adapter]
     if len(adapter) != n_seqs:
         raise ValueError(f"{len(adapter)} adapters for {n_seqs} sequences")
-    return torch.tensor([int(i) for i in adapter], dtype=torch.int32).to(device)
+    if any(not -1 <= i < count for i in adapter):
+        raise ValueError(f"adapters {adapter} of {count}")
+    return adapter
 
 
 class BatchAdapters:
@@ -408,8 +411,9 @@ def prefill(x, layers, shape: DecoderShape, attn: Attention, lm_head=None, store
     B, N, _ = x.shape
     own = None
     if adapter is not None:
-        index = adapter_index(adapter, B, adapters, x.device)
-        own = BatchAdapters(adapters, check_adapters(adapters, layers), index, B * N)
+        count = 0 if adapters is None else check_adapters(adapters, layers)
+        index = torch.tensor(check_choice(adapter, B, adapters, count), dtype=torch.int32)
+        own = BatchAdapters(adapters, count, index.to(x.device), B * N)
     cos, sin = rope_tables(N, shape.head_dim, shape.rope_theta, x.device)
     y = None
     with store if hasattr(store, "__exit__") else contextlib.nullcontext():

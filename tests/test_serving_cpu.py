@@ -127,6 +127,9 @@ def test_adapters_are_checked():
         pf.prefill(x, layers, SHAPE, attn, adapter=[0])
     with pytest.raises(ValueError):
         pf.prefill(x, layers, SHAPE, attn, adapters=good, adapter=[0, 1])
+    for bad in ([3], [-2]):
+        with pytest.raises(ValueError):
+            pf.prefill(x, layers, SHAPE, attn, adapters=good, adapter=bad)
     with pytest.raises(ValueError):
         dec.generate(torch.zeros((2, 5)), torch.zeros((5, 64)), seqs, 1, None)
 

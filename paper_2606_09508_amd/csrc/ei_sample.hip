@@ -223,16 +223,22 @@ struct Settings {
   float p;               // 1: no limit
   Weights w;
 };
-__device__ __forceinline__ Settings settings_of(const SampleArgs& a, int64_t row, float top) {
+// As the caller gives them.  (Asked for by themselves, before the largest logit is known.)
+struct Given {
+  float t, p, m;
+  int k;
+  __device__ __forceinline__ Given(const SampleArgs& a, int64_t row)
+      : t(a.temperature ? a.temperature[row] : 1.0f), p(a.top_p ? a.top_p[row] : 1.0f),
+        m(a.min_p ? a.min_p[row] : 0.0f), k(a.top_k ? a.top_k[row] : 0) {}
+};
+__device__ __forceinline__ Settings settings_of(const SampleArgs& a, const Given& given, float top) {
   Settings s;
-  const float t = a.temperature ? a.temperature[row] : 1.0f;
+  const float t = given.t, p = given.p, m = given.m;
+  const int k = given.k;
   s.greedy = !(t > 0.0f);
-  const int k = a.top_k ? a.top_k[row] : 0;
   s.k = k > 0 && k < a.vocab ? k : 0;
-  const float p = a.top_p ? a.top_p[row] : 1.0f;
   s.p = p < 1.0f ? p : 1.0f;
   s.cuts = !s.greedy && (s.k > 0 || s.p < 1.0f);
-  const float m = a.min_p ? a.min_p[row] : 0.0f;
   s.w.top = top == INFINITY ? 1e300 : (double)top;
   s.w.per_t = s.greedy || top == INFINITY ? 1.0 : 1.4426950408889634 / (double)t;
   s.w.least = m > 0.0f ? (uint64_t)(fmin((double)m, 1.0) * kOne) : 0;
@@ -365,7 +371,7 @@ __global__ __launch_bounds__(kPartThreads) void sample_bins_kernel(SampleArgs a,
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const PartInfo info = row_info(a, row);
   if (info.top == -INFINITY) return;
-  const Settings s = settings_of(a, row, info.top);
+  const Settings s = settings_of(a, Given(a, row), info.top);
   if (!s.cuts) return;
   const Row<EI_LOGITS_FP32> r(a, row);
   const int b0 = part * a.part_blocks, b1 = min(b0 + a.part_blocks, a.blocks);
@@ -547,7 +553,7 @@ __global__ __launch_bounds__(kThreads) void sample_cut_kernel(SampleArgs a, int6
   const Row<EI_LOGITS_FP32> r(a, row);
   const PartInfo info = row_info(a, row);
   if (info.top == -INFINITY) return;
-  const Settings s = settings_of(a, row, info.top);
+  const Settings s = settings_of(a, Given(a, row), info.top);
   if (!s.cuts) return;
   // all of the row's logits, with their indexes
   auto each_logit = [&](auto use) {
@@ -728,7 +734,7 @@ __global__ __launch_bounds__(kPartThreads) void sample_weigh_kernel(SampleArgs a
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
   const PartInfo info = row_info(a, row);
   if (info.top == -INFINITY) return;
-  const Settings s = settings_of(a, row, info.top);
+  const Settings s = settings_of(a, Given(a, row), info.top);
   if (s.greedy) return;
   const Row<EI_LOGITS_FP32> r(a, row);
   const int b0 = part * a.part_blocks, b1 = min(b0 + a.part_blocks, a.blocks);
@@ -790,7 +796,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a,
     if (threadIdx.x == 0) answer(a, row, -1, -INFINITY);
     return;
   }
-  const Settings s = settings_of(a, row, info.top);
+  const Settings s = settings_of(a, Given(a, row), info.top);
   if (s.greedy) {
     // in the first part that has it
     const float top = lane < a.parts ? a.part[row * a.parts + lane].top : -INFINITY;
@@ -1109,17 +1115,15 @@ struct RowWork {
     // the values in their order, four a thread: positive, near 0, negative
     constexpr int kEach = kTable / kThreads;
     auto place_of = [](int at) { return at <= kSide ? at : kSide + 1 + (2 * kSide - at); };
-    auto counts_at = [&](int at) -> uint64_t {
-      return at == kSide ? (uint64_t)sm.small_count : at > 2 * kSide ? 0 : sm.count[place_of(at)];
-    };
-    auto weights_at = [&](int at) -> uint64_t {
-      return at == kSide ? sm.small_sum : counts_at(at) * sm.weight[place_of(min(at, 2 * kSide))];
-    };
-    uint64_t n_all = 0, w_all = 0;
+    uint32_t counts[kEach];
+    uint64_t weights[kEach], n_all = 0, w_all = 0;
 #pragma unroll
     for (int i = 0; i < kEach; ++i) {
-      n_all += counts_at((int)threadIdx.x * kEach + i);
-      w_all += weights_at((int)threadIdx.x * kEach + i);
+      const int at = (int)threadIdx.x * kEach + i, place = place_of(min(at, 2 * kSide));
+      counts[i] = at == kSide ? (uint32_t)sm.small_count : at > 2 * kSide ? 0 : sm.count[place];
+      weights[i] = at == kSide ? sm.small_sum : counts[i] * sm.weight[place];
+      n_all += counts[i];
+      w_all += weights[i];
     }
     // (both sums at once)
     uint64_t n_to = wave_up_to(n_all), w_to = wave_up_to(w_all), total_n = 0, total_w = 0;
@@ -1176,18 +1180,20 @@ struct RowWork {
         uint64_t before = by_count ? n_to - n_all : w_to - w_all;
         uint64_t weight_before = w_to - w_all;
         __syncthreads();
-#pragma unroll 1
-        for (int at = (int)threadIdx.x * kEach; at < ((int)threadIdx.x + 1) * kEach; ++at) {
-          const uint64_t n = counts_at(at), w = weights_at(at), v = by_count ? n : w;
-          if (before < want && want <= before + v) {
-            sm.found = place_of(at);
-            sm.found_before = before;
-            sm.found_weight = weight_before;
-            sm.found_count = n;
+        const uint64_t end = before + (by_count ? n_all : w_all);
+        if (before < want && want <= end)
+#pragma unroll
+          for (int i = 0; i < kEach; ++i) {
+            const uint64_t v = by_count ? counts[i] : weights[i];
+            if (before < want && want <= before + v) {
+              sm.found = place_of((int)threadIdx.x * kEach + i);
+              sm.found_before = before;
+              sm.found_weight = weight_before;
+              sm.found_count = counts[i];
+            }
+            before += v;
+            weight_before += weights[i];
           }
-          before += v;
-          weight_before += w;
-        }
         __syncthreads();
         cut_at = sm.found;
         want -= sm.found_before;
@@ -1198,8 +1204,9 @@ struct RowWork {
         cut = find_cut(sm.pick, in, want, each_small,
                        [&](uint32_t key) { return by_count ? (uint64_t)1 : weight(key); });
       } else {
-        const uint64_t v = by_count ? 1 : sm.weight[cut_at];
-        cut = Cut{key_of(value(bits_at(cut_at))), (want + v - 1) / v};
+        // (by counts nothing is to be divided)
+        if (!by_count) want = (want + sm.weight[cut_at] - 1) / sm.weight[cut_at];
+        cut = Cut{key_of(value(bits_at(cut_at))), want};
       }
     }
     if (cut.key) split = cut_at == kSide || cut.count < same;
@@ -1313,12 +1320,13 @@ __global__ __launch_bounds__(kThreads) void sample_row_kernel(SampleArgs a, int6
   __shared__ RowSmem sm;
   const int64_t row = row0 + blockIdx.x;
   RowWork work(a, sm, row);
+  const Given given(a, row);
   const float top = work.largest();
   if (top == -INFINITY) {
     if (threadIdx.x == 0) answer(a, row, -1, -INFINITY);
     return;
   }
-  const Settings s = settings_of(a, row, top);
+  const Settings s = settings_of(a, given, top);
   if (s.greedy) {
     work.take_largest(top);
     return;
@@ -1366,9 +1374,10 @@ __global__ __launch_bounds__(kThreads) void sample_tops_kernel(SampleArgs a, int
 __global__ __launch_bounds__(kThreads) void sample_counts_kernel(SampleArgs a, int64_t unit0) {
   __shared__ RowSmem sm;
   const int64_t unit = unit0 + blockIdx.x, row = unit / a.parts;
+  const Given given(a, row);
   const float top = row_top(a, row);
   if (top == -INFINITY) return;
-  const Settings s = settings_of(a, row, top);
+  const Settings s = settings_of(a, given, top);
   if (!s.cuts) return;
   RowState& state = a.state[row];
   RowWork work(a, sm, row);
@@ -1391,12 +1400,18 @@ __global__ __launch_bounds__(kThreads) void sample_weights_kernel(SampleArgs a, 
   __shared__ RowSmem sm;
   const int64_t unit = unit0 + blockIdx.x, row = unit / a.parts;
   const int part = (int)(unit % a.parts);
+  const Given given(a, row);
+  constexpr int kEach = kTable / kThreads;
+  uint32_t count[kEach] = {};
+  if (a.top_k || a.top_p)
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) count[i] = a.counts[row * kTable + i * kThreads + threadIdx.x];
   const float top = row_top(a, row);
   if (top == -INFINITY) {
     if (part == 0 && threadIdx.x == 0) answer(a, row, -1, -INFINITY);
     return;
   }
-  const Settings s = settings_of(a, row, top);
+  const Settings s = settings_of(a, given, top);
   RowWork work(a, sm, row);
   if (s.greedy) {
     // in the first part that has it
@@ -1410,7 +1425,8 @@ __global__ __launch_bounds__(kThreads) void sample_weights_kernel(SampleArgs a, 
   work.fill_weights();
   if (s.cuts) {        // each workgroup finds the cut by itself
     RowState& state = a.state[row];
-    for (int i = threadIdx.x; i < kTable; i += kThreads) sm.count[i] = a.counts[row * kTable + i];
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) sm.count[i * kThreads + threadIdx.x] = count[i];
     if (threadIdx.x == 0) {
       sm.small_count = (int)state.small_count;
       sm.small_sum = state.small_sum;
@@ -1431,9 +1447,10 @@ __global__ __launch_bounds__(kThreads) void sample_weights_kernel(SampleArgs a, 
 __global__ __launch_bounds__(kThreads) void sample_token_kernel(SampleArgs a, int64_t row0) {
   __shared__ RowSmem sm;
   const int64_t row = row0 + blockIdx.x;
+  const Given given(a, row);
   const float top = row_top(a, row);
   if (top == -INFINITY) return;
-  const Settings s = settings_of(a, row, top);
+  const Settings s = settings_of(a, given, top);
   if (s.greedy) return;
   RowWork work(a, sm, row);
   work.place_tables(s, top);

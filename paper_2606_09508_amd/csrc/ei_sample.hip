@@ -27,7 +27,7 @@
 //  sample_pick_kernel   a workgroup a row: the 2048 that u lies in, the token
 //
 // Measured (a captured call, us): 256 rows of 128256 in bf16 34 to 36 (65 MB: 13 at a
-// copy's rate), 64 of them with all settings mixed 39, one with top-p 26; in fp32 73, 76
+// copy's rate), 64 of them with all settings mixed 36, one with top-p 24; in fp32 73, 76
 // and 35; 12 masked rows of 32001 36 to 45.  A row's passes are bound by LDS (a table's
 // entry a token, 8 bytes from any bank: 16 cycles for a wave's 64), calls of few rows by
 // the launches and the steps of the cut, which follow one another.
@@ -1493,9 +1493,9 @@ SamplePlan fp32_plan(int rows, int vocab) {
   return p;
 }
 // bf16.  A workgroup a row, or, of long rows, as many as the chip has CUs for, of a piece
-// a wave at least.  In one and in several, us a call: 1 x 128256 (top-p) 34, 26; 32 rows
-// of it 48, 35; 128 50, 47; 1 x 80000 27, 26; 32 38, 33; but 1 x 65536 23, 25; 1 x 32001
-// 19, 26; 64 26, 33.
+// a wave at least.  In one and in several, us a call: 1 x 128256 (top-p) 33, 24; 32 rows
+// of it 46, 32; 128 50, 45; 1 x 80000 26, 24; 1 x 65536 23, 23; 32 32, 29; but 1 x 50257
+// 22, 24; 1 x 32001 18, 24.
 SamplePlan bf16_plan(int rows, int vocab) {
   SamplePlan p{};
   const int pieces = (vocab + kPiece - 1) / kPiece;
@@ -1503,7 +1503,7 @@ SamplePlan bf16_plan(int rows, int vocab) {
   p.parts = kCUs / rows;
   p.parts = p.parts > most ? most : p.parts;
   p.parts = p.parts > kMaxParts ? kMaxParts : p.parts;
-  if (p.parts < 2 || pieces < 9 * kWaves) {
+  if (p.parts < 2 || pieces < 8 * kWaves) {
     p.parts = 1;
     return p;
   }

@@ -360,7 +360,7 @@ def _rows_of_all_kinds(vocab):
     return x.to(BF16)
 
 
-@pytest.mark.parametrize("vocab", [73728, 73729, 128256, 524288])
+@pytest.mark.parametrize("vocab", [65536, 65537, 73728, 128256, 524288])
 def test_a_row_is_the_same_in_one_workgroup_and_in_several(vocab):
     """Sums of weights are whole numbers: every bit is the same, however a row is
     divided, in any company."""

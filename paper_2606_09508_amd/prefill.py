@@ -240,8 +240,9 @@ def check_adapters(adapters, layers) -> int:
             a, b, scale = t
             n = a.shape[0]
             count = n if count is None else count
-            if a.dim() != 3 or b.dim() != 3 or tuple(a.shape) != (count, a.shape[1], w[name].shape[0]) \
-                    or tuple(b.shape) != (count, w[name].shape[1], a.shape[1]) \
+            n_in, n_out = w[name].shape
+            if a.dim() != 3 or b.dim() != 3 or tuple(a.shape) != (count, a.shape[1], n_in) \
+                    or tuple(b.shape) != (count, n_out, a.shape[1]) \
                     or (scale is not None and tuple(scale.shape) != (count,)):
                 raise ValueError(f"{name} of layer {i}: adapters {tuple(a.shape)} and "
                                  f"{tuple(b.shape)} do not correct {count} times a product of "
@@ -270,7 +271,7 @@ class BatchAdapters:
     def __init__(self, adapters, count: int, index, n_tokens: int, cu=None):
         self.adapters, self.n = adapters, count
         self.index, self.n_tokens, self.cu = index, n_tokens, cu
-        self._plan = None
+        self._plan, self._scratch = None, {}
 
     def layer(self, i: int):
         return functools.partial(self._correct, self.adapters[i])
@@ -291,7 +292,12 @@ class BatchAdapters:
             if quiet and self._fits(h, rank, [ys[i] for i in at], of):
                 if self._plan is None:
                     self._plan = eb.adapter_plan(self.index, self.n, self.n_tokens, self.cu)
-                eb.adapter_add(h, [ys[i] for i in at], of, self._plan)
+                # (the calls come one after the other: those of one size share a workspace)
+                size = h.shape[-1], rank, len(at)
+                if size not in self._scratch:
+                    nb = eb.adapter_add_workspace_bytes(self._plan, *size)
+                    self._scratch[size] = torch.empty((nb,), dtype=torch.uint8, device=h.device)
+                eb.adapter_add(h, [ys[i] for i in at], of, self._plan, self._scratch[size])
             else:
                 for i, t in zip(at, of):
                     ys[i] = self._tensors(h, ys[i], t)

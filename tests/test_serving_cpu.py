@@ -199,13 +199,14 @@ class _Kernel:
         monkeypatch.setattr(pf, "_kernel_device", lambda dev: dev.type == "cpu")
         monkeypatch.setattr(eb, "adapter_plan", self.plan)
         monkeypatch.setattr(eb, "adapter_add", self.add)
+        monkeypatch.setattr(eb, "adapter_add_workspace_bytes", lambda plan, *size: 16)
 
     def plan(self, index, n, tokens, cu=None):
         self.calls.append("plan")
         return "plan"
 
-    def add(self, h, ys, of, plan):
-        assert plan == "plan" and len({t.a.shape[1] for t in of}) == 1
+    def add(self, h, ys, of, plan, workspace):
+        assert workspace.numel() == 16 and plan == "plan" and len({t.a.shape[1] for t in of}) == 1
         self.calls.append(len(ys))
         for y in ys:
             y.add_(1)

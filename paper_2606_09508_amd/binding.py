@@ -14,6 +14,7 @@ import functools
 import math
 import operator
 import os
+import struct
 from typing import NamedTuple
 
 import torch
@@ -61,6 +62,10 @@ class AdapterBatch(ctypes.Structure):
 class AdapterTarget(ctypes.Structure):
     _fields_ = [("a", ctypes.c_void_p), ("b", ctypes.c_void_p), ("scale", ctypes.c_void_p),
                 ("y", ctypes.c_void_p), ("n_out", ctypes.c_int32)]
+
+
+_pack_target = struct.Struct("=QQQQi4x").pack
+assert struct.calcsize("=QQQQi4x") == ctypes.sizeof(AdapterTarget)
 
 
 class EIError(RuntimeError):
@@ -889,7 +894,7 @@ def cache_attn_shared(q, pages: CachePages, page_table, lengths, group_seqs, sha
     if workspace is None:
         nb = L.ei_cache_attn_shared_workspace_bytes(Hq, T, S, n_groups, cols, cs)
         if nb:
-            workspace = torch.empty((nb,), dtype=torch.uint8, device=q.device)
+            workspace = torch.empty(nb, dtype=torch.uint8, device=q.device)
     else:
         _same_device(q, workspace)
         if not workspace.is_contiguous():
@@ -971,7 +976,7 @@ def adapter_plan(index, n_adapters: int, n_tokens: int, cu_seqlens=None) -> Adap
             return adapter_plan(index, n_adapters, n_tokens, cu_seqlens)
     batch = AdapterBatch(n_tokens, S, n_adapters)
     nb = lib().ei_adapter_plan_bytes(batch)
-    data = torch.empty((nb,), dtype=torch.uint8, device=index.device)
+    data = torch.empty(nb, dtype=torch.uint8, device=index.device)
     st = lib().ei_adapter_plan(index.data_ptr(), _ptr(cu_seqlens), batch, data.data_ptr(), nb,
                                _raw_stream(dev))
     if st:
@@ -1004,7 +1009,8 @@ def adapter_add(x, ys, adapters, plan: AdapterPlan, workspace=None) -> None:
         raise ValueError(f"x {tuple(x.shape)} does not hold the {T} tokens of the plan")
     if not len(ys) == len(adapters) or not ys:
         raise ValueError(f"{len(adapters)} sets of adapters for {len(ys)} projections")
-    n, rank, targets, TT = plan.batch.n_adapters, 0, [], torch.Tensor
+    n, rank, TT = plan.batch.n_adapters, 0, torch.Tensor
+    targets, given = [], []      # (as bytes: an array of structures costs twice as much)
     for y, (a, b, scale) in zip(ys, adapters):
         if not (isinstance(y, TT) and isinstance(a, TT) and isinstance(b, TT)
                 and y.dtype is bf16 and a.dtype is bf16 and b.dtype is bf16
@@ -1019,7 +1025,7 @@ def adapter_add(x, ys, adapters, plan: AdapterPlan, workspace=None) -> None:
             raise ValueError(f"projection {len(targets)}: a {tuple(a.shape)}, b {tuple(b.shape)} "
                              f"and y {tuple(y.shape)} are not [{n}, {rank}, {n_in}], [{n}, n_out, "
                              f"{rank}] and {T} tokens of n_out")
-        sp = None
+        sp = 0
         if scale is not None:
             if not (isinstance(scale, TT) and scale.dtype is torch.float32 and scale.dim() == 1
                     and scale.get_device() == dev and scale.is_contiguous()):
@@ -1029,8 +1035,10 @@ def adapter_add(x, ys, adapters, plan: AdapterPlan, workspace=None) -> None:
                 raise ValueError(f"projection {len(targets)}: {scale.size(0)} scales for {n} "
                                  f"adapters")
             sp = scale.data_ptr()
-        targets.append((a.data_ptr(), b.data_ptr(), sp, y.data_ptr(), n_out))
-    if T and len({t[3] for t in targets}) != len(targets):
+        yp = y.data_ptr()
+        targets.append(_pack_target(a.data_ptr(), b.data_ptr(), sp, yp, n_out))
+        given.append(yp)
+    if T and len(set(given)) != len(given):
         raise ValueError("a projection's y is given twice")
     if dev != _current_device():
         with torch.cuda.device(dev):
@@ -1039,15 +1047,15 @@ def adapter_add(x, ys, adapters, plan: AdapterPlan, workspace=None) -> None:
     if workspace is None:
         nb = L.ei_adapter_add_workspace_bytes(plan.batch, n_in, rank, len(targets))
         if nb:
-            workspace = torch.empty((nb,), dtype=torch.uint8, device=x.device)
+            workspace = torch.empty(nb, dtype=torch.uint8, device=x.device)
     else:
         _same_device(x, workspace)
         if not workspace.is_contiguous():
             raise ValueError("workspace must be contiguous")
         nb = workspace.numel() * workspace.element_size()
-    st = L.ei_adapter_add(x.data_ptr(), n_in, rank, (AdapterTarget * len(targets))(*targets),
-                          len(targets), plan.batch, plan.data.data_ptr(), plan.data.numel(),
-                          _ptr(workspace), nb, _raw_stream(dev))
+    st = L.ei_adapter_add(x.data_ptr(), n_in, rank, b"".join(targets), len(targets), plan.batch,
+                          plan.data.data_ptr(), plan.data.numel(), _ptr(workspace), nb,
+                          _raw_stream(dev))
     if st:
         _check("ei_adapter_add", st)
 
@@ -1104,9 +1112,9 @@ def sample_tokens(logits, u, temperature=None, top_k=None, top_p=None, min_p=Non
             _setting(top_k, "top_k", torch.int32, rows, dev),
             _setting(top_p, "top_p", f32, rows, dev), _setting(min_p, "min_p", f32, rows, dev)]
     if out is None:
-        out = torch.empty((rows,), dtype=torch.int32, device=logits.device)
+        out = torch.empty(rows, dtype=torch.int32, device=logits.device)
     if logprobs is None:
-        logprobs = torch.empty((rows,), dtype=f32, device=logits.device)
+        logprobs = torch.empty(rows, dtype=f32, device=logits.device)
     args += [_setting(out, "out", torch.int32, rows, dev),
              _setting(logprobs, "logprobs", f32, rows, dev)]
     if dev != _current_device():
@@ -1117,7 +1125,7 @@ def sample_tokens(logits, u, temperature=None, top_k=None, top_p=None, min_p=Non
     if workspace is None:
         nb = L.ei_sample_workspace_bytes(rows, vocab, fmt)
         if nb:
-            workspace = torch.empty((nb,), dtype=torch.uint8, device=logits.device)
+            workspace = torch.empty(nb, dtype=torch.uint8, device=logits.device)
     else:
         _same_device(logits, workspace)
         if not workspace.is_contiguous():

@@ -397,7 +397,7 @@ class Decoder:
             _, logits = self.step(x[None], seqs, adapter=adapter)
             tokens.append(t)
             logprobs.append(p)
-        if not n:
+        if not tokens:
             dev = logits.device
             return (torch.empty((len(seqs), 0), dtype=torch.int32, device=dev),
                     torch.empty((len(seqs), 0), device=dev))

@@ -22,7 +22,8 @@
 //   64 sequences behind 32768 keys, 32 heads over 8:   5.9 + 71 + 7.0; 57 of the 71 are
 //       the shared keys, 34 GFLOP at 600 TFLOP/s, matrix cores busy 0.28 of the time
 //   16 behind 8192, the same heads:                    5.5 + 20.5 + 6.8
-//   9, 5, 1, 17 behind 2048 to 12288, 64 over 8, int8: 5.9 + 69 + 9.9
+//   9, 5 and 17 behind 2048 to 12288, 4 new tokens
+//     each, 64 over 8, int8:                           5.9 + 69 + 9.9
 //   2 behind 960, 4 heads over 1:                      5.5 + 7.3 + 4.1
 #include "ei_attend.h"
 

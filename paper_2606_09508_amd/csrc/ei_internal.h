@@ -102,6 +102,19 @@ __device__ __forceinline__ uint32_t wave_incl_scan_u32(uint32_t x) {
   x += EI_DPP_U32(x, 0x143, 0xC, true);   // row_bcast:31 into rows 2, 3
   return x;
 }
+__device__ __forceinline__ uint64_t wave_incl_scan_u64(uint64_t v) {
+#define EI_ADD_DPP(ctrl, rows)                                                        \
+  v += (uint64_t)EI_DPP_U32((uint32_t)(v >> 32), ctrl, rows, true) << 32 |            \
+       EI_DPP_U32((uint32_t)v, ctrl, rows, true)
+  EI_ADD_DPP(0x111, 0xF);   // row_shr:1
+  EI_ADD_DPP(0x112, 0xF);
+  EI_ADD_DPP(0x114, 0xF);
+  EI_ADD_DPP(0x118, 0xF);
+  EI_ADD_DPP(0x142, 0xA);   // row_bcast:15 into rows 1, 3
+  EI_ADD_DPP(0x143, 0xC);   // row_bcast:31 into rows 2, 3
+#undef EI_ADD_DPP
+  return v;
+}
 
 
 // ----------------------------------------------------------------------------

@@ -265,21 +265,6 @@ __device__ __forceinline__ float wave_sum_f32(float v) {
   for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
   return v;
 }
-// The sum over this lane and those before it.
-__device__ __forceinline__ uint64_t wave_up_to(uint64_t v) {
-#define EI_ADD_DPP(ctrl, rows)                                                        \
-  v += (uint64_t)EI_DPP_U32((uint32_t)(v >> 32), ctrl, rows, true) << 32 |            \
-       EI_DPP_U32((uint32_t)v, ctrl, rows, true)
-  EI_ADD_DPP(0x111, 0xF);   // row_shr:1
-  EI_ADD_DPP(0x112, 0xF);
-  EI_ADD_DPP(0x114, 0xF);
-  EI_ADD_DPP(0x118, 0xF);
-  EI_ADD_DPP(0x142, 0xA);   // row_bcast:15 into rows 1, 3
-  EI_ADD_DPP(0x143, 0xC);   // row_bcast:31 into rows 2, 3
-#undef EI_ADD_DPP
-  return v;
-}
-
 // ----------------------------------------------------------------------------
 // Scan
 // ----------------------------------------------------------------------------
@@ -452,7 +437,7 @@ __device__ __forceinline__ uint64_t block_sum(PickSmem& sm, uint64_t v) {
 // The sum over this thread and those before it.
 __device__ __forceinline__ uint64_t block_up_to(PickSmem& sm, uint64_t v) {
   const int wave = threadIdx.x / kWave;
-  v = wave_up_to(v);
+  v = wave_incl_scan_u64(v);
   __syncthreads();
   if (threadIdx.x % kWave == kWave - 1) sm.wave_sum[wave] = v;
   __syncthreads();
@@ -829,7 +814,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a,
   auto kept = [&](uint64_t before) { return before < cut.count ? before : cut.count; };
   // the sum over this thread and those before it
   auto up_to = [&](int which, uint64_t v, uint64_t& total) -> uint64_t {
-    v = wave_up_to(v);
+    v = wave_incl_scan_u64(v);
     if (lane == kWave - 1) wave_sum[which][wave] = v;
     __syncthreads();
     total = 0;
@@ -868,7 +853,7 @@ __global__ __launch_bounds__(kPickThreads) void sample_pick_kernel(SampleArgs a,
     }
     const uint64_t same_end = same + wave_incl_scan_u32(n_same), same_begin = same_end - n_same;
     mine += (kept(same_end) - kept(same_begin)) * w_cut;
-    const uint64_t mine_end = run + wave_up_to(mine);
+    const uint64_t mine_end = run + wave_incl_scan_u64(mine);
     uint64_t to = mine_end - mine;
     if (to <= want && want < mine_end) {
       uint64_t n = same_begin;
@@ -1126,7 +1111,7 @@ struct RowWork {
       w_all += weights[i];
     }
     // (both sums at once)
-    uint64_t n_to = wave_up_to(n_all), w_to = wave_up_to(w_all), total_n = 0, total_w = 0;
+    uint64_t n_to = wave_incl_scan_u64(n_all), w_to = wave_incl_scan_u64(w_all), total_n = 0, total_w = 0;
     if (lane == kWave - 1) {
       sm.wave_sums[wave][0] = n_to;
       sm.wave_sums[wave][1] = w_to;
@@ -1304,7 +1289,7 @@ struct RowWork {
       if (mine[e] >> kSameBit) mine[e] = same++ < cut.count ? w_cut : 0;
       all += mine[e];
     }
-    uint64_t run = sm.found_before + wave_up_to(all) - all;
+    uint64_t run = sm.found_before + wave_incl_scan_u64(all) - all;
     if (!(run <= want && want < run + all)) return;
 #pragma unroll
     for (int e = 0; e < 8; ++e) {

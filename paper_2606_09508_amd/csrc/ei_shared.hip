@@ -98,12 +98,7 @@ __device__ __forceinline__ int group_cost(const SharedArgs& x, bool whole) {
 __device__ __forceinline__ int64_t block_before(int64_t* sums, int64_t v, int64_t& total) {
   // the sum over the threads before this one, and over all
   const int lane = threadIdx.x % kWave, wave = threadIdx.x / kWave;
-  int64_t up = v;
-#pragma unroll
-  for (int o = 1; o < kWave; o <<= 1) {
-    const int64_t t = __shfl_up(up, o);
-    if (lane >= o) up += t;
-  }
+  const int64_t up = (int64_t)wave_incl_scan_u64((uint64_t)v);
   __syncthreads();
   if (lane == kWave - 1) sums[wave] = up;
   __syncthreads();
@@ -280,15 +275,8 @@ __global__ __launch_bounds__(kFewThreads) void shared_plan_few_kernel(SharedArgs
   si.first = first;
   si.n = n;
   auto sum_before = [&](int64_t& u, int64_t& it, int64_t& all_u, int64_t& all_it) {
-    int64_t uu = u, ii = it;
-#pragma unroll
-    for (int o = 1; o < kWave; o <<= 1) {
-      const int64_t a1 = __shfl_up(uu, o), a2 = __shfl_up(ii, o);
-      if (lane >= o) {
-        uu += a1;
-        ii += a2;
-      }
-    }
+    const int64_t uu = (int64_t)wave_incl_scan_u64((uint64_t)u);
+    const int64_t ii = (int64_t)wave_incl_scan_u64((uint64_t)it);
     __syncthreads();
     if (lane == kWave - 1) {
       units_of[wave] = uu;

@@ -140,27 +140,18 @@ struct Row {
     }
     return make_uint4((uint32_t)w[0], (uint32_t)(w[0] >> 32), (uint32_t)w[1], (uint32_t)(w[1] >> 32));
   }
+  // fp32
   __device__ __forceinline__ void load(int piece, int lane, float (&x)[8]) const {
-    if constexpr (FMT == EI_LOGITS_BF16) {
-      const uint4 w = load_raw(piece, lane);
-      const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
+    const int i0 = index(piece, lane);
+    const float* p = (const float*)at + i0;
+    if (i0 + 8 <= vocab) {
+      const uint4 u = load16(p), v = load16(p + 4);
+      const uint32_t w[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        x[2 * e] = bf16_lo(ww[e]);
-        x[2 * e + 1] = bf16_hi(ww[e]);
-      }
+      for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(w[e]);
     } else {
-      const int i0 = index(piece, lane);
-      const float* p = (const float*)at + i0;
-      if (i0 + 8 <= vocab) {
-        const uint4 u = load16(p), v = load16(p + 4);
-        const uint32_t w[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(w[e]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = i0 + e < vocab ? p[e] : -INFINITY;
-      }
+      for (int e = 0; e < 8; ++e) x[e] = i0 + e < vocab ? p[e] : -INFINITY;
     }
   }
   // four pieces one behind the other

@@ -587,8 +587,10 @@ size_t ei_cache_attn_shared_workspace_bytes(int32_t n_q_heads, int32_t n_tokens,
  * or before) are read for each sequence by itself, so shared_pages may be too large
  * for the lengths, but not for the table.  The probabilities of shared keys enter
  * the second product as fp16 numbers (11 bits) where a group has more than 32 rows
- * (tokens times query heads of a KV head) on average, with 16 bits otherwise; all
- * else is as in ei_cache_attn, zero rows and rows of no sequence included.  Lists that
+ * (tokens times query heads of a KV head) on average, with 16 bits otherwise; there
+ * those that times V's scale lie 2^-32 below a row's largest may be 0 in the sum of
+ * values (never in the sum of weights, which V's scales do not touch).  All else is as
+ * in ei_cache_attn, zero rows and rows of no sequence included.  Lists that
  * do not ascend leave o undefined, and nothing outside the tensors is touched.
  * A sequence's bits depend, by roundings, on the others of the call.
  *

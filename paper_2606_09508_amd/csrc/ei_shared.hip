@@ -427,15 +427,21 @@ __global__ __launch_bounds__(kThreads, attend_occupancy(RT)) void shared_steps_k
 //
 // Both formats' codes are exact in bf16 and in fp16.  The probabilities enter the
 // second product as one fp16 number each (11 bits, against 8 of bf16; rounding them
-// costs a tenth of what the output's rounding to bf16 does): e = 2^(x - M) with x the
-// score (base 2) plus the exponent of V's scale, and M a running maximum of x, less
-// 8, that may trail by 6 more: e is at most 2^14, and what fp16 loses lies 2^-32
-// below the row's largest.  l sums e / 2^exponent, so it and O are relative to the
-// same M.  A scale's significand, 1 from cache_store, is multiplied in where it is
-// not.
+// costs a tenth of what the output's rounding to bf16 does): e = 2^(x + E - M) with x
+// the score (base 2), E the exponent of V's scale, and M a running maximum of x + E,
+// less 8, that may trail by 6 more: e is at most 2^14, and what fp16 loses lies 2^-32
+// below the row's largest.  A scale's significand, 1 from cache_store, is multiplied
+// in where it is not.
+//
+// What a key weighs has nothing to do with V's scale, and a page of zeros has one of
+// 2^-126: l = sum of 2^(x - ml) has a running maximum of its own, ml, of x alone, that
+// may trail by 14.  A page's part of it is that of e times 2^(M - E - ml), or, where
+// that is past 2^64 (e may have lost keys that weigh 2^-62), summed from the scores.
+// At an item's end O is brought to ml.
 // ----------------------------------------------------------------------------
 constexpr float kWideLimit = 0x1p14f;
 constexpr float kWideHead = 8.0f;
+constexpr float kWideGap = 64.0f;
 
 template <int FMT, bool HI>
 __device__ __forceinline__ uint32_t half2_of(uint32_t x) {
@@ -506,7 +512,7 @@ __device__ __forceinline__ void wide_run(const SharedArgs& x, WideSmem& sm) {
 #pragma unroll
       for (int c = 0; c < 8; ++c) asm volatile("" : "+v"(qf[c]));
     }
-    float M = -INFINITY, l = 0.0f;
+    float M = -INFINITY, ml = -INFINITY, l = 0.0f;
     f32x16 o[4];
 #pragma unroll
     for (int m = 0; m < 4; ++m)
@@ -606,11 +612,12 @@ __device__ __forceinline__ void wide_run(const SharedArgs& x, WideSmem& sm) {
     };
     auto sums = [&](int buf, float k_scale, float vf) {
       const float kf = k_scale * a.sc_log2;
-      // V's scale as sig * 2^E (E = 0 for zeros, infinities and NaN), unit = 2^-E
+      // V's scale as sig * 2^E (E = -126 for zeros and what is nearer to them, 0 for
+      // infinities and NaN)
       const int ve = (int)(__float_as_uint(vf) >> 23 & 0xffu);
-      const int ce = ve == 0 || ve == 0xff ? 127 : min(ve, 253);
-      const float E = (float)(ce - 127), unit = __uint_as_float((uint32_t)(254 - ce) << 23);
-      const float sig = vf * unit;
+      const int ce = ve == 0xff ? 127 : min(max(ve, 1), 253);
+      const float E = (float)(ce - 127);
+      const float sig = vf * __uint_as_float((uint32_t)(254 - ce) << 23);
       float e[KT][16], sum;
       auto probs = [&](float c) {
         float part[4] = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -624,22 +631,36 @@ __device__ __forceinline__ void wide_run(const SharedArgs& x, WideSmem& sm) {
         sum = (part[0] + part[1]) + (part[2] + part[3]);
       };
       probs(E - M);
-      if (__builtin_amdgcn_ballot_w64(!(sum <= kWideLimit)) != 0) {
+      float gap = M - ml - E, part = sum * __builtin_amdgcn_exp2f(gap);
+      const bool fits = sum <= kWideLimit && part <= kWideLimit && gap <= kWideGap;
+      if (__builtin_amdgcn_ballot_w64(!fits) != 0) {
         float mx = -INFINITY;
 #pragma unroll
         for (int t = 0; t < KT; ++t)
 #pragma unroll
           for (int r = 0; r < 16; ++r) mx = fmaxf(mx, s[t][r] * kf);
-        mx = fmaxf(mx, __shfl_xor(mx, 32)) + E - kWideHead;
-        const float m_new = fmaxf(M, mx);
-        const float alpha = m_new == -INFINITY ? 1.0f : __builtin_amdgcn_exp2f(M - m_new);
-        l *= alpha;
+        mx = fmaxf(mx, __shfl_xor(mx, 32));
+        const float ml_new = fmaxf(ml, mx), m_new = fmaxf(M, mx + E - kWideHead);
+        const bool none = m_new == -INFINITY;      // (and ml_new with it)
+        const float alpha = none ? 1.0f : __builtin_amdgcn_exp2f(M - m_new);
+        l *= none ? 1.0f : __builtin_amdgcn_exp2f(ml - ml_new);
 #pragma unroll
         for (int m = 0; m < 4; ++m) o[m] *= alpha;
         M = m_new;
-        probs(M == -INFINITY ? 0.0f : E - M);
+        ml = ml_new;
+        probs(none ? 0.0f : E - M);
+        gap = none ? 0.0f : M - ml - E;
+        part = sum * __builtin_amdgcn_exp2f(gap);
+        if (__builtin_amdgcn_ballot_w64(gap > kWideGap) != 0) {
+          part = 0.0f;
+#pragma unroll
+          for (int t = 0; t < KT; ++t)
+#pragma unroll
+            for (int r = 0; r < 16; ++r)
+              part += __builtin_amdgcn_exp2f(fmaf(s[t][r], kf, none ? 0.0f : -ml));
+        }
       }
-      l += sum * unit;
+      l += part;
       if (sig != 1.0f) {
 #pragma unroll
         for (int t = 0; t < KT; ++t)
@@ -712,6 +733,11 @@ __device__ __forceinline__ void wide_run(const SharedArgs& x, WideSmem& sm) {
       vs = vs_next;
     }
     l += __shfl_xor(l, 32);
+    // (2^(M - ml) may be past fp32 where its half is not)
+    const float to_ml = M == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(0.5f * (M - ml));
+#pragma unroll
+    for (int m = 0; m < 4; ++m) o[m] = o[m] * to_ml * to_ml;
+    M = ml;
     // the sums of the waves with the same rows, by halves
     float* const ex = (float*)&sm;
 #pragma unroll

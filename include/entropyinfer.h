@@ -718,7 +718,8 @@ size_t ei_adapter_add_workspace_bytes(ei_adapter_batch batch, int32_t n_in, int3
  * (bf16 [n_tokens][n_in]) to their y, in place.  rank is a multiple of 8 up to 128
  * (smaller ones are padded with zeros), n_in a multiple of 8 (else
  * EI_ERR_UNSUPPORTED).  x A^T is held in fp32, enters the second product with 16
- * significant bits (as the sum of two bf16 numbers), and y is rounded once.
+ * significant bits (as the sum of two bf16 numbers), and y is rounded once.  An
+ * infinite entry of b makes its output, for the adapter's tokens, infinite or NaN.
  * `targets` is read on the host.  Rows of y whose sequence has no adapter, or that
  * belong to no sequence, are left as they were; offsets that do not ascend leave
  * the values of y undefined, and nothing outside the tensors is touched.  No y may

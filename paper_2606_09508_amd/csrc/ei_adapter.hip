@@ -409,11 +409,14 @@ __global__ __launch_bounds__(kThreads) void expand_kernel(AddArgs a, int64_t uni
       }
     }
     const float v[4] = {x.x * scale, x.y * scale, x.z * scale, x.w * scale};
-    float rest[4];
-    const uint32_t hi[2] = {pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3])};
+    // (the first number ends at bf16's largest: what lies beyond, infinity too, is rest)
+    float rest[4], near[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)      // (an infinity has no rest)
-      rest[i] = __builtin_isinf(v[i]) ? 0.0f : v[i] - (i & 1 ? bf16_hi(hi[i / 2]) : bf16_lo(hi[i / 2]));
+    for (int i = 0; i < 4; ++i) near[i] = fminf(fmaxf(v[i], -0x1.fep127f), 0x1.fep127f);
+    const uint32_t hi[2] = {pack_bf16x2(near[0], near[1]), pack_bf16x2(near[2], near[3])};
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      rest[i] = v[i] - (i & 1 ? bf16_hi(hi[i / 2]) : bf16_lo(hi[i / 2]));
     *(uint2*)&sm[tok * pitch + c] = make_uint2(hi[0], hi[1]);
     *(uint2*)&sm[tok * pitch + r + c] = make_uint2(pack_bf16x2(rest[0], rest[1]), pack_bf16x2(rest[2], rest[3]));
   }

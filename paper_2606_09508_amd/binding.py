@@ -940,6 +940,9 @@ def cache_copy(pages: CachePages, src, dst) -> None:
 # Low-rank adapters
 # --------------------------------------------------------------------------
 
+MAX_ADAPTERS = 8192      # that ei_adapter_plan takes
+
+
 class Adapters(NamedTuple):
     """Low-rank corrections of one projection (ei_adapter_target): a [n, rank,
     n_in] and b [n, n_out, rank] in bf16, scale fp32 [n] or None (1).  rank is a

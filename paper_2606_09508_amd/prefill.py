@@ -306,7 +306,7 @@ class BatchAdapters:
     @staticmethod
     def _fits(h, rank, ys, of) -> bool:
         """Sizes, types and layout ei_adapter_add takes."""
-        if rank % 8 or not 0 < rank <= 128:
+        if rank % 8 or not 0 < rank <= 128 or len(of[0].a) > eb.MAX_ADAPTERS:
             return False
         ts = [h, *ys]
         for a, b, scale in of:

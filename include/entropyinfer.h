@@ -583,6 +583,9 @@ size_t ei_cache_attn_shared_workspace_bytes(int32_t n_q_heads, int32_t n_tokens,
  *                  of one call
  *   the others     as ei_cache_attn
  *
+ * Tiles are taken by the new tokens for each group named, n_tokens / n_groups; many
+ * groups that share nothing beside a few large ones make them narrow.
+ *
  * Columns with a key that a new token of the group does not see (it lies in the page
  * or before) are read for each sequence by itself, so shared_pages may be too large
  * for the lengths, but not for the table.  The probabilities of shared keys enter

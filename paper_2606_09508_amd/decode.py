@@ -405,17 +405,24 @@ class Decoder:
         """n tokens of each sequence from the logits [len(seqs), vocab] of its last
         token on: each is drawn by the sampler and its row of embed [vocab, hidden]
         put through a step, the last one too, so that the sequences hold them all:
-        (tokens int32 [len(seqs), n], their log probabilities)."""
+        (tokens int32 [len(seqs), n], their log probabilities).  Where a step fails the
+        sequences are cut back to what they held before the first, as truncate does."""
         if self.lm_head is None:
             raise ValueError("generate draws from logits: the decoder has no LM head")
         tokens, logprobs = [], []
-        for _ in range(n):
-            t, p = sampler(logits)
-            # (a row without tokens has -1: it goes on from the first)
-            x = embed.index_select(0, t.clamp(min=0))
-            _, logits = self.step(x[None], seqs, adapter=adapter)
-            tokens.append(t)
-            logprobs.append(p)
+        held = {s: self.cache.length(s) for s in seqs}
+        try:
+            for _ in range(n):
+                t, p = sampler(logits)
+                # (a row without tokens has -1: it goes on from the first)
+                x = embed.index_select(0, t.clamp(min=0))
+                _, logits = self.step(x[None], seqs, adapter=adapter)
+                tokens.append(t)
+                logprobs.append(p)
+        except BaseException:
+            for s, length in held.items():
+                self.cache.truncate(s, length)
+            raise
         if not tokens:
             dev = logits.device
             return (torch.empty((len(seqs), 0), dtype=torch.int32, device=dev),

@@ -65,3 +65,27 @@ def test_lone_sequences_do_not_thin_the_groups(monkeypatch, forks, lone, new):
     told = len(seqs) * new / len(pages)
     assert own / 2 <= told <= own * (1 + 1 / len(forks))
     assert np.diff(first).sum() <= len(seqs)
+
+
+def test_generate_that_fails_leaves_no_unknown_tokens(monkeypatch):
+    """The cache ends before the tokens do: whoever called has none of those drawn."""
+    monkeypatch.setattr(eb, "cache_copy", lambda pages, src, dst: None)
+    cache = decode.PagedCache(SHAPE, 1, 10, 4, 128, 64, torch.int8, "cpu")
+    dec = decode.Decoder([], SHAPE, cache, torch.zeros((64, 5)))
+    seqs = [cache.add(), cache.add()]
+    cache.extend(seqs, [126, 30])
+
+    def step(x, seqs, counts=None, adapter=None):
+        cache.extend(seqs, [1] * len(seqs))
+        return None, torch.zeros((2, 5))
+    monkeypatch.setattr(dec, "step", step)
+    embed, drawn = torch.zeros((5, 64)), []
+
+    def sampler(logits):
+        drawn.append(1)
+        return torch.zeros(2, dtype=torch.int32), torch.zeros(2)
+    with pytest.raises(decode.CacheFull):
+        dec.generate(torch.zeros((2, 5)), embed, seqs, 4, sampler)
+    assert len(drawn) == 3 and [cache.length(s) for s in seqs] == [126, 30]
+    tokens, _ = dec.generate(torch.zeros((2, 5)), embed, seqs, 2, sampler)
+    assert tokens.shape == (2, 2) and [cache.length(s) for s in seqs] == [128, 32]

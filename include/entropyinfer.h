@@ -570,7 +570,8 @@ size_t ei_cache_attn_shared_workspace_bytes(int32_t n_q_heads, int32_t n_tokens,
 /*
  * ei_cache_attn_shared -- ei_cache_attn for sequences that share their first pages
  * (continuations of one prompt, requests behind one system prompt): the keys there
- * are read once for all of a group's new tokens.
+ * are read once for all of a group's new tokens.  That costs two launches more: with
+ * less than about 650000 keys (times KV heads) saved ei_cache_attn is as fast or faster.
  *
  *   group_seqs     i32 [n_groups + 1]: group g is the sequences group_seqs[g] ..
  *                  group_seqs[g+1]-1 (ascending, clamped to [0, n_seqs]); sequences

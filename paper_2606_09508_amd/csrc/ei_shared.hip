@@ -19,11 +19,11 @@
 // along the units, so no two parts meet, and items + workers slots suffice.
 //
 // Measured, us (plan, keys, join):
-//   64 sequences behind 32768 keys, 32 heads over 8:   5.9 + 71 + 7.0; 57 of the 71 are
-//       the shared keys, 34 GFLOP at 600 TFLOP/s, matrix cores busy 0.28 of the time
-//   16 behind 8192, the same heads:                    5.5 + 20.5 + 6.8
+//   64 sequences behind 32768 keys, 32 heads over 8:   5.9 + 71.5 + 7.0; 57 of the 71.5
+//       are the shared keys, 34 GFLOP at 600 TFLOP/s, matrix cores busy 0.27 of the time
+//   16 behind 8192, the same heads:                    5.2 + 21 + 6.9
 //   9, 5 and 17 behind 2048 to 12288, 4 new tokens
-//     each, 64 over 8, int8:                           5.9 + 69 + 9.9
+//     each, 64 over 8, int8:                           6.0 + 71.6 + 10.2
 //   2 behind 960, 4 heads over 1:                      5.5 + 7.3 + 4.1
 #include "ei_attend.h"
 
@@ -86,7 +86,10 @@ __device__ __forceinline__ int64_t group_steps(const SharedArgs& x, int pages) {
   return x.wide_rows ? (keys + kWideKeys - 1) / kWideKeys : keys / kKeys;
 }
 // Whether items of so many steps are whole runs when all workers have the same: an item's
-// cost in units would then only push the runs off the items' ends.
+// cost in units would then only push the runs off the items' ends.  Without and with
+// this, 32 heads over 8, us a call: 16 sequences behind 8192 keys 35, 33; 16 behind 16384
+// 40, 36; 64 behind 32768 79, 77; but 64 behind 8192 51, 52 and 64 behind 4096 44, 47.  A
+// page more, where it does not apply, is no jump: 8256 32, 16448 37, 33024 79.
 __device__ __forceinline__ bool whole_runs(int64_t units, int64_t steps) {
   const int64_t per = units / kWideWorkers;
   return per >= kWideLeast && units % kWideWorkers == 0 && steps % per == 0;

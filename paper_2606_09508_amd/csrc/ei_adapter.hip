@@ -96,7 +96,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
   __shared__ int first_tile[kMaxAdapters];
   __shared__ __attribute__((aligned(16))) int seq_a[kPlanThreads], seq_n[kPlanThreads];
   __shared__ int seq_first[kPlanThreads], longest;
-  __shared__ int wave_tokens[kPlanThreads / kWave], wave_tiles[kPlanThreads / kWave];
+  __shared__ uint32_t wave_tokens[kPlanThreads / kWave], wave_tiles[kPlanThreads / kWave];
   const int tid = threadIdx.x, lane = tid % kWave, wave = tid / kWave;
   const int n = a.p.adapters;
   // a sequence's adapter (-1: none), first token and how many
@@ -124,38 +124,39 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
   __syncthreads();
   // the adapters' first places and tiles; a thread has `per` of them in a row
   const int per = (n + kPlanThreads - 1) / kPlanThreads, i0 = tid * per;
-  int tokens = 0, tiles = 0;
+  // (in unsigned numbers: offsets that do not ascend may count past 2^32)
+  const uint32_t rows = (uint32_t)a.p.rows;
+  uint32_t tokens = 0, tiles = 0;
   for (int i = i0; i < min(i0 + per, n); ++i) {
-    tokens += place[i];
-    tiles += (place[i] + a.p.rows - 1) / a.p.rows;
+    tokens += (uint32_t)place[i];
+    tiles += ((uint32_t)place[i] + rows - 1) / rows;
   }
-  const int up_tokens = (int)wave_incl_scan_u32((uint32_t)tokens);
-  const int up_tiles = (int)wave_incl_scan_u32((uint32_t)tiles);
+  const uint32_t up_tokens = wave_incl_scan_u32(tokens), up_tiles = wave_incl_scan_u32(tiles);
   if (lane == kWave - 1) {
     wave_tokens[wave] = up_tokens;
     wave_tiles[wave] = up_tiles;
   }
   __syncthreads();
-  int at = up_tokens - tokens, tile = up_tiles - tiles, all = 0;
+  uint32_t at = up_tokens - tokens, tile = up_tiles - tiles, sum = 0;
   for (int w = 0; w < kPlanThreads / kWave; ++w) {
     if (w < wave) {
       at += wave_tokens[w];
       tile += wave_tiles[w];
     }
-    all += wave_tiles[w];
+    sum += wave_tiles[w];
   }
   for (int i = i0; i < min(i0 + per, n); ++i) {
-    const int count = place[i];
-    first_tile[i] = tile;
-    place[i] = at;
+    const uint32_t count = (uint32_t)place[i];
+    first_tile[i] = (int)tile;
+    place[i] = (int)at;
     at += count;
-    tile += (count + a.p.rows - 1) / a.p.rows;
+    tile += (count + rows - 1) / rows;
   }
-  // (Offsets that do not ascend may count more tokens than there are, past 2^31 even:
-  // a tile then ends with the list or is empty.)
-  all = min(all, a.p.max_tiles);
+  // (Such offsets' places and tiles mean nothing, but every tile lies in the list: its
+  // begin is not below 0, and it ends with the list at the latest or is empty.)
+  const int all = (int)min(sum, (uint32_t)a.p.max_tiles);
   if (tid == 0) a.head[0] = all;
-  if (tid == kPlanThreads - 1) seq_n[0] = at;
+  if (tid == kPlanThreads - 1) seq_n[0] = (int)at;
   __syncthreads();
   const int total = seq_n[0];
   for (int t = tid; t < all; t += kPlanThreads) {
@@ -164,8 +165,8 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
       const int mid = (lo + hi + 1) / 2;
       if (first_tile[mid] <= t) lo = mid; else hi = mid - 1;
     }
-    const int begin = place[lo] + (t - first_tile[lo]) * a.p.rows;
-    const int stop = min(lo + 1 < n ? place[lo + 1] : total, a.p.tokens);
+    const int begin = (int)((uint32_t)place[lo] + ((uint32_t)t - (uint32_t)first_tile[lo]) * rows);
+    const int stop = min(max(lo + 1 < n ? place[lo + 1] : total, 0), a.p.tokens);
     a.tiles[t] = Tile{lo, begin, begin < 0 ? 0 : min(stop - begin, a.p.rows), 0};
   }
   __syncthreads();

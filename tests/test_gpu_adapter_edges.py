@@ -49,3 +49,39 @@ def test_an_infinite_entry_of_b_is_no_finite_output(tokens):
     assert not torch.isfinite(got[tokens:, 70]).any()
     got[tokens:, 70] = clean[tokens:, 70]
     assert torch.equal(got, clean)
+
+
+@pytest.mark.parametrize("T,counts", [
+    # of adapters 0, 1, 2: the places behind the second one pass 2^31, or 2^32
+    (65536, [100, 2 ** 31 - 64, 0]), (65536, [100, 2 ** 31 - 64, 2 ** 31 + 300]),
+    (65535, [2 ** 31, 40, 2 ** 31 - 16]), (40000, [2 ** 31 - 1, 2 ** 31 - 1, 500])])
+def test_offsets_that_count_past_32_bits_touch_nothing_outside(T, counts):
+    """Sequences that name the tokens again and again (and go back between)."""
+    index, cu = [], [0]
+    for a in reversed(range(3)):
+        left = counts[a]
+        while left:
+            n = min(left, T)
+            index += [a, -1]
+            cu += [n, 0]
+            left -= n
+    g = torch.Generator().manual_seed(T)
+    x = torch.randn((T, 64), generator=g).to(BF16).cuda()
+    y = torch.randn((T + 256, 64), generator=g).to(BF16)
+    ad = eb.Adapters(torch.randn((3, 8, 64), generator=g).to(BF16).cuda(),
+                     torch.randn((3, 64, 8), generator=g).to(BF16).cuda())
+    i32 = lambda v: torch.tensor(v, dtype=torch.int32).cuda()
+    plan = eb.adapter_plan(i32(index), 3, T, i32(cu))
+    need = eb.adapter_add_workspace_bytes(plan, 64, 8, 1)
+    ws = torch.full((need + 65536,), 0x5a, dtype=torch.uint8, device="cuda")
+    # tiles of the plan: their adapter, first place and tokens, behind 64 bytes
+    n = int(plan.data[:4].view(torch.int32))
+    tiles = plan.data[64:64 + 16 * n].view(torch.int32).view(n, 4).cpu()
+    some = tiles[tiles[:, 2] > 0]
+    assert (some[:, 1] >= 0).all() and (some[:, 1] + some[:, 2] <= T).all()
+    assert ((some[:, 0] >= 0) & (some[:, 0] < 3)).all()
+    dev = y.cuda()
+    eb.adapter_add(x, [dev[128:128 + T]], [ad], plan, ws)
+    got = dev.cpu()
+    assert torch.equal(got[:128], y[:128]) and torch.equal(got[128 + T:], y[128 + T:])
+    assert (ws[need:] == 0x5a).all()

@@ -721,9 +721,10 @@ size_t ei_adapter_add_workspace_bytes(ei_adapter_batch batch, int32_t n_in, int3
  * ei_adapter_add -- adds the corrections of up to four projections of the same x
  * (bf16 [n_tokens][n_in]) to their y, in place.  rank is a multiple of 8 up to 128
  * (smaller ones are padded with zeros), n_in a multiple of 8 (else
- * EI_ERR_UNSUPPORTED).  x A^T is held in fp32, enters the second product with 16
- * significant bits (as the sum of two bf16 numbers), and y is rounded once.  An
- * infinite entry of b makes its output, for the adapter's tokens, infinite or NaN.
+ * EI_ERR_UNSUPPORTED); n_in and n_out are below 2^31 - 4096 (else EI_ERR_SHAPE).
+ * x A^T is held in fp32, enters the second product with 16 significant bits (as the
+ * sum of two bf16 numbers), and y is rounded once.  An infinite entry of b makes its
+ * output, for the adapter's tokens, infinite or NaN.
  * `targets` is read on the host.  Rows of y whose sequence has no adapter, or that
  * belong to no sequence, are left as they were; offsets that do not ascend leave
  * the values of y undefined, and nothing outside the tensors is touched.  No y may

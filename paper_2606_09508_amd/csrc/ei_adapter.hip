@@ -516,8 +516,9 @@ int spans_of(const PlanShape& p, const ei_adapter_target* t, int n) {
   const int64_t s = blocks * p.max_tiles / 1024;
   return s < 1 ? 1 : s > 4 ? 4 : (int)s;
 }
+constexpr int kMostWidth = INT_MAX - 4096;   // (the kernels' steps go past a row's end)
 ei_status check_sizes(int32_t n_in, int32_t rank, int32_t n_targets) {
-  if (n_in <= 0 || rank <= 0 || n_targets < 0) return EI_ERR_SHAPE;
+  if (n_in <= 0 || n_in > kMostWidth || rank <= 0 || n_targets < 0) return EI_ERR_SHAPE;
   if (n_in % 8 || rank % 8 || rank > kMaxRank || n_targets > kMaxTargets) return EI_ERR_UNSUPPORTED;
   return EI_OK;
 }
@@ -567,7 +568,7 @@ ei_status ei_adapter_add(const uint16_t* x, int32_t n_in, int32_t rank,
   if ((st = ei::check_sizes(n_in, rank, n_targets)) != EI_OK) return st;
   if (n_targets > 0 && !targets) return EI_ERR_NULL;
   for (int i = 0; i < n_targets; ++i) {
-    if (targets[i].n_out <= 0) return EI_ERR_SHAPE;
+    if (targets[i].n_out <= 0 || targets[i].n_out > ei::kMostWidth) return EI_ERR_SHAPE;
     if (targets[i].n_out % 8) return EI_ERR_UNSUPPORTED;
   }
   if (ei::nothing(batch) || n_targets == 0) return EI_OK;

@@ -101,12 +101,12 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
   const int n = a.p.adapters;
   // a sequence's adapter (-1: none), first token and how many
   int ad = -1, first = 0, count = 0;
-  auto look = [&](int s) {
+  auto look = [&](uint32_t s) {
     ad = -1;
     first = count = 0;
-    if (s < a.p.seqs) {
+    if (s < (uint32_t)a.p.seqs) {
       ad = a.index[s];
-      rows_of(a, s, first, count);
+      rows_of(a, (int)s, first, count);
       if (ad < 0 || ad >= n) ad = -1;
     }
   };
@@ -115,7 +115,7 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
   __syncthreads();
   if (ad >= 0) atomicAdd(&place[ad], count);
   if (a.p.seqs > kPlanThreads) {
-    for (int s = tid + kPlanThreads; s < a.p.seqs; s += kPlanThreads) {
+    for (uint32_t s = tid + kPlanThreads; s < (uint32_t)a.p.seqs; s += kPlanThreads) {
       look(s);
       if (ad >= 0) atomicAdd(&place[ad], count);
     }
@@ -170,9 +170,10 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
     a.tiles[t] = Tile{lo, begin, begin < 0 ? 0 : min(stop - begin, a.p.rows), 0};
   }
   __syncthreads();
-  // the sequences in their order, kPlanThreads at a time
-  for (int s0 = 0; s0 < a.p.seqs; s0 += kPlanThreads) {
-    const int here = min(a.p.seqs - s0, kPlanThreads);
+  // the sequences in their order, kPlanThreads at a time (unsigned: their number, and a
+  // sequence's tokens, may end a step before 2^31)
+  for (uint32_t s0 = 0; s0 < (uint32_t)a.p.seqs; s0 += kPlanThreads) {
+    const int here = min(a.p.seqs - (int)s0, kPlanThreads);
     if (s0 > 0) look(s0 + tid);
     if (tid == 0) longest = 0;
     seq_a[tid] = ad;
@@ -192,9 +193,9 @@ __global__ __launch_bounds__(kPlanThreads) void plan_kernel(PlanArgs a) {
     if (ad >= 0 && count > kShort) atomicMax(&longest, count);
     // their tokens: of short sequences by a lane each, of longer ones by a wave, of long
     // ones by all
-    auto write = [&](int p, int f, int c, int i0, int step) {
-      for (int i = i0; i < c; i += step)
-        if ((unsigned)(p + i) < (unsigned)a.p.tokens) a.list[p + i] = f + i;
+    auto write = [&](uint32_t p, uint32_t f, uint32_t c, uint32_t i0, uint32_t step) {
+      for (uint32_t i = i0; i < c; i += step)
+        if (p + i < (uint32_t)a.p.tokens) a.list[p + i] = (int)(f + i);
     };
     if (ad >= 0 && count <= kShort) write(to, first, count, 0, 1);
     seq_a[tid] = to;

@@ -151,7 +151,7 @@ __global__ __launch_bounds__(kPlanThreads) void shared_plan_kernel(SharedArgs x)
       for (int s = b + lane; s < e; s += kWave) {
         int first, n;
         seq_rows(a.tk, s, first, n);
-        if (n > 0) pages = min(pages, max(a.lengths[s] - n, 0) / P);
+        if (n > 0) pages = min(pages, max(max(a.lengths[s], 0) - n, 0) / P);
       }
       pages = (int)wave_min_u32_f((uint32_t)pages);
       int n0, end, n1;
@@ -259,7 +259,7 @@ __global__ __launch_bounds__(kFewThreads) void shared_plan_few_kernel(SharedArgs
       if (g_first[mid] <= t) lo = mid; else hi = mid - 1;
     }
     if (g_first[lo] <= t && t < g_first[lo + 1]) group = lo;
-    if (group >= 0 && n > 0) atomicMin(&g_pages[group], max(length - n, 0) / P);
+    if (group >= 0 && n > 0) atomicMin(&g_pages[group], max(max(length, 0) - n, 0) / P);
   }
   __syncthreads();
   GroupInfo gi{};

@@ -123,3 +123,25 @@ def test_a_step_behind_hidden_states_of_zeros(forks):
     assert (dec.cache.pages.v_scale[0] == TINY).any() and (dec.cache.pages.v_scale[1] == TINY).any()
     for _ in range(2):
         _check_step(dec, _hidden(g, len(seqs)), seqs, None, None)
+
+
+@pytest.mark.parametrize("size", SIZES)
+@pytest.mark.parametrize("below", [8, 16, 20, 24])
+@pytest.mark.parametrize("first", [0, 1])
+def test_dims_that_only_light_keys_have(size, below, first):
+    """Keys far below the others are all that some dims have: an fp16 number that is not
+    normal still counts."""
+    b = Batch([size], [2], [1] * size, [1] * size, 4, 1, 64, E4M3, seed=size)
+    b.q *= 2.0 ** -8
+    b.q[..., 0] = 16.0
+    b.scales[0], b.scales[1] = 1.0, 2.0 ** -7
+    heavy, light = b.table[0][first], b.table[0][1 - first]
+    for page in range(b.codes.shape[1]):
+        b.codes[0, page, :, :, 0] = 0.0
+    b.codes[0, heavy, :, :, 0] = float(round(below / 2.04))
+    b.codes.view(torch.uint8)[1, heavy, :, :, 64:] = 0
+    b.codes[1, light, :, :, 64:] = 448.0
+    for s in range(size):
+        b.codes.view(torch.uint8)[1, b.table[s][2], :, :, 64:] = 0
+    got = _check(b)
+    assert (got[..., 64:] > 0).all()
